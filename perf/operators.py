@@ -4,9 +4,9 @@ Four kinds of case, each through the package's public entry points:
 
   append     paged_kv_append: new keys, rotated at their positions, and values into
              their page slots, the queries rotated on the way
-  attention  paged_attention: one or several query tokens per trajectory over bf16
+  attention  paged_token_attention: one or several query tokens per trajectory over bf16
              pages, or over E4M3 pages with a scale for each page and KV head
-  sparse     paged_select, then paged_attention over the pages it selected
+  sparse     paged_select, then paged_token_attention over the pages it selected
   verify     verify_drafts: drafted tokens against the target's probabilities
 
 `run` computes them in plain torch operations, or, with `own`, through the package.
@@ -366,8 +366,8 @@ def _softmax_mix(q, k, v, seen):
 def _attention(st):
     if own:
         import paper_2609_36899_amd as P
-        return P.paged_attention(st["q"], st["k"], st["v"], st["table"], st["lens"], st["out"],
-                                 k_scales=st["ks"], v_scales=st["vs"])
+        return P.paged_token_attention(st["q"], st["k"], st["v"], st["table"], st["lens"],
+                                       st["out"], k_scales=st["ks"], v_scales=st["vs"])
     case, q = st["case"], st["q"]
     B, nq, hq, dh = q.shape
     hkv = case["hkv"]
@@ -391,8 +391,8 @@ def _sparse(st):
     if own:
         import paper_2609_36899_amd as P
         P.paged_select(q, st["means"], st["table"], st["lens"], st["selected"])
-        P.paged_attention(q, st["k"], st["v"], st["table"], st["lens"], st["out"],
-                          k_scales=st["ks"], v_scales=st["vs"], selected=st["selected"])
+        P.paged_token_attention(q, st["k"], st["v"], st["table"], st["lens"], st["out"],
+                                k_scales=st["ks"], v_scales=st["vs"], selected=st["selected"])
         return st["selected"], st["out"]
     B, hq, dh = q.shape
     hkv, top = case["hkv"], case["top"]
