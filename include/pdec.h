@@ -506,6 +506,154 @@ int paged_decode_attention_fp8(int32_t batch, int32_t n_q_heads, int32_t n_kv_he
 int paged_check_pages(int32_t batch, const int32_t* block_table, int32_t bt_stride,
                       const int32_t* lens, int64_t n_pages, int32_t* words, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Operators over caller-owned pages (one layer, no engine): appending keys and
+ * values, attention of one or several query tokens, and the choice of the
+ * pages that an attention reads; and the verification of drafted tokens.
+ * Together they are one decode step of a caller that drafts tokens or reads
+ * part of a long context.
+ *
+ * Lengths and tables are read on the device when the call runs, so the calls
+ * wait for nothing, copy nothing and can be captured into a graph that is
+ * replayed as the lengths grow.  They are not trusted: a page id outside
+ * [0, n_pages), a position past the table or below 0 and a row past a
+ * sequence's own lead to no access outside the buffers (what is left out is
+ * said at each call).  paged_check_pages names a table's bad rows.
+ *
+ * Pages are laid out as above: K [n_pages][n_kv_heads][16][head_dim],
+ * V [n_pages][n_kv_heads][head_dim][16]; head_dim 64 or 128, up to 16 query
+ * heads per KV head.  E4M3 pages (PDEC_FP8_E4M3) carry a scale for each page
+ * and KV head, k_scales / v_scales device fp32 [n_pages][n_kv_heads]: an
+ * element reads back as value(code) * scale.
+ * Pages, q, out, tables of angles and workspaces are 16-byte aligned.
+ * All calls are asynchronous on stream and touch nothing but their arguments;
+ * calls that share a workspace must not overlap.
+ * ------------------------------------------------------------------------- */
+
+/* table[p][i] = (cos, sin)(p * base^(-2i / head_dim)), device fp32
+ * [max_pos][head_dim / 2][2], angles in double precision.
+ * Errors: PDEC_INVALID_ARG. */
+int rope_table(int32_t max_pos, int32_t head_dim, float base, float* table_dev, void* stream);
+
+/* Append the keys and values of n_rows new tokens of n_seqs sequences.
+ *   Row r belongs to the sequence b with row_start[b] <= r < row_start[b + 1]
+ *   (device int32 [n_seqs + 1], ascending) and to position
+ *   lens[b] - (row_start[b + 1] - r): lens (device int32 [n_seqs]) counts the
+ *   new tokens.  k and v are rows of [n_kv_heads][head_dim] in src_dtype,
+ *   k_stride / v_stride elements apart (the q|k|v rows of one projection serve
+ *   as they are); k's head pairs (i, i + head_dim / 2) are rotated by the
+ *   table's angle of the position.  q (nullable): rows of
+ *   [n_q_heads][head_dim] in src_dtype, rotated likewise into q_out [n_rows]
+ *   [n_q_heads][head_dim] (fp32 for fp32 pages, else bf16).
+ *   Token at position p goes to slot p % 16 of page block_table[b][p / 16].
+ *   src_dtype PDEC_F32 or PDEC_BF16; kv_dtype PDEC_F32 (from fp32 rows),
+ *   PDEC_BF16, or PDEC_FP8_E4M3 with scales: a page's scale for a KV head is
+ *   the smallest power of two (2^-100 .. 2^100) that brings its largest
+ *   element to 448.  A page that is part full keeps the larger of its scale
+ *   and what the new tokens need; where it grows, earlier codes are rounded
+ *   again (value(code) * old / new, to nearest even).  A page written from
+ *   slot 0 starts anew.  Larger elements saturate, NaN too.
+ *   k_means (nullable; bf16 and E4M3 pages): device bf16 [n_pages]
+ *   [n_kv_heads][head_dim]; each page written gets the mean over its filled
+ *   slots, the new ones the last, of the keys as they read back.
+ * Left as they were: slots behind a page's new tokens, pages without a new
+ * token, and everything of a row whose position is below 0 or at or past
+ * max_pos or the table's bt_stride * 16, whose page id is not in
+ * [0, n_pages), or that no sequence holds (q_out rows too).
+ * Two sequences of a call must not append to the same page.
+ * Errors: PDEC_INVALID_ARG, PDEC_UNSUPPORTED, PDEC_HIP_ERROR. */
+int paged_kv_append(int32_t src_dtype, int32_t kv_dtype, int32_t n_rows, int32_t n_seqs,
+                    int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const void* q,
+                    int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                    int64_t v_stride, const int32_t* lens_dev, const int32_t* row_start_dev,
+                    const int32_t* block_table_dev, int32_t bt_stride, int64_t n_pages,
+                    const float* rope_dev, int32_t max_pos, void* q_out, void* k_pages,
+                    void* v_pages, float* k_scales, float* v_scales, void* k_means, void* stream);
+
+/* Attention of the last n_q tokens of each sequence (1: a decode step; more:
+ * drafted tokens or a short prompt) over its pages:
+ *   out[b][j][h] = softmax(q[b][j][h] . K_g^T / sqrt(head_dim)) V_g over the
+ *   positions 0 .. lens[b] - n_q + j, the token's own among them.
+ *   q, out: device bf16 [batch][n_q][n_q_heads][head_dim]; lens: device int32
+ *   [batch], counting the n_q tokens, taken as in [0, bt_stride * 16]; a token
+ *   that sees no key (position below 0) gets zeros.  kv_dtype PDEC_BF16, or
+ *   PDEC_FP8_E4M3 with positive scales.
+ *   selected (nullable, n_q = 1): device int32 [batch][n_kv_heads]
+ *   [n_selected], logical page indices, distinct; the first min(n_selected,
+ *   ceil(lens[b] / 16)) of them are read, and the softmax runs over the
+ *   positions below lens[b] in those pages alone.
+ *   Scores, softmax and sums are fp32; the weights enter the second product
+ *   rounded to bf16.
+ *   workspace: device, paged_token_attention_workspace_bytes(...) bytes.
+ * Entries that are not page indices (paged_select's -1 among them) or whose
+ * page id is outside [0, n_pages) have no keys.
+ * Errors: PDEC_INVALID_ARG (n_q outside [1, 4096], ...), PDEC_UNSUPPORTED,
+ * PDEC_HIP_ERROR. */
+int64_t paged_token_attention_workspace_bytes(int32_t batch, int32_t n_q, int32_t n_q_heads,
+                                              int32_t n_kv_heads, int32_t head_dim);
+int paged_token_attention(int32_t kv_dtype, int32_t batch, int32_t n_q, int32_t n_q_heads,
+                          int32_t n_kv_heads, int32_t head_dim, const void* q,
+                          const void* k_pages, const void* v_pages, const float* k_scales,
+                          const float* v_scales, int64_t n_pages, const int32_t* block_table_dev,
+                          int32_t bt_stride, const int32_t* lens_dev, const int32_t* selected_dev,
+                          int32_t n_selected, void* out, void* workspace, int64_t workspace_bytes,
+                          void* stream);
+
+/* The pages a query token's attention reads when it reads n_selected of them:
+ * for each sequence and KV head those of the largest score
+ *   max over the KV head's query heads h of q[b][h] . k_means[page][g]
+ * (ties: the lower page), the first keep_first and the last keep_last pages
+ * whatever their scores; listed in page order, -1 behind them where a sequence
+ * has fewer pages.  Scores are summed in fp64 and rounded to fp32 once; a NaN
+ * counts as the lowest, as does a page id outside [0, n_pages).
+ *   q: device bf16 [batch][n_q_heads][head_dim]; k_means as paged_kv_append
+ *   keeps them; lens: device int32 [batch]; selected_dev: device int32
+ *   [batch][n_kv_heads][n_selected]; keep_first >= 0, keep_last >= 1 (the page
+ *   of the newest token), together at most n_selected.
+ *   workspace: device, paged_select_workspace_bytes(...) bytes.
+ * Errors: PDEC_INVALID_ARG, PDEC_UNSUPPORTED, PDEC_HIP_ERROR. */
+int64_t paged_select_workspace_bytes(int32_t batch, int32_t n_kv_heads, int32_t bt_stride);
+int paged_select(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                 const void* q, const void* k_means, int64_t n_pages,
+                 const int32_t* block_table_dev, int32_t bt_stride, const int32_t* lens_dev,
+                 int32_t n_selected, int32_t keep_first, int32_t keep_last, int32_t* selected_dev,
+                 void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Verification of drafted tokens against the target's probabilities, so that
+ * what comes out is distributed as the target's own sampling (temperature, no
+ * nucleus).  Random numbers are inputs.  With a row's whole-number masses
+ *   m_v = rint(exp((z_v - max z) * (1/T)) * 2^40),  S = sum m_v
+ * (as sample_top_p), P of target rows and D of draft rows, and in doubles
+ *   p_v = P_v * (2^50 / S_P),  d_v = D_v * (2^50 / S_D):
+ * draft i = 0, 1, .. of a sequence, token x, is accepted while
+ *   floor(u_i * 2^24) * d_x < 2^24 * p_x.
+ * The next token is drawn with u_{n_drafts} from
+ *   r_v = rint(max(p_v - d_v, 0)) of the first draft refused,
+ *   r_v = rint(p_v) where none was, or where the former is 0 throughout:
+ * Z = sum r_v, the first v whose running sum exceeds
+ * floor(floor(u * 2^24) * Z / 2^24).
+ *   target_logits: device fp32 [batch][n_drafts + 1][vocab], row i the
+ *   target's logits after draft i - 1; draft_logits: device fp32 [batch]
+ *   [n_drafts][vocab] of the drafting model, or null for drafts without
+ *   probabilities (d is then 2^50 at the draft and 0 elsewhere); draft_tokens:
+ *   device int32 [batch][n_drafts]; an id outside [0, vocab) ends a sequence's
+ *   drafts there; uniforms: device fp32 [batch][n_drafts + 1], clamped to
+ *   [0, 1).
+ *   tokens_out: device int32 [batch][n_drafts + 1]: the accepted drafts, the
+ *   next token, then -1; accepted_out: device int32 [batch], their number.
+ * NaN logits have no mass, nor has a row whose maximum is not finite; with no
+ * mass at all the next token is 0.
+ *   workspace: device, verify_drafts_workspace_bytes(...) bytes.
+ * Errors: PDEC_INVALID_ARG (temperature <= 0 or not finite, n_drafts outside
+ * [1, 1024], vocab above 2^22, null pointers, a small workspace). */
+int64_t verify_drafts_workspace_bytes(int32_t batch, int32_t n_drafts, int32_t vocab,
+                                      int32_t with_drafter);
+int verify_drafts(int32_t batch, int32_t n_drafts, int32_t vocab, const float* target_logits_dev,
+                  const float* draft_logits_dev, const int32_t* draft_tokens_dev,
+                  const float* uniforms_dev, float temperature, int32_t* tokens_dev_out,
+                  int32_t* accepted_dev_out, void* workspace, int64_t workspace_bytes,
+                  void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -2,7 +2,7 @@
 
 The compiled library (libpdec.so, see include/pdec.h) holds every kernel;
 this package only builds it (``build``) and marshals torch tensors into its
-calls (``engine``).
+calls (``engine``, ``paged``).
 """
 
 from ._native import PAGE_TOKENS, PdecError, BF16, F32, FP8_E4M3  # noqa: F401
@@ -19,6 +19,12 @@ def __getattr__(name):
                 "paged_decode_attention_fp8"):
         from . import engine
         return getattr(engine, name)
+    if name in ("rope_table", "paged_kv_append", "paged_token_attention",
+                "paged_token_attention_workspace_bytes", "paged_select",
+                "paged_select_workspace_bytes", "verify_drafts",
+                "verify_drafts_workspace_bytes"):
+        from . import paged
+        return getattr(paged, name)
     if name in ("PacedRollout", "pacing_plan"):
         from . import driver
         return getattr(driver, name)

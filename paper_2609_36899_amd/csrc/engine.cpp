@@ -21,6 +21,7 @@
 #include "kernels.h"
 #include "pacing.h"
 #include "pagepool.h"
+#include "status.h"
 
 using namespace pdec;
 
@@ -28,17 +29,14 @@ namespace {
 
 thread_local std::string g_err;
 
-int fail(int code, const std::string& msg) {
+}  // namespace
+
+int pdec::fail(int code, const std::string& msg) {
   g_err = msg;
   return code;
 }
 
-#define HIP_OR_FAIL(expr)                                                                \
-  do {                                                                                   \
-    hipError_t e_ = (expr);                                                              \
-    if (e_ != hipSuccess)                                                                \
-      return fail(PDEC_HIP_ERROR, std::string(#expr) + ": " + hipGetErrorString(e_));    \
-  } while (0)
+namespace {
 
 constexpr size_t kAlign = 256;
 size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }

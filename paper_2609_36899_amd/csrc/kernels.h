@@ -169,6 +169,67 @@ hipError_t launch_check_pages(int row0, int n, const CheckRows& rows, const int3
 hipError_t launch_rope_table(int max_pos, int head_dim, double base, float2* cs,
                              hipStream_t stream);
 
+// ---- operators over a caller's pages -----------------------------------------
+// Device-side lengths and tables are not trusted: rows, positions and page ids out of
+// range are left out (append) or have no keys (attention, selection).
+struct AppendArgs {  // append.hip
+  const void *k, *v, *q;  // [n_rows][heads][head_dim], rows *_stride elements apart; q nullable
+  int64_t k_stride, v_stride, q_stride;
+  int32_t n_rows, n_seqs, n_q_heads, n_kv_heads;
+  const int32_t *lens, *row_start, *block_table;
+  int32_t bt_stride;
+  int64_t n_pages;
+  const float2* rope;
+  int32_t max_pos;
+  void *q_out, *k_pages, *v_pages;
+  float *k_scales, *v_scales;  // E4M3 pages
+  uint16_t* k_means;           // nullable
+};
+// kv_dtype: 0 fp32, 1 bf16, 2 E4M3 pages.
+hipError_t launch_kv_append(int src_dtype, int kv_dtype, int head_dim, const AppendArgs& a,
+                            hipStream_t stream);
+
+struct PagedAttnPlan {
+  int32_t row_tiles, tok_per_block, blocks_per_seq, n_groups;
+  int64_t n_units;
+};
+PagedAttnPlan plan_paged_attention(int batch, int n_q, int n_q_heads, int n_kv_heads);
+struct PagedAttnArgs {  // attention_paged.hip
+  const void *q, *k_pages, *v_pages;
+  const float *k_scales, *v_scales;
+  const int32_t *block_table, *lens, *selected;  // selected nullable
+  int32_t bt_stride, n_selected, max_len, n_q, n_q_heads, n_kv_heads;
+  int64_t n_pages;
+  int32_t tok_per_block, blocks_per_seq, n_units, n_groups, min_pairs;
+  float scale_log2;
+  float *part_ml, *part_acc;  // [n_groups + n_units][Hkv][16 row_tiles][2 | head_dim]
+  void* out;
+};
+hipError_t launch_paged_attention(int kv_fp8, int head_dim, int row_tiles, const PagedAttnArgs& a,
+                                  hipStream_t stream);
+
+struct SelectArgs {  // select.hip
+  const uint16_t *q, *k_means;
+  const int32_t *block_table, *lens;
+  int32_t batch, n_q_heads, n_kv_heads, bt_stride, n_selected, keep_first, keep_last;
+  int64_t n_pages;
+  float* scores;  // [batch][Hkv][bt_stride]
+  int32_t* selected;
+};
+hipError_t launch_paged_select(int head_dim, const SelectArgs& a, hipStream_t stream);
+
+struct VerifyArgs {  // verify.hip
+  const float *target, *drafter;  // drafter nullable
+  const int32_t* drafts;
+  const float* uniforms;
+  int32_t *tokens, *accepted;
+  int32_t batch, n_drafts, vocab;
+  double inv_t;
+  void* workspace;
+};
+int64_t verify_workspace_bytes(int batch, int n_drafts, bool drafter, int vocab);
+hipError_t launch_verify(const VerifyArgs& a, hipStream_t stream);
+
 // ---- KV snapshot / restore ---------------------------------------------------
 // Copy whole pages between the pool and a host buffer mapped for the device.
 // Page i of the list moves between pool block [layer][kind][pages[i]] and

@@ -1,0 +1,278 @@
+"""paged_token_attention against the float64 oracle.
+
+Tolerance of an output element, with A the same mix of |v| in the place of v:
+  2^-8 A      the weights' rounding to bf16 before the second product,
+  2^-8 |out|  the output's rounding to bf16,
+  E A         the scores' fp32 errors in the exponent, E = 2 * 2^-24 * (Dh + 4) * max over
+              keys of sum_d |q_d k_d| / sqrt(Dh) (both the element's weight and the sum), and
+  2^-24 (N + 64) A   sums of N keys in fp32.
+"""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators as oo
+from oracle.fp8 import e4m3_decode
+
+pytestmark = pytest.mark.gpu
+
+
+def _P():
+    import paper_2609_36899_amd as P
+    return P
+
+
+class Case:
+    """Random pages of which the slots behind each length hold NaN."""
+
+    def __init__(self, lens, hq, hkv, dh, n_q=1, fp8=True, seed=0, share=False):
+        rng = np.random.default_rng(seed)
+        self.lens = np.asarray(lens, np.int32)
+        self.fp8, self.n_q = fp8, n_q
+        B = len(lens)
+        n = [-(-max(int(x), 0) // 16) for x in lens]
+        self.P = sum(n) + 1
+        perm = rng.permutation(self.P)
+        self.table = rng.integers(0, self.P, (B, max(n + [1]) + 2)).astype(np.int32)
+        at = 0
+        for b in range(B):
+            self.table[b, :n[b]] = perm[at:at + n[b]]
+            at += n[b]
+        ks, vs = (self.P, hkv, 16, dh), (self.P, hkv, dh, 16)
+        if fp8:
+            draw = lambda s: (rng.integers(0, 127, s) | (rng.integers(0, 2, s) << 7)).astype(np.uint8)
+            self.k, self.v = draw(ks), draw(vs)
+            # Scales that are no powers of two, as other writers choose them.
+            self.ks = (rng.uniform(0.5, 2.0, (self.P, hkv)) / 200).astype(np.float32)
+            self.vs = np.exp2(rng.uniform(-12, 3, (self.P, hkv))).astype(np.float32)
+            nan = 0x7F
+        else:
+            bf = lambda x: torch.from_numpy(x.astype(np.float32)).to(torch.bfloat16).float().numpy()
+            self.k, self.v = bf(rng.standard_normal(ks)), bf(rng.standard_normal(vs))
+            self.ks = self.vs = None
+            nan = np.nan
+        for b in range(B):
+            if n[b] and lens[b] % 16:
+                self.k[self.table[b, n[b] - 1], :, lens[b] % 16:] = nan
+                self.v[self.table[b, n[b] - 1], :, :, lens[b] % 16:] = nan
+        self.q = torch.from_numpy(rng.standard_normal((B, n_q, hq, dh)).astype(np.float32)
+                                  ).to(torch.bfloat16)
+        self.selected = None
+
+    def device(self):
+        g = lambda a: None if a is None else torch.from_numpy(np.ascontiguousarray(a)).cuda()
+        k, v = g(self.k), g(self.v)
+        if not self.fp8:
+            k, v = k.to(torch.bfloat16), v.to(torch.bfloat16)
+        return dict(q=self.q.cuda(), k_pages=k, v_pages=v, block_table=g(self.table),
+                    lens=g(self.lens), k_scales=g(self.ks), v_scales=g(self.vs),
+                    selected=g(self.selected))
+
+    def run(self):
+        d = self.device()
+        out = torch.full(d["q"].shape, 9.0, dtype=torch.bfloat16, device="cuda")
+        _P().paged_token_attention(out=out, **d)
+        torch.cuda.synchronize()
+        return out.float().cpu().numpy()
+
+    def values(self):
+        if not self.fp8:
+            return self.k.astype(np.float64), self.v.astype(np.float64)
+        return (e4m3_decode(self.k) * self.ks[:, :, None, None].astype(np.float64),
+                e4m3_decode(self.v) * self.vs[:, :, None, None].astype(np.float64))
+
+    def bound(self, ref, size, k):
+        q = self.q.float().numpy().astype(np.float64)
+        dh = q.shape[-1]
+        top = np.abs(np.nan_to_num(k, posinf=0, neginf=0)).max() if k.size else 0.0
+        e = 2.0 ** -23 * (dh + 4) * (np.abs(q).sum(-1) * top / np.sqrt(dh))[..., None]
+        return (2.0 ** -8 + e + 2.0 ** -24 * (int(self.lens.max()) + 64)) * size + \
+            2.0 ** -8 * np.abs(ref) + 1e-30
+
+    def check(self):
+        k, v = self.values()
+        ref, size = oo.token_attention(self.q.float().numpy(), k, v, self.table, self.lens,
+                                       self.selected)
+        got = self.run()
+        assert np.isfinite(got).all()
+        assert (np.abs(got - ref) <= self.bound(ref, size, k)).all(), \
+            np.max(np.abs(got - ref) / self.bound(ref, size, k))
+
+
+EDGE_LENS = [0, 1, 2, 15, 16, 17, 31, 32, 33, 48, 127, 128, 129, 300, 1000, 2049]
+HEADS = [(32, 8, 128), (8, 2, 64), (10, 2, 128), (16, 1, 64), (3, 3, 128), (13, 1, 128)]
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+@pytest.mark.parametrize("hq,hkv,dh", HEADS)
+def test_edge_lengths(hq, hkv, dh, fp8):
+    Case(EDGE_LENS, hq, hkv, dh, fp8=fp8, seed=1).check()
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+@pytest.mark.parametrize("n_q", [2, 3, 4, 5, 8, 9, 17, 40])
+def test_several_tokens(n_q, fp8):
+    """Lengths below n_q leave tokens without a key: zeros."""
+    Case([0, 1, n_q - 1, n_q, 16, 31, 33, 200, 511], 8, 2, 128, n_q=n_q, fp8=fp8, seed=2).check()
+
+
+@pytest.mark.parametrize("hq,hkv,dh,n_q", [(16, 1, 64, 3), (5, 1, 128, 7), (6, 6, 64, 33),
+                                            (40, 8, 128, 4), (12, 1, 64, 70), (2, 1, 128, 150)])
+def test_several_tokens_of_other_groups(hq, hkv, dh, n_q):
+    Case([n_q, 77, 260, 5], hq, hkv, dh, n_q=n_q, seed=3).check()
+
+
+def test_long_contexts_split_over_many_groups():
+    Case([40000, 3, 0, 900], 8, 2, 128, seed=4).check()
+    Case([20000], 8, 2, 128, n_q=5, fp8=False, seed=5).check()
+
+
+def test_many_short_sequences():
+    """More sequences than one prefix-sum step of a work group takes."""
+    rng = np.random.default_rng(6)
+    Case(rng.integers(0, 40, 700), 4, 2, 64, seed=6).check()
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+def test_masked_infinities(fp8):
+    """What a token does not see may hold anything: keys and values of the tokens after
+    it are infinite or NaN, and only the tokens that see them turn NaN."""
+    c = Case([37, 64, 19], 8, 2, 64, n_q=4, fp8=fp8, seed=7)
+    bad = (0x7F, 0x7F) if fp8 else (np.nan, np.inf)
+    for b, n in enumerate(c.lens):
+        page, slot = c.table[b, (n - 1) // 16], (n - 1) % 16
+        c.k[page, :, slot] = bad[0]
+        c.v[page, :, :, slot] = bad[1]
+    got = c.run()
+    assert np.isnan(got[:, 3]).all()
+    k, v = c.values()
+    ref, size = oo.token_attention(c.q.float().numpy()[:, :3], k, v, c.table, c.lens - 1)
+    c.q, c.n_q = c.q[:, :3], 3
+    assert (np.abs(got[:, :3] - ref) <= c.bound(ref, size, k)).all()
+
+
+def test_scores_of_minus_infinity_and_the_lowest_value():
+    """Keys whose scores are -inf weigh nothing; a row that has no others gives zeros."""
+    c = Case([20, 16], 2, 1, 64, fp8=False, seed=8)
+    c.q = torch.ones_like(c.q)
+    low = np.float32(torch.finfo(torch.bfloat16).min)
+    c.k[c.table[0, 0], 0, :7] = -np.inf
+    c.k[c.table[0, 0], 0, 7:12] = low  # 64 of them: -inf in the sum
+    c.k[c.table[1, 0], 0] = -np.inf
+    got = c.run()
+    keep = np.r_[12:20]
+    pages = [c.k[c.table[0, i], 0] for i in (0, 1)], [c.v[c.table[0, i], 0].T for i in (0, 1)]
+    k, v = (np.concatenate(p)[keep].astype(np.float64) for p in pages)
+    ref, size = oo.mix(np.ones(64), k, v)
+    assert (np.abs(got[0, 0] - ref) <= 2.0 ** -7 * size + 1e-6).all()
+    assert (got[1] == 0).all()
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+def test_page_ids_outside_the_pool_have_no_keys(fp8):
+    c = Case([100, 50, 16], 8, 2, 64, fp8=fp8, seed=9)
+    c.table[0, 2], c.table[0, 5], c.table[1, 0], c.table[2, 0] = -1, c.P, 2 ** 31 - 1, -2 ** 31
+    c.check()
+    assert (c.run()[2] == 0).all()
+
+
+def test_lengths_past_the_table_are_cut_and_negative_ones_empty():
+    c = Case([64, 30], 4, 2, 64, seed=10)
+    c.table = np.ascontiguousarray(c.table[:, :4])
+    c.check()
+    want = c.run()
+    c.lens = np.array([70000, -5], np.int32)
+    got = c.run()
+    np.testing.assert_array_equal(got[0], want[0])
+    assert (got[1] == 0).all()
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+@pytest.mark.parametrize("n_sel", [1, 2, 3, 9, 64])
+def test_selected_pages(n_sel, fp8):
+    """Lists in any order, shorter than n_selected, with entries that name nothing."""
+    rng = np.random.default_rng(11)
+    lens = [0, 1, 16, 33, 200, 1000, 37]
+    c = Case(lens, 8, 2, 128, fp8=fp8, seed=11)
+    c.selected = np.full((len(lens), 2, n_sel), -1, np.int32)
+    for b, n in enumerate(lens):
+        pages = -(-n // 16)
+        for g in range(2):
+            m = min(pages, n_sel)
+            c.selected[b, g, :m] = rng.permutation(pages)[:m]
+            c.selected[b, g, m:] = rng.integers(-1, 2, n_sel - m)  # behind the list: not read
+    c.selected[5, 0, 0] = 2 ** 30
+    c.check()
+
+
+def test_all_pages_selected_equals_none_selected():
+    c = Case([1, 100, 555, 2000], 8, 2, 128, seed=12)
+    want = c.run()
+    c.selected = np.tile(np.arange(125, dtype=np.int32), (4, 2, 1))
+    np.testing.assert_array_equal(c.run(), want)
+
+
+def test_same_call_same_bits_and_page_order():
+    c = Case([5, 700, 1500, 33], 8, 2, 128, seed=13)
+    a = c.run()
+    np.testing.assert_array_equal(a, c.run())
+    perm = np.random.default_rng(9).permutation(c.P)
+    back = np.argsort(perm)
+    for name in ("k", "v", "ks", "vs"):
+        setattr(c, name, getattr(c, name)[perm])
+    c.table = back[c.table].astype(np.int32)
+    np.testing.assert_array_equal(a, c.run())
+
+
+def test_offsets_past_32_bits():
+    """Pages at the end of a pool of more than 2^32 elements."""
+    hkv, dh, P = 8, 128, 270000
+    k = torch.zeros((P, hkv, 16, dh), dtype=torch.uint8, device="cuda")
+    v = torch.zeros((P, hkv, dh, 16), dtype=torch.uint8, device="cuda")
+    assert k.numel() > 2 ** 32
+    scales = torch.ones((P, hkv), dtype=torch.float32, device="cuda")
+    small = Case([40, 90], 8, 8, 128, seed=14)
+    d = small.device()
+    at = torch.arange(P - small.P, P, device="cuda")
+    k[at], v[at] = d["k_pages"], d["v_pages"]
+    ks, vs = scales.clone(), scales.clone()
+    ks[at], vs[at] = d["k_scales"], d["v_scales"]
+    out = torch.empty(d["q"].shape, dtype=torch.bfloat16, device="cuda")
+    _P().paged_token_attention(d["q"], k, v, d["block_table"] + (P - small.P), d["lens"], out,
+                               k_scales=ks, v_scales=vs)
+    np.testing.assert_array_equal(out.float().cpu().numpy(), small.run())
+
+
+def test_replayed_graph_follows_the_lengths():
+    c = Case([300, 80], 8, 2, 64, n_q=2, seed=15)
+    d = c.device()
+    d["lens"] = torch.tensor([2, 1], dtype=torch.int32, device="cuda")
+    out = torch.empty(d["q"].shape, dtype=torch.bfloat16, device="cuda")
+    eager = torch.empty_like(out)
+    ws = torch.empty(_P().paged_token_attention_workspace_bytes(2, 2, 8, 2, 64),
+                     dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        _P().paged_token_attention(out=out, workspace=ws, **d)
+    for step in range(12):
+        graph.replay()
+        _P().paged_token_attention(out=eager, workspace=ws, **d)
+        torch.cuda.synchronize()
+        assert torch.equal(out.view(torch.int16), eager.view(torch.int16)), step
+        d["lens"] += 7
+
+
+def test_calls_on_two_streams_with_their_own_workspaces():
+    c = Case([2000, 700, 33], 8, 2, 128, seed=16)
+    d = c.device()
+    want = torch.from_numpy(c.run())
+    outs = [torch.empty(d["q"].shape, dtype=torch.bfloat16, device="cuda") for _ in range(8)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for i, o in enumerate(outs):
+        _P().paged_token_attention(out=o, stream=streams[i % 2], **d)
+    torch.cuda.synchronize()
+    for o in outs:
+        assert torch.equal(o.float().cpu(), want)
