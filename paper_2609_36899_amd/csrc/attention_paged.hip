@@ -23,6 +23,7 @@
 #include "kernels.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace pdec {
 
@@ -30,6 +31,11 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kThreads = 256, kWaves = 4;
+// Work groups of a launch: one for each compute unit.  More of them cost their beginnings
+// (lengths, queries, first pages) and their partials: us at 256 / 512 / 1024 groups, 64
+// sequences of 1K to 8K tokens 120 / 119 / 126 (E4M3) and 179 / 178 / 180 (bf16), five
+// tokens each over 8 x 64K to 128K 267 / 281 / 315, four over 16 x 1K to 16K 102 / 114 / 133.
+constexpr int kGroups = 256;
 constexpr int kPair = 2 * kPage;        // keys of a pair of pages
 constexpr int kNowhere = 0x40000000;    // a key position past every limit
 
@@ -81,35 +87,53 @@ __device__ __forceinline__ int group_scan(int v, int* red, int* total) {
   return before;
 }
 
-__device__ __forceinline__ Split split_of(const PagedAttnArgs& a, int* red) {
+// The pairs of all units and of a group, and the unit that the group's first pair lies in
+// with that unit's first pair; to all threads.  One look at the lengths, but for more
+// units than threads.
+__device__ __forceinline__ Split split_of(const PagedAttnArgs& a, int w, int* red, int* found) {
+  const bool few = a.n_units <= kThreads;
   int mine = 0, total;
-  for (int u = threadIdx.x; u < a.n_units; u += blockDim.x) mine += unit_pairs(a, u);
-  group_scan(mine, red, &total);
-  return {total, max((total + a.n_groups - 1) / a.n_groups, a.min_pairs)};
-}
-
-// The unit that pair `at` (< total) belongs to and its first pair, to all threads.
-__device__ __forceinline__ void find_unit(const PagedAttnArgs& a, int at, int* red, int* found) {
-  int base = 0;
-  for (int u0 = 0; u0 < a.n_units; u0 += blockDim.x) {
-    const int u = u0 + threadIdx.x, n = u < a.n_units ? unit_pairs(a, u) : 0;
-    int total;
-    const int first = base + group_scan(n, red, &total);
-    if (first <= at && at < first + n) {
-      found[0] = u;
+  for (int u = threadIdx.x; u < a.n_units; u += kThreads) mine += unit_pairs(a, u);
+  int first = group_scan(mine, red, &total);
+  const Split s = {total, max((total + a.n_groups - 1) / a.n_groups, a.min_pairs)};
+  const int at = w * s.per;
+  if (at >= total) return s;
+  if (few) {
+    if (first <= at && at < first + mine) {
+      found[0] = threadIdx.x;
       found[1] = first;
     }
-    base += total;
-    if (base > at) break;
+  } else {
+    int base = 0;
+    for (int u0 = 0; base <= at; u0 += kThreads) {
+      const int u = u0 + threadIdx.x, n = u < a.n_units ? unit_pairs(a, u) : 0;
+      first = base + group_scan(n, red, &total);
+      if (first <= at && at < first + n) {
+        found[0] = u;
+        found[1] = first;
+      }
+      base += total;
+    }
   }
   __syncthreads();
+  return s;
 }
 
-template <typename KT>
-__device__ __forceinline__ bf16x8 load8(const KT* p) {
-  if constexpr (sizeof(KT) == 2) return load_stream<bf16x8>(p);
-  else return e4m3x8_to_bf16(load_stream<u32x2>(p));
+// Eight codes (code i in byte i of the two dwords) to bf16, exactly, two an instruction.
+__device__ __forceinline__ bf16x8 decode8(u32x2 w) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.x, 1.f, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.x, 1.f, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, 1.f, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, 1.f, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
+
+// What a pair of pages needs beside the products.
+enum Cut {
+  kNone,   // every row sees every key
+  kLimit,  // keys past a row's limit count as -inf, and V of keys without data as 0
+  kToken,  // the block's tokens see different keys of the pair
+};
 
 // Lane l: c16 = l % 16, q4 = l / 16.  The MFMA operand order is the one of the
 // engine's decode attention: S^T = K Q^T with the keys permuted so that a lane's
@@ -117,20 +141,26 @@ __device__ __forceinline__ bf16x8 load8(const KT* p) {
 // tokens 8 (q4 % 2) ..), which is the P operand of O^T = V^T P^T against one load
 // of the transposed V page.
 template <int DH, int RT, typename KT, bool LIST>
-__global__ __launch_bounds__(kThreads) void paged_attn_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(kThreads)
+__attribute__((amdgpu_waves_per_eu(RT == 1 ? (sizeof(KT) == 1 ? 2 : 3) : 1))) void paged_attn_kernel(
+    PagedAttnArgs a, const int32_t* __restrict__ table, const int32_t* __restrict__ lists) {
   constexpr int KC = DH / 32, DT = DH / 16;
   constexpr bool kFp8 = sizeof(KT) == 1;
+  // Whether the next pair's loads are in flight while one is used.  With one row tile of
+  // bf16 pages the registers that this takes cost more (64 x 1K to 8K: 179 us without, 188
+  // with).
+  constexpr bool kAhead = kFp8 || RT > 1;
+  typedef typename std::conditional<kFp8, u32x2, u32x4>::type VRaw;
   __shared__ int red[kWaves];
   __shared__ int found[2];
   __shared__ float sm[kWaves - 1][64][RT * (4 * DT + 2)];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int c16 = lane & 15, q4 = lane >> 4;
   const int g = blockIdx.x, w = blockIdx.y;
-  const Split split = split_of(a, red);
+  const Split split = split_of(a, w, red, found);
   int at = w * split.per;
   if (at >= split.total) return;
   const int end = min(at + split.per, split.total);
-  find_unit(a, at, red, found);
   int u = found[0], first = found[1];
   const int G = a.n_q_heads / a.n_kv_heads;
   const uint16_t* q = (const uint16_t*)a.q;
@@ -174,46 +204,90 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(PagedAttnArgs a) {
       for (int d = 0; d < DT; ++d) acc[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    const int32_t* bt = a.block_table + (int64_t)b * a.bt_stride;
+    const int32_t* bt = table + (int64_t)b * a.bt_stride;
     const int32_t* list =
-        LIST ? a.selected + ((int64_t)b * a.n_kv_heads + g) * a.n_selected : nullptr;
-    // Page i of the unit: its place in the pool and the position of its first key.
-    // An entry that names no page of the pool has no keys.
-    auto page_at = [&](int i, int* key0) -> int {
-      int logical = i;
-      if constexpr (LIST) logical = i < n_pages ? list[i] : -1;
-      const bool in = LIST ? logical >= 0 && logical < a.bt_stride : i < n_pages;
-      const int page = in ? bt[logical] : -1;
-      const bool ok = page >= 0 && page < a.n_pages;
-      *key0 = ok ? logical * kPage : kNowhere;
-      return ok ? page : 0;
+        LIST ? lists + ((int64_t)b * a.n_kv_heads + g) * a.n_selected : nullptr;
+    // A pair of pages: their places in the pool and the positions of their first keys.
+    // A page that the table or the list does not name has no keys.  All uniform over the
+    // wave and from pointers of the kernel's own that nothing aliases, so these are scalar
+    // loads: vector loads return in order, so waiting for one would drain the pages' in
+    // flight (five tokens over 8 x 64K to 128K: 326 us with both waits, 267 without).
+    struct Pair {
+      int page[2], key0[2];
     };
-
-    for (int pr = p_begin + wave; pr < p_end; pr += kWaves) {
+    auto look = [&](int pr) {
+      Pair r;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int n = 2 * pr + i;
+        int logical = n;
+        if constexpr (LIST) logical = n < n_pages ? list[n] : -1;
+        const bool in = LIST ? logical >= 0 && logical < a.bt_stride : n < n_pages;
+        const int page = in ? bt[logical] : -1;
+        const bool ok = page >= 0 && page < a.n_pages;
+        r.key0[i] = ok ? logical * kPage : kNowhere;
+        r.page[i] = ok ? page : 0;
+      }
+      return r;
+    };
+    // The pair's bytes as they are in memory, and its scales.
+    struct Raw {
+      u32x4 k[2][kFp8 ? KC / 2 : KC];
+      VRaw v[DT];
+      float ks, vs;  // of the page of this lane's keys
       int key0[2];
-      const int page0 = page_at(2 * pr, &key0[0]), page1 = page_at(2 * pr + 1, &key0[1]);
-      const int64_t base0 = page0 * page_stride + head_off, base1 = page1 * page_stride + head_off;
+    };
+    auto load = [&](const Pair& p, Raw& r) {
+      const int64_t base0 = p.page[0] * page_stride + head_off;
+      const int64_t base1 = p.page[1] * page_stride + head_off;
       const KT* kb = (const KT*)a.k_pages + (k_sel ? base1 : base0);
       const KT* vb = (const KT*)a.v_pages + (v_sel ? base1 : base0) + v_tok0;
-      float k_mul = a.scale_log2, v_mul = 1.f;
+      // The scales come as vector loads, in order with the pages': scalar loads return out
+      // of order, so that using one would wait for all, the next pair's among them.
       if constexpr (kFp8) {
-        const int64_t at0 = (int64_t)page0 * a.n_kv_heads + g, at1 = (int64_t)page1 * a.n_kv_heads + g;
-        k_mul *= v_sel ? a.k_scales[at1] : a.k_scales[at0];
-        v_mul = v_sel ? a.v_scales[at1] : a.v_scales[at0];
+        const int64_t at = (int64_t)(v_sel ? p.page[1] : p.page[0]) * a.n_kv_heads + g;
+        r.ks = a.k_scales[at];
+        r.vs = a.v_scales[at];
       }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        r.key0[i] = p.key0[i];
+#pragma unroll
+        for (int c = 0; c < (kFp8 ? KC / 2 : KC); ++c)
+          r.k[i][c] = load_stream<u32x4>(kb + (k_tok + 4 * i) * DH + qk_dim(kFp8 ? 2 * c : c, q4));
+      }
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+        r.v[d] = load_stream<VRaw>(vb + (d * 16 + c16) * kPage);
+    };
+    auto use = [&](const Raw& r, auto cut_) {
+      constexpr Cut kCut = decltype(cut_)::value;
       bf16x8 kf[2][KC];
       u16x8 vf[DT];
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int c = 0; c < KC; ++c) kf[i][c] = load8<KT>(kb + (k_tok + 4 * i) * DH + qk_dim(c, q4));
+        for (int c = 0; c < KC; ++c) {
+          if constexpr (kFp8) {
+            const u32x4 w4 = r.k[i][c / 2];
+            kf[i][c] = decode8(c % 2 ? u32x2{w4.z, w4.w} : u32x2{w4.x, w4.y});
+          } else {
+            kf[i][c] = __builtin_bit_cast(bf16x8, r.k[i][c]);
+          }
+        }
 #pragma unroll
-      for (int d = 0; d < DT; ++d)
-        vf[d] = __builtin_bit_cast(u16x8, load8<KT>(vb + (d * 16 + c16) * kPage));
-
-      const int kbase = (v_sel ? key0[1] : key0[0]) + v_tok0;  // position of this lane's key 0
-      const int pair_end = max(key0[0], key0[1]) + kPage;      // uniform over the wave
-      if (pair_end > kv_lim) {  // keys without data: 0 times what they hold may be NaN
+      for (int d = 0; d < DT; ++d) {
+        if constexpr (kFp8) vf[d] = __builtin_bit_cast(u16x8, decode8(r.v[d]));
+        else vf[d] = __builtin_bit_cast(u16x8, r.v[d]);
+      }
+      const float k_mul = kFp8 ? a.scale_log2 * r.ks : a.scale_log2;
+      const float v_mul = kFp8 ? r.vs : 1.f;
+      const float v_inv = kFp8 ? __builtin_amdgcn_rcpf(v_mul) : 1.f;
+      const int kbase = (v_sel ? r.key0[1] : r.key0[0]) + v_tok0;  // position of this lane's key 0
+      // Keys without data: 0 times what they hold may be NaN.  (Uniform over the wave;
+      // with kNone only where the table names no page.)
+      const bool hole = max(r.key0[0], r.key0[1]) + kPage > kv_lim;
+      if (kCut == kToken || hole) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
           if (kbase + e >= kv_lim)
@@ -230,10 +304,15 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(PagedAttnArgs a) {
           for (int c = 0; c < KC; ++c)
             s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[i][c], qf[t][c], s[i], 0, 0, 0);
         }
+        if (kCut == kNone && hole) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (kbase >= kNowhere) s[e / 4][e % 4] = -INFINITY;
+        }
         float sv[8], mloc = -INFINITY;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          sv[e] = kbase + e < row_lim[t] ? s[e / 4][e % 4] * k_mul : -INFINITY;
+          sv[e] = kCut == kNone || kbase + e < row_lim[t] ? s[e / 4][e % 4] * k_mul : -INFINITY;
           mloc = fmaxf(mloc, sv[e]);
         }
         mloc = max_over_key_groups(mloc);
@@ -245,20 +324,23 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(PagedAttnArgs a) {
           for (int d = 0; d < DT; ++d) acc[t][d] *= alpha;
         }
         m[t] = m_new;
-        // The weights enter the second product in bf16 (half a step, 2^-9 of each,
-        // as the values are E4M3 or bf16 themselves); their sum is kept in fp32.  A
-        // page's V scale goes into its weights.
+        // The weights enter the second product in bf16, each off by at most half a step
+        // (2^-8), a page's V scale with them; the normaliser is the fp32 sum of the
+        // weights as they were rounded, so that what the rounding does to a row's large
+        // weights cancels.
         uint32_t pw[4];
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
           const float p0 = __builtin_amdgcn_exp2f(sv[e] - m_use);
           const float p1 = __builtin_amdgcn_exp2f(sv[e + 1] - m_use);
-          l[t] += p0 + p1;
           const f32x2 pv = {kFp8 ? p0 * v_mul : p0, kFp8 ? p1 * v_mul : p1};
-          pw[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(pv, bf16x2));
+          const uint32_t bits = __builtin_bit_cast(uint32_t, __builtin_convertvector(pv, bf16x2));
+          pw[e / 2] = bits;
+          const float sum = __uint_as_float(bits << 16) + __uint_as_float(bits & 0xFFFF0000u);
+          l[t] = kFp8 ? __builtin_fmaf(sum, v_inv, l[t]) : l[t] + sum;
         }
         const u16x8 pbits = __builtin_bit_cast(u16x8, u32x4{pw[0], pw[1], pw[2], pw[3]});
-        if (pair_end > pos0 + 1 && n_tok > 1) {
+        if constexpr (kCut == kToken) {
           // Keys that some of the block's tokens do not see: token by token, with the
           // keys past its own taken as 0 and the sums of its rows alone, since a weight
           // of 0 times an infinity in V would not be 0.
@@ -270,9 +352,9 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(PagedAttnArgs a) {
 #pragma unroll
               for (int e = 0; e < 8; ++e)
                 if (kbase + e > pos0 + j) v[e] = 0;
-              const f32x4 r = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              const f32x4 o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
                   __builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, pbits), acc[t][d], 0, 0, 0);
-              acc[t][d] = mine ? r : acc[t][d];
+              acc[t][d] = mine ? o : acc[t][d];
             }
           }
         } else {
@@ -282,6 +364,49 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(PagedAttnArgs a) {
             acc[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[d]),
                                                                 pf, acc[t][d], 0, 0, 0);
         }
+      }
+    };
+    // Pairs that every row sees whole, and the one or few at the block's end.  A list's
+    // pages come in any order: each pair looks whether its keys end.
+    const int p_cut = LIST ? p_end : min(p_end, max(max(pos0 + 1, 0) / kPair, p_begin));
+    int pr = p_begin + wave;
+    typedef std::integral_constant<Cut, LIST ? kLimit : kNone> Main;
+    if constexpr (kAhead) {
+      // The next pair's bytes are in flight while one is used, in two buffers in turn, and
+      // the page after it is looked up.  Past the end the last pair stands in.  (A third
+      // buffer, and refilling each behind its use, measured the same or up to 8% slower.)
+      if (pr < p_cut) {
+        auto next = [&](int i) { return i + kWaves < p_cut ? i + kWaves : i; };
+        Raw r[2];
+        load(look(pr), r[0]);
+        int fetch = next(pr);
+        Pair ahead = look(fetch);
+        for (bool more = true; more;) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            load(ahead, r[1 - i]);
+            fetch = next(fetch);
+            ahead = look(fetch);
+            __builtin_amdgcn_sched_barrier(0);
+            use(r[i], Main{});
+            pr += kWaves;
+            more = pr < p_cut;
+            if (!more) break;
+          }
+        }
+      }
+    } else {
+      for (; pr < p_cut; pr += kWaves) {
+        Raw r;
+        load(look(pr), r);
+        use(r, Main{});
+      }
+    }
+    if constexpr (!LIST) {
+      for (; pr < p_end; pr += kWaves) {
+        Raw r;
+        load(look(pr), r);
+        use(r, std::integral_constant<Cut, kToken>{});
       }
     }
 
@@ -346,43 +471,87 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(PagedAttnArgs a) {
 }
 
 // Merges the pieces of each unit, and writes zeros for the rows of a unit that sees
-// no key.  A work group per (unit, KV head); 16 lanes a row, pieces in slot order.
+// no key.  A work group per (unit, KV head, four rows): 16 lanes a row, wave v taking
+// pieces v, v + 4, .. in order, four loads of each in flight, then the four results in
+// wave order.
 template <int DH>
 __global__ __launch_bounds__(kThreads) void paged_merge_kernel(PagedAttnArgs a, int rows_per_unit) {
   constexpr int DPL = DH / 16;
-  __shared__ int red[kWaves];
+  __shared__ int red[2][kWaves];
+  __shared__ float sh[kWaves - 1][64][DPL + 2];
   const int u = blockIdx.x, g = blockIdx.y, G = a.n_q_heads / a.n_kv_heads;
-  const Split split = split_of(a, red);
-  int mine = 0, first;
-  for (int v = threadIdx.x; v < u; v += blockDim.x) mine += unit_pairs(a, v);
-  group_scan(mine, red, &first);
-  const int pairs = unit_pairs(a, u), w0 = first / split.per;
-  const int w1 = (first + pairs - 1) / split.per;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  int all = 0, before = 0;
+  for (int v = threadIdx.x; v < a.n_units; v += kThreads) {
+    const int n = unit_pairs(a, v);
+    all += n;
+    before += v < u ? n : 0;
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    all += __shfl_xor(all, o, 64);
+    before += __shfl_xor(before, o, 64);
+  }
+  if (lane == 0) {
+    red[0][wave] = all;
+    red[1][wave] = before;
+  }
+  __syncthreads();
+  const int total = red[0][0] + red[0][1] + red[0][2] + red[0][3];
+  const int first = red[1][0] + red[1][1] + red[1][2] + red[1][3];
+  const int per = max((total + a.n_groups - 1) / a.n_groups, a.min_pairs);
+  const int pairs = unit_pairs(a, u), w0 = first / per;
+  const int w1 = pairs > 0 ? (first + pairs - 1) / per : w0 - 1;
   if (pairs > 0 && w0 == w1) return;
   const int b = u / a.blocks_per_seq, j0 = u % a.blocks_per_seq * a.tok_per_block;
-  const int rows = min(a.tok_per_block, a.n_q - j0) * G;
-  const int d0 = (threadIdx.x & 15) * DPL;
-  for (int row = threadIdx.x / 16; row < rows; row += kThreads / 16) {
-    float m = -INFINITY, l = 0.f, o[DPL];
+  const int rows = min(a.tok_per_block, a.n_q - j0) * G, row = blockIdx.z * 4 + lane / 16;
+  if (blockIdx.z * 4 >= rows) return;
+  const int d0 = (lane & 15) * DPL, r = min(row, rows - 1);
+  float m = -INFINITY, l = 0.f, o[DPL];
 #pragma unroll
-    for (int e = 0; e < DPL; ++e) o[e] = 0.f;
-    if (pairs > 0) {
-      for (int w = w0; w <= w1; ++w) {
-        const int64_t pr = (((int64_t)w + u) * a.n_kv_heads + g) * rows_per_unit + row;
-        const float mi = a.part_ml[pr * 2], li = a.part_ml[pr * 2 + 1];
-        const float mn = fmaxf(m, mi), mu = mn == -INFINITY ? 0.f : mn;
-        const float so = exp2f(m - mu), si = exp2f(mi - mu);
-        l = l * so + li * si;
+  for (int e = 0; e < DPL; ++e) o[e] = 0.f;
+  auto join = [&](float mi, float li, const float* oi) {
+    const float mn = fmaxf(m, mi), mu = mn == -INFINITY ? 0.f : mn;
+    const float so = exp2f(m - mu), si = exp2f(mi - mu);
+    l = l * so + li * si;
 #pragma unroll
-        for (int e = 0; e < DPL; ++e) o[e] = o[e] * so + a.part_acc[pr * DH + d0 + e] * si;
-        m = mn;
-      }
+    for (int e = 0; e < DPL; ++e) o[e] = o[e] * so + oi[e] * si;
+    m = mn;
+  };
+  for (int w = w0 + wave; w <= w1; w += 4 * kWaves) {
+    float2 ml[4];
+    float x[4][DPL];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t pr =
+          (((int64_t)min(w + i * kWaves, w1) + u) * a.n_kv_heads + g) * rows_per_unit + r;
+      ml[i] = *(const float2*)(a.part_ml + pr * 2);
+#pragma unroll
+      for (int e = 0; e < DPL; e += 4) *(f32x4*)(x[i] + e) = *(const f32x4*)(a.part_acc + pr * DH + d0 + e);
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    uint16_t* dst = (uint16_t*)a.out +
-                    (((int64_t)b * a.n_q + j0 + row / G) * a.n_q_heads + g * G + row % G) * DH + d0;
 #pragma unroll
-    for (int e = 0; e < DPL; ++e) dst[e] = f32_to_bf16(o[e] * inv);
+    for (int i = 0; i < 4; ++i)
+      if (w + i * kWaves <= w1) join(ml[i].x, ml[i].y, x[i]);
+  }
+  if (wave > 0) {
+    float* d = sh[wave - 1][lane];
+    d[0] = m;
+    d[1] = l;
+#pragma unroll
+    for (int e = 0; e < DPL; ++e) d[2 + e] = o[e];
+  }
+  __syncthreads();
+  if (wave > 0 || row >= rows) return;
+#pragma unroll
+  for (int v = 0; v < kWaves - 1; ++v) join(sh[v][lane][0], sh[v][lane][1], &sh[v][lane][2]);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  uint16_t* dst = (uint16_t*)a.out +
+                  (((int64_t)b * a.n_q + j0 + row / G) * a.n_q_heads + g * G + row % G) * DH + d0;
+#pragma unroll
+  for (int e = 0; e < DPL; e += 4) {
+    const f32x2 lo = {o[e] * inv, o[e + 1] * inv}, hi = {o[e + 2] * inv, o[e + 3] * inv};
+    *(u32x2*)(dst + e) = u32x2{__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2)),
+                               __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2))};
   }
 }
 
@@ -391,7 +560,7 @@ __global__ __launch_bounds__(kThreads) void paged_merge_kernel(PagedAttnArgs a, 
 // Row tiles per block of query rows.
 static int row_tiles(int n_q, int group) {
   const int rows = n_q * group;
-  return rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  return rows <= 16 ? 1 : 2;
 }
 
 PagedAttnPlan plan_paged_attention(int batch, int n_q, int n_q_heads, int n_kv_heads) {
@@ -401,7 +570,7 @@ PagedAttnPlan plan_paged_attention(int batch, int n_q, int n_q_heads, int n_kv_h
   p.tok_per_block = 16 * p.row_tiles / G;
   p.blocks_per_seq = (n_q + p.tok_per_block - 1) / p.tok_per_block;
   p.n_units = (int64_t)batch * p.blocks_per_seq;
-  p.n_groups = std::max(1, 1536 / n_kv_heads);
+  p.n_groups = std::max(1, kGroups / n_kv_heads);
   return p;
 }
 
@@ -410,14 +579,13 @@ hipError_t launch_paged_attention(int kv_fp8, int head_dim, int row_tiles, const
   const dim3 grid(a.n_kv_heads, a.n_groups), block(kThreads);
 #define PDEC_PAGED(DH_, RT_, KT_)                                                       \
   do {                                                                                  \
-    if (a.selected) paged_attn_kernel<DH_, RT_, KT_, true><<<grid, block, 0, stream>>>(a);  \
-    else paged_attn_kernel<DH_, RT_, KT_, false><<<grid, block, 0, stream>>>(a);        \
+    if (a.selected) paged_attn_kernel<DH_, RT_, KT_, true><<<grid, block, 0, stream>>>(a, a.block_table, a.selected);  \
+    else paged_attn_kernel<DH_, RT_, KT_, false><<<grid, block, 0, stream>>>(a, a.block_table, a.selected);        \
   } while (0)
 #define PDEC_PAGED_RT(DH_, KT_)                    \
   do {                                             \
     if (row_tiles == 1) PDEC_PAGED(DH_, 1, KT_);   \
-    else if (row_tiles == 2) paged_attn_kernel<DH_, 2, KT_, false><<<grid, block, 0, stream>>>(a); \
-    else paged_attn_kernel<DH_, 4, KT_, false><<<grid, block, 0, stream>>>(a);             \
+    else paged_attn_kernel<DH_, 2, KT_, false><<<grid, block, 0, stream>>>(a, a.block_table, a.selected);     \
   } while (0)
   if (head_dim == 128) {
     if (kv_fp8) PDEC_PAGED_RT(128, uint8_t);
@@ -430,7 +598,8 @@ hipError_t launch_paged_attention(int kv_fp8, int head_dim, int row_tiles, const
 #undef PDEC_PAGED
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const dim3 mgrid(a.n_units, a.n_kv_heads);
+  const int rows = std::min(a.tok_per_block, a.n_q) * (a.n_q_heads / a.n_kv_heads);
+  const dim3 mgrid(a.n_units, a.n_kv_heads, (rows + 3) / 4);
   if (head_dim == 128)
     paged_merge_kernel<128><<<mgrid, block, 0, stream>>>(a, 16 * row_tiles);
   else

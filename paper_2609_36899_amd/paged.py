@@ -10,6 +10,7 @@ is enqueued.
 from __future__ import annotations
 
 import contextlib
+import functools
 from typing import Optional
 
 import torch
@@ -18,76 +19,106 @@ from . import _native as N
 from ._native import PAGE_TOKENS, PdecError
 
 _KV_DTYPE = {torch.float32: N.F32, torch.bfloat16: N.BF16, torch.uint8: N.FP8_E4M3}
+_F32, _BF16, _I32 = torch.float32, torch.bfloat16, torch.int32
+
+# A decode step makes these calls many times a millisecond, so what is right is found by
+# few, cheap looks at a tensor, and what is wrong with it only then (10 us of a call of
+# 38 went into messages that nobody read).
 
 
-def _need(ok: bool, what: str) -> None:
-    if not ok:
-        raise PdecError(N.INVALID_ARG, what)
+def _refuse(what: str):
+    raise PdecError(N.INVALID_ARG, what)
 
 
-def _tensor(t, name: str, dtype, shape, device) -> None:
-    """A contiguous GPU tensor of this type and shape (None: any size)."""
-    _need(isinstance(t, torch.Tensor) and t.is_cuda, f"{name} must be a GPU tensor")
-    _need(device is None or t.device == device, f"{name} is on another device")
-    _need(t.dtype == dtype, f"{name} must be {dtype}")
-    _need(t.dim() == len(shape) and all(n is None or n == m for n, m in zip(shape, t.shape)),
-          f"{name} must have shape {tuple('*' if n is None else n for n in shape)}, "
-          f"not {tuple(t.shape)}")
-    _need(t.is_contiguous(), f"{name} must be contiguous")
+def _bad_tensor(t, name: str, dtype, shape, dev: int):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        _refuse(f"{name} must be a GPU tensor")
+    if t.get_device() != dev:
+        _refuse(f"{name} is on another device")
+    if t.dtype != dtype:
+        _refuse(f"{name} must be {dtype}, not {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        _refuse(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+    _refuse(f"{name} must be contiguous")
 
 
-def _rows(t, name: str, heads, head_dim, device):
-    """Rows of [heads][head_dim], any distance apart: what a slice of q|k|v rows is."""
-    _need(isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 3,
-          f"{name} must be a GPU tensor [rows][heads][head_dim]")
-    _need(device is None or t.device == device, f"{name} is on another device")
-    n, h, d = t.shape
-    _need((heads is None or h == heads) and (head_dim is None or d == head_dim),
-          f"{name} has other heads")
-    _need(n == 0 or (t.stride(2) == 1 and (h == 1 or t.stride(1) == d)
-                     and (n == 1 or t.stride(0) >= h * d)),
-          f"{name}'s heads must lie side by side")
-    return t.stride(0) if n > 1 else h * d
+def _check(t, name: str, dtype, shape, dev: int) -> None:
+    """A contiguous tensor of this type and shape on GPU dev."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape
+            and t.get_device() == dev and t.is_contiguous()):
+        _bad_tensor(t, name, dtype, shape, dev)
+
+
+def _dims(t, name: str, n: int):
+    """The sizes of a GPU tensor of n dims."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != n:
+        _refuse(f"{name} must be a GPU tensor of {n} dims")
+    return t.shape
+
+
+def _rows(t, name: str, dtype, shape, dev: int) -> int:
+    """Row distance of rows of [heads][head_dim], any distance apart: what a slice of
+    q|k|v rows is."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
+        _bad_tensor(t, name, dtype, shape, dev)
+    n, h, d = shape
+    row, head, one = t.stride()
+    if not (one == 1 and (head == d or h == 1) and (row >= h * d or n <= 1)) and n:
+        _refuse(f"{name}'s heads must lie side by side in a row")
+    return row if n > 1 else h * d
 
 
 class _Call:
-    """The device and stream of a call, and its workspace."""
+    """The stream of a call on GPU dev, and its workspace."""
 
-    def __init__(self, device: torch.device, stream: Optional[torch.cuda.Stream]):
-        self.device, self.stream = device, stream
-        _need(stream is None or stream.device == device, "stream is on another device")
-        self.guard = (contextlib.nullcontext() if torch.cuda.current_device() == device.index
-                      else torch.cuda.device(device))
-        s = stream if stream is not None else torch.cuda.current_stream(device)
-        self.handle = s.cuda_stream
+    __slots__ = ("dev", "stream", "handle")
+
+    def __init__(self, dev: int, stream: Optional[torch.cuda.Stream]):
+        self.dev, self.stream = dev, stream
+        if stream is None:
+            self.handle = torch._C._cuda_getCurrentRawStream(dev)
+        else:
+            if stream.device_index != dev:
+                _refuse("stream is on another device")
+            self.handle = stream.cuda_stream
 
     def workspace(self, given: Optional[torch.Tensor], need: int) -> torch.Tensor:
-        if given is not None:
-            _need(given.is_cuda and given.device == self.device and given.is_contiguous(),
-                  "workspace must be a contiguous tensor on the call's device")
-            _need(given.numel() * given.element_size() >= need,
-                  f"workspace too small: need {need} bytes")
-            return given
-        if self.stream is None:
-            return torch.empty(need, dtype=torch.uint8, device=self.device)
-        with torch.cuda.stream(self.stream):
-            return torch.empty(need, dtype=torch.uint8, device=self.device)
+        if given is None:
+            if self.stream is None:
+                return torch.empty(need, dtype=torch.uint8, device=self.dev)
+            with torch.cuda.stream(self.stream):
+                return torch.empty(need, dtype=torch.uint8, device=self.dev)
+        if not given.is_cuda or given.get_device() != self.dev or not given.is_contiguous():
+            _refuse("workspace must be a contiguous tensor on the call's device")
+        if given.numel() * given.element_size() < need:
+            _refuse(f"workspace too small: need {need} bytes")
+        return given
+
+    def run(self, fn, *args) -> None:
+        if torch.cuda.current_device() == self.dev:
+            N.check(fn(*args, self.handle))
+        else:
+            with torch.cuda.device(self.dev):
+                N.check(fn(*args, self.handle))
 
 
-def _pages(k_pages, v_pages, k_scales, v_scales, device):
-    """(n_pages, n_kv_heads, head_dim, kv dtype) of a pool."""
-    _need(isinstance(k_pages, torch.Tensor) and k_pages.dim() == 4, "k_pages must have 4 dims")
-    n, hkv, page, dh = k_pages.shape
-    _need(k_pages.dtype in _KV_DTYPE, "pages must be float32, bfloat16 or uint8 (E4M3 codes)")
-    _need(n >= 1 and page == PAGE_TOKENS, f"pages hold {PAGE_TOKENS} tokens")
-    _tensor(k_pages, "k_pages", k_pages.dtype, (n, hkv, PAGE_TOKENS, dh), device)
-    _tensor(v_pages, "v_pages", k_pages.dtype, (n, hkv, dh, PAGE_TOKENS), k_pages.device)
-    fp8 = k_pages.dtype == torch.uint8
-    for t, name in ((k_scales, "k_scales"), (v_scales, "v_scales")):
-        _need((t is not None) == fp8, "E4M3 pages take k_scales and v_scales, the others none")
-        if fp8:
-            _tensor(t, name, torch.float32, (n, hkv), k_pages.device)
-    return n, hkv, dh, _KV_DTYPE[k_pages.dtype]
+def _pages(k_pages, v_pages, k_scales, v_scales):
+    """(n_pages, n_kv_heads, head_dim, kv dtype, device) of a pool."""
+    n, hkv, page, dh = _dims(k_pages, "k_pages", 4)
+    kv = _KV_DTYPE.get(k_pages.dtype)
+    if kv is None:
+        _refuse("pages must be float32, bfloat16 or uint8 (E4M3 codes)")
+    if n < 1 or page != PAGE_TOKENS:
+        _refuse(f"pages hold {PAGE_TOKENS} tokens")
+    dev = k_pages.get_device()
+    _check(k_pages, "k_pages", k_pages.dtype, (n, hkv, PAGE_TOKENS, dh), dev)
+    _check(v_pages, "v_pages", k_pages.dtype, (n, hkv, dh, PAGE_TOKENS), dev)
+    if kv == N.FP8_E4M3 and k_scales is not None and v_scales is not None:
+        _check(k_scales, "k_scales", _F32, (n, hkv), dev)
+        _check(v_scales, "v_scales", _F32, (n, hkv), dev)
+    elif kv == N.FP8_E4M3 or k_scales is not None or v_scales is not None:
+        _refuse("E4M3 pages take k_scales and v_scales, the others none")
+    return n, hkv, dh, kv, dev
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -97,16 +128,13 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 def rope_table(max_pos: int, head_dim: int, base: float = 10000.0, device="cuda",
                stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """The (cos, sin) table [max_pos][head_dim / 2][2] that paged_kv_append rotates by."""
-    _need(max_pos >= 1 and head_dim >= 2 and head_dim % 2 == 0, "bad rotary table size")
-    device = torch.device(device)
-    if device.index is None:
-        device = torch.device("cuda", torch.cuda.current_device())
-    call = _Call(device, stream)
-    with call.guard, (torch.cuda.stream(stream) if stream is not None
-                      else contextlib.nullcontext()):
-        table = torch.empty((max_pos, head_dim // 2, 2), dtype=torch.float32, device=device)
-        N.check(N.load().rope_table(max_pos, head_dim, float(base), table.data_ptr(),
-                                    call.handle))
+    if max_pos < 1 or head_dim < 2 or head_dim % 2:
+        _refuse("bad rotary table size")
+    index = torch.device(device).index
+    call = _Call(torch.cuda.current_device() if index is None else index, stream)
+    with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+        table = torch.empty((max_pos, head_dim // 2, 2), dtype=_F32, device=call.dev)
+    call.run(N.load().rope_table, max_pos, head_dim, float(base), table.data_ptr())
     return table
 
 
@@ -126,40 +154,40 @@ def paged_kv_append(k: torch.Tensor, v: torch.Tensor, lens: torch.Tensor,
     or uint8 (E4M3 codes, with k_scales and v_scales float32 [P][Hkv], which the call
     keeps); k_means bfloat16 [P][Hkv][Dh], kept where given.
     """
-    n_pages, hkv, dh, kv = _pages(k_pages, v_pages, k_scales, v_scales, None)
-    dev = k_pages.device
-    k_stride = _rows(k, "k", hkv, dh, dev)
-    v_stride = _rows(v, "v", hkv, dh, dev)
-    rows = k.shape[0]
-    _need(v.shape[0] == rows and k.dtype == v.dtype, "k and v must agree")
-    _need(k.dtype in (torch.float32, torch.bfloat16), "rows must be float32 or bfloat16")
-    _tensor(lens, "lens", torch.int32, (None,), dev)
-    B = lens.shape[0]
-    _tensor(row_start, "row_start", torch.int32, (B + 1,), dev)
-    _tensor(block_table, "block_table", torch.int32, (B, None), dev)
-    _tensor(rope, "rope", torch.float32, (None, dh // 2, 2), dev)
-    _need((q is None) == (q_out is None), "q and q_out come together")
-    hq, q_stride = 0, 0
+    n_pages, hkv, dh, kv, dev = _pages(k_pages, v_pages, k_scales, v_scales)
+    rows = _dims(k, "k", 3)[0]
+    src = N.BF16 if k.dtype is _BF16 else N.F32
+    dtype = _BF16 if src == N.BF16 else _F32
+    k_stride = _rows(k, "k", dtype, (rows, hkv, dh), dev)
+    _dims(v, "v", 3)
+    v_stride = _rows(v, "v", dtype, (rows, hkv, dh), dev)
+    B = _dims(lens, "lens", 1)[0]
+    _check(lens, "lens", _I32, (B,), dev)
+    _check(row_start, "row_start", _I32, (B + 1,), dev)
+    stride = _dims(block_table, "block_table", 2)[1]
+    _check(block_table, "block_table", _I32, (B, stride), dev)
+    max_pos = _dims(rope, "rope", 3)[0]
+    _check(rope, "rope", _F32, (max_pos, dh // 2, 2), dev)
+    hq = q_stride = 0
     if q is not None:
-        q_stride = _rows(q, "q", None, dh, dev)
-        hq = q.shape[1]
-        _need(q.shape[0] == rows and q.dtype == k.dtype, "q and k must agree")
-        _tensor(q_out, "q_out", torch.float32 if kv == N.F32 else torch.bfloat16, (rows, hq, dh),
-                dev)
+        hq = _dims(q, "q", 3)[1]
+        q_stride = _rows(q, "q", dtype, (rows, hq, dh), dev)
+        _check(q_out, "q_out", _F32 if kv == N.F32 else _BF16, (rows, hq, dh), dev)
+    elif q_out is not None:
+        _refuse("q and q_out come together")
     if k_means is not None:
-        _tensor(k_means, "k_means", torch.bfloat16, (n_pages, hkv, dh), dev)
+        _check(k_means, "k_means", _BF16, (n_pages, hkv, dh), dev)
     call = _Call(dev, stream)
     if rows == 0:
         return
-    with call.guard:
-        N.check(N.load().paged_kv_append(
-            N.F32 if k.dtype == torch.float32 else N.BF16, kv, rows, B, hq, hkv, dh, _ptr(q),
-            q_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride, lens.data_ptr(),
-            row_start.data_ptr(), block_table.data_ptr(), block_table.shape[1], n_pages,
-            rope.data_ptr(), rope.shape[0], _ptr(q_out), k_pages.data_ptr(), v_pages.data_ptr(),
-            _ptr(k_scales), _ptr(v_scales), _ptr(k_means), call.handle))
+    call.run(N.load().paged_kv_append, src, kv, rows, B, hq, hkv, dh, _ptr(q), q_stride,
+             k.data_ptr(), k_stride, v.data_ptr(), v_stride, lens.data_ptr(),
+             row_start.data_ptr(), block_table.data_ptr(), stride, n_pages, rope.data_ptr(),
+             max_pos, _ptr(q_out), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(k_scales),
+             _ptr(v_scales), _ptr(k_means))
 
 
+@functools.lru_cache(maxsize=1024)
 def paged_token_attention_workspace_bytes(batch: int, n_q: int, n_q_heads: int, n_kv_heads: int,
                                           head_dim: int) -> int:
     return N.check(N.load().paged_token_attention_workspace_bytes(batch, n_q, n_q_heads,
@@ -180,32 +208,34 @@ def paged_token_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch
     k_scales and v_scales float32 [P][Hkv]; selected int32 [B][Hkv][n], one token each:
     the logical pages to read instead of all.
     """
-    n_pages, hkv, dh, kv = _pages(k_pages, v_pages, k_scales, v_scales, None)
-    dev = k_pages.device
-    _need(kv != N.F32, "pages must be bfloat16 or uint8")
-    _need(isinstance(q, torch.Tensor) and q.dim() in (3, 4), "q must be [B][n_q][Hq][Dh]")
-    B, hq, n_q = q.shape[0], q.shape[-2], q.shape[1] if q.dim() == 4 else 1
-    _tensor(q, "q", torch.bfloat16, (*q.shape[:-1], dh), dev)
-    _tensor(out, "out", torch.bfloat16, tuple(q.shape), dev)
-    _tensor(block_table, "block_table", torch.int32, (B, None), dev)
-    _tensor(lens, "lens", torch.int32, (B,), dev)
+    n_pages, hkv, dh, kv, dev = _pages(k_pages, v_pages, k_scales, v_scales)
+    if kv == N.F32:
+        _refuse("pages must be bfloat16 or uint8")
+    four = isinstance(q, torch.Tensor) and q.dim() == 4
+    shape = _dims(q, "q", 4 if four else 3)
+    B, n_q, hq = shape[0], shape[1] if four else 1, shape[-2]
+    want = (*shape[:-1], dh)
+    _check(q, "q", _BF16, want, dev)
+    _check(out, "out", _BF16, want, dev)
+    stride = _dims(block_table, "block_table", 2)[1]
+    _check(block_table, "block_table", _I32, (B, stride), dev)
+    _check(lens, "lens", _I32, (B,), dev)
+    n_sel = 0
     if selected is not None:
-        _need(n_q == 1, "selected pages take one query token")
-        _tensor(selected, "selected", torch.int32, (B, hkv, None), dev)
-    lib = N.load()
+        if n_q != 1:
+            _refuse("selected pages take one query token")
+        n_sel = _dims(selected, "selected", 3)[2]
+        _check(selected, "selected", _I32, (B, hkv, n_sel), dev)
     call = _Call(dev, stream)
-    with call.guard:
-        ws = call.workspace(workspace, N.check(
-            lib.paged_token_attention_workspace_bytes(B, n_q, hq, hkv, dh)))
-        N.check(lib.paged_token_attention(
-            kv, B, n_q, hq, hkv, dh, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
-            _ptr(k_scales), _ptr(v_scales), n_pages, block_table.data_ptr(),
-            block_table.shape[1], lens.data_ptr(), _ptr(selected),
-            0 if selected is None else selected.shape[2], out.data_ptr(), ws.data_ptr(),
-            ws.numel() * ws.element_size(), call.handle))
+    ws = call.workspace(workspace, paged_token_attention_workspace_bytes(B, n_q, hq, hkv, dh))
+    call.run(N.load().paged_token_attention, kv, B, n_q, hq, hkv, dh, q.data_ptr(),
+             k_pages.data_ptr(), v_pages.data_ptr(), _ptr(k_scales), _ptr(v_scales), n_pages,
+             block_table.data_ptr(), stride, lens.data_ptr(), _ptr(selected), n_sel,
+             out.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size())
     return out
 
 
+@functools.lru_cache(maxsize=1024)
 def paged_select_workspace_bytes(batch: int, n_kv_heads: int, bt_stride: int) -> int:
     return N.check(N.load().paged_select_workspace_bytes(batch, n_kv_heads, bt_stride))
 
@@ -219,27 +249,25 @@ def paged_select(q: torch.Tensor, k_means: torch.Tensor, block_table: torch.Tens
 
     q bfloat16 [B][Hq][Dh], k_means bfloat16 [P][Hkv][Dh] as paged_kv_append keeps
     them, block_table int32 [B][stride] and lens int32 [B] on the GPU."""
-    _need(isinstance(k_means, torch.Tensor) and k_means.dim() == 3, "k_means must have 3 dims")
-    n_pages, hkv, dh = k_means.shape
-    _tensor(k_means, "k_means", torch.bfloat16, (None, hkv, dh), None)
-    dev = k_means.device
-    _tensor(q, "q", torch.bfloat16, (None, None, dh), dev)
-    B, hq, _ = q.shape
-    _tensor(block_table, "block_table", torch.int32, (B, None), dev)
-    _tensor(lens, "lens", torch.int32, (B,), dev)
-    _tensor(selected, "selected", torch.int32, (B, hkv, None), dev)
-    lib = N.load()
+    n_pages, hkv, dh = _dims(k_means, "k_means", 3)
+    dev = k_means.get_device()
+    _check(k_means, "k_means", _BF16, (n_pages, hkv, dh), dev)
+    B, hq, _ = _dims(q, "q", 3)
+    _check(q, "q", _BF16, (B, hq, dh), dev)
+    stride = _dims(block_table, "block_table", 2)[1]
+    _check(block_table, "block_table", _I32, (B, stride), dev)
+    _check(lens, "lens", _I32, (B,), dev)
+    n_sel = _dims(selected, "selected", 3)[2]
+    _check(selected, "selected", _I32, (B, hkv, n_sel), dev)
     call = _Call(dev, stream)
-    stride = block_table.shape[1]
-    with call.guard:
-        ws = call.workspace(workspace, N.check(lib.paged_select_workspace_bytes(B, hkv, stride)))
-        N.check(lib.paged_select(
-            B, hq, hkv, dh, q.data_ptr(), k_means.data_ptr(), n_pages, block_table.data_ptr(),
-            stride, lens.data_ptr(), selected.shape[2], int(keep_first), int(keep_last),
-            selected.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(), call.handle))
+    ws = call.workspace(workspace, paged_select_workspace_bytes(B, hkv, stride))
+    call.run(N.load().paged_select, B, hq, hkv, dh, q.data_ptr(), k_means.data_ptr(), n_pages,
+             block_table.data_ptr(), stride, lens.data_ptr(), n_sel, int(keep_first),
+             int(keep_last), selected.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size())
     return selected
 
 
+@functools.lru_cache(maxsize=1024)
 def verify_drafts_workspace_bytes(batch: int, n_drafts: int, vocab: int,
                                   with_drafter: bool) -> int:
     return N.check(N.load().verify_drafts_workspace_bytes(batch, n_drafts, vocab,
@@ -257,23 +285,20 @@ def verify_drafts(target_logits: torch.Tensor, draft_tokens: torch.Tensor,
     target_logits float32 [B][n + 1][V], draft_tokens int32 [B][n], uniforms float32
     [B][n + 1], draft_logits float32 [B][n][V] or None; tokens_out int32 [B][n + 1],
     accepted_out int32 [B]."""
-    _tensor(target_logits, "target_logits", torch.float32, (None, None, None), None)
-    dev = target_logits.device
-    B, rows, V = target_logits.shape
-    n = rows - 1
-    _tensor(draft_tokens, "draft_tokens", torch.int32, (B, n), dev)
-    _tensor(uniforms, "uniforms", torch.float32, (B, rows), dev)
-    _tensor(tokens_out, "tokens_out", torch.int32, (B, rows), dev)
-    _tensor(accepted_out, "accepted_out", torch.int32, (B,), dev)
+    B, rows, V = _dims(target_logits, "target_logits", 3)
+    n, dev = rows - 1, target_logits.get_device()
+    _check(target_logits, "target_logits", _F32, (B, rows, V), dev)
+    _check(draft_tokens, "draft_tokens", _I32, (B, n), dev)
+    _check(uniforms, "uniforms", _F32, (B, rows), dev)
+    _check(tokens_out, "tokens_out", _I32, (B, rows), dev)
+    _check(accepted_out, "accepted_out", _I32, (B,), dev)
     if draft_logits is not None:
-        _tensor(draft_logits, "draft_logits", torch.float32, (B, n, V), dev)
-    lib = N.load()
+        _check(draft_logits, "draft_logits", _F32, (B, n, V), dev)
     call = _Call(dev, stream)
-    with call.guard:
-        ws = call.workspace(workspace, N.check(
-            lib.verify_drafts_workspace_bytes(B, n, V, int(draft_logits is not None))))
-        N.check(lib.verify_drafts(
-            B, n, V, target_logits.data_ptr(), _ptr(draft_logits), draft_tokens.data_ptr(),
-            uniforms.data_ptr(), float(temperature), tokens_out.data_ptr(),
-            accepted_out.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(), call.handle))
+    ws = call.workspace(workspace,
+                        verify_drafts_workspace_bytes(B, n, V, draft_logits is not None))
+    call.run(N.load().verify_drafts, B, n, V, target_logits.data_ptr(), _ptr(draft_logits),
+             draft_tokens.data_ptr(), uniforms.data_ptr(), float(temperature),
+             tokens_out.data_ptr(), accepted_out.data_ptr(), ws.data_ptr(),
+             ws.numel() * ws.element_size())
     return tokens_out
