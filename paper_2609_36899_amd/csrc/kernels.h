@@ -224,7 +224,8 @@ struct VerifyArgs {  // verify.hip
   const float* uniforms;
   int32_t *tokens, *accepted;
   int32_t batch, n_drafts, vocab;
-  double inv_t;
+  float temperature;
+  double inv_t;  // 1 / temperature
   void* workspace;
 };
 int64_t verify_workspace_bytes(int batch, int n_drafts, bool drafter, int vocab);

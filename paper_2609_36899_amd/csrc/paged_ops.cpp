@@ -216,6 +216,8 @@ int paged_select(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t h
   int rc = check_heads(n_q_heads, n_kv_heads, head_dim);
   if (rc == PDEC_OK) rc = check_table(batch, bt_stride, n_pages);
   if (rc != PDEC_OK) return rc;
+  if ((int64_t)batch * n_kv_heads > INT32_MAX)
+    return fail(PDEC_INVALID_ARG, "batch x n_kv_heads too large for one call");
   if (n_selected < 1 || n_selected > kMaxStride || keep_first < 0 || keep_last < 1 ||
       (int64_t)keep_first + keep_last > n_selected)
     return fail(PDEC_INVALID_ARG,
@@ -280,6 +282,7 @@ int verify_drafts(int32_t batch, int32_t n_drafts, int32_t vocab, const float* t
   a.n_drafts = n_drafts;
   a.vocab = vocab;
   a.inv_t = 1.0 / (double)temperature;
+  a.temperature = temperature;
   a.workspace = workspace;
   HIP_OR_FAIL(launch_verify(a, (hipStream_t)stream));
   return PDEC_OK;

@@ -19,136 +19,278 @@ namespace pdec {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kScorePages = 64;  // pages of one work group of the score pass
+constexpr int kTile = 16;  // pages a wave scores at a time
 
-__device__ __forceinline__ int seq_pages(const SelectArgs& a, int b) {
-  const int len = max(a.lens[b], 0);
-  return min(len / kPage + (len % kPage != 0), a.bt_stride);
+__device__ __forceinline__ int seq_pages(const int32_t* lens, int b, int bt_stride) {
+  const int len = max(lens[b], 0);
+  return min(len / kPage + (len % kPage != 0), bt_stride);
 }
 
-// 16 lanes per (page, KV head), DH / 16 dims each.
-template <int DH>
-__global__ __launch_bounds__(kThreads) void page_scores_kernel(SelectArgs a) {
-  constexpr int E = DH / 16;
-  const int b = blockIdx.x, p0 = blockIdx.y * kScorePages;
-  const int n = min(seq_pages(a, b) - p0, kScorePages);
-  const int G = a.n_q_heads / a.n_kv_heads, d0 = (threadIdx.x & 15) * E;
-  for (int t = threadIdx.x / 16; t < n * a.n_kv_heads; t += kThreads / 16) {
-    const int p = p0 + t / a.n_kv_heads, g = t % a.n_kv_heads;
-    const int page = a.block_table[(int64_t)b * a.bt_stride + p];
-    double best = -INFINITY;
-    if (page >= 0 && page < a.n_pages) {
-      const uint16_t* src = a.k_means + ((int64_t)page * a.n_kv_heads + g) * DH + d0;
-      double mean[E];
+// Scores.  A wave takes tiles of 16 pages of one (sequence, KV head).  The product runs
+// on v_mfma_f64_4x4x4_4b, whose four blocks of 4 x 4 x 4 multiply 16 pages with four
+// query heads, every lane busy and no sum across lanes: lane l holds page l % 16 and the
+// dims 32 j + 8 (l / 16) + e of chunk j, one 16-byte load each, and the same dims of
+// query head l % 4; result lane l has page 4 (l / 4 % 4) + l / 16 and head l % 4.  The
+// next tile's means are in flight meanwhile.  The bound is HBM (Dh bf16 a page and KV
+// head).  With 16 lanes a page, fp64 multiply-adds and sums by shuffles, 64 sequences of
+// 8K to 32K took 159 us.
+template <int DH, bool MANY>  // MANY: more than four query heads, kept in LDS
+__global__ __launch_bounds__(kThreads) void page_scores_kernel(
+    SelectArgs a, const int32_t* __restrict__ table, const int32_t* __restrict__ lens,
+    int group_pages) {
+  constexpr int NJ = DH / 32;
+  __shared__ double qs[MANY ? 4 : 1][NJ * 8][16];
+  const int b = blockIdx.x / a.n_kv_heads, g = blockIdx.x % a.n_kv_heads;
+  const int n = seq_pages(lens, b, a.bt_stride);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int begin = blockIdx.y * group_pages, end = min(begin + group_pages, n);
+  if (begin >= end) return;
+  const int c16 = lane & 15, k4 = lane >> 4;
+  const int G = a.n_q_heads / a.n_kv_heads, n_hg = MANY ? (G + 3) / 4 : 1;
+  const uint16_t* q0 = a.q + ((int64_t)b * a.n_q_heads + g * G) * DH;
+  // Groups of four heads; past the last one the first stands in, which moves no maximum.
+  auto q_at = [&](int hg, int j, int col, int k) {
+    const int h = 4 * hg + col;
+    return *(const u16x8*)(q0 + (int64_t)(h < G ? h : 0) * DH + j * 32 + k * 8);
+  };
+  double q[NJ * 8];
+  if constexpr (MANY) {
+    for (int i = threadIdx.x; i < n_hg * NJ * 16; i += kThreads) {
+      const int l = i % 16, j = i / 16 % NJ, hg = i / 16 / NJ;
+      const u16x8 v = q_at(hg, j, l % 4, l / 4);
 #pragma unroll
-      for (int e = 0; e < E; ++e) mean[e] = bf16_to_f32(src[e]);
-      for (int h = 0; h < G; ++h) {
-        const uint16_t* q = a.q + ((int64_t)b * a.n_q_heads + g * G + h) * DH + d0;
-        double s = 0.0;
-#pragma unroll
-        for (int e = 0; e < E; ++e) s += mean[e] * bf16_to_f32(q[e]);
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) s += __shfl_xor(s, o, 16);
-        best = fmax(best, s);  // a NaN never wins
-      }
+      for (int e = 0; e < 8; ++e) qs[hg][j * 8 + e][l] = bf16_to_f32(v[e]);
     }
-    if ((threadIdx.x & 15) == 0)
-      a.scores[((int64_t)b * a.n_kv_heads + g) * a.bt_stride + p] =
-          fminf(fmaxf((float)best, -FLT_MAX), FLT_MAX);
+    __syncthreads();
+  } else {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const u16x8 v = q_at(0, j, lane & 3, k4);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) q[j * 8 + e] = bf16_to_f32(v[e]);
+    }
+  }
+  const int32_t* bt = table + (int64_t)b * a.bt_stride;
+  auto page_of = [&](int p0) { return bt[min(p0 + c16, end - 1)]; };
+  auto load = [&](int page, u16x8(&m)[NJ]) {
+    const bool ok = page >= 0 && page < a.n_pages;
+    const uint16_t* src = a.k_means + ((int64_t)(ok ? page : 0) * a.n_kv_heads + g) * DH + k4 * 8;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) m[j] = load_stream<u16x8>(src + j * 32);
+  };
+  constexpr int kStep = kWaves * kTile;
+  int p0 = begin + wave * kTile;
+  if (p0 >= end) return;
+  float* scores = a.scores + (int64_t)blockIdx.x * a.bt_stride;
+  u16x8 next[NJ];
+  int page = page_of(p0), page1 = page_of(p0 + kStep);
+  load(page, next);
+  for (; p0 < end; p0 += kStep) {
+    u16x8 m[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) m[j] = next[j];
+    const bool ok = page >= 0 && page < a.n_pages;
+    page = page1;
+    if (p0 + kStep < end) {
+      load(page, next);
+      page1 = page_of(p0 + 2 * kStep);
+    }
+    double best = -INFINITY;
+    for (int hg = 0; hg < n_hg; ++hg) {
+      double s = 0.0;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          s = __builtin_amdgcn_mfma_f64_4x4x4f64((double)bf16_to_f32(m[j][e]),
+                                                 MANY ? qs[hg][j * 8 + e][k4 * 4 + (lane & 3)]
+                                                      : q[j * 8 + e],
+                                                 s, 0, 0, 0);
+      best = fmax(best, s);  // a NaN never wins
+    }
+    best = fmax(best, __shfl_xor(best, 1, 64));
+    best = fmax(best, __shfl_xor(best, 2, 64));
+    const int i = 4 * ((lane >> 2) & 3) + k4;  // the page of this lane's result
+    const bool named = __shfl((int)ok, i, 64);
+    if ((lane & 3) == 0 && p0 + i < end)
+      scores[p0 + i] = named ? fminf(fmaxf((float)best, -FLT_MAX), FLT_MAX) : -FLT_MAX;
   }
 }
 
-__device__ __forceinline__ int group_scan(int v, int* red, int* total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int incl = v;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int t = __shfl_up(incl, o, 64);
-    if (lane >= o) incl += t;
-  }
-  __syncthreads();
-  if (lane == 63) red[wave] = incl;
-  __syncthreads();
-  int before = incl - v, sum = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    before += w < wave ? red[w] : 0;
-    sum += red[w];
-  }
-  *total = sum;
-  return before;
-}
-
-// One work group per (sequence, KV head): the threshold by a radix select over the
-// order-preserving bits of the scores, eight at a time, then the list in page order.
-__global__ __launch_bounds__(kThreads) void take_pages_kernel(SelectArgs a) {
-  __shared__ int hist[256];
-  __shared__ int red[kWaves];
-  __shared__ int pick[2];
-  const int b = blockIdx.x, g = blockIdx.y, n = seq_pages(a, b);
-  const float* score = a.scores + ((int64_t)b * a.n_kv_heads + g) * a.bt_stride;
-  int32_t* out = a.selected + ((int64_t)b * a.n_kv_heads + g) * a.n_selected;
+// The list: one work group of T threads per (sequence, KV head).  The threshold is found
+// by histograms of T bins over the range that the wanted score lies in, at first from the
+// lowest to the highest of them, so that floats of one size spread over the bins: two or
+// three rounds, and none once a bin is taken whole.  Keys wait in LDS between the rounds.
+// Page order comes from ballots and one scan of the waves' counts.  Eight bits at a time
+// from the top of the float, pages one scan a step, took 57 us for 8188 pages.
+template <int T>
+__global__ __launch_bounds__(T) void take_pages_kernel(SelectArgs a) {
+  constexpr int W = T / 64, BITS = T == 1024 ? 10 : 8, CACHE = 8 * T, STEPS = 8;
+  __shared__ uint32_t keys[CACHE];
+  __shared__ int hist[T];
+  __shared__ int red[2][W];
+  __shared__ uint32_t range[2][W];
+  __shared__ int count[2][STEPS * W];
+  __shared__ int pick[3];
+  const int b = blockIdx.x / a.n_kv_heads, n = seq_pages(a.lens, b, a.bt_stride);
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const float* score = a.scores + (int64_t)blockIdx.x * a.bt_stride;
+  int32_t* out = a.selected + (int64_t)blockIdx.x * a.n_selected;
   const int take = min(n, a.n_selected);
-  for (int i = take + threadIdx.x; i < a.n_selected; i += kThreads) out[i] = -1;
+  for (int i = take + threadIdx.x; i < a.n_selected; i += T) out[i] = -1;
   if (take == n) {
-    for (int i = threadIdx.x; i < n; i += kThreads) out[i] = i;
+    for (int i = threadIdx.x; i < n; i += T) out[i] = i;
     return;
   }
-  // Larger key, better page; kept pages above every score.
-  auto key_of = [&](int i) -> uint32_t {
-    if (i < a.keep_first || i >= n - a.keep_last) return 0xFFFFFFFFu;
+  // Larger key, larger score.
+  auto read = [&](int i) {
     const uint32_t u = __float_as_uint(score[i] + 0.f);  // -0 counts as 0
     return u & 0x80000000u ? ~u : u | 0x80000000u;
   };
-  uint32_t prefix = 0;
-  int left = take;  // pages still to be taken among those with the prefix
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    hist[threadIdx.x] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-      const uint32_t k = key_of(i);
-      if (shift == 24 || (k ^ prefix) >> (shift + 8) == 0) atomicAdd(&hist[(k >> shift) & 255], 1);
+  auto key_at = [&](int i) { return i < CACHE ? keys[i] : read(i); };
+  auto kept = [&](int i) { return i < a.keep_first || i >= n - a.keep_last; };
+  uint32_t lo = 0xFFFFFFFFu, hi = 0;
+  for (int i = threadIdx.x; i < n; i += T) {
+    const uint32_t k = read(i);
+    if (i < CACHE) keys[i] = k;
+    if (!kept(i)) {
+      lo = min(lo, k);
+      hi = max(hi, k);
     }
-    __syncthreads();
-    // Bins from the top: thread t holds bin 255 - t.
-    int total;
-    const int c = hist[255 - threadIdx.x], above = group_scan(c, red, &total);
-    if (above < left && left <= above + c) {
-      pick[0] = 255 - threadIdx.x;
-      pick[1] = left - above;
-    }
-    __syncthreads();
-    prefix |= (uint32_t)pick[0] << shift;
-    left = pick[1];
-    __syncthreads();
   }
-  // Pages above the threshold, and the first `left` at it.
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, 64));
+    hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, 64));
+  }
+  if (lane == 0) {
+    range[0][wave] = lo;
+    range[1][wave] = hi;
+  }
+  __syncthreads();
+  for (int w = 0; w < W; ++w) {
+    lo = min(lo, range[0][w]);
+    hi = max(hi, range[1][w]);
+  }
+  // Wanted: the `left` highest keys of [lo, hi] that are not kept; all above hi are taken.
+  int left = take - a.keep_first - a.keep_last;
+  bool all = false;  // every key from lo on, else those above lo and `left` of lo itself
+  if (left == 0) {
+    lo = 0xFFFFFFFFu;  // (no score has this key)
+  } else {
+    for (;;) {
+      const uint32_t span = hi - lo;
+      const int shift = max(32 - BITS - (span ? __builtin_clz(span) : 32), 0);
+      hist[threadIdx.x] = 0;
+      __syncthreads();
+      for (int i = threadIdx.x; i < n; i += T) {
+        const uint32_t k = key_at(i);
+        if (k >= lo && k <= hi && !kept(i)) atomicAdd(&hist[(k - lo) >> shift], 1);
+      }
+      __syncthreads();
+      // Bins from the top: thread t holds bin T - 1 - t.
+      const int c = hist[T - 1 - threadIdx.x];
+      int incl = c;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int t = __shfl_up(incl, o, 64);
+        if (lane >= o) incl += t;
+      }
+      if (lane == 63) red[0][wave] = incl;
+      __syncthreads();
+      int above = incl - c;
+      for (int w = 0; w < wave; ++w) above += red[0][w];
+      if (above < left && left <= above + c) {
+        pick[0] = T - 1 - threadIdx.x;
+        pick[1] = left - above;
+        pick[2] = c;
+      }
+      __syncthreads();
+      lo += (uint32_t)pick[0] << shift;
+      hi = shift ? min(hi, lo + ((1u << shift) - 1)) : lo;
+      left = pick[1];
+      all = pick[2] == left;
+      if (all || shift == 0) break;
+    }
+  }
+  // Taken pages in order, STEPS x T at a time: of each step a wave's pages above the
+  // threshold and at it, then where they begin.
   int done = 0, ties = 0;
-  for (int i0 = 0; i0 < n; i0 += kThreads) {
-    const int i = i0 + threadIdx.x;
-    const uint32_t k = i < n ? key_of(i) : 0;
-    const bool tie = i < n && k == prefix;
-    int n_tie, n_in;
-    const int tie_rank = ties + group_scan(tie, red, &n_tie);
-    const bool in = i < n && (k > prefix || (tie && tie_rank < left));
-    const int at = done + group_scan(in, red, &n_in);
-    if (in) out[at] = i;
-    ties += n_tie;
-    done += n_in;
+  for (int i0 = 0; i0 < n; i0 += STEPS * T) {
+    uint32_t over = 0, at = 0;  // this lane's pages by step
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      const int i = i0 + s * T + threadIdx.x;
+      bool o = false, t = false;
+      if (i < n) {
+        const uint32_t k = key_at(i);
+        o = kept(i) || k > lo || (all && k == lo);
+        t = !o && k == lo;
+      }
+      over |= (uint32_t)o << s;
+      at |= (uint32_t)t << s;
+      const uint64_t bo = __ballot(o), bt = __ballot(t);
+      if (lane == 0) {
+        count[0][s * W + wave] = __popcll(bo);
+        count[1][s * W + wave] = __popcll(bt);
+      }
+    }
+    __syncthreads();
+    if (wave < 2) {  // wave 0: pages above, wave 1: ties; exclusive sums in place
+      int base = wave ? ties : done;
+      for (int j = 0; j < STEPS * W; j += 64) {
+        const int v = j + lane < STEPS * W ? count[wave][j + lane] : 0;
+        int incl = v;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+          const int t = __shfl_up(incl, o, 64);
+          if (lane >= o) incl += t;
+        }
+        if (j + lane < STEPS * W) count[wave][j + lane] = base + incl - v;
+        base += __shfl(incl, 63, 64);
+      }
+      if (lane == 0) red[wave][0] = base;
+    }
+    __syncthreads();
+    const uint64_t below = lane ? ~0ull >> (64 - lane) : 0;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      const bool o = over >> s & 1, t = at >> s & 1;
+      const int n_over = count[0][s * W + wave] + __popcll(__ballot(o) & below);
+      const int n_tie = count[1][s * W + wave] + __popcll(__ballot(t) & below);
+      if (o || (t && n_tie < left)) out[n_over + min(n_tie, left)] = i0 + s * T + threadIdx.x;
+    }
+    done = red[0][0];
+    ties = red[1][0];
+    __syncthreads();
   }
 }
 
 }  // namespace
 
 hipError_t launch_paged_select(int head_dim, const SelectArgs& a, hipStream_t stream) {
-  const dim3 grid(a.batch, (a.bt_stride + kScorePages - 1) / kScorePages), block(kThreads);
-  if (head_dim == 128)
-    page_scores_kernel<128><<<grid, block, 0, stream>>>(a);
-  else
-    page_scores_kernel<64><<<grid, block, 0, stream>>>(a);
+  const int64_t rows = (int64_t)a.batch * a.n_kv_heads;
+  // Four tiles a wave where that still makes four groups a CU, so that their queries and
+  // first loads weigh less; one otherwise.
+  const int tiles = rows * (a.bt_stride / 256) >= 1024 || a.bt_stride > 1 << 20 ? 4 : 1;
+  const int group_pages = kWaves * kTile * tiles;
+  const dim3 grid((uint32_t)rows, (a.bt_stride + group_pages - 1) / group_pages);
+  const bool many = a.n_q_heads / a.n_kv_heads > 4;
+#define PDEC_SCORES(DH_, MANY_)                                                         \
+  page_scores_kernel<DH_, MANY_><<<grid, kThreads, 0, stream>>>(a, a.block_table, a.lens, \
+                                                                group_pages)
+  if (head_dim == 128) {
+    if (many) PDEC_SCORES(128, true); else PDEC_SCORES(128, false);
+  } else {
+    if (many) PDEC_SCORES(64, true); else PDEC_SCORES(64, false);
+  }
+#undef PDEC_SCORES
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  take_pages_kernel<<<dim3(a.batch, a.n_kv_heads), block, 0, stream>>>(a);
+  if (a.bt_stride > 512)
+    take_pages_kernel<1024><<<(uint32_t)rows, 1024, 0, stream>>>(a);
+  else
+    take_pages_kernel<256><<<(uint32_t)rows, 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 
