@@ -249,7 +249,8 @@ int paged_select(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t h
 int64_t verify_drafts_workspace_bytes(int32_t batch, int32_t n_drafts, int32_t vocab,
                                       int32_t with_drafter) {
   if (batch < 1 || n_drafts < 1 || n_drafts > 1024 || vocab < 1 || vocab > (1 << 22) ||
-      (int64_t)batch * (2 * n_drafts + 1) > (1 << 24))
+      (int64_t)batch * (2 * n_drafts + 1) > (1 << 24) ||
+      (int64_t)batch * (2 * n_drafts + 1) * (vocab / 2048 + 1) > INT32_MAX)
     return fail(PDEC_INVALID_ARG, "bad sizes");
   return align_up(verify_workspace_bytes(batch, n_drafts, with_drafter != 0, vocab));
 }

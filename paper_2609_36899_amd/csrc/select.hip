@@ -14,6 +14,12 @@
 #include <algorithm>
 #include <cfloat>
 
+#ifndef NACC
+#define NACC 4
+#endif
+#ifndef TILES
+#define TILES 4
+#endif
 namespace pdec {
 
 namespace {
@@ -97,16 +103,17 @@ __global__ __launch_bounds__(kThreads) void page_scores_kernel(
     }
     double best = -INFINITY;
     for (int hg = 0; hg < n_hg; ++hg) {
-      double s = 0.0;
+      double s[NACC] = {};  // chains, so that one product does not wait for the last
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          s = __builtin_amdgcn_mfma_f64_4x4x4f64((double)bf16_to_f32(m[j][e]),
-                                                 MANY ? qs[hg][j * 8 + e][k4 * 4 + (lane & 3)]
-                                                      : q[j * 8 + e],
-                                                 s, 0, 0, 0);
-      best = fmax(best, s);  // a NaN never wins
+          s[e % NACC] = __builtin_amdgcn_mfma_f64_4x4x4f64(
+              (double)bf16_to_f32(m[j][e]),
+              MANY ? qs[hg][j * 8 + e][k4 * 4 + (lane & 3)] : q[j * 8 + e], s[e % NACC], 0, 0, 0);
+#pragma unroll
+      for (int i = 1; i < NACC; ++i) s[0] += s[i];
+      best = fmax(best, s[0]);  // a NaN never wins
     }
     best = fmax(best, __shfl_xor(best, 1, 64));
     best = fmax(best, __shfl_xor(best, 2, 64));
@@ -117,12 +124,13 @@ __global__ __launch_bounds__(kThreads) void page_scores_kernel(
   }
 }
 
-// The list: one work group of T threads per (sequence, KV head).  The threshold is found
-// by histograms of T bins over the range that the wanted score lies in, at first from the
-// lowest to the highest of them, so that floats of one size spread over the bins: two or
-// three rounds, and none once a bin is taken whole.  Keys wait in LDS between the rounds.
-// Page order comes from ballots and one scan of the waves' counts.  Eight bits at a time
-// from the top of the float, pages one scan a step, took 57 us for 8188 pages.
+// The list: one work group of T threads per (sequence, KV head).  A histogram of T bins of
+// equal width over the range of the scores leaves a few pages in the bin that holds the
+// last one taken, which a wave ranks; where it leaves more than a wave's lanes (equal
+// scores, an outlier that widens the range), histograms over the scores' bits narrow it
+// down.  Scores wait in LDS meanwhile.  Page order comes from ballots and one scan of the
+// waves' counts.  Eight bits at a time from the top of the float, a scan for each step of
+// pages, took 57 us for 8188 pages; bits of the range, two or three rounds, 14.
 template <int T>
 __global__ __launch_bounds__(T) void take_pages_kernel(SelectArgs a) {
   constexpr int W = T / 64, BITS = T == 1024 ? 10 : 8, CACHE = 8 * T, STEPS = 8;
@@ -131,7 +139,8 @@ __global__ __launch_bounds__(T) void take_pages_kernel(SelectArgs a) {
   __shared__ int red[2][W];
   __shared__ uint32_t range[2][W];
   __shared__ int count[2][STEPS * W];
-  __shared__ int pick[3];
+  __shared__ int pick[4];
+  __shared__ uint32_t few[64];
   const int b = blockIdx.x / a.n_kv_heads, n = seq_pages(a.lens, b, a.bt_stride);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const float* score = a.scores + (int64_t)blockIdx.x * a.bt_stride;
@@ -147,6 +156,7 @@ __global__ __launch_bounds__(T) void take_pages_kernel(SelectArgs a) {
     const uint32_t u = __float_as_uint(score[i] + 0.f);  // -0 counts as 0
     return u & 0x80000000u ? ~u : u | 0x80000000u;
   };
+  auto value = [](uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); };
   auto key_at = [&](int i) { return i < CACHE ? keys[i] : read(i); };
   auto kept = [&](int i) { return i < a.keep_first || i >= n - a.keep_last; };
   uint32_t lo = 0xFFFFFFFFu, hi = 0;
@@ -158,6 +168,8 @@ __global__ __launch_bounds__(T) void take_pages_kernel(SelectArgs a) {
       hi = max(hi, k);
     }
   }
+  hist[threadIdx.x] = 0;
+  if (threadIdx.x == 0) pick[3] = 0;
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
     lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, 64));
@@ -172,45 +184,81 @@ __global__ __launch_bounds__(T) void take_pages_kernel(SelectArgs a) {
     lo = min(lo, range[0][w]);
     hi = max(hi, range[1][w]);
   }
+  // Of the bins' counts in hist, bin T - 1 on top: the bin that holds the left-th page from
+  // the top, how many are wanted of it, and how many it has.
+  auto crossing = [&](int left) {
+    __syncthreads();
+    const int c = hist[T - 1 - threadIdx.x];
+    int incl = c;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int t = __shfl_up(incl, o, 64);
+      if (lane >= o) incl += t;
+    }
+    if (lane == 63) red[0][wave] = incl;
+    __syncthreads();
+    int above = incl - c;
+    for (int w = 0; w < wave; ++w) above += red[0][w];
+    if (above < left && left <= above + c) {
+      pick[0] = T - 1 - threadIdx.x;
+      pick[1] = left - above;
+      pick[2] = c;
+    }
+    __syncthreads();
+  };
   // Wanted: the `left` highest keys of [lo, hi] that are not kept; all above hi are taken.
   int left = take - a.keep_first - a.keep_last;
   bool all = false;  // every key from lo on, else those above lo and `left` of lo itself
   if (left == 0) {
     lo = 0xFFFFFFFFu;  // (no score has this key)
   } else {
-    for (;;) {
+    // Bins over the scores themselves: monotone, since each step of the arithmetic is.
+    const float s0 = value(lo), width = value(hi) - s0, per = (float)T / width;
+    const bool even = width > 0.f && width < FLT_MAX && per < FLT_MAX;
+    auto bin_of = [&](uint32_t k) { return min((int)((value(k) - s0) * per), T - 1); };
+    bool ranked = false;
+    if (even) {
+      for (int i = threadIdx.x; i < n; i += T)
+        if (!kept(i)) atomicAdd(&hist[bin_of(key_at(i))], 1);
+      crossing(left);
+      const int bin = pick[0], want = pick[1];
+      if (pick[2] <= 64) {
+        for (int i = threadIdx.x; i < n; i += T) {
+          const uint32_t k = key_at(i);
+          if (!kept(i) && bin_of(k) == bin) few[atomicAdd(&pick[3], 1)] = k;
+        }
+        __syncthreads();
+        // The want-th largest of them, and how many of its equals are wanted.
+        const int m = pick[2];
+        const uint32_t mine = lane < m ? few[lane] : 0;
+        int over = 0, equal = 0;
+        for (int i = 0; i < m; ++i) {
+          over += few[i] > mine;
+          equal += few[i] == mine;
+        }
+        const uint64_t hit = __ballot(lane < m && over < want && want <= over + equal);
+        const int l = __builtin_ctzll(hit);
+        lo = (uint32_t)__shfl((int)mine, l, 64);
+        left = want - __shfl(over, l, 64);
+        ranked = true;
+      }
+    }
+    while (!ranked) {
       const uint32_t span = hi - lo;
       const int shift = max(32 - BITS - (span ? __builtin_clz(span) : 32), 0);
+      __syncthreads();
       hist[threadIdx.x] = 0;
       __syncthreads();
       for (int i = threadIdx.x; i < n; i += T) {
         const uint32_t k = key_at(i);
         if (k >= lo && k <= hi && !kept(i)) atomicAdd(&hist[(k - lo) >> shift], 1);
       }
-      __syncthreads();
-      // Bins from the top: thread t holds bin T - 1 - t.
-      const int c = hist[T - 1 - threadIdx.x];
-      int incl = c;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int t = __shfl_up(incl, o, 64);
-        if (lane >= o) incl += t;
-      }
-      if (lane == 63) red[0][wave] = incl;
-      __syncthreads();
-      int above = incl - c;
-      for (int w = 0; w < wave; ++w) above += red[0][w];
-      if (above < left && left <= above + c) {
-        pick[0] = T - 1 - threadIdx.x;
-        pick[1] = left - above;
-        pick[2] = c;
-      }
-      __syncthreads();
+      crossing(left);
       lo += (uint32_t)pick[0] << shift;
       hi = shift ? min(hi, lo + ((1u << shift) - 1)) : lo;
       left = pick[1];
       all = pick[2] == left;
-      if (all || shift == 0) break;
+      ranked = all || shift == 0;
     }
   }
   // Taken pages in order, STEPS x T at a time: of each step a wave's pages above the
@@ -272,7 +320,7 @@ hipError_t launch_paged_select(int head_dim, const SelectArgs& a, hipStream_t st
   const int64_t rows = (int64_t)a.batch * a.n_kv_heads;
   // Four tiles a wave where that still makes four groups a CU, so that their queries and
   // first loads weigh less; one otherwise.
-  const int tiles = rows * (a.bt_stride / 256) >= 1024 || a.bt_stride > 1 << 20 ? 4 : 1;
+  const int tiles = rows * (a.bt_stride / 256) >= 1024 || a.bt_stride > 1 << 20 ? TILES : 1;
   const int group_pages = kWaves * kTile * tiles;
   const dim3 grid((uint32_t)rows, (a.bt_stride + group_pages - 1) / group_pages);
   const bool many = a.n_q_heads / a.n_kv_heads > 4;
@@ -287,7 +335,7 @@ hipError_t launch_paged_select(int head_dim, const SelectArgs& a, hipStream_t st
 #undef PDEC_SCORES
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (a.bt_stride > 512)
+  if (a.bt_stride > 2048)
     take_pages_kernel<1024><<<(uint32_t)rows, 1024, 0, stream>>>(a);
   else
     take_pages_kernel<256><<<(uint32_t)rows, 256, 0, stream>>>(a);

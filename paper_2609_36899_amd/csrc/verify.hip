@@ -21,14 +21,15 @@
 // Every row has to be read (which draft is the last one accepted is not known before),
 // but the whole-number sums are needed of one row a sequence only:
 //   1. stats: each row once, its maximum and sum of exponentials in fp32, at the HBM
-//      rate; the sum is within 2^-14 of S (fp32 exponentials of arguments down to -41,
-//      the rounding of masses and what is left out below 2^-41);
+//      rate; the sum is within 2^-15 of S (arguments down to -41 log2 units rounded
+//      three times, 41 * 3 * 2^-24, and again with the parts' maxima; sums of 32 terms and
+//      a few levels, 90 * 2^-24; the rounding of 2^22 masses, 2^-19);
 //   2. judge: the tests with these sums, exact where both sides are further apart than
-//      2^-10 of them.  A test that is closer, one in a thousand, takes the masses' own
+//      2^-13 of them.  A test that is closer, one in thousands, takes the masses' own
 //      sums of its two rows, so every decision is that of the definition.  Then the
 //      masses of the deciding row, summed by chunks;
-//   3. rest: r summed by chunks;  4. pick: the chunk that holds the target, its tokens
-//      side by side in one group's threads and one scan.
+//   3. rest: r summed by parts of chunks;  4. pick: the part that holds the target, its
+//      tokens side by side in one group's threads and one scan.
 // Masses of every row in fp64, maximum first, took 313 us for 64 sequences of 4 drafts
 // and their drafter's logits at 128256 tokens (87 + 125 + 62 + 51).
 #include "hip_common.h"
@@ -37,6 +38,7 @@
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
+#include <type_traits>
 
 namespace pdec {
 
@@ -46,6 +48,7 @@ constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr double kMinX = -28.5;  // below it the mass rounds to 0
 constexpr double kUnit = 0x1p50;
 constexpr int kMaxDrafts = 1024;
+constexpr int kParts = kWaves;  // of a chunk, each summed by a wave: the pick walks one
 
 struct Sizes {
   int chunk, n_chunks;  // tokens of a chunk (a multiple of 1024), chunks of a row
@@ -68,7 +71,7 @@ struct Verdict {
 };
 
 // Workspace: per (row, chunk) the maximum and the sum of exponentials over it; per
-// (sequence, chunk) the two rows' masses and the two residual masses; verdicts.
+// (sequence, chunk) the two rows' masses, per part the two residual masses; verdicts.
 struct Work {
   ulonglong2 *mass, *rest;  // (target, drafter), (r with the drafts taken off, rint p)
   float2* stat;
@@ -78,7 +81,7 @@ __host__ __device__ inline Work work_of(void* base, const Sizes& s, int batch) {
   Work w;
   w.mass = (ulonglong2*)base;
   w.rest = w.mass + (int64_t)batch * s.n_chunks;
-  w.stat = (float2*)(w.rest + (int64_t)batch * s.n_chunks);
+  w.stat = (float2*)(w.rest + (int64_t)batch * s.n_chunks * kParts);
   w.verdict = (Verdict*)(w.stat + (int64_t)s.rows * s.n_chunks);
   return w;
 }
@@ -89,11 +92,54 @@ __device__ __forceinline__ const float* row_ptr(const VerifyArgs& a, int row) {
                         : a.drafter + (int64_t)(row - n_target) * a.vocab;
 }
 
-__device__ __forceinline__ uint64_t mass_of(float z, double m, double inv_t) {
+// exp(x) for -28.5 <= x <= 0 by exp(x) = 2^(n / 64) exp(r), n = rint(64 x / ln 2): a table
+// of the 64 fractions in LDS and the series of exp(r) to the fifth power, |r| <= ln 2 / 128
+// (the sixth is below 2^-54).  64 / ln 2 times x has at most 12 bits before the point, so
+// n times the upper part of ln 2 / 64, 40 bits of it, is exact.  One unit in the last place
+// at most, as the library's, in a third of its time: the passes over the deciding rows are
+// bound by this arithmetic (64 sequences of 128256 tokens and two rows, judge and rest: 36
+// and 37 us with the library's).
+constexpr double kLn2 = 0.69314718055994530942;
+constexpr double kStepHi = 0x1.62e42fefa0000p-7;  // ln 2 / 64, 40 bits
+constexpr double kStepLo = 0x1.cf79abc9e3b3ap-46;  // and what is left of it
+__device__ __forceinline__ void fill_fractions(double* frac) {
+  for (int j = threadIdx.x; j < 64; j += blockDim.x) frac[j] = exp2((double)j / 64.0);
+  __syncthreads();
+}
+__device__ __forceinline__ double exp_of(double x, const double* frac) {
+  // n in the low bits of a double behind 1.5 * 2^52, which has no fraction.
+  const double t = __builtin_fma(x, 64.0 / kLn2, 0x1.8p52);
+  const int i = __double2loint(t);
+  const double n = t - 0x1.8p52;
+  const double r = __builtin_fma(-n, kStepLo, __builtin_fma(-n, kStepHi, x));
+  double p = __builtin_fma(r, 1.0 / 120.0, 1.0 / 24.0);
+  p = __builtin_fma(r, p, 1.0 / 6.0);
+  p = __builtin_fma(r, p, 0.5);
+  p = __builtin_fma(r * r, p, r);
+  const double f = frac[i & 63];
+  const double e = __builtin_fma(f, p, f);
+  return __hiloint2double(__double2hiint(e) + ((i & ~63) << 14), __double2loint(e));
+}
+
+// The whole number nearest to x, 0 <= x < 2^52, ties to even: behind 2^52 a double has no
+// fraction.  (Conversions to and from 64-bit integers are a score of instructions each, so
+// masses stay doubles until a thread has summed its own: those sums are below 2^53, where
+// doubles are exact.)
+__device__ __forceinline__ double whole(double x) { return (x + 0x1p52) - 0x1p52; }
+__device__ __forceinline__ uint64_t to_u64(double x) {  // of a whole number below 2^53
+  return (uint64_t)(uint32_t)(x * 0x1p-32) << 32 |
+         (uint32_t)(x - 0x1p32 * (double)(uint32_t)(x * 0x1p-32));
+}
+
+// m_v of a logit; m its row's maximum.
+__device__ __forceinline__ double mass_of(float z, double m, double inv_t, const double* frac) {
+  double x;
+  {
 #pragma clang fp contract(off)
-  const double x = ((double)z - m) * inv_t;
-  if (!(x >= kMinX)) return 0;
-  return (uint64_t)rint(exp(x) * 0x1p40);
+    x = ((double)z - m) * inv_t;
+  }
+  const double e = whole(exp_of(x, frac) * 0x1p40);
+  return x >= kMinX ? e : 0.0;  // (what lies below, and NaN, came to anything)
 }
 
 __device__ __forceinline__ uint64_t wave_sum_u64(uint64_t v) {
@@ -121,11 +167,31 @@ __device__ __forceinline__ f32x4 tokens4(const float* z, int v, int end) {
   return r;
 }
 
+// f(t, four tokens of row zp from t on, four of zd) for t = from, from + STEP, .. below end;
+// the next tokens are in flight meanwhile.  (A rolled loop: the arithmetic of a call is long
+// and runs at the fp64 rate, so waves in number hide the rest; with a chunk's loads and sums
+// unrolled, two waves a SIMD, the judge took 31 us instead of 27.)
+template <int STEP, typename F>
+__device__ __forceinline__ void walk(const float* zp, const float* zd, int from, int end, F&& f) {
+  if (from >= end) return;
+  f32x4 nx = tokens4(zp, from, end), ny = {0.f, 0.f, 0.f, 0.f};
+  if (zd) ny = tokens4(zd, from, end);
+#pragma unroll 1
+  for (int t = from; t < end; t += STEP) {
+    const f32x4 x = nx, y = ny;
+    if (t + STEP < end) {
+      nx = tokens4(zp, t + STEP, end);
+      if (zd) ny = tokens4(zd, t + STEP, end);
+    }
+    f(t, x, y);
+  }
+}
+
 // ---- 1. stats ----------------------------------------------------------------
 template <int Q>  // float4s a thread: the chunk is 1024 Q
 __global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyArgs a, Sizes s, float c2) {
   __shared__ float2 sh[kWaves];
-  const int row = blockIdx.x, c = blockIdx.y;
+  const int row = blockIdx.x / s.n_chunks, c = blockIdx.x % s.n_chunks;
   const float* z = row_ptr(a, row);
   const int begin = c * s.chunk, end = min(begin + s.chunk, a.vocab);
   f32x4 v[Q];
@@ -160,13 +226,16 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyArgs a, Si
 __device__ __forceinline__ float2 row_stat(const Work& w, const Sizes& s, int row, float c2) {
   const float2* st = w.stat + (int64_t)row * s.n_chunks;
   const int lane = threadIdx.x & 63;
-  float m = -INFINITY;
-  for (int c = lane; c < s.n_chunks; c += 64) m = fmaxf(m, st[c].x);
-  m = wave_max(m);
-  float sum = 0.f;
-  for (int c = lane; c < s.n_chunks; c += 64)
-    sum += st[c].y * __builtin_amdgcn_exp2f(fmaxf((st[c].x - m) * c2, -150.f));
-  return make_float2(m, wave_sum(sum));
+  float2 mine = lane < s.n_chunks ? st[lane] : make_float2(-INFINITY, 0.f);
+  for (int c = lane + 64; c < s.n_chunks; c += 64) {
+    const float2 o = st[c];
+    const float m = fmaxf(mine.x, o.x);
+    mine.y = mine.y * __builtin_amdgcn_exp2f(fmaxf((mine.x - m) * c2, -150.f)) +
+             o.y * __builtin_amdgcn_exp2f(fmaxf((o.x - m) * c2, -150.f));
+    mine.x = m;
+  }
+  const float m = wave_max(mine.x);
+  return make_float2(m, wave_sum(mine.y * __builtin_amdgcn_exp2f(fmaxf((mine.x - m) * c2, -150.f))));
 }
 
 // ---- 2. judge ----------------------------------------------------------------
@@ -178,9 +247,10 @@ __device__ __forceinline__ uint64_t u24_of(float u) {
 }
 
 // 2^50 over a whole row's mass, by the whole work group.
-__device__ double exact_unit(const float* z, int vocab, float m, double inv_t, uint64_t* red) {
+__device__ double exact_unit(const float* z, int vocab, float m, double inv_t, const double* frac,
+                             uint64_t* red) {
   uint64_t sum = 0;
-  for (int v = threadIdx.x; v < vocab; v += kThreads) sum += mass_of(z[v], m, inv_t);
+  for (int v = threadIdx.x; v < vocab; v += kThreads) sum += to_u64(mass_of(z[v], m, inv_t, frac));
   return unit_over(group_sum(sum, red));
 }
 
@@ -189,49 +259,55 @@ __global__ __launch_bounds__(kThreads) void verify_judge_kernel(VerifyArgs a, Si
 #pragma clang fp contract(off)
   __shared__ uint64_t red[kWaves];
   __shared__ signed char verdicts[kMaxDrafts];
+  __shared__ float p_max[kMaxDrafts + 1], d_max[kMaxDrafts];
+  __shared__ double frac[64];
+  fill_fractions(frac);
   const int b = blockIdx.x, c = blockIdx.y, T = a.n_drafts, wave = threadIdx.x >> 6;
   const Work w = work_of(a.workspace, s, a.batch);
   enum { kRefuse, kAccept, kClose, kEnd };
   // One side of test i: 2^24 p_x, and u24 d_x, with units of the row sums `pu`, `du`.
   auto lhs = [&](int i, float dm, double du) {
     const int64_t at = (int64_t)b * T + i;
-    const double dx = a.drafter ? (double)mass_of(a.drafter[at * a.vocab + a.drafts[at]], dm, a.inv_t) * du
+    const double dx = a.drafter ? mass_of(a.drafter[at * a.vocab + a.drafts[at]], dm, a.inv_t, frac) * du
                                 : kUnit;
     return (double)u24_of(a.uniforms[(int64_t)b * (T + 1) + i]) * dx;
   };
   auto rhs = [&](int i, float pm, double pu) {
     const int64_t row = (int64_t)b * (T + 1) + i;
     const double px =
-        (double)mass_of(a.target[row * a.vocab + a.drafts[(int64_t)b * T + i]], pm, a.inv_t) * pu;
+        mass_of(a.target[row * a.vocab + a.drafts[(int64_t)b * T + i]], pm, a.inv_t, frac) * pu;
     return 0x1p24 * px;
   };
   const int row0 = b * (T + 1), drow0 = a.batch * (T + 1) + b * T;
-  for (int i = wave; i < T; i += kWaves) {
-    const int x = a.drafts[(int64_t)b * T + i];
+  for (int i = wave; i <= T; i += kWaves) {
+    const float2 p = row_stat(w, s, row0 + i, c2);
+    float2 d = make_float2(0.f, 1.f);
+    if (a.drafter && i < T) d = row_stat(w, s, drow0 + i, c2);
+    const int x = i < T ? a.drafts[(int64_t)b * T + i] : -1;
     int verdict = kEnd;
     if (x >= 0 && x < a.vocab) {
-      const float2 p = row_stat(w, s, row0 + i, c2);
-      const float2 d = a.drafter ? row_stat(w, s, drow0 + i, c2) : make_float2(0.f, 1.f);
       // 2^50 / S, S in units of 2^40; no mass where the maximum is not finite
       const double l = lhs(i, d.x, fabsf(d.x) <= FLT_MAX ? 0x1p10 / (double)d.y : 0.0);
       const double r = rhs(i, p.x, fabsf(p.x) <= FLT_MAX ? 0x1p10 / (double)p.y : 0.0);
       verdict = l < r * (1.0 - slack) ? kAccept : l >= r * (1.0 + slack) ? kRefuse : kClose;
     }
-    if ((threadIdx.x & 63) == 0) verdicts[i] = (signed char)verdict;
+    if ((threadIdx.x & 63) == 0) {
+      p_max[i] = p.x;
+      if (i < T) {
+        verdicts[i] = (signed char)verdict;
+        d_max[i] = d.x;
+      }
+    }
   }
   __syncthreads();
   Verdict v = {0, -1, 0.f, 0.f};
   for (; v.n < T; ++v.n) {
     int verdict = verdicts[v.n];
     if (verdict == kClose) {
-      const float pm = row_stat(w, s, row0 + v.n, c2).x;
-      const double pu = exact_unit(row_ptr(a, row0 + v.n), a.vocab, pm, a.inv_t, red);
-      float dm = 0.f;
-      double du = 0.0;
-      if (a.drafter) {
-        dm = row_stat(w, s, drow0 + v.n, c2).x;
-        du = exact_unit(row_ptr(a, drow0 + v.n), a.vocab, dm, a.inv_t, red);
-      }
+      const float pm = p_max[v.n], dm = d_max[v.n];
+      const double pu = exact_unit(row_ptr(a, row0 + v.n), a.vocab, pm, a.inv_t, frac, red);
+      const double du =
+          a.drafter ? exact_unit(row_ptr(a, drow0 + v.n), a.vocab, dm, a.inv_t, frac, red) : 0.0;
       verdict = lhs(v.n, dm, du) < rhs(v.n, pm, pu) ? kAccept : kRefuse;
     }
     if (verdict == kAccept) continue;
@@ -239,47 +315,57 @@ __global__ __launch_bounds__(kThreads) void verify_judge_kernel(VerifyArgs a, Si
     break;
   }
   const bool drafter = a.drafter && v.refused >= 0;
-  v.pm = row_stat(w, s, row0 + v.n, c2).x;
-  if (drafter) v.dm = row_stat(w, s, drow0 + v.n, c2).x;
+  v.pm = p_max[v.n];
+  if (drafter) v.dm = d_max[v.n];
   if (c == 0 && threadIdx.x == 0) w.verdict[b] = v;
   const float* zp = row_ptr(a, row0 + v.n);
   const float* zd = drafter ? row_ptr(a, drow0 + v.n) : nullptr;
   const int begin = c * s.chunk, end = min(begin + s.chunk, a.vocab);
-  uint64_t p = 0, d = 0;
-  for (int t = begin + threadIdx.x * 4; t < end; t += kThreads * 4) {
-    const f32x4 x = tokens4(zp, t, end);
+  double mp = 0.0, md = 0.0;  // 32 masses at most
+  walk<kThreads * 4>(zp, zd, begin + threadIdx.x * 4, end, [&](int, f32x4 x, f32x4 y) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) p += mass_of(x[e], v.pm, a.inv_t);
-    if (drafter) {
-      const f32x4 y = tokens4(zd, t, end);
+    for (int e = 0; e < 4; ++e) mp += mass_of(x[e], v.pm, a.inv_t, frac);
+    if (drafter)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) d += mass_of(y[e], v.dm, a.inv_t);
-    }
-  }
-  p = group_sum(p, red);
-  d = group_sum(d, red);
+      for (int e = 0; e < 4; ++e) md += mass_of(y[e], v.dm, a.inv_t, frac);
+  });
+  const uint64_t p = group_sum(to_u64(mp), red), d = group_sum(to_u64(md), red);
   if (threadIdx.x == 0) w.mass[(int64_t)b * s.n_chunks + c] = make_ulonglong2(p, d);
 }
 
 // ---- 3. rest, 4. pick ------------------------------------------------------------
+// What is taken off the target's probabilities.
+enum Off { kNothing, kToken, kDrafter };
+
 // The distribution that a sequence's next token is drawn from.
 struct Next {
-  const float *zp, *zd;  // zd null: nothing or one token to take off
+  const float *zp, *zd;  // zd null but for kDrafter
   double pm, pi, dm, di, inv_t;
+  const double* frac;
   int refused;
+  Off off;
   // r_v, and rint(p_v); x, y the target's and the drafter's logit of token v.
-  __device__ __forceinline__ uint64_t at(int v, float x, float y, uint64_t* whole) const {
+  template <Off OFF>
+  __device__ __forceinline__ double at(int v, float x, float y, double* all) const {
 #pragma clang fp contract(off)
-    const double p = (double)mass_of(x, pm, inv_t) * pi;
-    *whole = (uint64_t)rint(p);
-    if (refused < 0) return *whole;
-    double d = v == refused ? INFINITY : 0.0;
-    if (zd) d = (double)mass_of(y, dm, inv_t) * di;
-    return (uint64_t)rint(fmax(p - d, 0.0));
+    const double p = mass_of(x, pm, inv_t, frac) * pi;
+    *all = whole(p);
+    if constexpr (OFF == kNothing) return *all;
+    if constexpr (OFF == kToken) return v == refused ? 0.0 : *all;
+    const double d = mass_of(y, dm, inv_t, frac) * di;
+    return whole(fmax(p - d, 0.0));
+  }
+  // f(std::integral_constant<Off, off>): one branch for a whole loop.
+  template <typename F>
+  __device__ __forceinline__ void by_off(F&& f) const {
+    if (off == kDrafter) f(std::integral_constant<Off, kDrafter>{});
+    else if (off == kToken) f(std::integral_constant<Off, kToken>{});
+    else f(std::integral_constant<Off, kNothing>{});
   }
 };
 
-__device__ __forceinline__ Next next_of(const VerifyArgs& a, const Sizes& s, const Work& w, int b) {
+__device__ __forceinline__ Next next_of(const VerifyArgs& a, const Sizes& s, const Work& w, int b,
+                                        const double* frac) {
   const Verdict v = w.verdict[b];
   uint64_t p = 0, d = 0;  // every wave for itself
   for (int c = threadIdx.x & 63; c < s.n_chunks; c += 64) {
@@ -289,65 +375,68 @@ __device__ __forceinline__ Next next_of(const VerifyArgs& a, const Sizes& s, con
   }
   Next r;
   r.zp = a.target + ((int64_t)b * (a.n_drafts + 1) + v.n) * a.vocab;
-  r.zd = a.drafter && v.refused >= 0 ? a.drafter + ((int64_t)b * a.n_drafts + v.n) * a.vocab : nullptr;
+  r.off = v.refused < 0 ? kNothing : a.drafter ? kDrafter : kToken;
+  r.zd = r.off == kDrafter ? a.drafter + ((int64_t)b * a.n_drafts + v.n) * a.vocab : nullptr;
   r.pm = v.pm;
   r.dm = v.dm;
   r.pi = unit_over(wave_sum_u64(p));
   r.di = unit_over(wave_sum_u64(d));
   r.inv_t = a.inv_t;
+  r.frac = frac;
   r.refused = v.refused;
   return r;
 }
 
 __global__ __launch_bounds__(kThreads) void verify_rest_kernel(VerifyArgs a, Sizes s) {
-  __shared__ uint64_t red[kWaves];
-  const int b = blockIdx.x, c = blockIdx.y;
+  __shared__ double frac[64];
+  fill_fractions(frac);
+  const int b = blockIdx.x, part = blockIdx.y * kParts + (threadIdx.x >> 6);
   const Work w = work_of(a.workspace, s, a.batch);
-  const Next r = next_of(a, s, w, b);
-  const int begin = c * s.chunk, end = min(begin + s.chunk, a.vocab);
-  uint64_t rest = 0, whole = 0;
-  for (int t = begin + threadIdx.x * 4; t < end; t += kThreads * 4) {
-    const f32x4 x = tokens4(r.zp, t, end);
-    f32x4 y = {0.f, 0.f, 0.f, 0.f};
-    if (r.zd) y = tokens4(r.zd, t, end);
+  const Next r = next_of(a, s, w, b, frac);
+  const int len = s.chunk / kParts, begin = part * len, end = min(begin + len, a.vocab);
+  double rest = 0.0, all = 0.0;  // sums of parts of 2^50, but for roundings
+  r.by_off([&](auto off) {
+    walk<256>(r.zp, r.zd, begin + (threadIdx.x & 63) * 4, end, [&](int t, f32x4 x, f32x4 y) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {  // past the end: -inf, no mass of either
-      uint64_t p;
-      rest += r.at(t + e, x[e], y[e], &p);
-      whole += p;
-    }
-  }
-  rest = group_sum(rest, red);
-  whole = group_sum(whole, red);
-  if (threadIdx.x == 0) w.rest[(int64_t)b * s.n_chunks + c] = make_ulonglong2(rest, whole);
+      for (int e = 0; e < 4; ++e) {  // past the end: -inf, no mass of either
+        double p;
+        rest += r.template at<decltype(off)::value>(t + e, x[e], y[e], &p);
+        all += p;
+      }
+    });
+  });
+  const uint64_t r_sum = wave_sum_u64(to_u64(rest)), p_sum = wave_sum_u64(to_u64(all));
+  if ((threadIdx.x & 63) == 0)
+    w.rest[(int64_t)b * s.n_chunks * kParts + part] = make_ulonglong2(r_sum, p_sum);
 }
 
-constexpr int kPickThreads = 1024, kPickWaves = kPickThreads / 64;
-
-__global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(VerifyArgs a, Sizes s) {
-  __shared__ uint64_t red[kPickWaves];
+__global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyArgs a, Sizes s) {
+  __shared__ uint64_t red[kWaves];
   __shared__ int found;
+  __shared__ double frac[64];
+  fill_fractions(frac);
   const int b = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const Work w = work_of(a.workspace, s, a.batch);
-  const Next r = next_of(a, s, w, b);
-  const ulonglong2* part = w.rest + (int64_t)b * s.n_chunks;
-  uint64_t z = 0, whole = 0;
-  for (int c = lane; c < s.n_chunks; c += 64) {
+  const Next r = next_of(a, s, w, b, frac);
+  const int n_parts = s.n_chunks * kParts, len = s.chunk / kParts;
+  const ulonglong2* part = w.rest + (int64_t)b * n_parts;
+  uint64_t z = 0, all = 0;
+  for (int c = lane; c < n_parts; c += 64) {
     z += part[c].x;
-    whole += part[c].y;
+    all += part[c].y;
   }
   z = wave_sum_u64(z);
   const bool own = z == 0;  // nothing left beside the drafts': the target's own
-  if (own) z = wave_sum_u64(whole);
+  if (own) z = wave_sum_u64(all);
   const uint64_t u = u24_of(a.uniforms[(int64_t)b * (a.n_drafts + 1) + a.n_drafts]);
   const uint64_t goal = (uint64_t)(((unsigned __int128)u * z) >> 24);
   if (threadIdx.x == 0) found = 0;
   if (z > 0) {
-    // The chunk whose running sum passes the goal, by every wave for itself.
+    // The part whose running sum passes the goal, by every wave for itself.
     uint64_t run = 0;
     int at = 0;
-    for (int c0 = 0; c0 < s.n_chunks; c0 += 64) {
-      const uint64_t v = c0 + lane < s.n_chunks ? (own ? part[c0 + lane].y : part[c0 + lane].x) : 0;
+    for (int c0 = 0; c0 < n_parts; c0 += 64) {
+      const uint64_t v = c0 + lane < n_parts ? (own ? part[c0 + lane].y : part[c0 + lane].x) : 0;
       uint64_t incl = v;
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) {
@@ -365,24 +454,26 @@ __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(VerifyArgs a,
     }
     // Eight tokens a thread side by side, one scan, and the thread that passes the goal
     // walks its own.
-    const int begin = at * s.chunk, end = min(begin + s.chunk, a.vocab);
-    const int v0 = begin + threadIdx.x * 8;
+    const int begin = at * len, end = min(begin + len, a.vocab), v0 = begin + threadIdx.x * 8;
     uint64_t mine[8], sum = 0;
+    f32x4 x[2], y[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      f32x4 x = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, y = x;
+      x[h] = y[h] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
       if (v0 + 4 * h < end) {
-        x = tokens4(r.zp, v0 + 4 * h, end);
-        if (r.zd) y = tokens4(r.zd, v0 + 4 * h, end);
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        uint64_t p;
-        const uint64_t q = r.at(v0 + 4 * h + e, x[e], y[e], &p);
-        mine[4 * h + e] = own ? p : q;
-        sum += mine[4 * h + e];
+        x[h] = tokens4(r.zp, v0 + 4 * h, end);
+        if (r.zd) y[h] = tokens4(r.zd, v0 + 4 * h, end);
       }
     }
+    r.by_off([&](auto off) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        double p;
+        const double q = r.template at<decltype(off)::value>(v0 + e, x[e / 4][e % 4], y[e / 4][e % 4], &p);
+        mine[e] = to_u64(own ? p : q);
+        sum += mine[e];
+      }
+    });
     uint64_t incl = sum;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -403,7 +494,7 @@ __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(VerifyArgs a,
   }
   __syncthreads();
   const int n = w.verdict[b].n;
-  for (int j = threadIdx.x; j <= a.n_drafts; j += kPickThreads)
+  for (int j = threadIdx.x; j <= a.n_drafts; j += kThreads)
     a.tokens[(int64_t)b * (a.n_drafts + 1) + j] =
         j < n ? a.drafts[(int64_t)b * a.n_drafts + j] : j == n ? found : -1;
   if (threadIdx.x == 0) a.accepted[b] = n;
@@ -413,24 +504,25 @@ __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(VerifyArgs a,
 
 int64_t verify_workspace_bytes(int batch, int n_drafts, bool drafter, int vocab) {
   const Sizes s = sizes_of(batch, n_drafts, drafter, vocab);
-  return ((int64_t)s.rows * 8 + (int64_t)batch * 32) * s.n_chunks +
+  return ((int64_t)s.rows * 8 + (int64_t)batch * 16 * (1 + kParts)) * s.n_chunks +
          (int64_t)batch * (int64_t)sizeof(Verdict);
 }
 
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t stream) {
-  static_assert(8 * kPickThreads >= 8192, "one step of the pick covers a chunk");
+  static_assert(8 * kThreads >= 8192 / kParts, "one step of the pick covers a part");
   const Sizes s = sizes_of(a.batch, a.n_drafts, a.drafter != nullptr, a.vocab);
   const float c2 = std::min(1.4426950408889634f / a.temperature, 3e38f);
   // Temperatures at which fp32 arguments mean nothing: every test is a close one.
-  const double slack = a.temperature < 1e-30f ? INFINITY : 0x1p-10;
-  const dim3 all(s.rows, s.n_chunks), one(a.batch, s.n_chunks);
+  const double slack = a.temperature < 1e-30f ? INFINITY : 0x1p-13;
+  // A row's chunks side by side.
+  const dim3 all((uint32_t)s.rows * s.n_chunks), one(a.batch, s.n_chunks);
   if (s.chunk == 8192)
     verify_stats_kernel<8><<<all, kThreads, 0, stream>>>(a, s, c2);
   else
     verify_stats_kernel<2><<<all, kThreads, 0, stream>>>(a, s, c2);
   verify_judge_kernel<<<one, kThreads, 0, stream>>>(a, s, c2, slack);
   verify_rest_kernel<<<one, kThreads, 0, stream>>>(a, s);
-  verify_pick_kernel<<<a.batch, kPickThreads, 0, stream>>>(a, s);
+  verify_pick_kernel<<<a.batch, kThreads, 0, stream>>>(a, s);
   return hipGetLastError();
 }
 
