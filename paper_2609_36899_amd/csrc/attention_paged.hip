@@ -21,6 +21,7 @@
 // group covers whole is written out at once.
 #include "hip_common.h"
 #include "kernels.h"
+#include "stretch.h"
 
 #include <algorithm>
 #include <type_traits>
@@ -30,7 +31,7 @@ namespace pdec {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kThreads = 256, kWaves = 4;
+constexpr int kThreads = kStretchThreads, kWaves = kThreads / 64;
 // Work groups of a launch: one for each compute unit.  More of them cost their beginnings
 // (lengths, queries, first pages) and their partials: us at 256 / 512 / 1024 groups, 64
 // sequences of 1K to 8K tokens 120 / 119 / 126 (E4M3) and 179 / 178 / 180 (bf16), five
@@ -38,12 +39,6 @@ constexpr int kThreads = 256, kWaves = 4;
 constexpr int kGroups = 256;
 constexpr int kPair = 2 * kPage;        // keys of a pair of pages
 constexpr int kNowhere = 0x40000000;    // a key position past every limit
-
-// Sizes of a call that both passes derive their split from.
-struct Split {
-  int total;  // pairs of pages of all units
-  int per;    // pairs per work group
-};
 
 __device__ __forceinline__ int clamp_len(const PagedAttnArgs& a, int b) {
   return min(max(a.lens[b], 0), a.max_len);
@@ -60,63 +55,6 @@ __device__ __forceinline__ int unit_pages(const PagedAttnArgs& a, int u) {
 }
 __device__ __forceinline__ int unit_pairs(const PagedAttnArgs& a, int u) {
   return (unit_pages(a, u) + 1) / 2;
-}
-
-__device__ __forceinline__ int wave_scan(int v) {  // inclusive
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int t = __shfl_up(v, o, 64);
-    if (lane >= o) v += t;
-  }
-  return v;
-}
-
-// Sum of v over the work group's threads before this one, and of all of them.
-__device__ __forceinline__ int group_scan(int v, int* red, int* total) {
-  const int incl = wave_scan(v), wave = threadIdx.x >> 6, nw = blockDim.x >> 6;
-  __syncthreads();
-  if ((threadIdx.x & 63) == 63) red[wave] = incl;
-  __syncthreads();
-  int before = incl - v, sum = 0;
-  for (int w = 0; w < nw; ++w) {
-    before += w < wave ? red[w] : 0;
-    sum += red[w];
-  }
-  *total = sum;
-  return before;
-}
-
-// The pairs of all units and of a group, and the unit that the group's first pair lies in
-// with that unit's first pair; to all threads.  One look at the lengths, but for more
-// units than threads.
-__device__ __forceinline__ Split split_of(const PagedAttnArgs& a, int w, int* red, int* found) {
-  const bool few = a.n_units <= kThreads;
-  int mine = 0, total;
-  for (int u = threadIdx.x; u < a.n_units; u += kThreads) mine += unit_pairs(a, u);
-  int first = group_scan(mine, red, &total);
-  const Split s = {total, max((total + a.n_groups - 1) / a.n_groups, a.min_pairs)};
-  const int at = w * s.per;
-  if (at >= total) return s;
-  if (few) {
-    if (first <= at && at < first + mine) {
-      found[0] = threadIdx.x;
-      found[1] = first;
-    }
-  } else {
-    int base = 0;
-    for (int u0 = 0; base <= at; u0 += kThreads) {
-      const int u = u0 + threadIdx.x, n = u < a.n_units ? unit_pairs(a, u) : 0;
-      first = base + group_scan(n, red, &total);
-      if (first <= at && at < first + n) {
-        found[0] = u;
-        found[1] = first;
-      }
-      base += total;
-    }
-  }
-  __syncthreads();
-  return s;
 }
 
 // Eight codes (code i in byte i of the two dwords) to bf16, exactly, two an instruction.
@@ -157,11 +95,12 @@ __attribute__((amdgpu_waves_per_eu(RT == 1 ? (sizeof(KT) == 1 ? 2 : 3) : 1))) vo
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int c16 = lane & 15, q4 = lane >> 4;
   const int g = blockIdx.x, w = blockIdx.y;
-  const Split split = split_of(a, w, red, found);
-  int at = w * split.per;
-  if (at >= split.total) return;
-  const int end = min(at + split.per, split.total);
-  int u = found[0], first = found[1];
+  const Stretch mine = stretch_of(a.n_units, a.n_groups, a.min_pairs, w, red, found,
+                                  [&](int u) { return unit_pairs(a, u); });
+  int at = w * mine.per;
+  if (at >= mine.total) return;
+  const int end = min(at + mine.per, mine.total);
+  int u = mine.unit, first = mine.first;
   const int G = a.n_q_heads / a.n_kv_heads;
   const uint16_t* q = (const uint16_t*)a.q;
   auto qk_dim = [](int c, int q4_) { return kFp8 ? q4_ * (DH / 4) + c * 8 : c * 32 + q4_ * 8; };

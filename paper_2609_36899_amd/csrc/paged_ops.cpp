@@ -216,8 +216,8 @@ int paged_select(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t h
   int rc = check_heads(n_q_heads, n_kv_heads, head_dim);
   if (rc == PDEC_OK) rc = check_table(batch, bt_stride, n_pages);
   if (rc != PDEC_OK) return rc;
-  if ((int64_t)batch * n_kv_heads > INT32_MAX)
-    return fail(PDEC_INVALID_ARG, "batch x n_kv_heads too large for one call");
+  if ((int64_t)batch * n_kv_heads > INT32_MAX || (int64_t)batch * (bt_stride / 16 + 1) > INT32_MAX)
+    return fail(PDEC_INVALID_ARG, "batch too large for one call");
   if (n_selected < 1 || n_selected > kMaxStride || keep_first < 0 || keep_last < 1 ||
       (int64_t)keep_first + keep_last > n_selected)
     return fail(PDEC_INVALID_ARG,

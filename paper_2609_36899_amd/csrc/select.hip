@@ -10,21 +10,16 @@
 // not by the order of a sum.
 #include "hip_common.h"
 #include "kernels.h"
+#include "stretch.h"
 
 #include <algorithm>
 #include <cfloat>
 
-#ifndef NACC
-#define NACC 4
-#endif
-#ifndef TILES
-#define TILES 4
-#endif
 namespace pdec {
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kThreads = kStretchThreads, kWaves = kThreads / 64;
 constexpr int kTile = 16;  // pages a wave scores at a time
 
 __device__ __forceinline__ int seq_pages(const int32_t* lens, int b, int bt_stride) {
@@ -32,95 +27,112 @@ __device__ __forceinline__ int seq_pages(const int32_t* lens, int b, int bt_stri
   return min(len / kPage + (len % kPage != 0), bt_stride);
 }
 
-// Scores.  A wave takes tiles of 16 pages of one (sequence, KV head).  The product runs
-// on v_mfma_f64_4x4x4_4b, whose four blocks of 4 x 4 x 4 multiply 16 pages with four
-// query heads, every lane busy and no sum across lanes: lane l holds page l % 16 and the
-// dims 32 j + 8 (l / 16) + e of chunk j, one 16-byte load each, and the same dims of
-// query head l % 4; result lane l has page 4 (l / 4 % 4) + l / 16 and head l % 4.  The
-// next tile's means are in flight meanwhile.  The bound is HBM (Dh bf16 a page and KV
-// head).  With 16 lanes a page, fp64 multiply-adds and sums by shuffles, 64 sequences of
-// 8K to 32K took 159 us.
+// Scores.  A wave takes tiles of 16 pages of one KV head.  The product runs on
+// v_mfma_f64_4x4x4_4b, whose four blocks of 4 x 4 x 4 multiply 16 pages with four query
+// heads, every lane busy and no sum across lanes: lane l holds page l % 16 and the dims
+// 32 j + 8 (l / 16) + e of chunk j, one 16-byte load each, and the same dims of query head
+// l % 4; result lane l has page 4 (l / 4 % 4) + l / 16 and head l % 4.  The next tile's
+// means are in flight meanwhile.
+//
+// The bound is HBM: Dh bf16 a page and KV head, 256 bytes at a random place each; the
+// products take 9 us of 64 sequences of 8K to 32K (17 cycles a tile and dim quad).  As many
+// work groups as stay resident, with equal stretches of tiles, so that the lengths, the
+// queries and the first pages are waited for once: WHAT.  The non-temporal hint costs 8%:
+// an instruction takes half of a line, and the other half's finds it gone.
+constexpr int kScoreGroups = 1024;
+
 template <int DH, bool MANY>  // MANY: more than four query heads, kept in LDS
-__global__ __launch_bounds__(kThreads) void page_scores_kernel(
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) void page_scores_kernel(
     SelectArgs a, const int32_t* __restrict__ table, const int32_t* __restrict__ lens,
-    int group_pages) {
+    int n_groups) {
   constexpr int NJ = DH / 32;
+  __shared__ int red[kWaves], found[2];
   __shared__ double qs[MANY ? 4 : 1][NJ * 8][16];
-  const int b = blockIdx.x / a.n_kv_heads, g = blockIdx.x % a.n_kv_heads;
-  const int n = seq_pages(lens, b, a.bt_stride);
+  const int g = blockIdx.x, w = blockIdx.y;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int begin = blockIdx.y * group_pages, end = min(begin + group_pages, n);
-  if (begin >= end) return;
   const int c16 = lane & 15, k4 = lane >> 4;
   const int G = a.n_q_heads / a.n_kv_heads, n_hg = MANY ? (G + 3) / 4 : 1;
-  const uint16_t* q0 = a.q + ((int64_t)b * a.n_q_heads + g * G) * DH;
-  // Groups of four heads; past the last one the first stands in, which moves no maximum.
-  auto q_at = [&](int hg, int j, int col, int k) {
-    const int h = 4 * hg + col;
-    return *(const u16x8*)(q0 + (int64_t)(h < G ? h : 0) * DH + j * 32 + k * 8);
-  };
-  double q[NJ * 8];
-  if constexpr (MANY) {
-    for (int i = threadIdx.x; i < n_hg * NJ * 16; i += kThreads) {
-      const int l = i % 16, j = i / 16 % NJ, hg = i / 16 / NJ;
-      const u16x8 v = q_at(hg, j, l % 4, l / 4);
+  auto tiles_of = [&](int b) { return (seq_pages(lens, b, a.bt_stride) + kTile - 1) / kTile; };
+  const Stretch mine = stretch_of(a.batch, n_groups, kWaves, w, red, found, tiles_of);
+  int at = w * mine.per, first = mine.first;
+  if (at >= mine.total) return;
+  const int stop = min(at + mine.per, mine.total);
+  for (int b = mine.unit; at < stop; ++b) {
+    const int tiles = tiles_of(b);
+    if (tiles == 0) continue;
+    const int n = seq_pages(lens, b, a.bt_stride);
+    // This stretch's pages of the sequence.
+    const int begin = (at - first) * kTile, end = min(n, min(tiles, stop - first) * kTile);
+    first += tiles;
+    at = min(first, stop);
+    const uint16_t* q0 = a.q + ((int64_t)b * a.n_q_heads + g * G) * DH;
+    // Groups of four heads; past the last one the first stands in, which moves no maximum.
+    auto q_at = [&](int hg, int j, int col, int k) {
+      const int h = 4 * hg + col;
+      return *(const u16x8*)(q0 + (int64_t)(h < G ? h : 0) * DH + j * 32 + k * 8);
+    };
+    double q[NJ * 8];
+    if constexpr (MANY) {
+      __syncthreads();  // the sequence before is done with
+      for (int i = threadIdx.x; i < n_hg * NJ * 16; i += kThreads) {
+        const int l = i % 16, j = i / 16 % NJ, hg = i / 16 / NJ;
+        const u16x8 v = q_at(hg, j, l % 4, l / 4);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) qs[hg][j * 8 + e][l] = bf16_to_f32(v[e]);
+        for (int e = 0; e < 8; ++e) qs[hg][j * 8 + e][l] = bf16_to_f32(v[e]);
+      }
+      __syncthreads();
+    } else {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const u16x8 v = q_at(0, j, lane & 3, k4);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) q[j * 8 + e] = bf16_to_f32(v[e]);
+      }
     }
-    __syncthreads();
-  } else {
+    const int32_t* bt = table + (int64_t)b * a.bt_stride;
+    auto page_of = [&](int p0) { return bt[min(p0 + c16, n - 1)]; };
+    auto load = [&](int page, u16x8(&m)[NJ]) {
+      const bool ok = page >= 0 && page < a.n_pages;
+      const uint16_t* src = a.k_means + ((int64_t)(ok ? page : 0) * a.n_kv_heads + g) * DH + k4 * 8;
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const u16x8 v = q_at(0, j, lane & 3, k4);
+      for (int j = 0; j < NJ; ++j) m[j] = *(const u16x8*)(src + j * 32);
+    };
+    constexpr int kStep = kWaves * kTile;
+    int p0 = begin + wave * kTile;
+    if (p0 >= end) continue;
+    float* scores = a.scores + ((int64_t)b * a.n_kv_heads + g) * a.bt_stride;
+    u16x8 next[NJ];
+    int page = page_of(p0), page1 = page_of(p0 + kStep);
+    load(page, next);
+    for (; p0 < end; p0 += kStep) {
+      u16x8 m[NJ];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) q[j * 8 + e] = bf16_to_f32(v[e]);
+      for (int j = 0; j < NJ; ++j) m[j] = next[j];
+      const bool ok = page >= 0 && page < a.n_pages;
+      page = page1;
+      if (p0 + kStep < end) {
+        load(page, next);
+        page1 = page_of(p0 + 2 * kStep);
+      }
+      double best = -INFINITY;
+      for (int hg = 0; hg < n_hg; ++hg) {
+        double s[2] = {};  // two chains, so that a product does not wait for the last
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            s[e % 2] = __builtin_amdgcn_mfma_f64_4x4x4f64(
+                (double)bf16_to_f32(m[j][e]),
+                MANY ? qs[hg][j * 8 + e][k4 * 4 + (lane & 3)] : q[j * 8 + e], s[e % 2], 0, 0, 0);
+        best = fmax(best, s[0] + s[1]);  // a NaN never wins
+      }
+      best = fmax(best, __shfl_xor(best, 1, 64));
+      best = fmax(best, __shfl_xor(best, 2, 64));
+      const int i = 4 * ((lane >> 2) & 3) + k4;  // the page of this lane's result
+      const bool named = __shfl((int)ok, i, 64);
+      if ((lane & 3) == 0 && p0 + i < end)
+        scores[p0 + i] = named ? fminf(fmaxf((float)best, -FLT_MAX), FLT_MAX) : -FLT_MAX;
     }
-  }
-  const int32_t* bt = table + (int64_t)b * a.bt_stride;
-  auto page_of = [&](int p0) { return bt[min(p0 + c16, end - 1)]; };
-  auto load = [&](int page, u16x8(&m)[NJ]) {
-    const bool ok = page >= 0 && page < a.n_pages;
-    const uint16_t* src = a.k_means + ((int64_t)(ok ? page : 0) * a.n_kv_heads + g) * DH + k4 * 8;
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) m[j] = load_stream<u16x8>(src + j * 32);
-  };
-  constexpr int kStep = kWaves * kTile;
-  int p0 = begin + wave * kTile;
-  if (p0 >= end) return;
-  float* scores = a.scores + (int64_t)blockIdx.x * a.bt_stride;
-  u16x8 next[NJ];
-  int page = page_of(p0), page1 = page_of(p0 + kStep);
-  load(page, next);
-  for (; p0 < end; p0 += kStep) {
-    u16x8 m[NJ];
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) m[j] = next[j];
-    const bool ok = page >= 0 && page < a.n_pages;
-    page = page1;
-    if (p0 + kStep < end) {
-      load(page, next);
-      page1 = page_of(p0 + 2 * kStep);
-    }
-    double best = -INFINITY;
-    for (int hg = 0; hg < n_hg; ++hg) {
-      double s[NACC] = {};  // chains, so that one product does not wait for the last
-#pragma unroll
-      for (int j = 0; j < NJ; ++j)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          s[e % NACC] = __builtin_amdgcn_mfma_f64_4x4x4f64(
-              (double)bf16_to_f32(m[j][e]),
-              MANY ? qs[hg][j * 8 + e][k4 * 4 + (lane & 3)] : q[j * 8 + e], s[e % NACC], 0, 0, 0);
-#pragma unroll
-      for (int i = 1; i < NACC; ++i) s[0] += s[i];
-      best = fmax(best, s[0]);  // a NaN never wins
-    }
-    best = fmax(best, __shfl_xor(best, 1, 64));
-    best = fmax(best, __shfl_xor(best, 2, 64));
-    const int i = 4 * ((lane >> 2) & 3) + k4;  // the page of this lane's result
-    const bool named = __shfl((int)ok, i, 64);
-    if ((lane & 3) == 0 && p0 + i < end)
-      scores[p0 + i] = named ? fminf(fmaxf((float)best, -FLT_MAX), FLT_MAX) : -FLT_MAX;
   }
 }
 
@@ -318,15 +330,12 @@ __global__ __launch_bounds__(T) void take_pages_kernel(SelectArgs a) {
 
 hipError_t launch_paged_select(int head_dim, const SelectArgs& a, hipStream_t stream) {
   const int64_t rows = (int64_t)a.batch * a.n_kv_heads;
-  // Four tiles a wave where that still makes four groups a CU, so that their queries and
-  // first loads weigh less; one otherwise.
-  const int tiles = rows * (a.bt_stride / 256) >= 1024 || a.bt_stride > 1 << 20 ? TILES : 1;
-  const int group_pages = kWaves * kTile * tiles;
-  const dim3 grid((uint32_t)rows, (a.bt_stride + group_pages - 1) / group_pages);
+  const int n_groups = std::max(1, kScoreGroups / a.n_kv_heads);
+  const dim3 grid(a.n_kv_heads, n_groups);
   const bool many = a.n_q_heads / a.n_kv_heads > 4;
 #define PDEC_SCORES(DH_, MANY_)                                                         \
   page_scores_kernel<DH_, MANY_><<<grid, kThreads, 0, stream>>>(a, a.block_table, a.lens, \
-                                                                group_pages)
+                                                                n_groups)
   if (head_dim == 128) {
     if (many) PDEC_SCORES(128, true); else PDEC_SCORES(128, false);
   } else {
