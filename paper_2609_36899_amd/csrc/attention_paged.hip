@@ -31,7 +31,7 @@ namespace pdec {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kThreads = kStretchThreads, kWaves = kThreads / 64;
+constexpr int kThreads = 256, kWaves = kThreads / 64;
 // Work groups of a launch: one for each compute unit.  More of them cost their beginnings
 // (lengths, queries, first pages) and their partials: us at 256 / 512 / 1024 groups, 64
 // sequences of 1K to 8K tokens 120 / 119 / 126 (E4M3) and 179 / 178 / 180 (bf16), five
@@ -95,8 +95,8 @@ __attribute__((amdgpu_waves_per_eu(RT == 1 ? (sizeof(KT) == 1 ? 2 : 3) : 1))) vo
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int c16 = lane & 15, q4 = lane >> 4;
   const int g = blockIdx.x, w = blockIdx.y;
-  const Stretch mine = stretch_of(a.n_units, a.n_groups, a.min_pairs, w, red, found,
-                                  [&](int u) { return unit_pairs(a, u); });
+  const Stretch mine = stretch_of<kThreads>(a.n_units, a.n_groups, a.min_pairs, w, red, found,
+                                            [&](int u) { return unit_pairs(a, u); });
   int at = w * mine.per;
   if (at >= mine.total) return;
   const int end = min(at + mine.per, mine.total);

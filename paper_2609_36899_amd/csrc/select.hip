@@ -19,7 +19,7 @@ namespace pdec {
 
 namespace {
 
-constexpr int kThreads = kStretchThreads, kWaves = kThreads / 64;
+constexpr int kThreads = 512, kWaves = kThreads / 64;  // of the scores
 constexpr int kTile = 16;  // pages a wave scores at a time
 
 __device__ __forceinline__ int seq_pages(const int32_t* lens, int b, int bt_stride) {
@@ -34,28 +34,31 @@ __device__ __forceinline__ int seq_pages(const int32_t* lens, int b, int bt_stri
 // l % 4; result lane l has page 4 (l / 4 % 4) + l / 16 and head l % 4.  The next tile's
 // means are in flight meanwhile.
 //
-// The bound is HBM: Dh bf16 a page and KV head, 256 bytes at a random place each; the
-// products take 9 us of 64 sequences of 8K to 32K (17 cycles a tile and dim quad).  As many
-// work groups as stay resident, with equal stretches of tiles, so that the lengths, the
-// queries and the first pages are waited for once: WHAT.  The non-temporal hint costs 8%:
+// The bound is HBM: Dh bf16 a page and KV head, 256 bytes, the KV heads of a page side by
+// side.  They are taken by the waves of one work group, so that a page's means are read as
+// one run, and as many groups as stay resident have equal stretches of tiles, so that the
+// lengths, the queries and the first pages are waited for once.  64 sequences of 8K to 32K,
+// 168 MB: 38 us; with groups of one KV head 41, with groups of 256 pages each 42; the
+// products take 9 of it (17 cycles a tile and dim quad).  The non-temporal hint costs 8%:
 // an instruction takes half of a line, and the other half's finds it gone.
-constexpr int kScoreGroups = 1024;
+constexpr int kScoreGroups = 512;
 
 template <int DH, bool MANY>  // MANY: more than four query heads, kept in LDS
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) void page_scores_kernel(
-    SelectArgs a, const int32_t* __restrict__ table, const int32_t* __restrict__ lens,
-    int n_groups) {
+    SelectArgs a, const int32_t* __restrict__ table, const int32_t* __restrict__ lens, int heads) {
   constexpr int NJ = DH / 32;
   __shared__ int red[kWaves], found[2];
-  __shared__ double qs[MANY ? 4 : 1][NJ * 8][16];
-  const int g = blockIdx.x, w = blockIdx.y;
+  __shared__ double qs[MANY ? kWaves : 1][MANY ? 4 : 1][NJ * 8][16];
+  const int w = blockIdx.y;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  // This wave's KV head, and its row among the rows of waves that share the tiles.
+  const int g = blockIdx.x * heads + wave % heads, row = wave / heads, rows = kWaves / heads;
   const int c16 = lane & 15, k4 = lane >> 4;
   const int G = a.n_q_heads / a.n_kv_heads, n_hg = MANY ? (G + 3) / 4 : 1;
   auto tiles_of = [&](int b) { return (seq_pages(lens, b, a.bt_stride) + kTile - 1) / kTile; };
-  const Stretch mine = stretch_of(a.batch, n_groups, kWaves, w, red, found, tiles_of);
+  const Stretch mine = stretch_of<kThreads>(a.batch, gridDim.y, rows, w, red, found, tiles_of);
   int at = w * mine.per, first = mine.first;
-  if (at >= mine.total) return;
+  if (at >= mine.total || g >= a.n_kv_heads || row >= rows) return;
   const int stop = min(at + mine.per, mine.total);
   for (int b = mine.unit; at < stop; ++b) {
     const int tiles = tiles_of(b);
@@ -73,14 +76,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) v
     };
     double q[NJ * 8];
     if constexpr (MANY) {
-      __syncthreads();  // the sequence before is done with
-      for (int i = threadIdx.x; i < n_hg * NJ * 16; i += kThreads) {
+      // A wave writes and reads its own part, in order: no barrier.
+      for (int i = lane; i < n_hg * NJ * 16; i += 64) {
         const int l = i % 16, j = i / 16 % NJ, hg = i / 16 / NJ;
         const u16x8 v = q_at(hg, j, l % 4, l / 4);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) qs[hg][j * 8 + e][l] = bf16_to_f32(v[e]);
+        for (int e = 0; e < 8; ++e) qs[wave][hg][j * 8 + e][l] = bf16_to_f32(v[e]);
       }
-      __syncthreads();
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     } else {
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
@@ -97,22 +100,22 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) v
 #pragma unroll
       for (int j = 0; j < NJ; ++j) m[j] = *(const u16x8*)(src + j * 32);
     };
-    constexpr int kStep = kWaves * kTile;
-    int p0 = begin + wave * kTile;
+    const int step = rows * kTile;
+    int p0 = begin + row * kTile;
     if (p0 >= end) continue;
     float* scores = a.scores + ((int64_t)b * a.n_kv_heads + g) * a.bt_stride;
     u16x8 next[NJ];
-    int page = page_of(p0), page1 = page_of(p0 + kStep);
+    int page = page_of(p0), page1 = page_of(p0 + step);
     load(page, next);
-    for (; p0 < end; p0 += kStep) {
+    for (; p0 < end; p0 += step) {
       u16x8 m[NJ];
 #pragma unroll
       for (int j = 0; j < NJ; ++j) m[j] = next[j];
       const bool ok = page >= 0 && page < a.n_pages;
       page = page1;
-      if (p0 + kStep < end) {
+      if (p0 + step < end) {
         load(page, next);
-        page1 = page_of(p0 + 2 * kStep);
+        page1 = page_of(p0 + 2 * step);
       }
       double best = -INFINITY;
       for (int hg = 0; hg < n_hg; ++hg) {
@@ -123,7 +126,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) v
           for (int e = 0; e < 8; ++e)
             s[e % 2] = __builtin_amdgcn_mfma_f64_4x4x4f64(
                 (double)bf16_to_f32(m[j][e]),
-                MANY ? qs[hg][j * 8 + e][k4 * 4 + (lane & 3)] : q[j * 8 + e], s[e % 2], 0, 0, 0);
+                MANY ? qs[wave][hg][j * 8 + e][k4 * 4 + (lane & 3)] : q[j * 8 + e], s[e % 2], 0, 0, 0);
         best = fmax(best, s[0] + s[1]);  // a NaN never wins
       }
       best = fmax(best, __shfl_xor(best, 1, 64));
@@ -330,12 +333,12 @@ __global__ __launch_bounds__(T) void take_pages_kernel(SelectArgs a) {
 
 hipError_t launch_paged_select(int head_dim, const SelectArgs& a, hipStream_t stream) {
   const int64_t rows = (int64_t)a.batch * a.n_kv_heads;
-  const int n_groups = std::max(1, kScoreGroups / a.n_kv_heads);
-  const dim3 grid(a.n_kv_heads, n_groups);
+  const int heads = std::min(a.n_kv_heads, kWaves), head_blocks = (a.n_kv_heads + heads - 1) / heads;
+  const dim3 grid(head_blocks, std::max(1, kScoreGroups / head_blocks));
   const bool many = a.n_q_heads / a.n_kv_heads > 4;
 #define PDEC_SCORES(DH_, MANY_)                                                         \
   page_scores_kernel<DH_, MANY_><<<grid, kThreads, 0, stream>>>(a, a.block_table, a.lens, \
-                                                                n_groups)
+                                                                heads)
   if (head_dim == 128) {
     if (many) PDEC_SCORES(128, true); else PDEC_SCORES(128, false);
   } else {

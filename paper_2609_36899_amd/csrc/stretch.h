@@ -6,9 +6,8 @@
 
 namespace pdec {
 
-constexpr int kStretchThreads = 256;  // of a work group that makes these calls
-
-// Sum of v over the work group's threads before this one, and of all of them.
+// Sum of v over the work group's T threads before this one, and of all of them.
+template <int T>
 __device__ __forceinline__ int group_scan(int v, int* red, int* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int incl = v;
@@ -22,7 +21,7 @@ __device__ __forceinline__ int group_scan(int v, int* red, int* total) {
   __syncthreads();
   int before = incl - v, sum = 0;
 #pragma unroll
-  for (int w = 0; w < kStretchThreads / 64; ++w) {
+  for (int w = 0; w < T / 64; ++w) {
     before += w < wave ? red[w] : 0;
     sum += red[w];
   }
@@ -36,28 +35,28 @@ struct Stretch {
 };
 
 // Stretch w of n_groups, at least min_per long; size(u) is unit u's work, u < n_units.
-// Every thread of the group calls it and gets the same; unit and first mean nothing where
-// w * per >= total.  red: kStretchThreads / 64 ints of LDS, found: two.  One look at the
+// Every thread of the group (T of them) calls it and gets the same; unit and first mean nothing where
+// w * per >= total.  red: T / 64 ints of LDS, found: two.  One look at the
 // sizes, but for more units than threads.
-template <typename F>
+template <int T, typename F>
 __device__ __forceinline__ Stretch stretch_of(int n_units, int n_groups, int min_per, int w,
                                               int* red, int* found, F&& size) {
   int mine = 0, total;
-  for (int u = threadIdx.x; u < n_units; u += kStretchThreads) mine += size(u);
-  int first = group_scan(mine, red, &total);
+  for (int u = threadIdx.x; u < n_units; u += T) mine += size(u);
+  int first = group_scan<T>(mine, red, &total);
   Stretch s = {total, max((total + n_groups - 1) / n_groups, min_per), 0, 0};
   const int at = w * s.per;
   if (at >= total) return s;
-  if (n_units <= kStretchThreads) {
+  if (n_units <= T) {
     if (first <= at && at < first + mine) {
       found[0] = threadIdx.x;
       found[1] = first;
     }
   } else {
     int base = 0;
-    for (int u0 = 0; base <= at; u0 += kStretchThreads) {
+    for (int u0 = 0; base <= at; u0 += T) {
       const int u = u0 + threadIdx.x, n = u < n_units ? size(u) : 0;
-      first = base + group_scan(n, red, &total);
+      first = base + group_scan<T>(n, red, &total);
       if (first <= at && at < first + n) {
         found[0] = u;
         found[1] = first;
