@@ -10,7 +10,7 @@
 // bound by HBM up to a few hundred rows per head.
 //
 // Work split.  A unit is a block of query tokens of one sequence (their n_tok * G
-// rows, at most 16 RT); its work is its key range in pairs of pages.  The units' pairs
+// rows, 16 to 128 of them); its work is its key range in pairs of pages.  The units' pairs
 // laid end to end are cut into n_groups equal stretches, one for each work group of a
 // KV head, whatever the lengths: a group finds its stretch from a prefix sum of the
 // lengths that it makes itself, so no plan is built on the host or uploaded, and a
@@ -73,27 +73,33 @@ enum Cut {
   kToken,  // the block's tokens see different keys of the pair
 };
 
+// RT row tiles of 16 a wave, RW waves side by side along the rows, the others along the
+// pairs.  RW waves load the same pages, from HBM once and from L1 and L2 after that (no
+// non-temporal hint then), where a block for each would have read them again.
+//
 // Lane l: c16 = l % 16, q4 = l / 16.  The MFMA operand order is the one of the
 // engine's decode attention: S^T = K Q^T with the keys permuted so that a lane's
 // eight scores are eight consecutive tokens of one page (page q4 / 2 of the pair,
 // tokens 8 (q4 % 2) ..), which is the P operand of O^T = V^T P^T against one load
 // of the transposed V page.
-template <int DH, int RT, typename KT, bool LIST>
+template <int DH, int RT, int RW, typename KT, bool LIST>
 __global__ __launch_bounds__(kThreads)
-__attribute__((amdgpu_waves_per_eu(RT == 1 ? (sizeof(KT) == 1 ? 2 : 3) : 1))) void paged_attn_kernel(
+__attribute__((amdgpu_waves_per_eu((sizeof(KT) == 1 ? 3 : 4) - RT))) void paged_attn_kernel(
     PagedAttnArgs a, const int32_t* __restrict__ table, const int32_t* __restrict__ lists) {
   constexpr int KC = DH / 32, DT = DH / 16;
   constexpr bool kFp8 = sizeof(KT) == 1;
-  // Whether the next pair's loads are in flight while one is used.  With one row tile of
-  // bf16 pages the registers that this takes cost more (64 x 1K to 8K: 179 us without, 188
-  // with).
-  constexpr bool kAhead = kFp8 || RT > 1;
+  // Whether the next pair's loads are in flight while one is used.  The registers that this
+  // takes of bf16 pages cost a resident group, and more (64 x 1K to 8K: 179 us without, 188
+  // with; four tokens over 16 x 1K to 16K: 97 and 102).
+  constexpr bool kAhead = kFp8;
   typedef typename std::conditional<kFp8, u32x2, u32x4>::type VRaw;
   __shared__ int red[kWaves];
   __shared__ int found[2];
-  __shared__ float sm[kWaves - 1][64][RT * (4 * DT + 2)];
+  constexpr int PW = kWaves / RW;  // waves that share a row tile's pairs
+  __shared__ float sm[PW > 1 ? (PW - 1) * RW : 1][64][PW > 1 ? RT * (4 * DT + 2) : 1];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int c16 = lane & 15, q4 = lane >> 4;
+  const int rw = wave % RW, pw = wave / RW, row0 = rw * RT * 16;
   const int g = blockIdx.x, w = blockIdx.y;
   const Stretch mine = stretch_of<kThreads>(a.n_units, a.n_groups, a.min_pairs, w, red, found,
                                             [&](int u) { return unit_pairs(a, u); });
@@ -124,7 +130,7 @@ __attribute__((amdgpu_waves_per_eu(RT == 1 ? (sizeof(KT) == 1 ? 2 : 3) : 1))) vo
     int row_lim[RT];  // keys a row sees (exclusive end); nothing for rows past the block's
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      const int row = t * 16 + c16, j = row / G;
+      const int row = row0 + t * 16 + c16, j = row / G;
       const bool on = j < n_tok;
       row_lim[t] = on ? pos0 + j + 1 : 0;
       const uint16_t* src =
@@ -169,6 +175,10 @@ __attribute__((amdgpu_waves_per_eu(RT == 1 ? (sizeof(KT) == 1 ? 2 : 3) : 1))) vo
       }
       return r;
     };
+    auto read = [](auto* p, auto v) {
+      if constexpr (RW == 1) return load_stream<decltype(v)>(p);
+      else return *(const decltype(v)*)p;
+    };
     // The pair's bytes as they are in memory, and its scales.
     struct Raw {
       u32x4 k[2][kFp8 ? KC / 2 : KC];
@@ -193,11 +203,11 @@ __attribute__((amdgpu_waves_per_eu(RT == 1 ? (sizeof(KT) == 1 ? 2 : 3) : 1))) vo
         r.key0[i] = p.key0[i];
 #pragma unroll
         for (int c = 0; c < (kFp8 ? KC / 2 : KC); ++c)
-          r.k[i][c] = load_stream<u32x4>(kb + (k_tok + 4 * i) * DH + qk_dim(kFp8 ? 2 * c : c, q4));
+          r.k[i][c] = read(kb + (k_tok + 4 * i) * DH + qk_dim(kFp8 ? 2 * c : c, q4), u32x4{});
       }
 #pragma unroll
       for (int d = 0; d < DT; ++d)
-        r.v[d] = load_stream<VRaw>(vb + (d * 16 + c16) * kPage);
+        r.v[d] = read(vb + (d * 16 + c16) * kPage, VRaw{});
     };
     auto use = [&](const Raw& r, auto cut_) {
       constexpr Cut kCut = decltype(cut_)::value;
@@ -283,8 +293,9 @@ __attribute__((amdgpu_waves_per_eu(RT == 1 ? (sizeof(KT) == 1 ? 2 : 3) : 1))) vo
           // Keys that some of the block's tokens do not see: token by token, with the
           // keys past its own taken as 0 and the sums of its rows alone, since a weight
           // of 0 times an infinity in V would not be 0.
-          for (int j = 0; j < n_tok; ++j) {
-            const bool mine = (t * 16 + c16) / G == j;
+          const int r0 = row0 + t * 16, j_end = min((r0 + 15) / G + 1, n_tok);
+          for (int j = r0 / G; j < j_end; ++j) {
+            const bool mine = (r0 + c16) / G == j;
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
               u16x8 v = vf[d];
@@ -308,14 +319,14 @@ __attribute__((amdgpu_waves_per_eu(RT == 1 ? (sizeof(KT) == 1 ? 2 : 3) : 1))) vo
     // Pairs that every row sees whole, and the one or few at the block's end.  A list's
     // pages come in any order: each pair looks whether its keys end.
     const int p_cut = LIST ? p_end : min(p_end, max(max(pos0 + 1, 0) / kPair, p_begin));
-    int pr = p_begin + wave;
+    int pr = p_begin + pw;
     typedef std::integral_constant<Cut, LIST ? kLimit : kNone> Main;
     if constexpr (kAhead) {
       // The next pair's bytes are in flight while one is used, in two buffers in turn, and
       // the page after it is looked up.  Past the end the last pair stands in.  (A third
       // buffer, and refilling each behind its use, measured the same or up to 8% slower.)
       if (pr < p_cut) {
-        auto next = [&](int i) { return i + kWaves < p_cut ? i + kWaves : i; };
+        auto next = [&](int i) { return i + PW < p_cut ? i + PW : i; };
         Raw r[2];
         load(look(pr), r[0]);
         int fetch = next(pr);
@@ -328,49 +339,52 @@ __attribute__((amdgpu_waves_per_eu(RT == 1 ? (sizeof(KT) == 1 ? 2 : 3) : 1))) vo
             ahead = look(fetch);
             __builtin_amdgcn_sched_barrier(0);
             use(r[i], Main{});
-            pr += kWaves;
+            pr += PW;
             more = pr < p_cut;
             if (!more) break;
           }
         }
       }
     } else {
-      for (; pr < p_cut; pr += kWaves) {
+      for (; pr < p_cut; pr += PW) {
         Raw r;
         load(look(pr), r);
         use(r, Main{});
       }
     }
     if constexpr (!LIST) {
-      for (; pr < p_end; pr += kWaves) {
+      for (; pr < p_end; pr += PW) {
         Raw r;
         load(look(pr), r);
         use(r, std::integral_constant<Cut, kToken>{});
       }
     }
 
-    // The waves' partials meet in wave 0, in wave order.
+    // The partials of the waves that share a row tile meet in the first of them, in wave
+    // order.
 #pragma unroll
     for (int t = 0; t < RT; ++t) l[t] = sum_over_key_groups(l[t]);
-    __syncthreads();  // the piece before has been read
-    if (wave > 0) {
-      float* d = sm[wave - 1][lane];
+    if constexpr (PW > 1) {
+      __syncthreads();  // the piece before has been read
+      if (pw > 0) {
+        float* d = sm[(pw - 1) * RW + rw][lane];
 #pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        d[t * (4 * DT + 2)] = m[t];
-        d[t * (4 * DT + 2) + 1] = l[t];
+        for (int t = 0; t < RT; ++t) {
+          d[t * (4 * DT + 2)] = m[t];
+          d[t * (4 * DT + 2) + 1] = l[t];
 #pragma unroll
-        for (int i = 0; i < 4 * DT; ++i) d[t * (4 * DT + 2) + 2 + i] = acc[t][i / 4][i % 4];
+          for (int i = 0; i < 4 * DT; ++i) d[t * (4 * DT + 2) + 2 + i] = acc[t][i / 4][i % 4];
+        }
       }
+      __syncthreads();
     }
-    __syncthreads();
-    if (wave == 0) {
+    if (pw == 0) {
       const bool whole = p_begin == 0 && p_end == pairs;
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
 #pragma unroll
-        for (int v = 0; v < kWaves - 1; ++v) {
-          const float* d = sm[v][lane] + t * (4 * DT + 2);
+        for (int v = 0; v < PW - 1; ++v) {
+          const float* d = sm[v * RW + rw][lane] + t * (4 * DT + 2);
           const float mn = fmaxf(m[t], d[0]), mu = mn == -INFINITY ? 0.f : mn;
           const float so = exp2f(m[t] - mu), sw = exp2f(d[0] - mu);
           l[t] = l[t] * so + d[1] * sw;
@@ -379,7 +393,7 @@ __attribute__((amdgpu_waves_per_eu(RT == 1 ? (sizeof(KT) == 1 ? 2 : 3) : 1))) vo
             acc[t][i / 4][i % 4] = acc[t][i / 4][i % 4] * so + d[2 + i] * sw;
           m[t] = mn;
         }
-        const int row = t * 16 + c16, j = row / G;
+        const int row = row0 + t * 16 + c16, j = row / G;
         if (j >= n_tok) continue;
         if (whole) {
           const float inv = l[t] == 0.f ? 0.f : 1.f / l[t];
@@ -394,7 +408,7 @@ __attribute__((amdgpu_waves_per_eu(RT == 1 ? (sizeof(KT) == 1 ? 2 : 3) : 1))) vo
                       __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2))};
           }
         } else {
-          const int64_t pr = (((int64_t)w + u) * a.n_kv_heads + g) * (16 * RT) + row;
+          const int64_t pr = (((int64_t)w + u) * a.n_kv_heads + g) * (16 * RT * RW) + row;
           if (q4 == 0) {
             a.part_ml[pr * 2] = m[t];
             a.part_ml[pr * 2 + 1] = l[t];
@@ -496,16 +510,13 @@ __global__ __launch_bounds__(kThreads) void paged_merge_kernel(PagedAttnArgs a, 
 
 }  // namespace
 
-// Row tiles per block of query rows.
-static int row_tiles(int n_q, int group) {
-  const int rows = n_q * group;
-  return rows <= 16 ? 1 : 2;
-}
-
 PagedAttnPlan plan_paged_attention(int batch, int n_q, int n_q_heads, int n_kv_heads) {
   PagedAttnPlan p;
   const int G = n_q_heads / n_kv_heads;
-  p.row_tiles = row_tiles(n_q, G);
+  // The smallest block that holds a sequence's rows of a KV head, or blocks of 128: one row
+  // tile, then two for one, two or all four waves side by side.
+  const int64_t rows = (int64_t)n_q * G;
+  p.row_tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 ? 4 : 8;
   p.tok_per_block = 16 * p.row_tiles / G;
   p.blocks_per_seq = (n_q + p.tok_per_block - 1) / p.tok_per_block;
   p.n_units = (int64_t)batch * p.blocks_per_seq;
@@ -516,15 +527,16 @@ PagedAttnPlan plan_paged_attention(int batch, int n_q, int n_q_heads, int n_kv_h
 hipError_t launch_paged_attention(int kv_fp8, int head_dim, int row_tiles, const PagedAttnArgs& a,
                                   hipStream_t stream) {
   const dim3 grid(a.n_kv_heads, a.n_groups), block(kThreads);
-#define PDEC_PAGED(DH_, RT_, KT_)                                                       \
-  do {                                                                                  \
-    if (a.selected) paged_attn_kernel<DH_, RT_, KT_, true><<<grid, block, 0, stream>>>(a, a.block_table, a.selected);  \
-    else paged_attn_kernel<DH_, RT_, KT_, false><<<grid, block, 0, stream>>>(a, a.block_table, a.selected);        \
-  } while (0)
-#define PDEC_PAGED_RT(DH_, KT_)                    \
-  do {                                             \
-    if (row_tiles == 1) PDEC_PAGED(DH_, 1, KT_);   \
-    else paged_attn_kernel<DH_, 2, KT_, false><<<grid, block, 0, stream>>>(a, a.block_table, a.selected);     \
+#define PDEC_PAGED(DH_, RT_, RW_, KT_, LIST_)                          \
+  paged_attn_kernel<DH_, RT_, RW_, KT_, LIST_><<<grid, block, 0, stream>>>(a, a.block_table, \
+                                                                           a.selected)
+#define PDEC_PAGED_RT(DH_, KT_)                                  \
+  do {                                                           \
+    if (a.selected) PDEC_PAGED(DH_, 1, 1, KT_, true);            \
+    else if (row_tiles == 1) PDEC_PAGED(DH_, 1, 1, KT_, false);  \
+    else if (row_tiles == 2) PDEC_PAGED(DH_, 2, 1, KT_, false);  \
+    else if (row_tiles == 4) PDEC_PAGED(DH_, 2, 2, KT_, false);  \
+    else PDEC_PAGED(DH_, 2, 4, KT_, false);                      \
   } while (0)
   if (head_dim == 128) {
     if (kv_fp8) PDEC_PAGED_RT(128, uint8_t);
