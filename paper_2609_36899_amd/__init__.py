@@ -24,7 +24,8 @@ def __getattr__(name):
                 "paged_select_workspace_bytes", "verify_drafts",
                 "verify_drafts_workspace_bytes"):
         from . import paged
-        return getattr(paged, name)
+        globals()[name] = getattr(paged, name)  # found at once from now on
+        return globals()[name]
     if name in ("PacedRollout", "pacing_plan"):
         from . import driver
         return getattr(driver, name)

@@ -40,6 +40,11 @@ __device__ __forceinline__ float e4m3_to_f32(uint32_t code) {
   return __builtin_amdgcn_cvt_f32_fp8((int)code, 0);
 }
 
+// To nearest even, NaN of any payload to NaN.
+__device__ __forceinline__ uint16_t to_bf16(float v) {
+  return __builtin_bit_cast(uint16_t, (__bf16)v);
+}
+
 // Page elements.  inv: one over the page's scale (a power of two), 1 where pages
 // are not scaled; back() is what a reader of the page sees, over the scale.
 template <typename T>
@@ -51,7 +56,7 @@ struct Elem<float> {
 };
 template <>
 struct Elem<uint16_t> {
-  static __device__ __forceinline__ uint16_t put(float v, float) { return f32_to_bf16(v); }
+  static __device__ __forceinline__ uint16_t put(float v, float) { return to_bf16(v); }
   static __device__ __forceinline__ float back(uint16_t e) { return bf16_to_f32(e); }
 };
 template <>
@@ -194,7 +199,7 @@ __device__ __forceinline__ void append_k(const AppendArgs& a, const Run& run, in
       float sum = 0.f;
       for (int s = 0; s < n; ++s) sum += cols[s][threadIdx.x];
       a.k_means[(run.page * a.n_kv_heads + g) * DH + threadIdx.x] =
-          f32_to_bf16(sum * scale / (float)n);
+          to_bf16(sum * scale / (float)n);
     }
   }
 }
@@ -273,8 +278,8 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs a, int q
       Vec4<QT> lo, hi;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        lo.e[e] = Store<QT>::from(x[e]);
-        hi.e[e] = Store<QT>::from(y[e]);
+        lo.e[e] = Elem<QT>::put(x[e], 1.f);
+        hi.e[e] = Elem<QT>::put(y[e], 1.f);
       }
       *(Vec4<QT>*)(dst + at) = lo;
       *(Vec4<QT>*)(dst + at + H) = hi;

@@ -18,7 +18,8 @@
 // one unit and the beginning of the next: the piece of unit u in group w leaves its
 // softmax partial (maximum, sum, unnormalised output) in slot w + u, which no other
 // piece has, and the merge pass finds a unit's pieces side by side.  A unit that one
-// group covers whole is written out at once.
+// group covers whole is written out at once.  Where no unit can be long, each has a group
+// of its own.
 #include "hip_common.h"
 #include "kernels.h"
 #include "stretch.h"
@@ -55,6 +56,13 @@ __device__ __forceinline__ int unit_pages(const PagedAttnArgs& a, int u) {
 }
 __device__ __forceinline__ int unit_pairs(const PagedAttnArgs& a, int u) {
   return (unit_pages(a, u) + 1) / 2;
+}
+
+// Offset of row `row` (token, query head) of a block in q and out.
+template <int DH>
+__device__ __forceinline__ int64_t row_at(const PagedAttnArgs& a, int b, int j0, int g, int row) {
+  const int G = a.n_q_heads / a.n_kv_heads;
+  return (((int64_t)b * a.n_q + j0 + row / G) * a.n_q_heads + g * G + row % G) * DH;
 }
 
 // Eight codes (code i in byte i of the two dwords) to bf16, exactly, two an instruction.
@@ -101,13 +109,28 @@ __attribute__((amdgpu_waves_per_eu((sizeof(KT) == 1 ? 3 : 4) - RT))) void paged_
   const int c16 = lane & 15, q4 = lane >> 4;
   const int rw = wave % RW, pw = wave / RW, row0 = rw * RT * 16;
   const int g = blockIdx.x, w = blockIdx.y;
-  const Stretch mine = stretch_of<kThreads>(a.n_units, a.n_groups, a.min_pairs, w, red, found,
-                                            [&](int u) { return unit_pairs(a, u); });
-  int at = w * mine.per;
-  if (at >= mine.total) return;
-  const int end = min(at + mine.per, mine.total);
-  int u = mine.unit, first = mine.first;
   const int G = a.n_q_heads / a.n_kv_heads;
+  int at = 0, end, u = w, first = 0;
+  if (a.unit_groups) {  // a group takes unit w whole
+    end = unit_pairs(a, u);
+    if (end == 0) {
+      const int b = u / a.blocks_per_seq, j0 = u % a.blocks_per_seq * a.tok_per_block;
+      const int rows = min(a.tok_per_block, a.n_q - j0) * G;
+      for (int i = threadIdx.x; i < rows * (DH / 4); i += kThreads) {
+        const int row = i / (DH / 4);
+        *(u32x2*)((uint16_t*)a.out + row_at<DH>(a, b, j0, g, row) + i % (DH / 4) * 4) = u32x2{0, 0};
+      }
+      return;
+    }
+  } else {
+    const Stretch mine = stretch_of<kThreads>(a.n_units, a.n_groups, a.min_pairs, w, red, found,
+                                              [&](int v) { return unit_pairs(a, v); });
+    at = w * mine.per;
+    if (at >= mine.total) return;
+    end = min(at + mine.per, mine.total);
+    u = mine.unit;
+    first = mine.first;
+  }
   const uint16_t* q = (const uint16_t*)a.q;
   auto qk_dim = [](int c, int q4_) { return kFp8 ? q4_ * (DH / 4) + c * 8 : c * 32 + q4_ * 8; };
   const int k_tok = 8 * ((c16 >> 2) & 1) + (c16 & 3);  // + 4u
@@ -133,8 +156,7 @@ __attribute__((amdgpu_waves_per_eu((sizeof(KT) == 1 ? 3 : 4) - RT))) void paged_
       const int row = row0 + t * 16 + c16, j = row / G;
       const bool on = j < n_tok;
       row_lim[t] = on ? pos0 + j + 1 : 0;
-      const uint16_t* src =
-          q + (((int64_t)b * a.n_q + j0 + j) * a.n_q_heads + g * G + row % G) * DH;
+      const uint16_t* src = q + row_at<DH>(a, b, j0, g, row);
 #pragma unroll
       for (int c = 0; c < KC; ++c)
         qf[t][c] = on ? *(const bf16x8*)(src + qk_dim(c, q4)) : bf16x8{};
@@ -397,8 +419,7 @@ __attribute__((amdgpu_waves_per_eu((sizeof(KT) == 1 ? 3 : 4) - RT))) void paged_
         if (j >= n_tok) continue;
         if (whole) {
           const float inv = l[t] == 0.f ? 0.f : 1.f / l[t];
-          uint16_t* o = (uint16_t*)a.out +
-                        (((int64_t)b * a.n_q + j0 + j) * a.n_q_heads + g * G + row % G) * DH;
+          uint16_t* o = (uint16_t*)a.out + row_at<DH>(a, b, j0, g, row);
 #pragma unroll
           for (int d = 0; d < DT; ++d) {
             const f32x2 lo = {acc[t][d][0] * inv, acc[t][d][1] * inv};
@@ -498,8 +519,7 @@ __global__ __launch_bounds__(kThreads) void paged_merge_kernel(PagedAttnArgs a, 
 #pragma unroll
   for (int v = 0; v < kWaves - 1; ++v) join(sh[v][lane][0], sh[v][lane][1], &sh[v][lane][2]);
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  uint16_t* dst = (uint16_t*)a.out +
-                  (((int64_t)b * a.n_q + j0 + row / G) * a.n_q_heads + g * G + row % G) * DH + d0;
+  uint16_t* dst = (uint16_t*)a.out + row_at<DH>(a, b, j0, g, row) + d0;
 #pragma unroll
   for (int e = 0; e < DPL; e += 4) {
     const f32x2 lo = {o[e] * inv, o[e + 1] * inv}, hi = {o[e + 2] * inv, o[e + 3] * inv};
@@ -510,7 +530,8 @@ __global__ __launch_bounds__(kThreads) void paged_merge_kernel(PagedAttnArgs a, 
 
 }  // namespace
 
-PagedAttnPlan plan_paged_attention(int batch, int n_q, int n_q_heads, int n_kv_heads) {
+PagedAttnPlan plan_paged_attention(int batch, int n_q, int n_q_heads, int n_kv_heads,
+                                   int max_pages) {
   PagedAttnPlan p;
   const int G = n_q_heads / n_kv_heads;
   // The smallest block that holds a sequence's rows of a KV head, or blocks of 128: one row
@@ -521,12 +542,19 @@ PagedAttnPlan plan_paged_attention(int batch, int n_q, int n_q_heads, int n_kv_h
   p.blocks_per_seq = (n_q + p.tok_per_block - 1) / p.tok_per_block;
   p.n_units = (int64_t)batch * p.blocks_per_seq;
   p.n_groups = std::max(1, kGroups / n_kv_heads);
+  // A work group for each unit needs no scan of the lengths and no merge, and waits for the
+  // longest.  us, equal stretches / a group a unit, one token, 8 KV heads of four: table of
+  // 512 tokens, 8 sequences 15.0 / 11.8 (E4M3), 14.0 / 11.4 (bf16), 64 26.1 / 16.2, 256
+  // 74.9 / 53.4; 1024 tokens, 8 sequences 15.4 / 12.9 and 15.7 / 17.9 (bf16), 64 32.8 /
+  // 24.9; 2048 tokens, 1 sequence 15.1 / 15.3 and 13.8 / 20.8, 64 47.9 / 42.7 and 70.6 /
+  // 71.4, 256 166.9 / 151.8.
+  p.unit_groups = p.n_units <= 65535 && (max_pages + 1) / 2 <= (p.n_units * n_kv_heads >= 512 ? 66 : 24);
   return p;
 }
 
 hipError_t launch_paged_attention(int kv_fp8, int head_dim, int row_tiles, const PagedAttnArgs& a,
                                   hipStream_t stream) {
-  const dim3 grid(a.n_kv_heads, a.n_groups), block(kThreads);
+  const dim3 grid(a.n_kv_heads, a.unit_groups ? a.n_units : a.n_groups), block(kThreads);
 #define PDEC_PAGED(DH_, RT_, RW_, KT_, LIST_)                          \
   paged_attn_kernel<DH_, RT_, RW_, KT_, LIST_><<<grid, block, 0, stream>>>(a, a.block_table, \
                                                                            a.selected)
@@ -548,7 +576,7 @@ hipError_t launch_paged_attention(int kv_fp8, int head_dim, int row_tiles, const
 #undef PDEC_PAGED_RT
 #undef PDEC_PAGED
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || a.unit_groups) return e;
   const int rows = std::min(a.tok_per_block, a.n_q) * (a.n_q_heads / a.n_kv_heads);
   const dim3 mgrid(a.n_units, a.n_kv_heads, (rows + 3) / 4);
   if (head_dim == 128)

@@ -192,15 +192,18 @@ hipError_t launch_kv_append(int src_dtype, int kv_dtype, int head_dim, const App
 struct PagedAttnPlan {
   int32_t row_tiles, tok_per_block, blocks_per_seq, n_groups;
   int64_t n_units;
+  bool unit_groups;  // a work group for each unit and no merge, instead of equal stretches
 };
-PagedAttnPlan plan_paged_attention(int batch, int n_q, int n_q_heads, int n_kv_heads);
+// max_pages: what no sequence can read more of.
+PagedAttnPlan plan_paged_attention(int batch, int n_q, int n_q_heads, int n_kv_heads,
+                                   int max_pages);
 struct PagedAttnArgs {  // attention_paged.hip
   const void *q, *k_pages, *v_pages;
   const float *k_scales, *v_scales;
   const int32_t *block_table, *lens, *selected;  // selected nullable
   int32_t bt_stride, n_selected, max_len, n_q, n_q_heads, n_kv_heads;
   int64_t n_pages;
-  int32_t tok_per_block, blocks_per_seq, n_units, n_groups, min_pairs;
+  int32_t tok_per_block, blocks_per_seq, n_units, n_groups, min_pairs, unit_groups;
   float scale_log2;
   float *part_ml, *part_acc;  // [n_groups + n_units][Hkv][16 row_tiles][2 | head_dim]
   void* out;

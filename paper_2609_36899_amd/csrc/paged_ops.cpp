@@ -4,6 +4,7 @@
 // allocates, and every call can be captured into a graph.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <string>
@@ -137,7 +138,7 @@ int64_t paged_token_attention_workspace_bytes(int32_t batch, int32_t n_q, int32_
                                               int32_t n_kv_heads, int32_t head_dim) {
   const int rc = check_token_attention(batch, n_q, n_q_heads, n_kv_heads, head_dim);
   if (rc != PDEC_OK) return rc;
-  const TokenAttnLayout l = layout_of(plan_paged_attention(batch, n_q, n_q_heads, n_kv_heads),
+  const TokenAttnLayout l = layout_of(plan_paged_attention(batch, n_q, n_q_heads, n_kv_heads, 1),
                                       n_kv_heads, head_dim);
   return l.ml + l.acc;
 }
@@ -164,7 +165,9 @@ int paged_token_attention(int32_t kv_dtype, int32_t batch, int32_t n_q, int32_t 
   if (!aligned(q, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(out, 16) ||
       !aligned(workspace, 16))
     return fail(PDEC_INVALID_ARG, "q, pages, out and workspace must be 16-byte aligned");
-  const PagedAttnPlan p = plan_paged_attention(batch, n_q, n_q_heads, n_kv_heads);
+  const PagedAttnPlan p =
+      plan_paged_attention(batch, n_q, n_q_heads, n_kv_heads,
+                           selected_dev ? std::min(n_selected, bt_stride) : bt_stride);
   if (p.n_units * ((int64_t)bt_stride + 1) > INT32_MAX)
     return fail(PDEC_INVALID_ARG, "batch x bt_stride too large for one call");
   const TokenAttnLayout l = layout_of(p, n_kv_heads, head_dim);
@@ -191,6 +194,7 @@ int paged_token_attention(int32_t kv_dtype, int32_t batch, int32_t n_q, int32_t 
   a.n_units = (int32_t)p.n_units;
   a.n_groups = p.n_groups;
   a.min_pairs = 4;
+  a.unit_groups = p.unit_groups;
   a.scale_log2 = 1.4426950408889634f / std::sqrt((float)head_dim);
   a.part_ml = (float*)workspace;
   a.part_acc = (float*)((char*)workspace + l.ml);

@@ -48,7 +48,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) v
     SelectArgs a, const int32_t* __restrict__ table, const int32_t* __restrict__ lens, int heads) {
   constexpr int NJ = DH / 32;
   __shared__ int red[kWaves], found[2];
-  __shared__ double qs[MANY ? kWaves : 1][MANY ? 4 : 1][NJ * 8][16];
+  __shared__ float qs[MANY ? kWaves : 1][MANY ? 4 : 1][NJ * 8][16];
   const int w = blockIdx.y;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   // This wave's KV head, and its row among the rows of waves that share the tiles.
@@ -126,7 +126,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) v
           for (int e = 0; e < 8; ++e)
             s[e % 2] = __builtin_amdgcn_mfma_f64_4x4x4f64(
                 (double)bf16_to_f32(m[j][e]),
-                MANY ? qs[wave][hg][j * 8 + e][k4 * 4 + (lane & 3)] : q[j * 8 + e], s[e % 2], 0, 0, 0);
+                MANY ? (double)qs[wave][hg][j * 8 + e][k4 * 4 + (lane & 3)] : q[j * 8 + e], s[e % 2], 0, 0, 0);
         best = fmax(best, s[0] + s[1]);  // a NaN never wins
       }
       best = fmax(best, __shfl_xor(best, 1, 64));

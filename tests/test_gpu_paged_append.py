@@ -207,6 +207,19 @@ def test_infinities_and_nan_saturate_and_stay_in_their_head():
     assert float(c.vs[page, 0]) < 1.0
 
 
+def test_nan_of_any_payload_stays_nan_in_bf16():
+    c = Case([4], [4], 2, 2, 64, "bf16", "f32", seed=8)
+    c.rows.view(torch.int32)[1] = 0x7FFFFFFF
+    c.rows.view(torch.int32)[2] = -1
+    c.call()
+    page = c.table[0, 0]
+    for t in (1, 2):
+        assert torch.isnan(c.kp[page, :, t].float()).all()
+        assert torch.isnan(c.vp[page, :, :, t].float()).all()
+        assert torch.isnan(c.q_out[t].float()).all()
+    assert torch.isfinite(c.kp[page, :, 3].float()).all() and torch.isnan(c.means[page].float()).all()
+
+
 @pytest.mark.parametrize("kind", ["fp8", "bf16"])
 def test_what_is_out_of_range_is_left_out(kind):
     """Page ids outside the pool, positions past the angles and past the table, and a

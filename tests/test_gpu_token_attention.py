@@ -107,14 +107,19 @@ HEADS = [(32, 8, 128), (8, 2, 64), (10, 2, 128), (16, 1, 64), (3, 3, 128), (13, 
 @pytest.mark.parametrize("fp8", [True, False])
 @pytest.mark.parametrize("hq,hkv,dh", HEADS)
 def test_edge_lengths(hq, hkv, dh, fp8):
+    """A long sequence in the batch (its table takes equal stretches), and short ones alone
+    (a work group for each)."""
     Case(EDGE_LENS, hq, hkv, dh, fp8=fp8, seed=1).check()
+    Case(EDGE_LENS[:-2], hq, hkv, dh, fp8=fp8, seed=1).check()
 
 
 @pytest.mark.parametrize("fp8", [True, False])
 @pytest.mark.parametrize("n_q", [2, 3, 4, 5, 8, 9, 17, 40])
 def test_several_tokens(n_q, fp8):
     """Lengths below n_q leave tokens without a key: zeros."""
-    Case([0, 1, n_q - 1, n_q, 16, 31, 33, 200, 511], 8, 2, 128, n_q=n_q, fp8=fp8, seed=2).check()
+    lens = [0, 1, n_q - 1, n_q, 16, 31, 33, 200, 511]
+    Case(lens, 8, 2, 128, n_q=n_q, fp8=fp8, seed=2).check()
+    Case(lens + [1500], 8, 2, 128, n_q=n_q, fp8=fp8, seed=2).check()
 
 
 @pytest.mark.parametrize("hq,hkv,dh,n_q", [(16, 1, 64, 3), (5, 1, 128, 7), (6, 6, 64, 33),
@@ -129,9 +134,13 @@ def test_long_contexts_split_over_many_groups():
 
 
 def test_many_short_sequences():
-    """More sequences than one prefix-sum step of a work group takes."""
+    """A work group for each; and, with a long one among them, more sequences than one
+    prefix-sum step of a work group takes."""
     rng = np.random.default_rng(6)
-    Case(rng.integers(0, 40, 700), 4, 2, 64, seed=6).check()
+    lens = rng.integers(0, 40, 700)
+    Case(lens, 4, 2, 64, seed=6).check()
+    lens[[5, 300]] = 3000, 2500
+    Case(lens, 4, 2, 64, seed=6).check()
 
 
 @pytest.mark.parametrize("fp8", [True, False])
@@ -171,7 +180,7 @@ def test_scores_of_minus_infinity_and_the_lowest_value():
 
 @pytest.mark.parametrize("fp8", [True, False])
 def test_page_ids_outside_the_pool_have_no_keys(fp8):
-    c = Case([100, 50, 16], 8, 2, 64, fp8=fp8, seed=9)
+    c = Case([100, 50, 16, 1700], 8, 2, 64, fp8=fp8, seed=9)
     c.table[0, 2], c.table[0, 5], c.table[1, 0], c.table[2, 0] = -1, c.P, 2 ** 31 - 1, -2 ** 31
     c.check()
     assert (c.run()[2] == 0).all()
