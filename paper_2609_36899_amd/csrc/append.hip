@@ -40,33 +40,6 @@ __device__ __forceinline__ float e4m3_to_f32(uint32_t code) {
   return __builtin_amdgcn_cvt_f32_fp8((int)code, 0);
 }
 
-// To nearest even, NaN of any payload to NaN.
-__device__ __forceinline__ uint16_t to_bf16(float v) {
-  return __builtin_bit_cast(uint16_t, (__bf16)v);
-}
-
-// Page elements.  inv: one over the page's scale (a power of two), 1 where pages
-// are not scaled; back() is what a reader of the page sees, over the scale.
-template <typename T>
-struct Elem;
-template <>
-struct Elem<float> {
-  static __device__ __forceinline__ float put(float v, float) { return v; }
-  static __device__ __forceinline__ float back(float e) { return e; }
-};
-template <>
-struct Elem<uint16_t> {
-  static __device__ __forceinline__ uint16_t put(float v, float) { return to_bf16(v); }
-  static __device__ __forceinline__ float back(uint16_t e) { return bf16_to_f32(e); }
-};
-template <>
-struct Elem<uint8_t> {
-  static __device__ __forceinline__ uint8_t put(float v, float inv) {
-    return (uint8_t)e4m3_from_f32(v * inv);
-  }
-  static __device__ __forceinline__ float back(uint8_t e) { return e4m3_to_f32(e); }
-};
-
 template <typename T>
 struct alignas(4 * sizeof(T)) Vec4 {
   T e[4];
@@ -75,6 +48,49 @@ template <typename T>
 struct alignas(8 * sizeof(T) > 16 ? 16 : 8 * sizeof(T)) Vec8 {
   T e[8];
 };
+
+// Page elements, to nearest even.  inv: one over the page's scale (a power of two), 1
+// where pages are not scaled; back() is what a reader of the page sees, over the scale.
+template <typename T>
+struct Elem;
+template <>
+struct Elem<float> {
+  static __device__ __forceinline__ void put2(float* e, float a, float b, float) {
+    e[0] = a;
+    e[1] = b;
+  }
+  static __device__ __forceinline__ float back(float e) { return e; }
+};
+template <>
+struct Elem<uint16_t> {  // the hardware conversion: NaN of any payload stays NaN
+  static __device__ __forceinline__ void put2(uint16_t* e, float a, float b, float) {
+    const uint32_t bits =
+        __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+    e[0] = (uint16_t)bits;
+    e[1] = (uint16_t)(bits >> 16);
+  }
+  static __device__ __forceinline__ float back(uint16_t e) { return bf16_to_f32(e); }
+};
+template <>
+struct Elem<uint8_t> {
+  static __device__ __forceinline__ void put2(uint8_t* e, float a, float b, float inv) {
+    e[0] = (uint8_t)e4m3_from_f32(a * inv);
+    e[1] = (uint8_t)e4m3_from_f32(b * inv);
+  }
+  static __device__ __forceinline__ float back(uint8_t e) { return e4m3_to_f32(e); }
+};
+template <typename T>
+__device__ __forceinline__ Vec4<T> put4(f32x4 v, float inv) {
+  Vec4<T> r;
+  Elem<T>::put2(r.e, v.x, v.y, inv);
+  Elem<T>::put2(r.e + 2, v.z, v.w, inv);
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ f32x4 back4(const Vec4<T>& v) {
+  return f32x4{Elem<T>::back(v.e[0]), Elem<T>::back(v.e[1]), Elem<T>::back(v.e[2]),
+               Elem<T>::back(v.e[3])};
+}
 
 // The smallest power of two s, 2^-100 to 2^100, with amax <= 448 s (448 = 1.75 * 2^8).
 __device__ __forceinline__ float scale_for(float amax) {
@@ -94,26 +110,31 @@ __device__ __forceinline__ float inverse_pow2(float s) {
   return __uint_as_float((254u << 23) - __float_as_uint(s));
 }
 
-__device__ __forceinline__ float group_max(float v, float* red) {
+// Over the work group; `turn` counts its calls, which take two places in red in turn.
+__device__ __forceinline__ float group_max(float v, float (*red)[kWaves], int turn) {
+  float* at = red[turn & 1];
   v = wave_max(v);
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = v;
   __syncthreads();
-  float t = red[0];
+  float t = at[0];
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) t = fmaxf(t, red[w]);
-  __syncthreads();
+  for (int w = 1; w < kWaves; ++w) t = fmaxf(t, at[w]);
   return t;
 }
 
-// The sequence that holds row r, or -1; every thread of the group calls it.
-__device__ __forceinline__ int find_seq(const AppendArgs& a, int r, int* sh) {
-  __syncthreads();
-  if (threadIdx.x == 0) *sh = -1;
-  __syncthreads();
-  for (int b = threadIdx.x; b < a.n_seqs; b += kThreads)
-    if (a.row_start[b] <= r && r < a.row_start[b + 1]) *sh = b;
-  __syncthreads();
-  return *sh;
+// The sequence that holds row r, or -1, by every wave for itself: 64 sequences at a time,
+// from where r lies if all have as many rows.
+__device__ __forceinline__ int find_seq(const AppendArgs& a, int r) {
+  const int lane = threadIdx.x & 63, chunks = (a.n_seqs + 63) / 64;
+  int c = (int)((int64_t)r * a.n_seqs / a.n_rows) / 64;
+  for (int i = 0; i < chunks; ++i) {
+    const int b = c * 64 + lane;
+    const bool in = b < a.n_seqs && a.row_start[b] <= r && r < a.row_start[b + 1];
+    const uint64_t hit = __ballot(in);
+    if (hit) return c * 64 + __builtin_ctzll(hit);
+    c = c + 1 < chunks ? c + 1 : 0;
+  }
+  return -1;
 }
 
 __device__ __forceinline__ void rotate4(f32x4& x, f32x4& y, const float2* cs) {
@@ -132,8 +153,8 @@ struct Run {
 };
 
 template <typename ST, typename KT, int DH>
-__device__ __forceinline__ void append_k(const AppendArgs& a, const Run& run, int g, float* red,
-                                         float (*cols)[DH]) {
+__device__ __forceinline__ void append_k(const AppendArgs& a, const Run& run, int g, int turn,
+                                         float (*red)[kWaves], float (*cols)[DH]) {
   constexpr int QR = DH / 8, H = DH / 2;  // threads per slot: four pairs each
   constexpr bool kFp8 = sizeof(KT) == 1;
   const int slot = threadIdx.x / QR, i = threadIdx.x % QR * 4;
@@ -153,7 +174,7 @@ __device__ __forceinline__ void append_k(const AppendArgs& a, const Run& run, in
     float m = 0.f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) m = fmaxf(m, fmaxf(fabsf(x[e]), fabsf(y[e])));
-    scale = scale_for(group_max(m, red));
+    scale = scale_for(group_max(m, red, turn));
     if (run.s0 > 0) scale = fmaxf(scale, kept_scale(old));
     inv = inverse_pow2(scale);
     if (threadIdx.x == 0) a.k_scales[at] = scale;
@@ -161,22 +182,16 @@ __device__ __forceinline__ void append_k(const AppendArgs& a, const Run& run, in
   Vec4<KT> lo, hi;
   bool held = fresh;
   if (fresh) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      lo.e[e] = Elem<KT>::put(x[e], inv);
-      hi.e[e] = Elem<KT>::put(y[e], inv);
-    }
+    lo = put4<KT>(x, inv);
+    hi = put4<KT>(y, inv);
   } else if (earlier && (a.k_means || (kFp8 && scale != old))) {
     lo = *(const Vec4<KT>*)(dst + i);
     hi = *(const Vec4<KT>*)(dst + i + H);
     held = true;
     if constexpr (kFp8) {
       if (scale != old) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          lo.e[e] = Elem<KT>::put(Elem<KT>::back(lo.e[e]) * old, inv);
-          hi.e[e] = Elem<KT>::put(Elem<KT>::back(hi.e[e]) * old, inv);
-        }
+        lo = put4<KT>(back4<KT>(lo) * old, inv);
+        hi = put4<KT>(back4<KT>(hi) * old, inv);
       }
     }
   }
@@ -199,13 +214,14 @@ __device__ __forceinline__ void append_k(const AppendArgs& a, const Run& run, in
       float sum = 0.f;
       for (int s = 0; s < n; ++s) sum += cols[s][threadIdx.x];
       a.k_means[(run.page * a.n_kv_heads + g) * DH + threadIdx.x] =
-          to_bf16(sum * scale / (float)n);
+          __builtin_bit_cast(uint16_t, (__bf16)(sum * scale / (float)n));
     }
   }
 }
 
 template <typename ST, typename KT, int DH>
-__device__ __forceinline__ void append_v(const AppendArgs& a, const Run& run, int g, float* red) {
+__device__ __forceinline__ void append_v(const AppendArgs& a, const Run& run, int g, int turn,
+                                         float (*red)[kWaves]) {
   constexpr bool kFp8 = sizeof(KT) == 1;
   const int d = threadIdx.x / 2, t0 = threadIdx.x % 2 * 8;  // one dim, eight slots
   const bool on = d < DH;
@@ -224,7 +240,7 @@ __device__ __forceinline__ void append_v(const AppendArgs& a, const Run& run, in
   if constexpr (kFp8) {
     const int64_t at = run.page * a.n_kv_heads + g;
     if (run.s0 > 0) old = a.v_scales[at];
-    scale = scale_for(group_max(m, red));
+    scale = scale_for(group_max(m, red, turn));
     if (run.s0 > 0) scale = fmaxf(scale, kept_scale(old));
     inv = inverse_pow2(scale);
     if (threadIdx.x == 0) a.v_scales[at] = scale;
@@ -232,16 +248,14 @@ __device__ __forceinline__ void append_v(const AppendArgs& a, const Run& run, in
   if (!on) return;
   const bool moved = kFp8 && run.s0 > t0 && scale != old;
   Vec8<KT> e;
-  if (moved) e = *(const Vec8<KT>*)dst;
+  if (moved) {
+    e = *(const Vec8<KT>*)dst;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int k = t0 + j - run.s0;
-    if (k >= 0 && k < run.m) {
-      e.e[j] = Elem<KT>::put(x[j], inv);
-    } else if (kFp8 && moved && k < 0) {
-      e.e[j] = Elem<KT>::put(Elem<KT>::back(e.e[j]) * old, inv);
-    }
+    for (int j = 0; j < 8; ++j)
+      if (t0 + j < run.s0) x[j] = Elem<KT>::back(e.e[j]) * old;
   }
+#pragma unroll
+  for (int j = 0; j < 8; j += 2) Elem<KT>::put2(e.e + j, x[j], x[j + 1], inv);
   const int first = moved ? 0 : run.s0, end = run.s0 + run.m;
   if (first <= t0 && t0 + 8 <= end) {
     *(Vec8<KT>*)dst = e;
@@ -259,13 +273,12 @@ template <typename ST, typename KT, int DH>
 __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs a, int q_groups,
                                                              int window) {
   typedef typename std::conditional<sizeof(KT) == 4, float, uint16_t>::type QT;
-  __shared__ int sh_seq;
-  __shared__ float red[kWaves];
+  __shared__ float red[2][kWaves];
   __shared__ float cols[kPage][DH];
   const int limit = (int)min((int64_t)a.max_pos, (int64_t)a.bt_stride * kPage);
   if ((int)blockIdx.x < q_groups) {
     constexpr int H = DH / 2, QR = DH / 8;
-    const int r = blockIdx.x, b = find_seq(a, r, &sh_seq);
+    const int r = blockIdx.x, b = find_seq(a, r);
     if (b < 0) return;
     const int pos = a.lens[b] - (a.row_start[b + 1] - r);
     if (pos < 0 || pos >= limit) return;
@@ -275,24 +288,18 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs a, int q
       const int at = t / QR * DH + t % QR * 4;
       f32x4 x = read4(src + at), y = read4(src + at + H);
       rotate4(x, y, a.rope + (int64_t)pos * H + t % QR * 4);
-      Vec4<QT> lo, hi;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        lo.e[e] = Elem<QT>::put(x[e], 1.f);
-        hi.e[e] = Elem<QT>::put(y[e], 1.f);
-      }
-      *(Vec4<QT>*)(dst + at) = lo;
-      *(Vec4<QT>*)(dst + at + H) = hi;
+      *(Vec4<QT>*)(dst + at) = put4<QT>(x, 1.f);
+      *(Vec4<QT>*)(dst + at + H) = put4<QT>(y, 1.f);
     }
     return;
   }
   const int id = blockIdx.x - q_groups, part = id % (2 * a.n_kv_heads), g = part / 2;
   const int r_end = min((id / (2 * a.n_kv_heads) + 1) * window, a.n_rows);
   int r = id / (2 * a.n_kv_heads) * window;
-  int b = -1, seq_row0 = 0, seq_end = 0, len = 0;
+  int b = -1, seq_row0 = 0, seq_end = 0, len = 0, turn = 0;
   while (r < r_end) {
     if (b < 0 || r >= seq_end) {
-      b = find_seq(a, r, &sh_seq);
+      b = find_seq(a, r);
       if (b < 0) {
         ++r;
         continue;
@@ -315,10 +322,11 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs a, int q
       const int64_t page = a.block_table[(int64_t)b * a.bt_stride + pos / kPage];
       if (page >= 0 && page < a.n_pages) {
         const Run run = {page, r, m, slot, pos};
+        ++turn;
         if (part & 1)
-          append_v<ST, KT, DH>(a, run, g, red);
+          append_v<ST, KT, DH>(a, run, g, turn, red);
         else
-          append_k<ST, KT, DH>(a, run, g, red, cols);
+          append_k<ST, KT, DH>(a, run, g, turn, red, cols);
       }
     }
     r += m;
