@@ -525,7 +525,8 @@ int paged_check_pages(int32_t batch, const int32_t* block_table, int32_t bt_stri
  * heads per KV head.  E4M3 pages (PDEC_FP8_E4M3) carry a scale for each page
  * and KV head, k_scales / v_scales device fp32 [n_pages][n_kv_heads]: an
  * element reads back as value(code) * scale.
- * Pages, q, out, tables of angles and workspaces are 16-byte aligned.
+ * Pages, q, out, tables of angles and workspaces are 16-byte aligned; what a
+ * call writes overlaps nothing else that it is given.
  * All calls are asynchronous on stream and touch nothing but their arguments;
  * calls that share a workspace must not overlap.
  * ------------------------------------------------------------------------- */
@@ -557,9 +558,9 @@ int rope_table(int32_t max_pos, int32_t head_dim, float base, float* table_dev, 
  *   [n_kv_heads][head_dim]; each page written gets the mean over its filled
  *   slots, the new ones the last, of the keys as they read back.
  * Left as they were: slots behind a page's new tokens, pages without a new
- * token, and everything of a row whose position is below 0 or at or past
- * max_pos or the table's bt_stride * 16, whose page id is not in
- * [0, n_pages), or that no sequence holds (q_out rows too).
+ * token, and everything, q_out too, of a row that no sequence holds or whose
+ * position is below 0 or at or past max_pos or the table's bt_stride * 16.  A
+ * row whose page id is not in [0, n_pages) appends nothing; its q is rotated.
  * Two sequences of a call must not append to the same page.
  * Errors: PDEC_INVALID_ARG, PDEC_UNSUPPORTED, PDEC_HIP_ERROR. */
 int paged_kv_append(int32_t src_dtype, int32_t kv_dtype, int32_t n_rows, int32_t n_seqs,

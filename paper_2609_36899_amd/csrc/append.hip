@@ -15,6 +15,7 @@
 // them (the page's leader) finds the page, and the others' rows do nothing.
 #include "hip_common.h"
 #include "kernels.h"
+#include "wave.h"
 
 #include <algorithm>
 #include <type_traits>
@@ -113,7 +114,7 @@ __device__ __forceinline__ float inverse_pow2(float s) {
 // Over the work group; `turn` counts its calls, which take two places in red in turn.
 __device__ __forceinline__ float group_max(float v, float (*red)[kWaves], int turn) {
   float* at = red[turn & 1];
-  v = wave_max(v);
+  v = wave_top(v);
   if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = v;
   __syncthreads();
   float t = at[0];
@@ -280,14 +281,14 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs a, int q
     constexpr int H = DH / 2, QR = DH / 8;
     const int r = blockIdx.x, b = find_seq(a, r);
     if (b < 0) return;
-    const int pos = a.lens[b] - (a.row_start[b + 1] - r);
+    const int64_t pos = (int64_t)a.lens[b] - ((int64_t)a.row_start[b + 1] - r);
     if (pos < 0 || pos >= limit) return;
     const ST* src = (const ST*)a.q + (int64_t)r * a.q_stride;
     QT* dst = (QT*)a.q_out + (int64_t)r * a.n_q_heads * DH;
     for (int t = threadIdx.x; t < a.n_q_heads * QR; t += kThreads) {
       const int at = t / QR * DH + t % QR * 4;
       f32x4 x = read4(src + at), y = read4(src + at + H);
-      rotate4(x, y, a.rope + (int64_t)pos * H + t % QR * 4);
+      rotate4(x, y, a.rope + pos * H + t % QR * 4);
       *(Vec4<QT>*)(dst + at) = put4<QT>(x, 1.f);
       *(Vec4<QT>*)(dst + at + H) = put4<QT>(y, 1.f);
     }
@@ -296,7 +297,8 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs a, int q
   const int id = blockIdx.x - q_groups, part = id % (2 * a.n_kv_heads), g = part / 2;
   const int r_end = min((id / (2 * a.n_kv_heads) + 1) * window, a.n_rows);
   int r = id / (2 * a.n_kv_heads) * window;
-  int b = -1, seq_row0 = 0, seq_end = 0, len = 0, turn = 0;
+  int b = -1, seq_row0 = 0, seq_end = 0, turn = 0;
+  int64_t end_pos = 0;  // position behind row seq_end - 1; whatever the lengths hold fits
   while (r < r_end) {
     if (b < 0 || r >= seq_end) {
       b = find_seq(a, r);
@@ -306,17 +308,18 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs a, int q
       }
       seq_row0 = a.row_start[b];
       seq_end = min(a.row_start[b + 1], a.n_rows);
-      len = a.lens[b] - (a.row_start[b + 1] - seq_end);
+      end_pos = (int64_t)a.lens[b] - ((int64_t)a.row_start[b + 1] - seq_end);
     }
-    const int pos = len - (seq_end - r);
-    if (pos < 0) {  // more rows than the sequence has tokens
-      r = min(seq_end, r + min(-pos, seq_end - r));
+    const int64_t at = end_pos - (seq_end - r);
+    if (at < 0) {  // more rows than the sequence has tokens
+      r = -at < seq_end - r ? r + (int)-at : seq_end;
       continue;
     }
-    if (pos >= limit) {
+    if (at >= limit) {
       r = seq_end;
       continue;
     }
+    const int pos = (int)at;
     const int slot = pos % kPage, m = min(min(kPage - slot, seq_end - r), limit - pos);
     if (r == seq_row0 || slot == 0) {
       const int64_t page = a.block_table[(int64_t)b * a.bt_stride + pos / kPage];

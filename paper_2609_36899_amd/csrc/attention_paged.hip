@@ -461,11 +461,8 @@ __global__ __launch_bounds__(kThreads) void paged_merge_kernel(PagedAttnArgs a, 
     all += n;
     before += v < u ? n : 0;
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    all += __shfl_xor(all, o, 64);
-    before += __shfl_xor(before, o, 64);
-  }
+  all = wave_add(all);
+  before = wave_add(before);
   if (lane == 0) {
     red[0][wave] = all;
     red[1][wave] = before;

@@ -27,6 +27,11 @@ __device__ __forceinline__ int seq_pages(const int32_t* lens, int b, int bt_stri
   return min(len / kPage + (len % kPage != 0), bt_stride);
 }
 
+template <int CTRL>
+__device__ __forceinline__ double swapped(double v) {
+  return __longlong_as_double((int64_t)dpp<CTRL>((uint64_t)__double_as_longlong(v)));
+}
+
 // Scores.  A wave takes tiles of 16 pages of one KV head.  The product runs on
 // v_mfma_f64_4x4x4_4b, whose four blocks of 4 x 4 x 4 multiply 16 pages with four query
 // heads, every lane busy and no sum across lanes: lane l holds page l % 16 and the dims
@@ -129,8 +134,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) v
                 MANY ? (double)qs[wave][hg][j * 8 + e][k4 * 4 + (lane & 3)] : q[j * 8 + e], s[e % 2], 0, 0, 0);
         best = fmax(best, s[0] + s[1]);  // a NaN never wins
       }
-      best = fmax(best, __shfl_xor(best, 1, 64));
-      best = fmax(best, __shfl_xor(best, 2, 64));
+      best = fmax(best, swapped<0xB1>(best));  // with lane ^ 1
+      best = fmax(best, swapped<0x4E>(best));  // with lane ^ 2
       const int i = 4 * ((lane >> 2) & 3) + k4;  // the page of this lane's result
       const bool named = __shfl((int)ok, i, 64);
       if ((lane & 3) == 0 && p0 + i < end)
@@ -185,11 +190,8 @@ __global__ __launch_bounds__(T) void take_pages_kernel(SelectArgs a) {
   }
   hist[threadIdx.x] = 0;
   if (threadIdx.x == 0) pick[3] = 0;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, 64));
-    hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, 64));
-  }
+  lo = wave_all(lo, [](uint32_t x, uint32_t y) { return min(x, y); });
+  hi = wave_all(hi, [](uint32_t x, uint32_t y) { return max(x, y); });
   if (lane == 0) {
     range[0][wave] = lo;
     range[1][wave] = hi;
@@ -204,12 +206,7 @@ __global__ __launch_bounds__(T) void take_pages_kernel(SelectArgs a) {
   auto crossing = [&](int left) {
     __syncthreads();
     const int c = hist[T - 1 - threadIdx.x];
-    int incl = c;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int t = __shfl_up(incl, o, 64);
-      if (lane >= o) incl += t;
-    }
+    const int incl = wave_prefix(c);
     if (lane == 63) red[0][wave] = incl;
     __syncthreads();
     int above = incl - c;
@@ -253,8 +250,8 @@ __global__ __launch_bounds__(T) void take_pages_kernel(SelectArgs a) {
         }
         const uint64_t hit = __ballot(lane < m && over < want && want <= over + equal);
         const int l = __builtin_ctzll(hit);
-        lo = (uint32_t)__shfl((int)mine, l, 64);
-        left = want - __shfl(over, l, 64);
+        lo = (uint32_t)lane_of((int)mine, l);
+        left = want - lane_of(over, l);
         ranked = true;
       }
     }
@@ -303,14 +300,9 @@ __global__ __launch_bounds__(T) void take_pages_kernel(SelectArgs a) {
       int base = wave ? ties : done;
       for (int j = 0; j < STEPS * W; j += 64) {
         const int v = j + lane < STEPS * W ? count[wave][j + lane] : 0;
-        int incl = v;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-          const int t = __shfl_up(incl, o, 64);
-          if (lane >= o) incl += t;
-        }
+        const int incl = wave_prefix(v);
         if (j + lane < STEPS * W) count[wave][j + lane] = base + incl - v;
-        base += __shfl(incl, 63, 64);
+        base += lane_of(incl, 63);
       }
       if (lane == 0) red[wave][0] = base;
     }

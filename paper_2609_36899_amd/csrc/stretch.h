@@ -2,7 +2,7 @@
 // equal stretches, one for each work group, from lengths that only the device knows.
 #pragma once
 
-#include "hip_common.h"
+#include "wave.h"
 
 namespace pdec {
 
@@ -10,12 +10,7 @@ namespace pdec {
 template <int T>
 __device__ __forceinline__ int group_scan(int v, int* red, int* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int incl = v;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int t = __shfl_up(incl, o, 64);
-    if (lane >= o) incl += t;
-  }
+  const int incl = wave_prefix(v);
   __syncthreads();
   if (lane == 63) red[wave] = incl;
   __syncthreads();

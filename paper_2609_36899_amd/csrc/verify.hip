@@ -34,6 +34,7 @@
 // and their drafter's logits at 128256 tokens (87 + 125 + 62 + 51).
 #include "hip_common.h"
 #include "kernels.h"
+#include "wave.h"
 
 #include <algorithm>
 #include <cfloat>
@@ -142,13 +143,8 @@ __device__ __forceinline__ double mass_of(float z, double m, double inv_t, const
   return x >= kMinX ? e : 0.0;  // (what lies below, and NaN, came to anything)
 }
 
-__device__ __forceinline__ uint64_t wave_sum_u64(uint64_t v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
-}
 __device__ __forceinline__ uint64_t group_sum(uint64_t v, uint64_t* red) {
-  v = wave_sum_u64(v);
+  v = wave_add(v);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
@@ -200,14 +196,14 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyArgs a, Si
   float m = -INFINITY;  // fmaxf takes no NaN
 #pragma unroll
   for (int k = 0; k < Q; ++k) m = fmaxf(m, fmaxf(fmaxf(v[k].x, v[k].y), fmaxf(v[k].z, v[k].w)));
-  m = wave_max(m);
+  m = wave_top(m);
   float sum = 0.f;
 #pragma unroll
   for (int k = 0; k < Q; ++k)
 #pragma unroll
     for (int e = 0; e < 4; ++e)  // -inf and NaN: 2^-150, which is 0
       sum += __builtin_amdgcn_exp2f(fmaxf((v[k][e] - m) * c2, -150.f));
-  sum = wave_sum(sum);
+  sum = wave_add(sum);
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = make_float2(m, sum);
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -234,8 +230,8 @@ __device__ __forceinline__ float2 row_stat(const Work& w, const Sizes& s, int ro
              o.y * __builtin_amdgcn_exp2f(fmaxf((o.x - m) * c2, -150.f));
     mine.x = m;
   }
-  const float m = wave_max(mine.x);
-  return make_float2(m, wave_sum(mine.y * __builtin_amdgcn_exp2f(fmaxf((mine.x - m) * c2, -150.f))));
+  const float m = wave_top(mine.x);
+  return make_float2(m, wave_add(mine.y * __builtin_amdgcn_exp2f(fmaxf((mine.x - m) * c2, -150.f))));
 }
 
 // ---- 2. judge ----------------------------------------------------------------
@@ -379,8 +375,8 @@ __device__ __forceinline__ Next next_of(const VerifyArgs& a, const Sizes& s, con
   r.zd = r.off == kDrafter ? a.drafter + ((int64_t)b * a.n_drafts + v.n) * a.vocab : nullptr;
   r.pm = v.pm;
   r.dm = v.dm;
-  r.pi = unit_over(wave_sum_u64(p));
-  r.di = unit_over(wave_sum_u64(d));
+  r.pi = unit_over(wave_add(p));
+  r.di = unit_over(wave_add(d));
   r.inv_t = a.inv_t;
   r.frac = frac;
   r.refused = v.refused;
@@ -405,7 +401,7 @@ __global__ __launch_bounds__(kThreads) void verify_rest_kernel(VerifyArgs a, Siz
       }
     });
   });
-  const uint64_t r_sum = wave_sum_u64(to_u64(rest)), p_sum = wave_sum_u64(to_u64(all));
+  const uint64_t r_sum = wave_add(to_u64(rest)), p_sum = wave_add(to_u64(all));
   if ((threadIdx.x & 63) == 0)
     w.rest[(int64_t)b * s.n_chunks * kParts + part] = make_ulonglong2(r_sum, p_sum);
 }
@@ -425,9 +421,9 @@ __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyArgs a, Siz
     z += part[c].x;
     all += part[c].y;
   }
-  z = wave_sum_u64(z);
+  z = wave_add(z);
   const bool own = z == 0;  // nothing left beside the drafts': the target's own
-  if (own) z = wave_sum_u64(all);
+  if (own) z = wave_add(all);
   const uint64_t u = u24_of(a.uniforms[(int64_t)b * (a.n_drafts + 1) + a.n_drafts]);
   const uint64_t goal = (uint64_t)(((unsigned __int128)u * z) >> 24);
   if (threadIdx.x == 0) found = 0;
@@ -437,20 +433,15 @@ __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyArgs a, Siz
     int at = 0;
     for (int c0 = 0; c0 < n_parts; c0 += 64) {
       const uint64_t v = c0 + lane < n_parts ? (own ? part[c0 + lane].y : part[c0 + lane].x) : 0;
-      uint64_t incl = v;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const uint64_t t = __shfl_up(incl, o, 64);
-        if (lane >= o) incl += t;
-      }
+      const uint64_t incl = wave_prefix(v);
       const uint64_t hit = __ballot(run + incl > goal);
       if (hit) {
         const int l = __builtin_ctzll(hit);
         at = c0 + l;
-        run += __shfl(incl, l, 64) - __shfl(v, l, 64);
+        run += lane_of(incl, l) - lane_of(v, l);
         break;
       }
-      run += __shfl(incl, 63, 64);
+      run += lane_of(incl, 63);
     }
     // Eight tokens a thread side by side, one scan, and the thread that passes the goal
     // walks its own.
@@ -474,12 +465,7 @@ __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyArgs a, Siz
         sum += mine[e];
       }
     });
-    uint64_t incl = sum;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint64_t t = __shfl_up(incl, o, 64);
-      if (lane >= o) incl += t;
-    }
+    const uint64_t incl = wave_prefix(sum);
     if (lane == 63) red[wave] = incl;
     __syncthreads();
     run += incl - sum;

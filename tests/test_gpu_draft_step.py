@@ -121,3 +121,65 @@ def test_decode_loop_with_drafts(fp8):
         # Refused drafts go by the length; their slots are written again.
         lens -= T - n
         tokens = new[torch.arange(B), n.long()][:, None].contiguous()
+
+
+def test_binding_refuses_wrong_tensors():
+    import paper_2609_36899_amd as P
+    from paper_2609_36899_amd import PdecError
+    bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    new = lambda dt, *s: torch.zeros(s, dtype=dt, device="cuda")
+    kp, vp = new(bf, 3, 2, 16, 64), new(bf, 3, 2, 64, 16)
+    c8, v8, sc = new(torch.uint8, 3, 2, 16, 64), new(torch.uint8, 3, 2, 64, 16), new(f32, 3, 2)
+    q, bt, lens, out = new(bf, 2, 4, 64), new(i32, 2, 3), new(i32, 2), new(bf, 2, 4, 64)
+    good = dict(q=q, k_pages=kp, v_pages=vp, block_table=bt, lens=lens, out=out)
+    P.paged_token_attention(**good)
+    for change, word in [
+            (dict(q=q.float()), "q must be"), (dict(q=q[:, :3]), "contiguous|multiple"),
+            (dict(q=None), "GPU tensor"), (dict(out=new(bf, 2, 4, 128)), "out must have shape"),
+            (dict(lens=lens.long()), "lens must be"), (dict(lens=lens.cpu()), "GPU tensor"),
+            (dict(lens=new(i32, 3)), "lens must have"), (dict(block_table=bt.t()), "block_table"),
+            (dict(v_pages=kp), "v_pages must have"), (dict(k_pages=kp.float()), "v_pages must be"),
+            (dict(k_pages=kp[:, :, :8]), "16 tokens"), (dict(k_pages=c8, v_pages=v8), "k_scales"),
+            (dict(k_scales=sc), "others none"),
+            (dict(k_pages=c8, v_pages=v8, k_scales=sc, v_scales=new(f32, 2, 2)), "v_scales"),
+            (dict(selected=new(i32, 2, 2, 5).long()), "selected"),
+            (dict(q=new(bf, 2, 3, 4, 64), out=new(bf, 2, 3, 4, 64), selected=new(i32, 2, 2, 5)),
+             "one query token"),
+            (dict(workspace=new(torch.uint8, 16)), "too small"),
+            (dict(workspace=torch.zeros(1 << 20)), "workspace must be"),
+            (dict(q=new(bf, 2 * 4 * 64 + 1)[1:].view(2, 4, 64)), "aligned")]:
+        with pytest.raises(PdecError, match=word):
+            P.paged_token_attention(**{**good, **change})
+    k, rope, starts = new(bf, 5, 2, 64), P.rope_table(40, 64), new(i32, 3)
+    append = dict(k=k, v=k, lens=lens, row_start=starts, block_table=bt, rope=rope, k_pages=kp,
+                  v_pages=vp)
+    P.paged_kv_append(**append)
+    for change, word in [
+            (dict(k=k.float()), "v must be"), (dict(v=new(bf, 4, 2, 64)), "v must have"),
+            (dict(k=k.transpose(0, 1).contiguous().transpose(0, 1), v=k), "side by side"),
+            (dict(k=k.half(), v=k.half()), "k must be"), (dict(row_start=lens), "row_start"),
+            (dict(rope=rope[:, :16]), "rope"), (dict(q=k), "q_out"), (dict(q_out=k), "together"),
+            (dict(k_means=new(f32, 3, 2, 64)), "k_means"), (dict(k_pages=kp.float()), "v_pages")]:
+        with pytest.raises(PdecError, match=word):
+            P.paged_kv_append(**{**append, **change})
+    means, sel = new(bf, 3, 2, 64), new(i32, 2, 2, 3)
+    P.paged_select(q, means, bt, lens, sel)
+    for args, word in [((q, means.float(), bt, lens, sel), "k_means"),
+                       ((q, means, bt, lens, sel[:1]), "selected"),
+                       ((new(bf, 2, 3, 64), means, bt, lens, sel), "multiple"),
+                       ((q, means, bt[:1], lens, sel), "block_table")]:
+        with pytest.raises(PdecError, match=word):
+            P.paged_select(*args)
+    with pytest.raises(PdecError, match="keep_first"):
+        P.paged_select(q, means, bt, lens, sel, keep_first=3)
+    z, u, n = new(f32, 2, 4, 50), new(f32, 2, 4), new(i32, 2)
+    verify = dict(target_logits=z, draft_tokens=new(i32, 2, 3), uniforms=u,
+                  tokens_out=new(i32, 2, 4), accepted_out=n)
+    P.verify_drafts(**verify)
+    for change, word in [(dict(target_logits=z.double()), "target_logits"),
+                         (dict(draft_tokens=new(i32, 2, 4)), "draft_tokens"),
+                         (dict(draft_logits=z), "draft_logits"), (dict(temperature=0.0), "temp"),
+                         (dict(uniforms=u[:, :3]), "uniforms")]:
+        with pytest.raises(PdecError, match=word):
+            P.verify_drafts(**{**verify, **change})
+    torch.cuda.synchronize()

@@ -235,6 +235,15 @@ def test_what_is_out_of_range_is_left_out(kind):
     c.check()
 
 
+def test_lengths_at_the_ends_of_their_type_append_nothing():
+    c = Case([40, 40, 40, 40], [4, 4, 4, 4], 4, 2, 64, "fp8", "f32", seed=14)
+    before = [t.clone() for t in (c.kp, c.vp, c.ks, c.vs, c.q_out, c.means)]
+    c.lens = np.array([-2 ** 31, -2 ** 31 + 2, -1, 2 ** 31 - 1], np.int32)
+    c.call()
+    for t, old in zip((c.kp, c.vp, c.ks, c.vs, c.q_out, c.means), before):
+        assert torch.equal(t, old)
+
+
 def test_token_by_token_equals_at_once():
     """bf16 pages: the same bytes either way.  E4M3 pages: the same scales, and codes that
     differ only where a growing scale took earlier ones below the normal range."""
