@@ -148,13 +148,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) v
 // equal width over the range of the scores leaves a few pages in the bin that holds the
 // last one taken, which a wave ranks; where it leaves more than a wave's lanes (equal
 // scores, an outlier that widens the range), histograms over the scores' bits narrow it
-// down.  Scores wait in LDS meanwhile.  Page order comes from ballots and one scan of the
+// down.  A thread holds eight scores meanwhile and reads again what is past them.  Page order comes from ballots and one scan of the
 // waves' counts.  Eight bits at a time from the top of the float, a scan for each step of
 // pages, took 57 us for 8188 pages; bits of the range, two or three rounds, 14.
 template <int T>
 __global__ __launch_bounds__(T) void take_pages_kernel(SelectArgs a) {
-  constexpr int W = T / 64, BITS = T == 1024 ? 10 : 8, CACHE = 8 * T, STEPS = 8;
-  __shared__ uint32_t keys[CACHE];
+  constexpr int W = T / 64, BITS = T == 1024 ? 10 : T == 512 ? 9 : 8, STEPS = 8;
   __shared__ int hist[T];
   __shared__ int red[2][W];
   __shared__ uint32_t range[2][W];
@@ -177,17 +176,28 @@ __global__ __launch_bounds__(T) void take_pages_kernel(SelectArgs a) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
   };
   auto value = [](uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); };
-  auto key_at = [&](int i) { return i < CACHE ? keys[i] : read(i); };
   auto kept = [&](int i) { return i < a.keep_first || i >= n - a.keep_last; };
-  uint32_t lo = 0xFFFFFFFFu, hi = 0;
-  for (int i = threadIdx.x; i < n; i += T) {
-    const uint32_t k = read(i);
-    if (i < CACHE) keys[i] = k;
-    if (!kept(i)) {
-      lo = min(lo, k);
-      hi = max(hi, k);
-    }
+  uint32_t held[STEPS];
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s) {
+    const int i = s * T + threadIdx.x;
+    if (i < n) held[s] = read(i);
   }
+  // f(key) for this thread's pages that are not kept.
+  auto each = [&](auto&& f) {
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      const int i = s * T + threadIdx.x;
+      if (i < n && !kept(i)) f(held[s]);
+    }
+    for (int i = STEPS * T + threadIdx.x; i < n; i += T)
+      if (!kept(i)) f(read(i));
+  };
+  uint32_t lo = 0xFFFFFFFFu, hi = 0;
+  each([&](uint32_t k) {
+    lo = min(lo, k);
+    hi = max(hi, k);
+  });
   hist[threadIdx.x] = 0;
   if (threadIdx.x == 0) pick[3] = 0;
   lo = wave_all(lo, [](uint32_t x, uint32_t y) { return min(x, y); });
@@ -230,15 +240,13 @@ __global__ __launch_bounds__(T) void take_pages_kernel(SelectArgs a) {
     auto bin_of = [&](uint32_t k) { return min((int)((value(k) - s0) * per), T - 1); };
     bool ranked = false;
     if (even) {
-      for (int i = threadIdx.x; i < n; i += T)
-        if (!kept(i)) atomicAdd(&hist[bin_of(key_at(i))], 1);
+      each([&](uint32_t k) { atomicAdd(&hist[bin_of(k)], 1); });
       crossing(left);
       const int bin = pick[0], want = pick[1];
       if (pick[2] <= 64) {
-        for (int i = threadIdx.x; i < n; i += T) {
-          const uint32_t k = key_at(i);
-          if (!kept(i) && bin_of(k) == bin) few[atomicAdd(&pick[3], 1)] = k;
-        }
+        each([&](uint32_t k) {
+          if (bin_of(k) == bin) few[atomicAdd(&pick[3], 1)] = k;
+        });
         __syncthreads();
         // The want-th largest of them, and how many of its equals are wanted.
         const int m = pick[2];
@@ -261,10 +269,9 @@ __global__ __launch_bounds__(T) void take_pages_kernel(SelectArgs a) {
       __syncthreads();
       hist[threadIdx.x] = 0;
       __syncthreads();
-      for (int i = threadIdx.x; i < n; i += T) {
-        const uint32_t k = key_at(i);
-        if (k >= lo && k <= hi && !kept(i)) atomicAdd(&hist[(k - lo) >> shift], 1);
-      }
+      each([&](uint32_t k) {
+        if (k >= lo && k <= hi) atomicAdd(&hist[(k - lo) >> shift], 1);
+      });
       crossing(left);
       lo += (uint32_t)pick[0] << shift;
       hi = shift ? min(hi, lo + ((1u << shift) - 1)) : lo;
@@ -283,7 +290,7 @@ __global__ __launch_bounds__(T) void take_pages_kernel(SelectArgs a) {
       const int i = i0 + s * T + threadIdx.x;
       bool o = false, t = false;
       if (i < n) {
-        const uint32_t k = key_at(i);
+        const uint32_t k = i0 == 0 ? held[s] : read(i);
         o = kept(i) || k > lo || (all && k == lo);
         t = !o && k == lo;
       }
@@ -339,8 +346,11 @@ hipError_t launch_paged_select(int head_dim, const SelectArgs& a, hipStream_t st
 #undef PDEC_SCORES
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (a.bt_stride > 2048)
+  // Threads for eight pages each, up to what a work group holds.
+  if (a.bt_stride > 4096)
     take_pages_kernel<1024><<<(uint32_t)rows, 1024, 0, stream>>>(a);
+  else if (a.bt_stride > 512)
+    take_pages_kernel<512><<<(uint32_t)rows, 512, 0, stream>>>(a);
   else
     take_pages_kernel<256><<<(uint32_t)rows, 256, 0, stream>>>(a);
   return hipGetLastError();
