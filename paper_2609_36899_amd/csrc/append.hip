@@ -13,6 +13,11 @@
 // exact but for codes that become subnormal, since both scales are powers of two.
 // So one work group handles all of a page's new tokens of one head: the first of
 // them (the page's leader) finds the page, and the others' rows do nothing.
+//
+// Prompts are bound by HBM (4096 fp32 rows of 32 + 8 + 8 heads into bf16 pages, 153 MB read
+// and written: 34 us, 4.5 TB/s, where a copy reaches 4.9; 1600 rows into E4M3 pages, 52 MB,
+// 17), single tokens by one chain of loads: row, length, page, scale (64 sequences 7 us).
+// V is taken eight slots of a dim a thread, so that a whole page half is one store.
 #include "hip_common.h"
 #include "kernels.h"
 #include "wave.h"

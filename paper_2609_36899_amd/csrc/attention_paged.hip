@@ -34,9 +34,11 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 // Work groups of a launch: one for each compute unit.  More of them cost their beginnings
-// (lengths, queries, first pages) and their partials: us at 256 / 512 / 1024 groups, 64
-// sequences of 1K to 8K tokens 120 / 119 / 126 (E4M3) and 179 / 178 / 180 (bf16), five
-// tokens each over 8 x 64K to 128K 267 / 281 / 315, four over 16 x 1K to 16K 102 / 114 / 133.
+// (lengths, queries, first pages) and their partials: us at 256 / 512 groups, 64 sequences
+// of 1K to 8K tokens 120 / 119 (E4M3, 648 MB: 5.4 TB/s) and 180 / 179 (bf16, 1136 MB: 6.3),
+// five tokens each over 8 x 64K to 128K 267 / 283 (E4M3, 1580 MB: 5.9), four over 16 x 1K to
+// 16K 94 / 96 (bf16, 512 MB: 5.4), 16 over 16 x 4K to 8K 77 / 112; 1024 groups are slower by
+// 5 to 20% more.
 constexpr int kGroups = 256;
 constexpr int kPair = 2 * kPage;        // keys of a pair of pages
 constexpr int kNowhere = 0x40000000;    // a key position past every limit
@@ -251,10 +253,12 @@ __attribute__((amdgpu_waves_per_eu((sizeof(KT) == 1 ? 3 : 4) - RT))) void paged_
         if constexpr (kFp8) vf[d] = __builtin_bit_cast(u16x8, decode8(r.v[d]));
         else vf[d] = __builtin_bit_cast(u16x8, r.v[d]);
       }
-      const float k_mul = kFp8 ? a.scale_log2 * r.ks : a.scale_log2;
-      const float v_mul = kFp8 ? r.vs : 1.f;
-      const float v_inv = kFp8 ? __builtin_amdgcn_rcpf(v_mul) : 1.f;
       const int kbase = (v_sel ? r.key0[1] : r.key0[0]) + v_tok0;  // position of this lane's key 0
+      // The scales of page 0 stand in for those of no page, and may be anything.
+      const bool scaled = kFp8 && kbase < kNowhere;
+      const float k_mul = scaled ? a.scale_log2 * r.ks : a.scale_log2;
+      const float v_mul = scaled ? r.vs : 1.f;
+      const float v_inv = kFp8 ? __builtin_amdgcn_rcpf(v_mul) : 1.f;
       // Keys without data: 0 times what they hold may be NaN.  (Uniform over the wave;
       // with kNone only where the table names no page.)
       const bool hole = max(r.key0[0], r.key0[1]) + kPage > kv_lim;

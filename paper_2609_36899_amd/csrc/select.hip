@@ -150,7 +150,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) v
 // scores, an outlier that widens the range), histograms over the scores' bits narrow it
 // down.  A thread holds eight scores meanwhile and reads again what is past them.  Page order comes from ballots and one scan of the
 // waves' counts.  Eight bits at a time from the top of the float, a scan for each step of
-// pages, took 57 us for 8188 pages; bits of the range, two or three rounds, 14.
+// pages, took 57 us for 8188 pages; bits of the range, two or three rounds, 14; this 10.
 template <int T>
 __global__ __launch_bounds__(T) void take_pages_kernel(SelectArgs a) {
   constexpr int W = T / 64, BITS = T == 1024 ? 10 : T == 512 ? 9 : 8, STEPS = 8;

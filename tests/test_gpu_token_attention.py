@@ -186,6 +186,38 @@ def test_page_ids_outside_the_pool_have_no_keys(fp8):
     assert (c.run()[2] == 0).all()
 
 
+@pytest.mark.parametrize("n_q", [1, 3])
+@pytest.mark.parametrize("garbage", [np.nan, np.inf, -np.inf, -1.0, 0.0])
+def test_pages_that_no_sequence_reads_may_hold_anything(garbage, n_q):
+    """Page 0 is nobody's: scales and codes of any kind there reach no output, neither where
+    a page stands alone at a sequence's end nor where an id names none."""
+    for lens in ([1, 16, 33, 100, 47], [1, 16, 33, 100, 47, 2000]):
+        c = Case(lens, 8, 2, 64, n_q=n_q, seed=17)
+        used = np.concatenate([c.table[b, :-(-n // 16)] for b, n in enumerate(lens)])
+        free = int(np.setdiff1d(np.arange(c.P), used)[0])
+        order = np.arange(c.P)
+        order[[0, free]] = free, 0
+        for name in ("k", "v", "ks", "vs"):
+            setattr(c, name, getattr(c, name)[order])
+        c.table = order[c.table].astype(np.int32)
+        c.k[0], c.v[0] = 0x7F, 0x7F
+        c.ks[0], c.vs[0] = garbage, garbage
+        want = c.run()
+        assert np.isfinite(want).all()
+        c.table[3, 2], c.table[4, 0] = -1, c.P
+        if n_q == 1:
+            pages = max(-(-n // 16) for n in lens)
+            c.selected = np.tile(np.arange(pages, dtype=np.int32)[::-1].copy(), (len(lens), 2, 1))
+            for b, n in enumerate(lens):
+                m = -(-n // 16)
+                c.selected[b, :, :m] = np.arange(m)[::-1]
+        got = c.run()
+        k, v = c.values()
+        k[0] = v[0] = 0.0
+        ref, size = oo.token_attention(c.q.float().numpy(), k, v, c.table, c.lens, c.selected)
+        assert (np.abs(got - ref) <= c.bound(ref, size, k)).all()
+
+
 def test_lengths_past_the_table_are_cut_and_negative_ones_empty():
     c = Case([64, 30], 4, 2, 64, seed=10)
     c.table = np.ascontiguousarray(c.table[:, :4])
