@@ -585,13 +585,16 @@ int paged_kv_append(int32_t src_dtype, int32_t kv_dtype, int32_t n_rows, int32_t
  *   positions below lens[b] in those pages alone.
  *   Scores, softmax and sums are fp32; the weights enter the second product
  *   rounded to bf16.
- *   workspace: device, paged_token_attention_workspace_bytes(...) bytes.
+ *   workspace: device, paged_token_attention_workspace_bytes(...) bytes for
+ *   the same sizes (0 where no table is long: then it may be null); max_pages
+ *   is bt_stride, or the smaller of it and n_selected with a selection.
  * Entries that are not page indices (paged_select's -1 among them) or whose
  * page id is outside [0, n_pages) have no keys.
  * Errors: PDEC_INVALID_ARG (n_q outside [1, 4096], ...), PDEC_UNSUPPORTED,
  * PDEC_HIP_ERROR. */
 int64_t paged_token_attention_workspace_bytes(int32_t batch, int32_t n_q, int32_t n_q_heads,
-                                              int32_t n_kv_heads, int32_t head_dim);
+                                              int32_t n_kv_heads, int32_t head_dim,
+                                              int32_t max_pages);
 int paged_token_attention(int32_t kv_dtype, int32_t batch, int32_t n_q, int32_t n_q_heads,
                           int32_t n_kv_heads, int32_t head_dim, const void* q,
                           const void* k_pages, const void* v_pages, const float* k_scales,

@@ -113,7 +113,7 @@ SIGNATURES = {
     "rope_table": (c_int32, [c_int32, c_int32, c_float, c_void_p, c_void_p]),
     "paged_kv_append": (c_int32, [c_int32] * 7 + [c_void_p, c_int64] * 3 + [c_void_p] * 3
                         + [c_int32, c_int64, c_void_p, c_int32] + [c_void_p] * 7),
-    "paged_token_attention_workspace_bytes": (c_int64, [c_int32] * 5),
+    "paged_token_attention_workspace_bytes": (c_int64, [c_int32] * 6),
     "paged_token_attention": (c_int32, [c_int32] * 6 + [c_void_p] * 5
                               + [c_int64, c_void_p, c_int32, c_void_p, c_void_p, c_int32,
                                  c_void_p, c_void_p, c_int64, c_void_p]),

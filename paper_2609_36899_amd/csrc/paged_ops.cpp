@@ -44,6 +44,7 @@ struct TokenAttnLayout {
   int64_t ml, acc;  // byte offsets end here: ml, then ml + acc
 };
 TokenAttnLayout layout_of(const PagedAttnPlan& p, int32_t n_kv_heads, int32_t head_dim) {
+  if (p.unit_groups) return {0, 0};  // no partials
   const int64_t rows = (p.n_groups + p.n_units) * n_kv_heads * 16 * p.row_tiles;
   return {align_up(rows * 2 * 4), align_up(rows * head_dim * 4)};
 }
@@ -135,11 +136,13 @@ int paged_kv_append(int32_t src_dtype, int32_t kv_dtype, int32_t n_rows, int32_t
 }
 
 int64_t paged_token_attention_workspace_bytes(int32_t batch, int32_t n_q, int32_t n_q_heads,
-                                              int32_t n_kv_heads, int32_t head_dim) {
+                                              int32_t n_kv_heads, int32_t head_dim,
+                                              int32_t max_pages) {
   const int rc = check_token_attention(batch, n_q, n_q_heads, n_kv_heads, head_dim);
   if (rc != PDEC_OK) return rc;
-  const TokenAttnLayout l = layout_of(plan_paged_attention(batch, n_q, n_q_heads, n_kv_heads, 1),
-                                      n_kv_heads, head_dim);
+  if (max_pages < 1 || max_pages > kMaxStride) return fail(PDEC_INVALID_ARG, "bad max_pages");
+  const TokenAttnLayout l = layout_of(
+      plan_paged_attention(batch, n_q, n_q_heads, n_kv_heads, max_pages), n_kv_heads, head_dim);
   return l.ml + l.acc;
 }
 
@@ -152,7 +155,7 @@ int paged_token_attention(int32_t kv_dtype, int32_t batch, int32_t n_q, int32_t 
                           void* stream) {
   if (kv_dtype != PDEC_BF16 && kv_dtype != PDEC_FP8_E4M3)
     return fail(PDEC_INVALID_ARG, "kv_dtype must be PDEC_BF16 or PDEC_FP8_E4M3");
-  if (!q || !k_pages || !v_pages || !block_table_dev || !lens_dev || !out || !workspace)
+  if (!q || !k_pages || !v_pages || !block_table_dev || !lens_dev || !out)
     return fail(PDEC_INVALID_ARG, "null argument");
   int rc = check_token_attention(batch, n_q, n_q_heads, n_kv_heads, head_dim);
   if (rc == PDEC_OK) rc = check_table(batch, bt_stride, n_pages);
@@ -171,7 +174,7 @@ int paged_token_attention(int32_t kv_dtype, int32_t batch, int32_t n_q, int32_t 
   if (p.n_units * ((int64_t)bt_stride + 1) > INT32_MAX)
     return fail(PDEC_INVALID_ARG, "batch x bt_stride too large for one call");
   const TokenAttnLayout l = layout_of(p, n_kv_heads, head_dim);
-  if (workspace_bytes < l.ml + l.acc)
+  if (workspace_bytes < l.ml + l.acc || (l.ml > 0 && !workspace))
     return fail(PDEC_INVALID_ARG, "workspace too small: need " + std::to_string(l.ml + l.acc));
   PagedAttnArgs a{};
   a.q = q;

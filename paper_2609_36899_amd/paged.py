@@ -76,38 +76,43 @@ def _rows(t, name: str, dtype, shape, dev: int) -> int:
     return row if n > 1 else h * d
 
 
-class _Call:
-    """The stream of a call on GPU dev, and its workspace."""
+def _handle(dev: int, stream: Optional[torch.cuda.Stream]) -> int:
+    """The stream handle of a call on GPU dev."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev)
+    if stream.device_index != dev:
+        _refuse("stream is on another device")
+    return stream.cuda_stream
 
-    __slots__ = ("dev", "stream", "handle")
 
-    def __init__(self, dev: int, stream: Optional[torch.cuda.Stream]):
-        self.dev, self.stream = dev, stream
+def _workspace(given: Optional[torch.Tensor], need: int, dev: int,
+               stream: Optional[torch.cuda.Stream]):
+    """(tensor, address, bytes) of a call's workspace."""
+    if given is None:
+        if need == 0:
+            return None, None, 0
         if stream is None:
-            self.handle = torch._C._cuda_getCurrentRawStream(dev)
+            given = torch.empty(need, dtype=torch.uint8, device=dev)
         else:
-            if stream.device_index != dev:
-                _refuse("stream is on another device")
-            self.handle = stream.cuda_stream
+            with torch.cuda.stream(stream):
+                given = torch.empty(need, dtype=torch.uint8, device=dev)
+        return given, given.data_ptr(), need
+    if given.get_device() != dev or not given.is_contiguous():
+        _refuse("workspace must be a contiguous tensor on the call's device")
+    have = given.numel() * given.element_size()
+    if have < need:
+        _refuse(f"workspace too small: need {need} bytes")
+    return given, given.data_ptr(), have
 
-    def workspace(self, given: Optional[torch.Tensor], need: int) -> torch.Tensor:
-        if given is None:
-            if self.stream is None:
-                return torch.empty(need, dtype=torch.uint8, device=self.dev)
-            with torch.cuda.stream(self.stream):
-                return torch.empty(need, dtype=torch.uint8, device=self.dev)
-        if not given.is_cuda or given.get_device() != self.dev or not given.is_contiguous():
-            _refuse("workspace must be a contiguous tensor on the call's device")
-        if given.numel() * given.element_size() < need:
-            _refuse(f"workspace too small: need {need} bytes")
-        return given
 
-    def run(self, fn, *args) -> None:
-        if torch.cuda.current_device() == self.dev:
-            N.check(fn(*args, self.handle))
-        else:
-            with torch.cuda.device(self.dev):
-                N.check(fn(*args, self.handle))
+def _run(dev: int, fn, *args) -> None:
+    if torch._C._cuda_getDevice() == dev:
+        rc = fn(*args)
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args)
+    if rc < 0:
+        N.check(rc)
 
 
 def _pages(k_pages, v_pages, k_scales, v_scales):
@@ -140,10 +145,11 @@ def rope_table(max_pos: int, head_dim: int, base: float = 10000.0, device="cuda"
     if max_pos < 1 or head_dim < 2 or head_dim % 2:
         _refuse("bad rotary table size")
     index = torch.device(device).index
-    call = _Call(torch.cuda.current_device() if index is None else index, stream)
+    dev = torch.cuda.current_device() if index is None else index
+    handle = _handle(dev, stream)
     with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
-        table = torch.empty((max_pos, head_dim // 2, 2), dtype=_F32, device=call.dev)
-    call.run(N.load().rope_table, max_pos, head_dim, float(base), table.data_ptr())
+        table = torch.empty((max_pos, head_dim // 2, 2), dtype=_F32, device=dev)
+    _run(dev, N.load().rope_table, max_pos, head_dim, float(base), table.data_ptr(), handle)
     return table
 
 
@@ -186,21 +192,22 @@ def paged_kv_append(k: torch.Tensor, v: torch.Tensor, lens: torch.Tensor,
         _refuse("q and q_out come together")
     if k_means is not None:
         _check(k_means, "k_means", _BF16, (n_pages, hkv, dh), dev)
-    call = _Call(dev, stream)
+    handle = _handle(dev, stream)
     if rows == 0:
         return
-    call.run(N.load().paged_kv_append, src, kv, rows, B, hq, hkv, dh, _ptr(q), q_stride,
+    _run(dev, N.load().paged_kv_append, src, kv, rows, B, hq, hkv, dh, _ptr(q), q_stride,
              k.data_ptr(), k_stride, v.data_ptr(), v_stride, lens.data_ptr(),
              row_start.data_ptr(), block_table.data_ptr(), stride, n_pages, rope.data_ptr(),
              max_pos, _ptr(q_out), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(k_scales),
-             _ptr(v_scales), _ptr(k_means))
+             _ptr(v_scales), _ptr(k_means), handle)
 
 
 @functools.lru_cache(maxsize=1024)
 def paged_token_attention_workspace_bytes(batch: int, n_q: int, n_q_heads: int, n_kv_heads: int,
-                                          head_dim: int) -> int:
-    return N.check(N.load().paged_token_attention_workspace_bytes(batch, n_q, n_q_heads,
-                                                                  n_kv_heads, head_dim))
+                                          head_dim: int, max_pages: int) -> int:
+    """Scratch bytes for a table (or a selection, if that is smaller) of max_pages pages."""
+    return N.check(N.load().paged_token_attention_workspace_bytes(
+        batch, n_q, n_q_heads, n_kv_heads, head_dim, max_pages))
 
 
 def paged_token_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
@@ -235,12 +242,14 @@ def paged_token_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch
             _refuse("selected pages take one query token")
         n_sel = _dims(selected, "selected", 3)[2]
         _check(selected, "selected", _I32, (B, hkv, n_sel), dev)
-    call = _Call(dev, stream)
-    ws = call.workspace(workspace, paged_token_attention_workspace_bytes(B, n_q, hq, hkv, dh))
-    call.run(N.load().paged_token_attention, kv, B, n_q, hq, hkv, dh, q.data_ptr(),
+    handle = _handle(dev, stream)
+    ws, at, size = _workspace(
+        workspace, paged_token_attention_workspace_bytes(
+            B, n_q, hq, hkv, dh, stride if selected is None else min(stride, n_sel)), dev, stream)
+    _run(dev, N.load().paged_token_attention, kv, B, n_q, hq, hkv, dh, q.data_ptr(),
              k_pages.data_ptr(), v_pages.data_ptr(), _ptr(k_scales), _ptr(v_scales), n_pages,
              block_table.data_ptr(), stride, lens.data_ptr(), _ptr(selected), n_sel,
-             out.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size())
+             out.data_ptr(), at, size, handle)
     return out
 
 
@@ -268,11 +277,11 @@ def paged_select(q: torch.Tensor, k_means: torch.Tensor, block_table: torch.Tens
     _check(lens, "lens", _I32, (B,), dev)
     n_sel = _dims(selected, "selected", 3)[2]
     _check(selected, "selected", _I32, (B, hkv, n_sel), dev)
-    call = _Call(dev, stream)
-    ws = call.workspace(workspace, paged_select_workspace_bytes(B, hkv, stride))
-    call.run(N.load().paged_select, B, hq, hkv, dh, q.data_ptr(), k_means.data_ptr(), n_pages,
+    handle = _handle(dev, stream)
+    ws, at, size = _workspace(workspace, paged_select_workspace_bytes(B, hkv, stride), dev, stream)
+    _run(dev, N.load().paged_select, B, hq, hkv, dh, q.data_ptr(), k_means.data_ptr(), n_pages,
              block_table.data_ptr(), stride, lens.data_ptr(), n_sel, int(keep_first),
-             int(keep_last), selected.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size())
+             int(keep_last), selected.data_ptr(), at, size, handle)
     return selected
 
 
@@ -303,11 +312,10 @@ def verify_drafts(target_logits: torch.Tensor, draft_tokens: torch.Tensor,
     _check(accepted_out, "accepted_out", _I32, (B,), dev)
     if draft_logits is not None:
         _check(draft_logits, "draft_logits", _F32, (B, n, V), dev)
-    call = _Call(dev, stream)
-    ws = call.workspace(workspace,
-                        verify_drafts_workspace_bytes(B, n, V, draft_logits is not None))
-    call.run(N.load().verify_drafts, B, n, V, target_logits.data_ptr(), _ptr(draft_logits),
+    handle = _handle(dev, stream)
+    ws, at, size = _workspace(
+        workspace, verify_drafts_workspace_bytes(B, n, V, draft_logits is not None), dev, stream)
+    _run(dev, N.load().verify_drafts, B, n, V, target_logits.data_ptr(), _ptr(draft_logits),
              draft_tokens.data_ptr(), uniforms.data_ptr(), float(temperature),
-             tokens_out.data_ptr(), accepted_out.data_ptr(), ws.data_ptr(),
-             ws.numel() * ws.element_size())
+             tokens_out.data_ptr(), accepted_out.data_ptr(), at, size, handle)
     return tokens_out

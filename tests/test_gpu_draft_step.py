@@ -145,7 +145,7 @@ def test_binding_refuses_wrong_tensors():
             (dict(selected=new(i32, 2, 2, 5).long()), "selected"),
             (dict(q=new(bf, 2, 3, 4, 64), out=new(bf, 2, 3, 4, 64), selected=new(i32, 2, 2, 5)),
              "one query token"),
-            (dict(workspace=new(torch.uint8, 16)), "too small"),
+            (dict(workspace=new(torch.uint8, 16), block_table=new(i32, 2, 300)), "too small"),
             (dict(workspace=torch.zeros(1 << 20)), "workspace must be"),
             (dict(q=new(bf, 2 * 4 * 64 + 1)[1:].view(2, 4, 64)), "aligned")]:
         with pytest.raises(PdecError, match=word):

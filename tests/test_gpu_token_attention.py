@@ -291,7 +291,7 @@ def test_replayed_graph_follows_the_lengths():
     d["lens"] = torch.tensor([2, 1], dtype=torch.int32, device="cuda")
     out = torch.empty(d["q"].shape, dtype=torch.bfloat16, device="cuda")
     eager = torch.empty_like(out)
-    ws = torch.empty(_P().paged_token_attention_workspace_bytes(2, 2, 8, 2, 64),
+    ws = torch.empty(_P().paged_token_attention_workspace_bytes(2, 2, 8, 2, 64, 1 << 20),
                      dtype=torch.uint8, device="cuda")
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()

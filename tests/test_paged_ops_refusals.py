@@ -47,14 +47,14 @@ def test_append_of_no_rows_is_nothing():
 
 def _attn(**kw):
     a = dict(kv=N.BF16, batch=2, n_q=1, hq=4, hkv=2, dh=64, q=A, kp=A, vp=A, ks=None, vs=None,
-             pages=9, bt=A, stride=8, lens=A, sel=None, n_sel=0, out=A, ws=A, ws_bytes=1 << 40)
+             pages=9, bt=A, stride=800, lens=A, sel=None, n_sel=0, out=A, ws=A, ws_bytes=1 << 40)
     a.update(kw)
     return N.load().paged_token_attention(*a.values(), None)
 
 
 @pytest.mark.parametrize("kw,code,word", [
     (dict(kv=N.F32), N.INVALID_ARG, b"kv_dtype"), (dict(q=None), N.INVALID_ARG, b"null"),
-    (dict(ws=None), N.INVALID_ARG, b"null"), (dict(n_q=0), N.INVALID_ARG, b"n_q"),
+    (dict(ws=None), N.INVALID_ARG, b"too small"), (dict(n_q=0), N.INVALID_ARG, b"n_q"),
     (dict(n_q=4097), N.INVALID_ARG, b"n_q"), (dict(batch=0), N.INVALID_ARG, b"batch"),
     (dict(hq=3), N.INVALID_ARG, b"multiple"), (dict(hq=34), N.UNSUPPORTED, b"at most 16"),
     (dict(dh=32), N.UNSUPPORTED, b"head_dim"), (dict(vs=A), N.INVALID_ARG, b"scales"),
@@ -118,13 +118,15 @@ def test_rope_table():
 
 def test_sizes_of_workspaces():
     lib = N.load()
-    a = paged.paged_token_attention_workspace_bytes(64, 1, 32, 8, 128)
-    b = paged.paged_token_attention_workspace_bytes(64, 5, 32, 8, 128)
+    a = paged.paged_token_attention_workspace_bytes(64, 1, 32, 8, 128, 512)
+    b = paged.paged_token_attention_workspace_bytes(64, 5, 32, 8, 128, 512)
     assert 0 < a < b < 1 << 30
+    assert paged.paged_token_attention_workspace_bytes(64, 5, 32, 8, 128, 16) == 0
     assert paged.paged_select_workspace_bytes(2, 8, 100) >= 2 * 8 * 100 * 4
     assert paged.verify_drafts_workspace_bytes(4, 3, 32000, True) > \
         paged.verify_drafts_workspace_bytes(4, 3, 32000, False) > 0
-    assert lib.paged_token_attention_workspace_bytes(0, 1, 4, 2, 64) == N.INVALID_ARG
+    assert lib.paged_token_attention_workspace_bytes(0, 1, 4, 2, 64, 9) == N.INVALID_ARG
+    assert lib.paged_token_attention_workspace_bytes(1, 1, 4, 2, 64, 0) == N.INVALID_ARG
     assert lib.paged_select_workspace_bytes(1, 0, 8) == N.INVALID_ARG
     assert lib.verify_drafts_workspace_bytes(1, 1, 0, 0) == N.INVALID_ARG
 
