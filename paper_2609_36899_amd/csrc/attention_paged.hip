@@ -37,8 +37,10 @@ constexpr int kThreads = 256, kWaves = kThreads / 64;
 // (lengths, queries, first pages) and their partials: us at 256 / 512 groups, 64 sequences
 // of 1K to 8K tokens 120 / 119 (E4M3, 648 MB: 5.4 TB/s) and 180 / 179 (bf16, 1136 MB: 6.3),
 // five tokens each over 8 x 64K to 128K 267 / 283 (E4M3, 1580 MB: 5.9), four over 16 x 1K to
-// 16K 94 / 96 (bf16, 512 MB: 5.4), 16 over 16 x 4K to 8K 77 / 112; 1024 groups are slower by
-// 5 to 20% more.
+// 16K 94 / 96 (bf16, 512 MB: 5.4); 1024 groups are slower by 5 to 20% more.  Blocks of more
+// than 32 rows hold two groups' waves in step with each other and gain from a second group:
+// 13 tokens over 16 x 4K to 16K 129 / 94 (E4M3), 137 / 137 (bf16), 26 tokens 229 / 149 and
+// 225 / 209.
 constexpr int kGroups = 256;
 constexpr int kPair = 2 * kPage;        // keys of a pair of pages
 constexpr int kNowhere = 0x40000000;    // a key position past every limit
@@ -94,14 +96,16 @@ enum Cut {
 // of the transposed V page.
 template <int DH, int RT, int RW, typename KT, bool LIST>
 __global__ __launch_bounds__(kThreads)
-__attribute__((amdgpu_waves_per_eu((sizeof(KT) == 1 ? 3 : 4) - RT))) void paged_attn_kernel(
+__attribute__((amdgpu_waves_per_eu((sizeof(KT) == 1 && RW == 1 ? 3 : 4) - RT))) void paged_attn_kernel(
     PagedAttnArgs a, const int32_t* __restrict__ table, const int32_t* __restrict__ lists) {
   constexpr int KC = DH / 32, DT = DH / 16;
   constexpr bool kFp8 = sizeof(KT) == 1;
   // Whether the next pair's loads are in flight while one is used.  The registers that this
   // takes of bf16 pages cost a resident group, and more (64 x 1K to 8K: 179 us without, 188
-  // with; four tokens over 16 x 1K to 16K: 97 and 102).
-  constexpr bool kAhead = kFp8;
+  // with; four tokens over 16 x 1K to 16K: 97 and 102), and so do those of E4M3 pages where
+  // waves share them (13 tokens over 53 x 0.5K to 4K 105 without, 117 with; 26 over 16 x 4K
+  // to 16K 149 and 184).
+  constexpr bool kAhead = kFp8 && RW == 1;
   typedef typename std::conditional<kFp8, u32x2, u32x4>::type VRaw;
   __shared__ int red[kWaves];
   __shared__ int found[2];
@@ -163,12 +167,12 @@ __attribute__((amdgpu_waves_per_eu((sizeof(KT) == 1 ? 3 : 4) - RT))) void paged_
       for (int c = 0; c < KC; ++c)
         qf[t][c] = on ? *(const bf16x8*)(src + qk_dim(c, q4)) : bf16x8{};
     }
-    float m[RT], l[RT];
-    f32x4 acc[RT][DT];
+    float m[RT];
+    f32x4 acc[RT][DT], sum[RT];  // sum: see `ones`
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       m[t] = -INFINITY;
-      l[t] = 0.f;
+      sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int d = 0; d < DT; ++d) acc[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -258,7 +262,19 @@ __attribute__((amdgpu_waves_per_eu((sizeof(KT) == 1 ? 3 : 4) - RT))) void paged_
       const bool scaled = kFp8 && kbase < kNowhere;
       const float k_mul = scaled ? a.scale_log2 * r.ks : a.scale_log2;
       const float v_mul = scaled ? r.vs : 1.f;
-      const float v_inv = kFp8 ? __builtin_amdgcn_rcpf(v_mul) : 1.f;
+      const float v_log = kFp8 ? __builtin_amdgcn_logf(v_mul) : 0.f;
+      // The weights' sum is a product too, by rows of ones, or of the inverse of the V scale
+      // that the weights carry: its high half in even rows and the rest in odd ones (2^-16
+      // of it is lost), so that a lane's first two results add up to its row's sum.
+      u32x4 ones;
+      {
+        const float inv = kFp8 ? __builtin_amdgcn_rcpf(v_mul) : 1.f;
+        uint32_t bits = __float_as_uint(inv) & 0xFFFF0000u;
+        if constexpr (kFp8)
+          if (c16 & 1) bits = __float_as_uint(inv - __uint_as_float(bits)) & 0xFFFF0000u;
+        bits |= bits >> 16;
+        ones = u32x4{bits, bits, bits, bits};
+      }
       // Keys without data: 0 times what they hold may be NaN.  (Uniform over the wave;
       // with kNone only where the table names no page.)
       const bool hole = max(r.key0[0], r.key0[1]) + kPage > kv_lim;
@@ -284,17 +300,16 @@ __attribute__((amdgpu_waves_per_eu((sizeof(KT) == 1 ? 3 : 4) - RT))) void paged_
           for (int e = 0; e < 8; ++e)
             if (kbase >= kNowhere) s[e / 4][e % 4] = -INFINITY;
         }
-        float sv[8], mloc = -INFINITY;
+        auto seen = [&](int e) { return kCut == kNone || kbase + e < row_lim[t]; };
+        float mloc = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          sv[e] = kCut == kNone || kbase + e < row_lim[t] ? s[e / 4][e % 4] * k_mul : -INFINITY;
-          mloc = fmaxf(mloc, sv[e]);
-        }
-        mloc = max_over_key_groups(mloc);
+        for (int e = 0; e < 8; ++e) mloc = fmaxf(mloc, seen(e) ? s[e / 4][e % 4] : -INFINITY);
+        mloc = max_over_key_groups(mloc * k_mul);  // a lane's keys are of one page
         const float m_new = fmaxf(m[t], mloc), m_use = m_new == -INFINITY ? 0.f : m_new;
         if (__any(m_new != m[t])) {
           const float alpha = __builtin_amdgcn_exp2f(m[t] - m_use);
-          l[t] *= alpha;
+          sum[t][0] *= alpha;
+          if constexpr (kFp8) sum[t][1] *= alpha;
 #pragma unroll
           for (int d = 0; d < DT; ++d) acc[t][d] *= alpha;
         }
@@ -303,18 +318,19 @@ __attribute__((amdgpu_waves_per_eu((sizeof(KT) == 1 ? 3 : 4) - RT))) void paged_
         // (2^-8), a page's V scale with them; the normaliser is the fp32 sum of the
         // weights as they were rounded, so that what the rounding does to a row's large
         // weights cancels.
+        const float base = v_log - m_use;
         uint32_t pw[4];
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
-          const float p0 = __builtin_amdgcn_exp2f(sv[e] - m_use);
-          const float p1 = __builtin_amdgcn_exp2f(sv[e + 1] - m_use);
-          const f32x2 pv = {kFp8 ? p0 * v_mul : p0, kFp8 ? p1 * v_mul : p1};
-          const uint32_t bits = __builtin_bit_cast(uint32_t, __builtin_convertvector(pv, bf16x2));
-          pw[e / 2] = bits;
-          const float sum = __uint_as_float(bits << 16) + __uint_as_float(bits & 0xFFFF0000u);
-          l[t] = kFp8 ? __builtin_fmaf(sum, v_inv, l[t]) : l[t] + sum;
+          const float x0 = __builtin_fmaf(s[e / 4][e % 4], k_mul, base);
+          const float x1 = __builtin_fmaf(s[e / 4][e % 4 + 1], k_mul, base);
+          const f32x2 pv = {__builtin_amdgcn_exp2f(seen(e) ? x0 : -INFINITY),
+                            __builtin_amdgcn_exp2f(seen(e + 1) ? x1 : -INFINITY)};
+          pw[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(pv, bf16x2));
         }
         const u16x8 pbits = __builtin_bit_cast(u16x8, u32x4{pw[0], pw[1], pw[2], pw[3]});
+        sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            __builtin_bit_cast(bf16x8, ones), __builtin_bit_cast(bf16x8, pbits), sum[t], 0, 0, 0);
         if constexpr (kCut == kToken) {
           // Keys that some of the block's tokens do not see: token by token, with the
           // keys past its own taken as 0 and the sums of its rows alone, since a weight
@@ -388,8 +404,9 @@ __attribute__((amdgpu_waves_per_eu((sizeof(KT) == 1 ? 3 : 4) - RT))) void paged_
 
     // The partials of the waves that share a row tile meet in the first of them, in wave
     // order.
+    float l[RT];
 #pragma unroll
-    for (int t = 0; t < RT; ++t) l[t] = sum_over_key_groups(l[t]);
+    for (int t = 0; t < RT; ++t) l[t] = kFp8 ? sum[t][0] + sum[t][1] : sum[t][0];
     if constexpr (PW > 1) {
       __syncthreads();  // the piece before has been read
       if (pw > 0) {
@@ -542,7 +559,7 @@ PagedAttnPlan plan_paged_attention(int batch, int n_q, int n_q_heads, int n_kv_h
   p.tok_per_block = 16 * p.row_tiles / G;
   p.blocks_per_seq = (n_q + p.tok_per_block - 1) / p.tok_per_block;
   p.n_units = (int64_t)batch * p.blocks_per_seq;
-  p.n_groups = std::max(1, kGroups / n_kv_heads);
+  p.n_groups = std::max(1, (p.row_tiles > 2 ? 512 : kGroups) / n_kv_heads);
   // A work group for each unit needs no scan of the lengths and no merge, and waits for the
   // longest.  us, equal stretches / a group a unit, one token, 8 KV heads of four: table of
   // 512 tokens, 8 sequences 15.0 / 11.8 (E4M3), 14.0 / 11.4 (bf16), 64 26.1 / 16.2, 256
