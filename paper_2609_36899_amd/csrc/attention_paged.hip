@@ -258,8 +258,9 @@ __attribute__((amdgpu_waves_per_eu((sizeof(KT) == 1 && RW == 1 ? 3 : 4) - RT))) 
         else vf[d] = __builtin_bit_cast(u16x8, r.v[d]);
       }
       const int kbase = (v_sel ? r.key0[1] : r.key0[0]) + v_tok0;  // position of this lane's key 0
-      // The scales of page 0 stand in for those of no page, and may be anything.
-      const bool scaled = kFp8 && kbase < kNowhere;
+      // Scales of pages without keys (of page 0, which stands in for no page, or of one that
+      // is listed from behind the length) may be anything.
+      const bool scaled = kFp8 && kbase < kv_lim;
       const float k_mul = scaled ? a.scale_log2 * r.ks : a.scale_log2;
       const float v_mul = scaled ? r.vs : 1.f;
       const float v_log = kFp8 ? __builtin_amdgcn_logf(v_mul) : 0.f;

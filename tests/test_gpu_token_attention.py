@@ -218,6 +218,29 @@ def test_pages_that_no_sequence_reads_may_hold_anything(garbage, n_q):
         assert (np.abs(got - ref) <= c.bound(ref, size, k)).all()
 
 
+@pytest.mark.parametrize("garbage", [np.nan, np.inf, -1.0, 0.0])
+def test_listed_pages_behind_the_length_have_no_keys(garbage):
+    """A list may name pages of the table that lie behind a length: what they hold, scales
+    among it, reaches no output."""
+    for lens in ([40, 16, 100], [40, 16, 2000]):
+        c = Case(lens, 8, 2, 64, seed=18)
+        used = np.concatenate([c.table[b, :-(-n // 16)] for b, n in enumerate(lens)])
+        free = int(np.setdiff1d(np.arange(c.P), used)[0])
+        c.k[free], c.v[free] = 0x7F, 0x7F
+        c.ks[free], c.vs[free] = garbage, garbage
+        c.table[0, 5] = c.table[1, 6] = free
+        c.selected = np.full((3, 2, 4), -1, np.int32)
+        c.selected[0, :, :3] = [5, 2, 0]
+        c.selected[1, :, 0] = 6
+        c.selected[2] = [4, 3, 6, 0]
+        got = c.run()
+        k, v = c.values()
+        k[free] = v[free] = 0.0
+        ref, size = oo.token_attention(c.q.float().numpy(), k, v, c.table, c.lens, c.selected)
+        assert (got[1] == 0).all() and (ref[1] == 0).all()
+        assert (np.abs(got - ref) <= c.bound(ref, size, k)).all()
+
+
 def test_lengths_past_the_table_are_cut_and_negative_ones_empty():
     c = Case([64, 30], 4, 2, 64, seed=10)
     c.table = np.ascontiguousarray(c.table[:, :4])
