@@ -38,10 +38,11 @@ constexpr int kThreads = 256, kWaves = kThreads / 64;
 // of 1K to 8K tokens 120 / 119 (E4M3, 648 MB: 5.4 TB/s) and 180 / 179 (bf16, 1136 MB: 6.3),
 // five tokens each over 8 x 64K to 128K 267 / 283 (E4M3, 1580 MB: 5.9), four over 16 x 1K to
 // 16K 94 / 96 (bf16, 512 MB: 5.4); 1024 groups are slower by 5 to 20% more.  Blocks of more
-// than 32 rows hold two groups' waves in step with each other and gain from a second group:
-// 13 tokens over 16 x 4K to 16K 129 / 94 (E4M3), 137 / 137 (bf16), 26 tokens 229 / 149 and
-// 225 / 209.
+// than 32 rows, whose waves go in step, gain from a second group on a unit: 13 tokens over 16 x
+// 4K to 16K 124 / 92 (E4M3), 126 / 118 (bf16), 26 tokens 177 / 140 and 168 / 152; 768 are as
+// slow as 256.
 constexpr int kGroups = 256;
+constexpr int SF = 2, SB = 2;  // stages
 constexpr int kPair = 2 * kPage;        // keys of a pair of pages
 constexpr int kNowhere = 0x40000000;    // a key position past every limit
 
@@ -86,8 +87,12 @@ enum Cut {
 };
 
 // RT row tiles of 16 a wave, RW waves side by side along the rows, the others along the
-// pairs.  RW waves load the same pages, from HBM once and from L1 and L2 after that (no
-// non-temporal hint then), where a block for each would have read them again.
+// pairs.  RW = 1: each wave loads its own pages.  RW = 2: two load the same, from HBM once and
+// from L1 and L2 after that (no non-temporal hint then), where a block for each would have
+// read them again.  RW = 4: the waves bring each page once, into LDS, and decode E4M3 once,
+// which is worth its LDS traffic for bf16 pages and for two row tiles a wave (13 tokens, 52
+// rows, over 16 x 4K to 16K: bf16 137 us with RW = 2, 118 with 4; E4M3 94 and 101; 26 tokens,
+// each wave loading its own pages, 209 and 151, E4M3 150 and 138).
 //
 // Lane l: c16 = l % 16, q4 = l / 16.  The MFMA operand order is the one of the
 // engine's decode attention: S^T = K Q^T with the keys permuted so that a lane's
@@ -96,21 +101,29 @@ enum Cut {
 // of the transposed V page.
 template <int DH, int RT, int RW, typename KT, bool LIST>
 __global__ __launch_bounds__(kThreads)
-__attribute__((amdgpu_waves_per_eu((sizeof(KT) == 1 && RW == 1 ? 3 : 4) - RT))) void paged_attn_kernel(
+__attribute__((amdgpu_waves_per_eu(RW > 1 ? 2 : (sizeof(KT) == 1 ? 3 : 4) - RT))) void
+paged_attn_kernel(
     PagedAttnArgs a, const int32_t* __restrict__ table, const int32_t* __restrict__ lists) {
   constexpr int KC = DH / 32, DT = DH / 16;
   constexpr bool kFp8 = sizeof(KT) == 1;
   // Whether the next pair's loads are in flight while one is used.  The registers that this
   // takes of bf16 pages cost a resident group, and more (64 x 1K to 8K: 179 us without, 188
   // with; four tokens over 16 x 1K to 16K: 97 and 102), and so do those of E4M3 pages where
-  // waves share them (13 tokens over 53 x 0.5K to 4K 105 without, 117 with; 26 over 16 x 4K
-  // to 16K 149 and 184).
-  constexpr bool kAhead = kFp8 && RW == 1;
+  // two waves share them (13 tokens over 53 x 0.5K to 4K 105 without, 117 with).
+  constexpr bool kStaged = RW == kWaves, kAhead = kFp8 && RW == 1;
+  constexpr int PW = kWaves / RW;  // waves that share a row tile's pairs
   typedef typename std::conditional<kFp8, u32x2, u32x4>::type VRaw;
   __shared__ int red[kWaves];
   __shared__ int found[2];
-  constexpr int PW = kWaves / RW;  // waves that share a row tile's pairs
   __shared__ float sm[PW > 1 ? (PW - 1) * RW : 1][64][PW > 1 ? RT * (4 * DT + 2) : 1];
+  // kStaged: K and V^T of four pages in bf16, their scales and the positions of their first
+  // keys, twice.  The 16-byte chunks of a K row lie exchanged by the token, so that the eight
+  // lanes that read at once meet different banks.
+  constexpr int kRegion = kPage * DH;
+  __shared__ __attribute__((aligned(16))) uint16_t stage[2][kStaged ? 8 * kRegion : 8];
+  __shared__ float scale[2][kStaged ? 8 : 1];
+  __shared__ int place[2][kStaged ? 4 : 1];
+  auto swz = [](int tok) { return (tok & 3) | (tok >> 1 & 4); };
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int c16 = lane & 15, q4 = lane >> 4;
   const int rw = wave % RW, pw = wave / RW, row0 = rw * RT * 16;
@@ -138,7 +151,9 @@ __attribute__((amdgpu_waves_per_eu((sizeof(KT) == 1 && RW == 1 ? 3 : 4) - RT))) 
     first = mine.first;
   }
   const uint16_t* q = (const uint16_t*)a.q;
-  auto qk_dim = [](int c, int q4_) { return kFp8 ? q4_ * (DH / 4) + c * 8 : c * 32 + q4_ * 8; };
+  auto qk_dim = [](int c, int q4_) {
+    return kFp8 && !kStaged ? q4_ * (DH / 4) + c * 8 : c * 32 + q4_ * 8;
+  };
   const int k_tok = 8 * ((c16 >> 2) & 1) + (c16 & 3);  // + 4u
   const int k_sel = c16 >> 3, v_sel = q4 >> 1, v_tok0 = 8 * (q4 & 1);
   const int64_t page_stride = (int64_t)a.n_kv_heads * kPage * DH, head_off = (int64_t)g * kPage * DH;
@@ -180,29 +195,26 @@ __attribute__((amdgpu_waves_per_eu((sizeof(KT) == 1 && RW == 1 ? 3 : 4) - RT))) 
     const int32_t* bt = table + (int64_t)b * a.bt_stride;
     const int32_t* list =
         LIST ? lists + ((int64_t)b * a.n_kv_heads + g) * a.n_selected : nullptr;
-    // A pair of pages: their places in the pool and the positions of their first keys.
-    // A page that the table or the list does not name has no keys.  All uniform over the
-    // wave and from pointers of the kernel's own that nothing aliases, so these are scalar
-    // loads: vector loads return in order, so waiting for one would drain the pages' in
-    // flight (five tokens over 8 x 64K to 128K: 326 us with both waits, 267 without).
+    // A page's place in the pool and the position of its first key.  One that the table or
+    // the list does not name has no keys.  All uniform over the wave and from pointers of the
+    // kernel's own that nothing aliases, so these are scalar loads: vector loads return in
+    // order, so waiting for one would drain the pages' in flight (five tokens over 8 x 64K to
+    // 128K: 326 us with both waits, 267 without).
+    struct Spot {
+      int page, key0;
+    };
+    auto spot = [&](int n) {
+      int logical = n;
+      if constexpr (LIST) logical = n < n_pages ? list[n] : -1;
+      const bool in = LIST ? logical >= 0 && logical < a.bt_stride : n < n_pages;
+      const int page = in ? bt[logical] : -1;
+      const bool ok = page >= 0 && page < a.n_pages;
+      return Spot{ok ? page : 0, ok ? logical * kPage : kNowhere};
+    };
     struct Pair {
-      int page[2], key0[2];
+      Spot at[2];
     };
-    auto look = [&](int pr) {
-      Pair r;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int n = 2 * pr + i;
-        int logical = n;
-        if constexpr (LIST) logical = n < n_pages ? list[n] : -1;
-        const bool in = LIST ? logical >= 0 && logical < a.bt_stride : n < n_pages;
-        const int page = in ? bt[logical] : -1;
-        const bool ok = page >= 0 && page < a.n_pages;
-        r.key0[i] = ok ? logical * kPage : kNowhere;
-        r.page[i] = ok ? page : 0;
-      }
-      return r;
-    };
+    auto look = [&](int pr) { return Pair{{spot(2 * pr), spot(2 * pr + 1)}}; };
     auto read = [](auto* p, auto v) {
       if constexpr (RW == 1) return load_stream<decltype(v)>(p);
       else return *(const decltype(v)*)p;
@@ -215,20 +227,20 @@ __attribute__((amdgpu_waves_per_eu((sizeof(KT) == 1 && RW == 1 ? 3 : 4) - RT))) 
       int key0[2];
     };
     auto load = [&](const Pair& p, Raw& r) {
-      const int64_t base0 = p.page[0] * page_stride + head_off;
-      const int64_t base1 = p.page[1] * page_stride + head_off;
+      const int64_t base0 = p.at[0].page * page_stride + head_off;
+      const int64_t base1 = p.at[1].page * page_stride + head_off;
       const KT* kb = (const KT*)a.k_pages + (k_sel ? base1 : base0);
       const KT* vb = (const KT*)a.v_pages + (v_sel ? base1 : base0) + v_tok0;
       // The scales come as vector loads, in order with the pages': scalar loads return out
       // of order, so that using one would wait for all, the next pair's among them.
       if constexpr (kFp8) {
-        const int64_t at = (int64_t)(v_sel ? p.page[1] : p.page[0]) * a.n_kv_heads + g;
+        const int64_t at = (int64_t)(v_sel ? p.at[1].page : p.at[0].page) * a.n_kv_heads + g;
         r.ks = a.k_scales[at];
         r.vs = a.v_scales[at];
       }
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        r.key0[i] = p.key0[i];
+        r.key0[i] = p.at[i].key0;
 #pragma unroll
         for (int c = 0; c < (kFp8 ? KC / 2 : KC); ++c)
           r.k[i][c] = read(kb + (k_tok + 4 * i) * DH + qk_dim(kFp8 ? 2 * c : c, q4), u32x4{});
@@ -237,26 +249,73 @@ __attribute__((amdgpu_waves_per_eu((sizeof(KT) == 1 && RW == 1 ? 3 : 4) - RT))) 
       for (int d = 0; d < DT; ++d)
         r.v[d] = read(vb + (d * 16 + c16) * kPage, VRaw{});
     };
-    auto use = [&](const Raw& r, auto cut_) {
-      constexpr Cut kCut = decltype(cut_)::value;
-      bf16x8 kf[2][KC];
-      u16x8 vf[DT];
+    // The pair as the products take it.
+    struct Tile {
+      bf16x8 k[2][KC];
+      u16x8 v[DT];
+      float ks, vs;
+      int key0[2];
+    };
+    auto decode = [&](const Raw& r) {
+      Tile o;
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < 2; ++i) {
+        o.key0[i] = r.key0[i];
 #pragma unroll
         for (int c = 0; c < KC; ++c) {
           if constexpr (kFp8) {
             const u32x4 w4 = r.k[i][c / 2];
-            kf[i][c] = decode8(c % 2 ? u32x2{w4.z, w4.w} : u32x2{w4.x, w4.y});
+            o.k[i][c] = decode8(c % 2 ? u32x2{w4.z, w4.w} : u32x2{w4.x, w4.y});
           } else {
-            kf[i][c] = __builtin_bit_cast(bf16x8, r.k[i][c]);
+            o.k[i][c] = __builtin_bit_cast(bf16x8, r.k[i][c]);
           }
         }
+      }
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
-        if constexpr (kFp8) vf[d] = __builtin_bit_cast(u16x8, decode8(r.v[d]));
-        else vf[d] = __builtin_bit_cast(u16x8, r.v[d]);
+        if constexpr (kFp8) o.v[d] = __builtin_bit_cast(u16x8, decode8(r.v[d]));
+        else o.v[d] = __builtin_bit_cast(u16x8, r.v[d]);
       }
+      o.ks = r.ks;
+      o.vs = r.vs;
+      return o;
+    };
+    // Pair p of a stage.  l is the lane, as a value that the compiler takes for new each time:
+    // addresses kept over the loop would cost registers that the products need.
+    auto fetch_k = [&](int st, int p, int l, Tile& o) {
+      const int tok = 8 * (l >> 2 & 1) + (l & 3), x = (l >> 4 ^ swz(tok)) * 8;
+      const uint16_t* at = stage[st] + (4 * p + 2 * (l >> 3 & 1)) * kRegion + tok * DH;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int c = 0; c < KC; ++c)
+          o.k[i][c] = *(const bf16x8*)(at + (x ^ (c & 1) * 32) + i * 4 * DH + (c >> 1) * 64);
+    };
+    auto fetch_v = [&](int st, int p, int l, Tile& o) {
+      const uint16_t* at = stage[st] + (4 * p + 2 * (l >> 5) + 1) * kRegion +
+                           (l & 15) * kPage + (l >> 1 & 8);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) o.key0[i] = __builtin_amdgcn_readfirstlane(place[st][2 * p + i]);
+      o.ks = kFp8 ? scale[st][4 * p + 2 * (l >> 5)] : 1.f;
+      o.vs = kFp8 ? scale[st][4 * p + 2 * (l >> 5) + 1] : 1.f;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o.v[d] = *(const u16x8*)(at + d * 16 * kPage);
+    };
+    auto products = [&](const Tile& r, f32x4 (*s)[2]) {
+#pragma unroll
+      for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          s[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int c = 0; c < KC; ++c)
+            s[t][i] =
+                __builtin_amdgcn_mfma_f32_16x16x32_bf16(r.k[i][c], qf[t][c], s[t][i], 0, 0, 0);
+        }
+    };
+    auto use = [&](Tile r, f32x4 (*scores)[2], auto cut_) {
+      constexpr Cut kCut = decltype(cut_)::value;
+      auto& vf = r.v;
       const int kbase = (v_sel ? r.key0[1] : r.key0[0]) + v_tok0;  // position of this lane's key 0
       // Scales of pages without keys (of page 0, which stands in for no page, or of one that
       // is listed from behind the length) may be anything.
@@ -288,14 +347,7 @@ __attribute__((amdgpu_waves_per_eu((sizeof(KT) == 1 && RW == 1 ? 3 : 4) - RT))) 
       }
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
-        f32x4 s[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int c = 0; c < KC; ++c)
-            s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[i][c], qf[t][c], s[i], 0, 0, 0);
-        }
+        auto& s = scores[t];
         if (kCut == kNone && hole) {
 #pragma unroll
           for (int e = 0; e < 8; ++e)
@@ -359,12 +411,95 @@ __attribute__((amdgpu_waves_per_eu((sizeof(KT) == 1 && RW == 1 ? 3 : 4) - RT))) 
         }
       }
     };
+    auto attend = [&](const Tile& r, auto cut) {
+      f32x4 s[RT][2];
+      products(r, s);
+      use(r, s, cut);
+    };
     // Pairs that every row sees whole, and the one or few at the block's end.  A list's
     // pages come in any order: each pair looks whether its keys end.
     const int p_cut = LIST ? p_end : min(p_end, max(max(pos0 + 1, 0) / kPair, p_begin));
     int pr = p_begin + pw;
     typedef std::integral_constant<Cut, LIST ? kLimit : kNone> Main;
-    if constexpr (kAhead) {
+    if constexpr (kStaged) {
+      // A stage is two pairs, of which wave w brings page w: loads into registers, one stage
+      // ahead, and from there, E4M3 decoded on the way, into the one of the two in LDS that is
+      // not in use.
+      constexpr int LP = kRegion * sizeof(KT) / 1024, EL = 16 / sizeof(KT);  // loads; elements
+      const int last = 2 * p_end - 1;
+      auto lane_now = [&] {
+        int l = threadIdx.x & 63;
+        asm volatile("" : "+v"(l));
+        return l;
+      };
+      auto ahead = [&](int p) { return spot(min(2 * p + wave, last)); };
+      u32x4 part[2][LP];
+      float part_scale[2];
+      int part_key0;
+      auto load = [&](const Spot& at) {
+        const int64_t from = at.page * page_stride + head_off + lane * EL;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const KT* src = (const KT*)(i ? a.v_pages : a.k_pages) + from;
+#pragma unroll
+          for (int j = 0; j < LP; ++j) part[i][j] = load_stream<u32x4>(src + j * 64 * EL);
+          if constexpr (kFp8)
+            part_scale[i] = (i ? a.v_scales : a.k_scales)[(int64_t)at.page * a.n_kv_heads + g];
+        }
+        part_key0 = at.key0;
+      };
+      auto put = [&](int st, int l) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          uint16_t* to = stage[st] + (2 * wave + i) * kRegion;
+#pragma unroll
+          for (int j = 0; j < LP; ++j) {
+            const int n = (j * 64 + l) * EL, x = i ? n : n ^ swz(n / DH) * 8;
+            if constexpr (kFp8) {
+              *(bf16x8*)(to + x) = decode8(u32x2{part[i][j].x, part[i][j].y});
+              *(bf16x8*)(to + (x ^ 8)) = decode8(u32x2{part[i][j].z, part[i][j].w});
+            } else {
+              *(u32x4*)(to + x) = part[i][j];
+            }
+          }
+        }
+        if (l == 0) {
+          if constexpr (kFp8) {
+            scale[st][2 * wave] = part_scale[0];
+            scale[st][2 * wave + 1] = part_scale[1];
+          }
+          place[st][wave] = part_key0;
+        }
+      };
+      auto one = [&](int st, int p, auto cut) {
+        Tile r;
+        f32x4 s[RT][2];
+        fetch_k(st, p, lane_now(), r);
+        products(r, s);
+        __builtin_amdgcn_sched_barrier(0);  // K's registers are V's now
+        fetch_v(st, p, lane_now(), r);
+        use(r, s, cut);
+      };
+      load(ahead(p_begin));
+      __syncthreads();  // the unit before has been used
+      put(0, lane);
+      load(ahead(p_begin + 2));
+      Spot next = ahead(p_begin + 4);
+      int st = 0, p = p_begin;
+      auto turn = [&](auto cut) {
+        wg_barrier();
+        put(st ^ 1, lane_now());
+        load(next);
+        next = ahead(p + 6);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (decltype(cut)::value == kNone || p + i < p_end) one(st, i, cut);
+        st ^= 1;
+        p += 2;
+      };
+      while (p + 2 <= p_cut) turn(std::integral_constant<Cut, kNone>{});
+      while (p < p_end) turn(std::integral_constant<Cut, kToken>{});
+    } else if constexpr (kAhead) {
       // The next pair's bytes are in flight while one is used, in two buffers in turn, and
       // the page after it is looked up.  Past the end the last pair stands in.  (A third
       // buffer, and refilling each behind its use, measured the same or up to 8% slower.)
@@ -381,7 +516,7 @@ __attribute__((amdgpu_waves_per_eu((sizeof(KT) == 1 && RW == 1 ? 3 : 4) - RT))) 
             fetch = next(fetch);
             ahead = look(fetch);
             __builtin_amdgcn_sched_barrier(0);
-            use(r[i], Main{});
+            attend(decode(r[i]), Main{});
             pr += PW;
             more = pr < p_cut;
             if (!more) break;
@@ -392,14 +527,14 @@ __attribute__((amdgpu_waves_per_eu((sizeof(KT) == 1 && RW == 1 ? 3 : 4) - RT))) 
       for (; pr < p_cut; pr += PW) {
         Raw r;
         load(look(pr), r);
-        use(r, Main{});
+        attend(decode(r), Main{});
       }
     }
-    if constexpr (!LIST) {
+    if constexpr (!LIST && !kStaged) {
       for (; pr < p_end; pr += PW) {
         Raw r;
         load(look(pr), r);
-        use(r, std::integral_constant<Cut, kToken>{});
+        attend(decode(r), std::integral_constant<Cut, kToken>{});
       }
     }
 
@@ -553,8 +688,7 @@ PagedAttnPlan plan_paged_attention(int batch, int n_q, int n_q_heads, int n_kv_h
                                    int max_pages) {
   PagedAttnPlan p;
   const int G = n_q_heads / n_kv_heads;
-  // The smallest block that holds a sequence's rows of a KV head, or blocks of 128: one row
-  // tile, then two for one, two or all four waves side by side.
+  // The smallest block that holds a sequence's rows of a KV head, or blocks of 128.
   const int64_t rows = (int64_t)n_q * G;
   p.row_tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 ? 4 : 8;
   p.tok_per_block = 16 * p.row_tiles / G;
@@ -582,7 +716,8 @@ hipError_t launch_paged_attention(int kv_fp8, int head_dim, int row_tiles, const
     if (a.selected) PDEC_PAGED(DH_, 1, 1, KT_, true);            \
     else if (row_tiles == 1) PDEC_PAGED(DH_, 1, 1, KT_, false);  \
     else if (row_tiles == 2) PDEC_PAGED(DH_, 2, 1, KT_, false);  \
-    else if (row_tiles == 4) PDEC_PAGED(DH_, 2, 2, KT_, false);  \
+    else if (row_tiles == 4 && sizeof(KT_) == 1) PDEC_PAGED(DH_, 2, 2, uint8_t, false); \
+    else if (row_tiles == 4) PDEC_PAGED(DH_, 1, 4, uint16_t, false); \
     else PDEC_PAGED(DH_, 2, 4, KT_, false);                      \
   } while (0)
   if (head_dim == 128) {

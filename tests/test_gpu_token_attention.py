@@ -128,6 +128,27 @@ def test_several_tokens_of_other_groups(hq, hkv, dh, n_q):
     Case([n_q, 77, 260, 5], hq, hkv, dh, n_q=n_q, seed=3).check()
 
 
+@pytest.mark.parametrize("fp8", [True, False])
+@pytest.mark.parametrize("n_q,dh", [(9, 128), (16, 64), (17, 64), (32, 128), (33, 128)])
+def test_blocks_of_many_rows(n_q, dh, fp8):
+    """36 to 132 rows for a KV head: lengths around two pairs of pages, pages that the table
+    does not name, and keys behind some tokens that hold NaN and infinities."""
+    lens = [n_q, 63, 64, 65, 95, 96, 97, 128, 129, 161, 700, 2049]
+    c = Case(lens, 8, 2, dh, n_q=n_q, fp8=fp8, seed=19)
+    c.table[4, 1], c.table[8, 0], c.table[10, 20], c.table[11, 64] = -1, c.P, -5, 2 ** 31 - 1
+    c.check()
+    for b, n in enumerate(lens):
+        page, slot = c.table[b, (n - 1) // 16], (n - 1) % 16
+        c.k[page, :, slot] = 0x7F if fp8 else np.nan
+        c.v[page, :, :, slot] = 0x7F if fp8 else np.inf
+    got = c.run()
+    assert np.isnan(got[:, -1]).all()
+    k, v = c.values()
+    ref, size = oo.token_attention(c.q.float().numpy()[:, :-1], k, v, c.table, c.lens - 1)
+    c.q = c.q[:, :-1]
+    assert (np.abs(got[:, :-1] - ref) <= c.bound(ref, size, k)).all()
+
+
 def test_long_contexts_split_over_many_groups():
     Case([40000, 3, 0, 900], 8, 2, 128, seed=4).check()
     Case([20000], 8, 2, 128, n_q=5, fp8=False, seed=5).check()
