@@ -301,19 +301,16 @@ paged_attn_kernel(
 #pragma unroll
       for (int d = 0; d < DT; ++d) o.v[d] = *(const u16x8*)(at + d * 16 * kPage);
     };
-    auto products = [&](const Tile& r, f32x4 (*s)[2]) {
+    auto products = [&](const Tile& r, int t, f32x4* s) {
 #pragma unroll
-      for (int t = 0; t < RT; ++t)
+      for (int i = 0; i < 2; ++i) {
+        s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          s[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int c = 0; c < KC; ++c)
-            s[t][i] =
-                __builtin_amdgcn_mfma_f32_16x16x32_bf16(r.k[i][c], qf[t][c], s[t][i], 0, 0, 0);
-        }
+        for (int c = 0; c < KC; ++c)
+          s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r.k[i][c], qf[t][c], s[i], 0, 0, 0);
+      }
     };
-    auto use = [&](Tile r, f32x4 (*scores)[2], auto cut_) {
+    auto use = [&](Tile r, auto scores, auto cut_) {
       constexpr Cut kCut = decltype(cut_)::value;
       auto& vf = r.v;
       const int kbase = (v_sel ? r.key0[1] : r.key0[0]) + v_tok0;  // position of this lane's key 0
@@ -347,7 +344,8 @@ paged_attn_kernel(
       }
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
-        auto& s = scores[t];
+        f32x4 s[2];
+        scores(r, t, s);
         if (kCut == kNone && hole) {
 #pragma unroll
           for (int e = 0; e < 8; ++e)
@@ -411,11 +409,7 @@ paged_attn_kernel(
         }
       }
     };
-    auto attend = [&](const Tile& r, auto cut) {
-      f32x4 s[RT][2];
-      products(r, s);
-      use(r, s, cut);
-    };
+    auto attend = [&](const Tile& r, auto cut) { use(r, products, cut); };
     // Pairs that every row sees whole, and the one or few at the block's end.  A list's
     // pages come in any order: each pair looks whether its keys end.
     const int p_cut = LIST ? p_end : min(p_end, max(max(pos0 + 1, 0) / kPair, p_begin));
@@ -475,10 +469,11 @@ paged_attn_kernel(
         Tile r;
         f32x4 s[RT][2];
         fetch_k(st, p, lane_now(), r);
-        products(r, s);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) products(r, t, s[t]);
         __builtin_amdgcn_sched_barrier(0);  // K's registers are V's now
         fetch_v(st, p, lane_now(), r);
-        use(r, s, cut);
+        use(r, [&](const Tile&, int t, f32x4* o) { o[0] = s[t][0], o[1] = s[t][1]; }, cut);
       };
       load(ahead(p_begin));
       __syncthreads();  // the unit before has been used
