@@ -342,6 +342,17 @@ paged_attn_kernel(
 #pragma unroll
             for (int d = 0; d < DT; ++d) vf[d][e] = 0;
       }
+      // Whether a weight of 0 leaves nothing of any key: 0 times all of V is 0 unless
+      // something in it is infinite or NaN.
+      bool finite = true;
+      if constexpr (kCut == kToken) {
+        f32x4 z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+          z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[d]), bf16x8{},
+                                                      z, 0, 0, 0);
+        finite = !__any(z[0] + z[1] + z[2] + z[3] != 0.f);
+      }
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
         f32x4 s[2];
@@ -385,16 +396,18 @@ paged_attn_kernel(
         if constexpr (kCut == kToken) {
           // Keys that some of the block's tokens do not see: token by token, with the
           // keys past its own taken as 0 and the sums of its rows alone, since a weight
-          // of 0 times an infinity in V would not be 0.
-          const int r0 = row0 + t * 16, j_end = min((r0 + 15) / G + 1, n_tok);
-          for (int j = r0 / G; j < j_end; ++j) {
-            const bool mine = (r0 + c16) / G == j;
+          // of 0 times an infinity in V would not be 0.  All at once where V is finite.
+          const int r0 = row0 + t * 16, j_begin = r0 / G;
+          const int j_end = finite ? j_begin + 1 : min((r0 + 15) / G + 1, n_tok);
+          for (int j = j_begin; j < j_end; ++j) {
+            const bool mine = finite || (r0 + c16) / G == j;
+            const int own = finite ? kNowhere : pos0 + j;
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
               u16x8 v = vf[d];
 #pragma unroll
               for (int e = 0; e < 8; ++e)
-                if (kbase + e > pos0 + j) v[e] = 0;
+                if (kbase + e > own) v[e] = 0;
               const f32x4 o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
                   __builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, pbits), acc[t][d], 0, 0, 0);
               acc[t][d] = mine ? o : acc[t][d];
