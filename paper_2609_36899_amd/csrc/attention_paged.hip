@@ -110,7 +110,7 @@ paged_attn_kernel(
   // takes of bf16 pages cost a resident group, and more (64 x 1K to 8K: 179 us without, 188
   // with; four tokens over 16 x 1K to 16K: 97 and 102), and so do those of E4M3 pages where
   // two waves share them (13 tokens over 53 x 0.5K to 4K 105 without, 117 with).
-  constexpr bool kStaged = RW == kWaves, kAhead = kFp8 && RW == 1;
+  constexpr bool kStaged = RW == kWaves, kAhead = kFp8 && (RW == 1 || RT == 1);
   constexpr int PW = kWaves / RW;  // waves that share a row tile's pairs
   typedef typename std::conditional<kFp8, u32x2, u32x4>::type VRaw;
   __shared__ int red[kWaves];
@@ -716,6 +716,16 @@ PagedAttnPlan plan_paged_attention(int batch, int n_q, int n_q_heads, int n_kv_h
 hipError_t launch_paged_attention(int kv_fp8, int head_dim, int row_tiles, const PagedAttnArgs& a,
                                   hipStream_t stream) {
   const dim3 grid(a.n_kv_heads, a.unit_groups ? a.n_units : a.n_groups), block(kThreads);
+  // 17 to 32 rows as a tile for each of two waves that load the same pages, or as two tiles of
+  // one wave: half the work at a stretch's two ends, or half the loads between them.  By what a
+  // work group reads if the table is full; us, tile a wave / two tiles, at KB a group: E4M3, 5 x
+  // 4 rows over 4 x 4K 17.7 / 22.7 (120), over 128 x 0.5K 31.5 / 51.1 (512), over 58 x 1.4K 56.6
+  // / 57.0 (640), 8 x 3 over 41 x 0 to 4K 34.7 / 39.9 (700), 5 x 4 61.0 / 60.0 (1400), over 16 x
+  // 16K 73.5 / 63.8 (2048); bf16, 5 x 4 over 4 x 4K 19.1 / 22.3 (240), 8 x 3 over 58 x 1.4K
+  // 49.2 / 42.0 (640).
+  const int64_t group_bytes = (int64_t)a.n_units * a.max_len * a.n_kv_heads / kGroups * head_dim *
+                              (kv_fp8 ? 2 : 4);
+  const bool little = group_bytes <= (kv_fp8 ? 1024 : 256) * 1024;
 #define PDEC_PAGED(DH_, RT_, RW_, KT_, LIST_)                          \
   paged_attn_kernel<DH_, RT_, RW_, KT_, LIST_><<<grid, block, 0, stream>>>(a, a.block_table, \
                                                                            a.selected)
@@ -723,6 +733,7 @@ hipError_t launch_paged_attention(int kv_fp8, int head_dim, int row_tiles, const
   do {                                                           \
     if (a.selected) PDEC_PAGED(DH_, 1, 1, KT_, true);            \
     else if (row_tiles == 1) PDEC_PAGED(DH_, 1, 1, KT_, false);  \
+    else if (row_tiles == 2 && little) PDEC_PAGED(DH_, 1, 2, KT_, false); \
     else if (row_tiles == 2) PDEC_PAGED(DH_, 2, 1, KT_, false);  \
     else if (row_tiles == 4 && sizeof(KT_) == 1) PDEC_PAGED(DH_, 2, 2, uint8_t, false); \
     else if (row_tiles == 4) PDEC_PAGED(DH_, 1, 4, uint16_t, false); \
