@@ -14,6 +14,7 @@
 
 #include <algorithm>
 #include <cfloat>
+#include <type_traits>
 
 namespace pdec {
 
@@ -48,18 +49,20 @@ __device__ __forceinline__ double swapped(double v) {
 // an instruction takes half of a line, and the other half's finds it gone.
 constexpr int kScoreGroups = 512;
 
-template <int DH, bool MANY>  // MANY: more than four query heads, kept in LDS
+template <int DH, int HG>  // HG groups of four query heads; more than one in LDS
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) void page_scores_kernel(
     SelectArgs a, const int32_t* __restrict__ table, const int32_t* __restrict__ lens, int heads) {
   constexpr int NJ = DH / 32;
   __shared__ int red[kWaves], found[2];
-  __shared__ float qs[MANY ? kWaves : 1][MANY ? 4 : 1][NJ * 8][16];
+  // Converted already where two groups of waves still share a compute unit's LDS.
+  typedef typename std::conditional<HG == 2, double, float>::type QT;
+  __shared__ QT qs[HG > 1 ? kWaves : 1][HG][HG > 1 ? NJ * 8 : 1][16];
   const int w = blockIdx.y;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   // This wave's KV head, and its row among the rows of waves that share the tiles.
   const int g = blockIdx.x * heads + wave % heads, row = wave / heads, rows = kWaves / heads;
   const int c16 = lane & 15, k4 = lane >> 4;
-  const int G = a.n_q_heads / a.n_kv_heads, n_hg = MANY ? (G + 3) / 4 : 1;
+  const int G = a.n_q_heads / a.n_kv_heads;
   auto tiles_of = [&](int b) { return (seq_pages(lens, b, a.bt_stride) + kTile - 1) / kTile; };
   const Stretch mine = stretch_of<kThreads>(a.batch, gridDim.y, rows, w, red, found, tiles_of);
   int at = w * mine.per, first = mine.first;
@@ -80,9 +83,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) v
       return *(const u16x8*)(q0 + (int64_t)(h < G ? h : 0) * DH + j * 32 + k * 8);
     };
     double q[NJ * 8];
-    if constexpr (MANY) {
+    if constexpr (HG > 1) {
       // A wave writes and reads its own part, in order: no barrier.
-      for (int i = lane; i < n_hg * NJ * 16; i += 64) {
+      for (int i = lane; i < HG * NJ * 16; i += 64) {
         const int l = i % 16, j = i / 16 % NJ, hg = i / 16 / NJ;
         const u16x8 v = q_at(hg, j, l % 4, l / 4);
 #pragma unroll
@@ -122,18 +125,24 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) v
         load(page, next);
         page1 = page_of(p0 + 2 * step);
       }
+      // Two chains for each group, so that a product does not wait for the last.
+      double s[HG][2] = {};
+      int col = k4 * 4 + (lane & 3);
+      asm volatile("" : "+v"(col));  // else all the queries of LDS are kept in registers
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const double mean = bf16_to_f32(m[j][e]);
+#pragma unroll
+          for (int hg = 0; hg < HG; ++hg)
+            s[hg][e % 2] = __builtin_amdgcn_mfma_f64_4x4x4f64(
+                mean, HG > 1 ? (double)qs[wave][hg][j * 8 + e][col] : q[j * 8 + e],
+                s[hg][e % 2], 0, 0, 0);
+        }
       double best = -INFINITY;
-      for (int hg = 0; hg < n_hg; ++hg) {
-        double s[2] = {};  // two chains, so that a product does not wait for the last
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            s[e % 2] = __builtin_amdgcn_mfma_f64_4x4x4f64(
-                (double)bf16_to_f32(m[j][e]),
-                MANY ? (double)qs[wave][hg][j * 8 + e][k4 * 4 + (lane & 3)] : q[j * 8 + e], s[e % 2], 0, 0, 0);
-        best = fmax(best, s[0] + s[1]);  // a NaN never wins
-      }
+      for (int hg = 0; hg < HG; ++hg) best = fmax(best, s[hg][0] + s[hg][1]);  // a NaN never wins
       best = fmax(best, swapped<0xB1>(best));  // with lane ^ 1
       best = fmax(best, swapped<0x4E>(best));  // with lane ^ 2
       const int i = 4 * ((lane >> 2) & 3) + k4;  // the page of this lane's result
@@ -334,15 +343,19 @@ hipError_t launch_paged_select(int head_dim, const SelectArgs& a, hipStream_t st
   const int64_t rows = (int64_t)a.batch * a.n_kv_heads;
   const int heads = std::min(a.n_kv_heads, kWaves), head_blocks = (a.n_kv_heads + heads - 1) / heads;
   const dim3 grid(head_blocks, std::max(1, kScoreGroups / head_blocks));
-  const bool many = a.n_q_heads / a.n_kv_heads > 4;
-#define PDEC_SCORES(DH_, MANY_)                                                         \
-  page_scores_kernel<DH_, MANY_><<<grid, kThreads, 0, stream>>>(a, a.block_table, a.lens, \
-                                                                heads)
-  if (head_dim == 128) {
-    if (many) PDEC_SCORES(128, true); else PDEC_SCORES(128, false);
-  } else {
-    if (many) PDEC_SCORES(64, true); else PDEC_SCORES(64, false);
-  }
+  const int groups = (a.n_q_heads / a.n_kv_heads + 3) / 4;
+#define PDEC_SCORES(DH_, HG_)                                                         \
+  page_scores_kernel<DH_, HG_><<<grid, kThreads, 0, stream>>>(a, a.block_table, a.lens, \
+                                                              heads)
+#define PDEC_SCORES_HG(DH_)                    \
+  do {                                         \
+    if (groups == 1) PDEC_SCORES(DH_, 1);      \
+    else if (groups == 2) PDEC_SCORES(DH_, 2); \
+    else PDEC_SCORES(DH_, 4);                  \
+  } while (0)
+  if (head_dim == 128) PDEC_SCORES_HG(128);
+  else PDEC_SCORES_HG(64);
+#undef PDEC_SCORES_HG
 #undef PDEC_SCORES
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
