@@ -377,9 +377,9 @@ paged_attn_kernel(
         }
         m[t] = m_new;
         // The weights enter the second product in bf16, each off by at most half a step
-        // (2^-8), a page's V scale with them; the normaliser is the fp32 sum of the
-        // weights as they were rounded, so that what the rounding does to a row's large
-        // weights cancels.
+        // (2^-8), a page's V scale with them (its logarithm, at most 100 in size, rounds the
+        // exponent by 2^-18); the normaliser is the fp32 sum of the weights as they were
+        // rounded, so that what the rounding does to a row's large weights cancels.
         const float base = v_log - m_use;
         uint32_t pw[4];
 #pragma unroll

@@ -262,6 +262,16 @@ def test_listed_pages_behind_the_length_have_no_keys(garbage):
         assert (np.abs(got - ref) <= c.bound(ref, size, k)).all()
 
 
+@pytest.mark.parametrize("n_q", [1, 9])
+def test_value_scales_far_apart(n_q):
+    """Scales at the ends of what the append writes, in one row's pages."""
+    c = Case([400, 33, 2000], 8, 2, 128, n_q=n_q, seed=20)
+    rng = np.random.default_rng(20)
+    c.vs = np.exp2(rng.choice([-100, -50, 0, 50, 100], c.vs.shape)).astype(np.float32)
+    c.ks = np.where(rng.random(c.ks.shape) < 0.2, np.float32(2.0 ** -100), c.ks)
+    c.check()
+
+
 def test_lengths_past_the_table_are_cut_and_negative_ones_empty():
     c = Case([64, 30], 4, 2, 64, seed=10)
     c.table = np.ascontiguousarray(c.table[:, :4])
