@@ -27,8 +27,8 @@
 //   2. judge: the tests with these sums, exact where both sides are further apart than
 //      2^-13 of them.  A test that is closer, one in thousands, takes the masses' own
 //      sums of its two rows, so every decision is that of the definition.  Then the
-//      masses of the deciding row, summed by chunks;
-//   3. rest: r summed by parts of chunks;  4. pick: the part that holds the target, its
+//      masses of the deciding row, summed by cuts;
+//   3. rest: r summed by parts of cuts;  4. pick: the part that holds the target, its
 //      tokens side by side in one group's threads and one scan.
 // 64 sequences of 4 drafts and their drafter's logits at 128256 tokens, 295 MB: 94 us (50,
 // 5.9 TB/s, + 22 + 20 + 6); with the masses of every row in fp64, maximum first, 313.
@@ -49,10 +49,11 @@ constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr double kMinX = -28.5;  // below it the mass rounds to 0
 constexpr double kUnit = 0x1p50;
 constexpr int kMaxDrafts = 1024;
-constexpr int kParts = kWaves;  // of a chunk, each summed by a wave: the pick walks one
+constexpr int kParts = kWaves;  // of a cut, each summed by a wave: the pick walks one
 
 struct Sizes {
   int chunk, n_chunks;  // tokens of a chunk (a multiple of 1024), chunks of a row
+  int cut, n_cuts;      // the same of a deciding row
   int rows;             // target rows, then drafter rows
 };
 inline Sizes sizes_of(int batch, int n_drafts, bool drafter, int vocab) {
@@ -61,6 +62,12 @@ inline Sizes sizes_of(int batch, int n_drafts, bool drafter, int vocab) {
   // 32 values a thread; few rows are cut finer, so that they meet more work groups.
   s.chunk = (int64_t)s.rows * vocab >= (1 << 23) ? 8192 : 2048;
   s.n_chunks = (vocab + s.chunk - 1) / s.chunk;
+  // Two passes over one or two rows a sequence, long arithmetic each: cut finer where few
+  // cuts of 8192 would leave compute units with one or two groups.  us at cuts of 8192 / 2048,
+  // drafter's logits beside the target's: 8 x 128256 33 / 29, 18 x 128256 36 / 33, 50 x 32003
+  // 32 / 30, 34 x 128256 70 / 73, 64 x 128256 106 / 123.
+  s.cut = (int64_t)batch * vocab >= 3 << 20 ? 8192 : 2048;
+  s.n_cuts = (vocab + s.cut - 1) / s.cut;
   return s;
 }
 
@@ -72,7 +79,7 @@ struct Verdict {
 };
 
 // Workspace: per (row, chunk) the maximum and the sum of exponentials over it; per
-// (sequence, chunk) the two rows' masses, per part the two residual masses; verdicts.
+// (sequence, cut) the two rows' masses, per part the two residual masses; verdicts.
 struct Work {
   ulonglong2 *mass, *rest;  // (target, drafter), (r with the drafts taken off, rint p)
   float2* stat;
@@ -81,8 +88,8 @@ struct Work {
 __host__ __device__ inline Work work_of(void* base, const Sizes& s, int batch) {
   Work w;
   w.mass = (ulonglong2*)base;
-  w.rest = w.mass + (int64_t)batch * s.n_chunks;
-  w.stat = (float2*)(w.rest + (int64_t)batch * s.n_chunks * kParts);
+  w.rest = w.mass + (int64_t)batch * s.n_cuts;
+  w.stat = (float2*)(w.rest + (int64_t)batch * s.n_cuts * kParts);
   w.verdict = (Verdict*)(w.stat + (int64_t)s.rows * s.n_chunks);
   return w;
 }
@@ -316,7 +323,7 @@ __global__ __launch_bounds__(kThreads) void verify_judge_kernel(VerifyArgs a, Si
   if (c == 0 && threadIdx.x == 0) w.verdict[b] = v;
   const float* zp = row_ptr(a, row0 + v.n);
   const float* zd = drafter ? row_ptr(a, drow0 + v.n) : nullptr;
-  const int begin = c * s.chunk, end = min(begin + s.chunk, a.vocab);
+  const int begin = c * s.cut, end = min(begin + s.cut, a.vocab);
   double mp = 0.0, md = 0.0;  // 32 masses at most
   walk<kThreads * 4>(zp, zd, begin + threadIdx.x * 4, end, [&](int, f32x4 x, f32x4 y) {
 #pragma unroll
@@ -326,7 +333,7 @@ __global__ __launch_bounds__(kThreads) void verify_judge_kernel(VerifyArgs a, Si
       for (int e = 0; e < 4; ++e) md += mass_of(y[e], v.dm, a.inv_t, frac);
   });
   const uint64_t p = group_sum(to_u64(mp), red), d = group_sum(to_u64(md), red);
-  if (threadIdx.x == 0) w.mass[(int64_t)b * s.n_chunks + c] = make_ulonglong2(p, d);
+  if (threadIdx.x == 0) w.mass[(int64_t)b * s.n_cuts + c] = make_ulonglong2(p, d);
 }
 
 // ---- 3. rest, 4. pick ------------------------------------------------------------
@@ -364,8 +371,8 @@ __device__ __forceinline__ Next next_of(const VerifyArgs& a, const Sizes& s, con
                                         const double* frac) {
   const Verdict v = w.verdict[b];
   uint64_t p = 0, d = 0;  // every wave for itself
-  for (int c = threadIdx.x & 63; c < s.n_chunks; c += 64) {
-    const ulonglong2 m = w.mass[(int64_t)b * s.n_chunks + c];
+  for (int c = threadIdx.x & 63; c < s.n_cuts; c += 64) {
+    const ulonglong2 m = w.mass[(int64_t)b * s.n_cuts + c];
     p += m.x;
     d += m.y;
   }
@@ -389,7 +396,7 @@ __global__ __launch_bounds__(kThreads) void verify_rest_kernel(VerifyArgs a, Siz
   const int b = blockIdx.x, part = blockIdx.y * kParts + (threadIdx.x >> 6);
   const Work w = work_of(a.workspace, s, a.batch);
   const Next r = next_of(a, s, w, b, frac);
-  const int len = s.chunk / kParts, begin = part * len, end = min(begin + len, a.vocab);
+  const int len = s.cut / kParts, begin = part * len, end = min(begin + len, a.vocab);
   double rest = 0.0, all = 0.0;  // sums of parts of 2^50, but for roundings
   r.by_off([&](auto off) {
     walk<256>(r.zp, r.zd, begin + (threadIdx.x & 63) * 4, end, [&](int t, f32x4 x, f32x4 y) {
@@ -403,7 +410,7 @@ __global__ __launch_bounds__(kThreads) void verify_rest_kernel(VerifyArgs a, Siz
   });
   const uint64_t r_sum = wave_add(to_u64(rest)), p_sum = wave_add(to_u64(all));
   if ((threadIdx.x & 63) == 0)
-    w.rest[(int64_t)b * s.n_chunks * kParts + part] = make_ulonglong2(r_sum, p_sum);
+    w.rest[(int64_t)b * s.n_cuts * kParts + part] = make_ulonglong2(r_sum, p_sum);
 }
 
 __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyArgs a, Sizes s) {
@@ -414,7 +421,7 @@ __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyArgs a, Siz
   const int b = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const Work w = work_of(a.workspace, s, a.batch);
   const Next r = next_of(a, s, w, b, frac);
-  const int n_parts = s.n_chunks * kParts, len = s.chunk / kParts;
+  const int n_parts = s.n_cuts * kParts, len = s.cut / kParts;
   const ulonglong2* part = w.rest + (int64_t)b * n_parts;
   uint64_t z = 0, all = 0;
   for (int c = lane; c < n_parts; c += 64) {
@@ -490,7 +497,7 @@ __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyArgs a, Siz
 
 int64_t verify_workspace_bytes(int batch, int n_drafts, bool drafter, int vocab) {
   const Sizes s = sizes_of(batch, n_drafts, drafter, vocab);
-  return ((int64_t)s.rows * 8 + (int64_t)batch * 16 * (1 + kParts)) * s.n_chunks +
+  return (int64_t)s.rows * 8 * s.n_chunks + (int64_t)batch * 16 * (1 + kParts) * s.n_cuts +
          (int64_t)batch * (int64_t)sizeof(Verdict);
 }
 
@@ -501,7 +508,7 @@ hipError_t launch_verify(const VerifyArgs& a, hipStream_t stream) {
   // Temperatures at which fp32 arguments mean nothing: every test is a close one.
   const double slack = a.temperature < 1e-30f ? INFINITY : 0x1p-13;
   // A row's chunks side by side.
-  const dim3 all((uint32_t)s.rows * s.n_chunks), one(a.batch, s.n_chunks);
+  const dim3 all((uint32_t)s.rows * s.n_chunks), one(a.batch, s.n_cuts);
   if (s.chunk == 8192)
     verify_stats_kernel<8><<<all, kThreads, 0, stream>>>(a, s, c2);
   else
