@@ -262,64 +262,78 @@ __global__ __launch_bounds__(kThreads) void verify_judge_kernel(VerifyArgs a, Si
 #pragma clang fp contract(off)
   __shared__ uint64_t red[kWaves];
   __shared__ signed char verdicts[kMaxDrafts];
-  __shared__ float p_max[kMaxDrafts + 1], d_max[kMaxDrafts];
+  __shared__ float2 p_stat[kMaxDrafts + 1], d_stat[kMaxDrafts];
   __shared__ double frac[64];
   fill_fractions(frac);
   const int b = blockIdx.x, c = blockIdx.y, T = a.n_drafts, wave = threadIdx.x >> 6;
   const Work w = work_of(a.workspace, s, a.batch);
   enum { kRefuse, kAccept, kClose, kEnd };
-  // One side of test i: 2^24 p_x, and u24 d_x, with units of the row sums `pu`, `du`.
-  auto lhs = [&](int i, float dm, double du) {
-    const int64_t at = (int64_t)b * T + i;
-    const double dx = a.drafter ? mass_of(a.drafter[at * a.vocab + a.drafts[at]], dm, a.inv_t, frac) * du
-                                : kUnit;
-    return (double)u24_of(a.uniforms[(int64_t)b * (T + 1) + i]) * dx;
-  };
-  auto rhs = [&](int i, float pm, double pu) {
-    const int64_t row = (int64_t)b * (T + 1) + i;
-    const double px =
-        mass_of(a.target[row * a.vocab + a.drafts[(int64_t)b * T + i]], pm, a.inv_t, frac) * pu;
-    return 0x1p24 * px;
-  };
   const int row0 = b * (T + 1), drow0 = a.batch * (T + 1) + b * T;
+  // What test i looks at: the draft, its logits, its uniform number.
+  struct Draft {
+    int x;
+    float zp, zd, u;
+  };
+  auto draft = [&](int i) {
+    Draft r = {a.drafts[(int64_t)b * T + i], 0.f, 0.f, a.uniforms[(int64_t)b * (T + 1) + i]};
+    if (r.x >= 0 && r.x < a.vocab) {
+      r.zp = row_ptr(a, row0 + i)[r.x];
+      if (a.drafter) r.zd = row_ptr(a, drow0 + i)[r.x];
+    }
+    return r;
+  };
+  // Its sides, with units of the row sums `pu`, `du`: u24 d_x, and 2^24 p_x.
+  auto lhs = [&](const Draft& r, float dm, double du) {
+    return (double)u24_of(r.u) * (a.drafter ? mass_of(r.zd, dm, a.inv_t, frac) * du : kUnit);
+  };
+  auto rhs = [&](const Draft& r, float pm, double pu) {
+    return 0x1p24 * (mass_of(r.zp, pm, a.inv_t, frac) * pu);
+  };
+  // A thread a test: the loads of one follow each other, so all are under way while the
+  // waves sum up the rows.
+  Draft mine = {-1, 0.f, 0.f, 0.f};
+  if (threadIdx.x < T) mine = draft(threadIdx.x);
   for (int i = wave; i <= T; i += kWaves) {
     const float2 p = row_stat(w, s, row0 + i, c2);
     float2 d = make_float2(0.f, 1.f);
     if (a.drafter && i < T) d = row_stat(w, s, drow0 + i, c2);
-    const int x = i < T ? a.drafts[(int64_t)b * T + i] : -1;
+    if ((threadIdx.x & 63) == 0) {
+      p_stat[i] = p;
+      if (i < T) d_stat[i] = d;
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < T; i += kThreads) {
+    if (i >= kThreads) mine = draft(i);
     int verdict = kEnd;
-    if (x >= 0 && x < a.vocab) {
+    if (mine.x >= 0 && mine.x < a.vocab) {
+      const float2 p = p_stat[i], d = d_stat[i];
       // 2^50 / S, S in units of 2^40; no mass where the maximum is not finite
-      const double l = lhs(i, d.x, fabsf(d.x) <= FLT_MAX ? 0x1p10 / (double)d.y : 0.0);
-      const double r = rhs(i, p.x, fabsf(p.x) <= FLT_MAX ? 0x1p10 / (double)p.y : 0.0);
+      const double l = lhs(mine, d.x, fabsf(d.x) <= FLT_MAX ? 0x1p10 / (double)d.y : 0.0);
+      const double r = rhs(mine, p.x, fabsf(p.x) <= FLT_MAX ? 0x1p10 / (double)p.y : 0.0);
       verdict = l < r * (1.0 - slack) ? kAccept : l >= r * (1.0 + slack) ? kRefuse : kClose;
     }
-    if ((threadIdx.x & 63) == 0) {
-      p_max[i] = p.x;
-      if (i < T) {
-        verdicts[i] = (signed char)verdict;
-        d_max[i] = d.x;
-      }
-    }
+    verdicts[i] = (signed char)verdict;
   }
   __syncthreads();
   Verdict v = {0, -1, 0.f, 0.f};
   for (; v.n < T; ++v.n) {
     int verdict = verdicts[v.n];
     if (verdict == kClose) {
-      const float pm = p_max[v.n], dm = d_max[v.n];
+      const float pm = p_stat[v.n].x, dm = d_stat[v.n].x;
       const double pu = exact_unit(row_ptr(a, row0 + v.n), a.vocab, pm, a.inv_t, frac, red);
       const double du =
           a.drafter ? exact_unit(row_ptr(a, drow0 + v.n), a.vocab, dm, a.inv_t, frac, red) : 0.0;
-      verdict = lhs(v.n, dm, du) < rhs(v.n, pm, pu) ? kAccept : kRefuse;
+      const Draft r = draft(v.n);
+      verdict = lhs(r, dm, du) < rhs(r, pm, pu) ? kAccept : kRefuse;
     }
     if (verdict == kAccept) continue;
     if (verdict == kRefuse) v.refused = a.drafts[(int64_t)b * T + v.n];
     break;
   }
   const bool drafter = a.drafter && v.refused >= 0;
-  v.pm = p_max[v.n];
-  if (drafter) v.dm = d_max[v.n];
+  v.pm = p_stat[v.n].x;
+  if (drafter) v.dm = d_stat[v.n].x;
   if (c == 0 && threadIdx.x == 0) w.verdict[b] = v;
   const float* zp = row_ptr(a, row0 + v.n);
   const float* zd = drafter ? row_ptr(a, drow0 + v.n) : nullptr;
