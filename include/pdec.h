@@ -540,7 +540,9 @@ int rope_table(int32_t max_pos, int32_t head_dim, float base, float* table_dev, 
  *   Row r belongs to the sequence b with row_start[b] <= r < row_start[b + 1]
  *   (device int32 [n_seqs + 1], ascending) and to position
  *   lens[b] - (row_start[b + 1] - r): lens (device int32 [n_seqs]) counts the
- *   new tokens.  k and v are rows of [n_kv_heads][head_dim] in src_dtype,
+ *   new tokens.  row_start[0] may be below 0 and row_start[n_seqs] above
+ *   n_rows: such rows are not the call's, the others' positions are the same.
+ *   k and v are rows of [n_kv_heads][head_dim] in src_dtype,
  *   k_stride / v_stride elements apart (the q|k|v rows of one projection serve
  *   as they are); k's head pairs (i, i + head_dim / 2) are rotated by the
  *   table's angle of the position.  q (nullable): rows of

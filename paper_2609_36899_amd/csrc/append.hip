@@ -311,7 +311,7 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs a, int q
         ++r;
         continue;
       }
-      seq_row0 = a.row_start[b];
+      seq_row0 = max(a.row_start[b], 0);  // its rows before the call's first are not here
       seq_end = min(a.row_start[b + 1], a.n_rows);
       end_pos = (int64_t)a.lens[b] - ((int64_t)a.row_start[b + 1] - seq_end);
     }

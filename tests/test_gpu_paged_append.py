@@ -310,3 +310,31 @@ def test_replayed_graph_follows_the_lengths():
                      (c.means, eager.means), (c.q_out, eager.q_out)):
             assert torch.equal(a, b), step
         lens += 1
+
+
+@pytest.mark.parametrize("kind", ["fp8", "bf16", "f32"])
+@pytest.mark.parametrize("lens,new,first", [([40, 21], [19, 4], -11), ([8, 30], [1, 1], -7),
+                                            ([70], [33], -2 ** 31)])
+def test_a_sequence_may_begin_before_the_calls_first_row(kind, lens, new, first):
+    """Rows of the first sequence that an earlier call appended: row_start[0] below 0 says
+    where they would be.  The positions count from the sequence's end, so the call is the
+    one with row_start[0] = 0."""
+    a, b = (Case(lens, new, 4, 2, 64, kind, "f32", seed=15) for _ in range(2))
+    b.starts[0] = first
+    a.call()
+    b.call()
+    for name in ("kp", "vp", "ks", "vs", "means", "q_out"):
+        x, y = getattr(a, name), getattr(b, name)
+        assert x is None or torch.equal(x, y), name
+
+
+@pytest.mark.parametrize("kind", ["fp8", "bf16"])
+def test_a_sequence_may_end_behind_the_calls_last_row(kind):
+    a, b = (Case([40, 29], [19, 14], 4, 2, 64, kind, "f32", seed=16) for _ in range(2))
+    b.starts[-1] += 7
+    b.lens[-1] += 7
+    a.call()
+    b.call()
+    for name in ("kp", "vp", "ks", "vs", "means", "q_out"):
+        x, y = getattr(a, name), getattr(b, name)
+        assert x is None or torch.equal(x, y), name
