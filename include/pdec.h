@@ -580,7 +580,8 @@ int paged_kv_append(int32_t src_dtype, int32_t kv_dtype, int32_t n_rows, int32_t
  *   q, out: device bf16 [batch][n_q][n_q_heads][head_dim]; lens: device int32
  *   [batch], counting the n_q tokens, taken as in [0, bt_stride * 16]; a token
  *   that sees no key (position below 0) gets zeros.  kv_dtype PDEC_BF16, or
- *   PDEC_FP8_E4M3 with positive scales, 2^-100 to 2^100 as paged_kv_append's.
+ *   PDEC_FP8_E4M3 with scales up to 2^100; one below 2^-100, the least that
+ *   paged_kv_append writes, counts as 2^-100 (0 among them: a page of zeros).
  *   selected (nullable, n_q = 1): device int32 [batch][n_kv_heads]
  *   [n_selected], logical page indices, distinct; the first min(n_selected,
  *   ceil(lens[b] / 16)) of them are read, and the softmax runs over the

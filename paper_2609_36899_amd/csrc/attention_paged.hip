@@ -45,6 +45,7 @@ constexpr int kGroups = 256;
 constexpr int SF = 2, SB = 2;  // stages
 constexpr int kPair = 2 * kPage;        // keys of a pair of pages
 constexpr int kNowhere = 0x40000000;    // a key position past every limit
+constexpr float kMinScale = 0x1p-100f;
 
 __device__ __forceinline__ int clamp_len(const PagedAttnArgs& a, int b) {
   return min(max(a.lens[b], 0), a.max_len);
@@ -317,8 +318,10 @@ paged_attn_kernel(
       // Scales of pages without keys (of page 0, which stands in for no page, or of one that
       // is listed from behind the length) may be anything.
       const bool scaled = kFp8 && kbase < kv_lim;
-      const float k_mul = scaled ? a.scale_log2 * r.ks : a.scale_log2;
-      const float v_mul = scaled ? r.vs : 1.f;
+      // A scale of 0 would meet -inf (masked scores, its logarithm) and its inverse: what lies
+      // below the least scale that the append writes counts as that one.
+      const float k_mul = scaled ? a.scale_log2 * max2(r.ks, kMinScale) : a.scale_log2;
+      const float v_mul = scaled ? max2(r.vs, kMinScale) : 1.f;
       const float v_log = kFp8 ? __builtin_amdgcn_logf(v_mul) : 0.f;
       // The weights' sum is a product too, by rows of ones, or of the inverse of the V scale
       // that the weights carry: its high half in even rows and the rest in odd ones (2^-16

@@ -371,3 +371,31 @@ def test_calls_on_two_streams_with_their_own_workspaces():
     torch.cuda.synchronize()
     for o in outs:
         assert torch.equal(o.float().cpu(), want)
+
+
+@pytest.mark.parametrize("n_q", [1, 5, 13, 26])
+@pytest.mark.parametrize("which", ["k", "v", "both"])
+def test_a_scale_of_zero_reads_as_zeros(n_q, which):
+    """Pages of zeros whose writer left the scale at 0, among others.  It counts as 2^-100:
+    whatever finite codes stand there read as 448 * 2^-100 < 2^-91 at most."""
+    c = Case([400, 33, 300, 2000, 16], 8, 2, 128, n_q=n_q, seed=21)
+    rng = np.random.default_rng(21)
+    none = rng.random(c.ks.shape) < 0.3
+    none[c.table[1, :3]], none[c.table[4, 0]] = True, True  # sequences of nothing else
+    for s, name in ((c.ks, "k"), (c.vs, "v")):
+        if which in (name, "both"):
+            s[none] = 0.0
+            s[c.table[2, 4]] = -0.0
+    for selected in (False, True) if n_q == 1 else (False,):
+        if selected:
+            c.selected = np.stack([rng.permutation(np.arange(127, dtype=np.int32))[:40]
+                                   for _ in range(10)]).reshape(5, 2, 40)
+        scales = c.ks, c.vs
+        got = c.run()
+        c.ks, c.vs = (np.maximum(s, np.float32(2.0 ** -100)) for s in scales)
+        k, v = c.values()
+        ref, size = oo.token_attention(c.q.float().numpy(), k, v, c.table, c.lens, c.selected)
+        assert (np.abs(got - ref) <= c.bound(ref, size, k)).all()
+        if which != "k":
+            assert np.abs(got[[1, 4]]).max() < 2.0 ** -91
+        c.ks, c.vs = scales
