@@ -589,8 +589,9 @@ int paged_kv_append(int32_t src_dtype, int32_t kv_dtype, int32_t n_rows, int32_t
  *   Scores, softmax and sums are fp32; the weights enter the second product
  *   rounded to bf16.
  *   workspace: device, paged_token_attention_workspace_bytes(...) bytes for
- *   the same sizes (0 where no table is long: then it may be null); max_pages
- *   is bt_stride, or the smaller of it and n_selected with a selection.
+ *   the same or larger batch, n_q and max_pages; max_pages is bt_stride, or the
+ *   smaller of it and n_selected with a selection.  It may be null where these
+ *   are 0 (no table is long).
  * Entries that are not page indices (paged_select's -1 among them) or whose
  * page id is outside [0, n_pages) have no keys.
  * Errors: PDEC_INVALID_ARG (n_q outside [1, 4096], ...), PDEC_UNSUPPORTED,
@@ -617,7 +618,8 @@ int paged_token_attention(int32_t kv_dtype, int32_t batch, int32_t n_q, int32_t 
  *   keeps them; lens: device int32 [batch]; selected_dev: device int32
  *   [batch][n_kv_heads][n_selected]; keep_first >= 0, keep_last >= 1 (the page
  *   of the newest token), together at most n_selected.
- *   workspace: device, paged_select_workspace_bytes(...) bytes.
+ *   workspace: device, paged_select_workspace_bytes(...) bytes for the same or
+ *   larger sizes.
  * Errors: PDEC_INVALID_ARG, PDEC_UNSUPPORTED, PDEC_HIP_ERROR. */
 int64_t paged_select_workspace_bytes(int32_t batch, int32_t n_kv_heads, int32_t bt_stride);
 int paged_select(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
@@ -650,7 +652,8 @@ int paged_select(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t h
  *   next token, then -1; accepted_out: device int32 [batch], their number.
  * NaN logits have no mass, nor has a row whose maximum is not finite; with no
  * mass at all the next token is 0.
- *   workspace: device, verify_drafts_workspace_bytes(...) bytes.
+ *   workspace: device, verify_drafts_workspace_bytes(...) bytes for the same
+ *   vocab and the same or larger batch and n_drafts, with_drafter for either.
  * Errors: PDEC_INVALID_ARG (temperature <= 0 or not finite, n_drafts outside
  * [1, 1024], vocab above 2^22, null pointers, a small workspace). */
 int64_t verify_drafts_workspace_bytes(int32_t batch, int32_t n_drafts, int32_t vocab,

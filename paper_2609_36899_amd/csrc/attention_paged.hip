@@ -712,7 +712,9 @@ PagedAttnPlan plan_paged_attention(int batch, int n_q, int n_q_heads, int n_kv_h
   // 74.9 / 53.4; 1024 tokens, 8 sequences 15.4 / 12.9 and 15.7 / 17.9 (bf16), 64 32.8 /
   // 24.9; 2048 tokens, 1 sequence 15.1 / 15.3 and 13.8 / 20.8, 64 47.9 / 42.7 and 70.6 /
   // 71.4, 256 166.9 / 151.8.
-  p.unit_groups = p.n_units <= 65535 && (max_pages + 1) / 2 <= (p.n_units * n_kv_heads >= 512 ? 66 : 24);
+  const int pairs = (max_pages + 1) / 2;
+  p.units_for_groups = pairs <= 24 ? 1 : pairs <= 66 ? (512 + n_kv_heads - 1) / n_kv_heads : INT32_MAX;
+  p.unit_groups = p.n_units <= 65535 && p.n_units >= p.units_for_groups;
   return p;
 }
 

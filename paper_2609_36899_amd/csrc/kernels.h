@@ -193,6 +193,7 @@ struct PagedAttnPlan {
   int32_t row_tiles, tok_per_block, blocks_per_seq, n_groups;
   int64_t n_units;
   bool unit_groups;  // a work group for each unit and no merge, instead of equal stretches
+  int32_t units_for_groups;  // the fewest units at which tables of max_pages give that
 };
 // max_pages: what no sequence can read more of.
 PagedAttnPlan plan_paged_attention(int batch, int n_q, int n_q_heads, int n_kv_heads,

@@ -43,10 +43,14 @@ int check_table(int32_t batch, int32_t bt_stride, int64_t n_pages) {
 struct TokenAttnLayout {
   int64_t ml, acc;  // byte offsets end here: ml, then ml + acc
 };
+TokenAttnLayout layout_of(int64_t n_units, const PagedAttnPlan& p, int32_t n_kv_heads,
+                          int32_t head_dim) {
+  const int64_t rows = (p.n_groups + n_units) * n_kv_heads * 16 * p.row_tiles;
+  return {align_up(rows * 2 * 4), align_up(rows * head_dim * 4)};
+}
 TokenAttnLayout layout_of(const PagedAttnPlan& p, int32_t n_kv_heads, int32_t head_dim) {
   if (p.unit_groups) return {0, 0};  // no partials
-  const int64_t rows = (p.n_groups + p.n_units) * n_kv_heads * 16 * p.row_tiles;
-  return {align_up(rows * 2 * 4), align_up(rows * head_dim * 4)};
+  return layout_of(p.n_units, p, n_kv_heads, head_dim);
 }
 
 int check_token_attention(int32_t batch, int32_t n_q, int32_t n_q_heads, int32_t n_kv_heads,
@@ -141,8 +145,12 @@ int64_t paged_token_attention_workspace_bytes(int32_t batch, int32_t n_q, int32_
   const int rc = check_token_attention(batch, n_q, n_q_heads, n_kv_heads, head_dim);
   if (rc != PDEC_OK) return rc;
   if (max_pages < 1 || max_pages > kMaxStride) return fail(PDEC_INVALID_ARG, "bad max_pages");
-  const TokenAttnLayout l = layout_of(
-      plan_paged_attention(batch, n_q, n_q_heads, n_kv_heads, max_pages), n_kv_heads, head_dim);
+  const PagedAttnPlan p = plan_paged_attention(batch, n_q, n_q_heads, n_kv_heads, max_pages);
+  TokenAttnLayout l = layout_of(p, n_kv_heads, head_dim);
+  // Where many units have a group each and no partials, fewer of the same would have some:
+  // the bytes serve every smaller batch too.
+  if (p.unit_groups && p.units_for_groups > 1)
+    l = layout_of(std::min<int64_t>(p.n_units, p.units_for_groups - 1), p, n_kv_heads, head_dim);
   return l.ml + l.acc;
 }
 

@@ -205,7 +205,8 @@ def paged_kv_append(k: torch.Tensor, v: torch.Tensor, lens: torch.Tensor,
 @functools.lru_cache(maxsize=1024)
 def paged_token_attention_workspace_bytes(batch: int, n_q: int, n_q_heads: int, n_kv_heads: int,
                                           head_dim: int, max_pages: int) -> int:
-    """Scratch bytes for a table (or a selection, if that is smaller) of max_pages pages."""
+    """Scratch bytes for a table (or a selection, if that is smaller) of max_pages pages, and
+    for smaller batches, n_q and tables."""
     return N.check(N.load().paged_token_attention_workspace_bytes(
         batch, n_q, n_q_heads, n_kv_heads, head_dim, max_pages))
 

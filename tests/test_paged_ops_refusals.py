@@ -144,3 +144,39 @@ def test_binding_refuses_tensors_of_the_host():
                             torch.zeros((2, 2), dtype=torch.int32), i)
     with pytest.raises(PdecError, match="table size"):
         paged.rope_table(0, 64)
+
+
+def test_a_workspace_of_the_largest_sizes_serves_all_smaller_ones():
+    """A batch that shrinks keeps its workspace: no size asks for more than a larger one."""
+    attn, verify = (paged.paged_token_attention_workspace_bytes,
+                    paged.verify_drafts_workspace_bytes)
+    for hq, hkv in ((32, 8), (8, 2), (16, 1), (5, 5)):
+        for n_q in (1, 5, 13, 40):
+            for pages in (8, 48, 49, 128, 132, 133, 4000):
+                need = [attn(b, n_q, hq, hkv, 128, pages) for b in range(1, 600)]
+                assert need == sorted(need), (hq, hkv, n_q, pages)
+        for batch in (1, 20, 63, 64, 500):
+            for pages in (48, 128, 133):
+                need = [attn(batch, n, hq, hkv, 128, pages) for n in range(1, 200)]
+                assert need == sorted(need), (hq, hkv, batch, pages)
+            need = [attn(batch, 3, hq, hkv, 128, p) for p in range(1, 300)]
+            assert need == sorted(need), (hq, hkv, batch)
+    for vocab in (1, 1024, 32003, 128256, 151936):
+        for drafter in (True, False):
+            for n in (1, 4, 9):
+                need = [verify(b, n, vocab, drafter) for b in range(1, 400)]
+                assert need == sorted(need), (vocab, drafter, n)
+            for batch in (1, 8, 25, 64):
+                need = [verify(batch, n, vocab, drafter) for n in range(1, 60)]
+                assert need == sorted(need), (vocab, drafter, batch)
+        assert all(verify(b, 4, vocab, False) <= verify(b, 4, vocab, True) for b in range(1, 400))
+
+
+def test_a_call_takes_the_workspace_of_a_larger_batch():
+    """63 sequences in the workspace of 64: refused for nothing but the launch itself, which
+    has no GPU here."""
+    need = paged.paged_token_attention_workspace_bytes(64, 1, 32, 8, 128, 128)
+    if torch.cuda.is_available():
+        pytest.skip("made-up addresses")
+    _attn(batch=63, hq=32, hkv=8, dh=128, stride=128, ws_bytes=need)
+    assert b"too small" not in N.load().last_error()
