@@ -343,16 +343,22 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs a, int q
 
 }  // namespace
 
+// Long runs: a leader in 16 rows, so a window of 16 holds about one page; single
+// tokens: every row is a leader.
+static int append_window(const AppendArgs& a) {
+  return a.n_rows >= 4 * (int64_t)a.n_seqs ? kPage : 1;
+}
+static int64_t append_groups(const AppendArgs& a) {
+  const int64_t windows = ((int64_t)a.n_rows + append_window(a) - 1) / append_window(a);
+  return (a.q ? a.n_rows : 0) + windows * 2 * a.n_kv_heads;
+}
+int64_t append_threads(const AppendArgs& a) { return append_groups(a) * kThreads; }
+
 hipError_t launch_kv_append(int src_dtype, int kv_dtype, int head_dim, const AppendArgs& a,
                             hipStream_t stream) {
   if (a.n_rows == 0) return hipSuccess;
-  // Long runs: a leader in 16 rows, so a window of 16 holds about one page; single
-  // tokens: every row is a leader.
-  const int window = a.n_rows >= 4 * (int64_t)a.n_seqs ? kPage : 1;
-  const int q_groups = a.q ? a.n_rows : 0;
-  const int64_t groups =
-      q_groups + ((int64_t)a.n_rows + window - 1) / window * 2 * a.n_kv_heads;
-  const dim3 grid((uint32_t)groups), block(kThreads);
+  const int window = append_window(a), q_groups = a.q ? a.n_rows : 0;
+  const dim3 grid((uint32_t)append_groups(a)), block(kThreads);
 #define PDEC_APPEND(ST_, KT_)                                                              \
   do {                                                                                     \
     if (head_dim == 128)                                                                   \

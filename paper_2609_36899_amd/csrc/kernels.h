@@ -185,6 +185,9 @@ struct AppendArgs {  // append.hip
   float *k_scales, *v_scales;  // E4M3 pages
   uint16_t* k_means;           // nullable
 };
+// A launch takes fewer than 2^32 threads in a dimension: callers refuse larger sizes.
+constexpr int64_t kMaxLaunch = UINT32_MAX;
+int64_t append_threads(const AppendArgs& a);
 // kv_dtype: 0 fp32, 1 bf16, 2 E4M3 pages.
 hipError_t launch_kv_append(int src_dtype, int kv_dtype, int head_dim, const AppendArgs& a,
                             hipStream_t stream);
@@ -220,6 +223,7 @@ struct SelectArgs {  // select.hip
   float* scores;  // [batch][Hkv][bt_stride]
   int32_t* selected;
 };
+int64_t select_threads(const SelectArgs& a);  // of its largest launch
 hipError_t launch_paged_select(int head_dim, const SelectArgs& a, hipStream_t stream);
 
 struct VerifyArgs {  // verify.hip

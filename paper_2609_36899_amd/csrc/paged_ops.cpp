@@ -108,9 +108,6 @@ int paged_kv_append(int32_t src_dtype, int32_t kv_dtype, int32_t n_rows, int32_t
   if (!aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(rope_dev, 16) ||
       !aligned(q_out, 16))
     return fail(PDEC_INVALID_ARG, "pages, table and q_out must be 16-byte aligned");
-  // Work groups of the launch: one a row for q, and two a KV head for a row or window.
-  if ((int64_t)n_rows * (1 + 2 * (int64_t)n_kv_heads) > INT32_MAX)
-    return fail(PDEC_INVALID_ARG, "too many rows for one call");
   AppendArgs a{};
   a.k = k;
   a.v = v;
@@ -135,6 +132,8 @@ int paged_kv_append(int32_t src_dtype, int32_t kv_dtype, int32_t n_rows, int32_t
   a.k_scales = k_scales;
   a.v_scales = v_scales;
   a.k_means = (uint16_t*)k_means;
+  if (append_threads(a) > kMaxLaunch)
+    return fail(PDEC_INVALID_ARG, "too many rows for one call");
   HIP_OR_FAIL(launch_kv_append(src_dtype, kv_dtype, head_dim, a, (hipStream_t)stream));
   return PDEC_OK;
 }
@@ -231,7 +230,7 @@ int paged_select(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t h
   int rc = check_heads(n_q_heads, n_kv_heads, head_dim);
   if (rc == PDEC_OK) rc = check_table(batch, bt_stride, n_pages);
   if (rc != PDEC_OK) return rc;
-  if ((int64_t)batch * n_kv_heads > INT32_MAX || (int64_t)batch * (bt_stride / 16 + 1) > INT32_MAX)
+  if ((int64_t)batch * (bt_stride / 16 + 1) > INT32_MAX)
     return fail(PDEC_INVALID_ARG, "batch too large for one call");
   if (n_selected < 1 || n_selected > kMaxStride || keep_first < 0 || keep_last < 1 ||
       (int64_t)keep_first + keep_last > n_selected)
@@ -257,6 +256,8 @@ int paged_select(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t h
   a.n_pages = n_pages;
   a.scores = (float*)workspace;
   a.selected = selected_dev;
+  if (select_threads(a) > kMaxLaunch)
+    return fail(PDEC_INVALID_ARG, "batch too large for one call");
   HIP_OR_FAIL(launch_paged_select(head_dim, a, (hipStream_t)stream));
   return PDEC_OK;
 }

@@ -339,6 +339,12 @@ __global__ __launch_bounds__(T) void take_pages_kernel(SelectArgs a) {
 
 }  // namespace
 
+// Threads for eight pages each, up to what a work group holds.
+static int list_threads(int bt_stride) { return bt_stride > 4096 ? 1024 : bt_stride > 512 ? 512 : 256; }
+int64_t select_threads(const SelectArgs& a) {
+  return (int64_t)a.batch * a.n_kv_heads * list_threads(a.bt_stride);
+}
+
 hipError_t launch_paged_select(int head_dim, const SelectArgs& a, hipStream_t stream) {
   const int64_t rows = (int64_t)a.batch * a.n_kv_heads;
   const int heads = std::min(a.n_kv_heads, kWaves), head_blocks = (a.n_kv_heads + heads - 1) / heads;
@@ -359,10 +365,10 @@ hipError_t launch_paged_select(int head_dim, const SelectArgs& a, hipStream_t st
 #undef PDEC_SCORES
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  // Threads for eight pages each, up to what a work group holds.
-  if (a.bt_stride > 4096)
+  const int threads = list_threads(a.bt_stride);
+  if (threads == 1024)
     take_pages_kernel<1024><<<(uint32_t)rows, 1024, 0, stream>>>(a);
-  else if (a.bt_stride > 512)
+  else if (threads == 512)
     take_pages_kernel<512><<<(uint32_t)rows, 512, 0, stream>>>(a);
   else
     take_pages_kernel<256><<<(uint32_t)rows, 256, 0, stream>>>(a);

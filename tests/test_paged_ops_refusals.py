@@ -180,3 +180,15 @@ def test_a_call_takes_the_workspace_of_a_larger_batch():
         pytest.skip("made-up addresses")
     _attn(batch=63, hq=32, hkv=8, dh=128, stride=128, ws_bytes=need)
     assert b"too small" not in N.load().last_error()
+
+
+@pytest.mark.parametrize("call", [
+    # one token for each of 2^20 sequences, 16 KV heads: 33 work groups a row
+    lambda: _append(rows=1 << 20, seqs=1 << 20, hq=16, hkv=16, qs=1024, ks=1024, vs=1024),
+    lambda: _append(rows=1 << 24, seqs=1, hq=2, qs=128, ks=128, vs=128),
+    lambda: _select(batch=1 << 20, hq=16, hkv=16),
+    lambda: _select(batch=1 << 20, hq=4, hkv=4, stride=8000),
+])
+def test_more_work_groups_than_a_launch_takes(call):
+    assert call() == N.INVALID_ARG
+    assert b"for one call" in N.load().last_error()
