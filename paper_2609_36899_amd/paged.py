@@ -144,6 +144,8 @@ def rope_table(max_pos: int, head_dim: int, base: float = 10000.0, device="cuda"
     """The (cos, sin) table [max_pos][head_dim / 2][2] that paged_kv_append rotates by."""
     if max_pos < 1 or head_dim < 2 or head_dim % 2:
         _refuse("bad rotary table size")
+    if torch.device(device).type != "cuda":
+        _refuse("the rotary table is made on a GPU")
     index = torch.device(device).index
     dev = torch.cuda.current_device() if index is None else index
     handle = _handle(dev, stream)

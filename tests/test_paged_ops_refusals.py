@@ -192,3 +192,9 @@ def test_a_call_takes_the_workspace_of_a_larger_batch():
 def test_more_work_groups_than_a_launch_takes(call):
     assert call() == N.INVALID_ARG
     assert b"for one call" in N.load().last_error()
+
+
+@pytest.mark.parametrize("device", ["cpu", "meta"])
+def test_rope_table_is_made_on_a_gpu(device):
+    with pytest.raises(PdecError, match="GPU"):
+        paged.rope_table(8, 64, device=device)
