@@ -33,15 +33,6 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-// Work groups of a launch: one for each compute unit.  More of them cost their beginnings
-// (lengths, queries, first pages) and their partials: us at 256 / 512 groups, 64 sequences
-// of 1K to 8K tokens 120 / 119 (E4M3, 648 MB: 5.4 TB/s) and 180 / 179 (bf16, 1136 MB: 6.3),
-// five tokens each over 8 x 64K to 128K 267 / 283 (E4M3, 1580 MB: 5.9), four over 16 x 1K to
-// 16K 94 / 96 (bf16, 512 MB: 5.4); 1024 groups are slower by 5 to 20% more.  Blocks of more
-// than 32 rows, whose waves go in step, gain from a second group on a unit: 13 tokens over 16 x
-// 4K to 16K 124 / 92 (E4M3), 126 / 118 (bf16), 26 tokens 177 / 140 and 168 / 152; 768 are as
-// slow as 256.
-constexpr int kGroups = 256;
 constexpr int SF = 2, SB = 2;  // stages
 constexpr int kPair = 2 * kPage;        // keys of a pair of pages
 constexpr int kNowhere = 0x40000000;    // a key position past every limit
@@ -695,54 +686,23 @@ __global__ __launch_bounds__(kThreads) void paged_merge_kernel(PagedAttnArgs a, 
 
 }  // namespace
 
-PagedAttnPlan plan_paged_attention(int batch, int n_q, int n_q_heads, int n_kv_heads,
-                                   int max_pages) {
-  PagedAttnPlan p;
-  const int G = n_q_heads / n_kv_heads;
-  // The smallest block that holds a sequence's rows of a KV head, or blocks of 128.
-  const int64_t rows = (int64_t)n_q * G;
-  p.row_tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 ? 4 : 8;
-  p.tok_per_block = 16 * p.row_tiles / G;
-  p.blocks_per_seq = (n_q + p.tok_per_block - 1) / p.tok_per_block;
-  p.n_units = (int64_t)batch * p.blocks_per_seq;
-  p.n_groups = std::max(1, (p.row_tiles > 2 ? 512 : kGroups) / n_kv_heads);
-  // A work group for each unit needs no scan of the lengths and no merge, and waits for the
-  // longest.  us, equal stretches / a group a unit, one token, 8 KV heads of four: table of
-  // 512 tokens, 8 sequences 15.0 / 11.8 (E4M3), 14.0 / 11.4 (bf16), 64 26.1 / 16.2, 256
-  // 74.9 / 53.4; 1024 tokens, 8 sequences 15.4 / 12.9 and 15.7 / 17.9 (bf16), 64 32.8 /
-  // 24.9; 2048 tokens, 1 sequence 15.1 / 15.3 and 13.8 / 20.8, 64 47.9 / 42.7 and 70.6 /
-  // 71.4, 256 166.9 / 151.8.
-  const int pairs = (max_pages + 1) / 2;
-  p.units_for_groups = pairs <= 24 ? 1 : pairs <= 66 ? (512 + n_kv_heads - 1) / n_kv_heads : INT32_MAX;
-  p.unit_groups = p.n_units <= 65535 && p.n_units >= p.units_for_groups;
-  return p;
-}
-
 hipError_t launch_paged_attention(int kv_fp8, int head_dim, int row_tiles, const PagedAttnArgs& a,
                                   hipStream_t stream) {
   const dim3 grid(a.n_kv_heads, a.unit_groups ? a.n_units : a.n_groups), block(kThreads);
-  // 17 to 32 rows as a tile for each of two waves that load the same pages, or as two tiles of
-  // one wave: half the work at a stretch's two ends, or half the loads between them.  By what a
-  // work group reads if the table is full; us, tile a wave / two tiles, at KB a group: E4M3, 5 x
-  // 4 rows over 4 x 4K 17.7 / 22.7 (120), over 128 x 0.5K 31.5 / 51.1 (512), over 58 x 1.4K 56.6
-  // / 57.0 (640), 8 x 3 over 41 x 0 to 4K 34.7 / 39.9 (700), 5 x 4 61.0 / 60.0 (1400), over 16 x
-  // 16K 73.5 / 63.8 (2048); bf16, 5 x 4 over 4 x 4K 19.1 / 22.3 (240), 8 x 3 over 58 x 1.4K
-  // 49.2 / 42.0 (640).
-  const int64_t group_bytes = (int64_t)a.n_units * a.max_len * a.n_kv_heads / kGroups * head_dim *
-                              (kv_fp8 ? 2 : 4);
-  const bool little = group_bytes <= (kv_fp8 ? 1024 : 256) * 1024;
+  const PagedAttnForm f = paged_attention_form(kv_fp8, head_dim, row_tiles, a.n_units, a.max_len,
+                                               a.n_kv_heads);
 #define PDEC_PAGED(DH_, RT_, RW_, KT_, LIST_)                          \
   paged_attn_kernel<DH_, RT_, RW_, KT_, LIST_><<<grid, block, 0, stream>>>(a, a.block_table, \
                                                                            a.selected)
 #define PDEC_PAGED_RT(DH_, KT_)                                  \
   do {                                                           \
     if (a.selected) PDEC_PAGED(DH_, 1, 1, KT_, true);            \
-    else if (row_tiles == 1) PDEC_PAGED(DH_, 1, 1, KT_, false);  \
-    else if (row_tiles == 2 && little) PDEC_PAGED(DH_, 1, 2, KT_, false); \
-    else if (row_tiles == 2) PDEC_PAGED(DH_, 2, 1, KT_, false);  \
-    else if (row_tiles == 4 && sizeof(KT_) == 1) PDEC_PAGED(DH_, 2, 2, uint8_t, false); \
-    else if (row_tiles == 4) PDEC_PAGED(DH_, 1, 4, uint16_t, false); \
-    else PDEC_PAGED(DH_, 2, 4, KT_, false);                      \
+    else if (f.waves == 4 && f.tiles == 1) PDEC_PAGED(DH_, 1, 4, uint16_t, false); \
+    else if (f.waves == 4) PDEC_PAGED(DH_, 2, 4, KT_, false);    \
+    else if (f.waves == 2 && f.tiles == 2) PDEC_PAGED(DH_, 2, 2, uint8_t, false); \
+    else if (f.waves == 2) PDEC_PAGED(DH_, 1, 2, KT_, false);    \
+    else if (f.tiles == 2) PDEC_PAGED(DH_, 2, 1, KT_, false);    \
+    else PDEC_PAGED(DH_, 1, 1, KT_, false);                      \
   } while (0)
   if (head_dim == 128) {
     if (kv_fp8) PDEC_PAGED_RT(128, uint8_t);

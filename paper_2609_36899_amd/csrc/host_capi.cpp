@@ -1,4 +1,5 @@
-// Host-only C entry points over the page pool and the attention planner.
+// Host-only C entry points over the page pool, the attention planner and the rules by which
+// the operators over caller-owned pages take their forms.
 //
 // Built with g++ into libpdec_host.so so that the bookkeeping half of the
 // library (admission, reservation, growth, departure, stale ids, work-list
@@ -10,6 +11,7 @@
 
 #include "fp8_e4m3.h"
 #include "pacing.h"
+#include "paged_plan.h"
 #include "pagepool.h"
 
 using namespace pdec;
@@ -159,6 +161,26 @@ int pp_validate_deltas(const int32_t* deltas, int32_t n, int32_t max_seqs, int32
   std::vector<BtDelta> d(n);
   for (int i = 0; i < n; ++i) d[i] = {deltas[3 * i], deltas[3 * i + 1], deltas[3 * i + 2], 0};
   return ret(validate_deltas(d, max_seqs, bt_stride, n_pages));
+}
+
+// The form that an attention of query tokens takes: (row tiles a wave, waves along the rows,
+// a work group for each unit).
+void pp_paged_attn_form(int32_t kv_fp8, int32_t batch, int32_t n_q, int32_t n_q_heads,
+                        int32_t n_kv_heads, int32_t head_dim, int32_t bt_stride, int32_t* out3) {
+  const PagedAttnPlan p = plan_paged_attention(batch, n_q, n_q_heads, n_kv_heads, bt_stride);
+  const PagedAttnForm f =
+      paged_attention_form(kv_fp8, head_dim, p.row_tiles, p.n_units, bt_stride * 16, n_kv_heads);
+  out3[0] = f.tiles;
+  out3[1] = f.waves;
+  out3[2] = p.unit_groups;
+}
+
+// Tokens of a chunk and of a cut of draft verification.
+void pp_verify_form(int32_t batch, int32_t n_drafts, int32_t drafter, int32_t vocab,
+                    int32_t* out2) {
+  const VerifySizes s = verify_sizes(batch, n_drafts, drafter != 0, vocab);
+  out2[0] = s.chunk;
+  out2[1] = s.cut;
 }
 
 // E4M3 codes of n floats, as the fp8 KV page writes compute them.

@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include "meta.h"
+#include "paged_plan.h"
 
 namespace pdec {
 
@@ -192,15 +193,6 @@ int64_t append_threads(const AppendArgs& a);
 hipError_t launch_kv_append(int src_dtype, int kv_dtype, int head_dim, const AppendArgs& a,
                             hipStream_t stream);
 
-struct PagedAttnPlan {
-  int32_t row_tiles, tok_per_block, blocks_per_seq, n_groups;
-  int64_t n_units;
-  bool unit_groups;  // a work group for each unit and no merge, instead of equal stretches
-  int32_t units_for_groups;  // the fewest units at which tables of max_pages give that
-};
-// max_pages: what no sequence can read more of.
-PagedAttnPlan plan_paged_attention(int batch, int n_q, int n_q_heads, int n_kv_heads,
-                                   int max_pages);
 struct PagedAttnArgs {  // attention_paged.hip
   const void *q, *k_pages, *v_pages;
   const float *k_scales, *v_scales;

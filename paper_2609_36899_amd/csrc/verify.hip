@@ -51,28 +51,7 @@ constexpr double kUnit = 0x1p50;
 constexpr int kMaxDrafts = 1024;
 constexpr int kParts = kWaves;  // of a cut, each summed by a wave: the pick walks one
 
-// Logits of a call, and tokens of its deciding rows, from which rows are cut coarser.
-constexpr int64_t kFineLogits = 1 << 23, kFineCuts = 3 << 20;
-
-struct Sizes {
-  int chunk, n_chunks;  // tokens of a chunk (a multiple of 1024), chunks of a row
-  int cut, n_cuts;      // the same of a deciding row
-  int rows;             // target rows, then drafter rows
-};
-inline Sizes sizes_of(int batch, int n_drafts, bool drafter, int vocab) {
-  Sizes s;
-  s.rows = batch * (n_drafts + 1 + (drafter ? n_drafts : 0));
-  // 32 values a thread; few rows are cut finer, so that they meet more work groups.
-  s.chunk = (int64_t)s.rows * vocab >= kFineLogits ? 8192 : 2048;
-  s.n_chunks = (vocab + s.chunk - 1) / s.chunk;
-  // Two passes over one or two rows a sequence, long arithmetic each: cut finer where few
-  // cuts of 8192 would leave compute units with one or two groups.  us at cuts of 8192 / 2048,
-  // drafter's logits beside the target's: 8 x 128256 33 / 29, 18 x 128256 36 / 33, 50 x 32003
-  // 32 / 30, 34 x 128256 70 / 73, 64 x 128256 106 / 123.
-  s.cut = (int64_t)batch * vocab >= kFineCuts ? 8192 : 2048;
-  s.n_cuts = (vocab + s.cut - 1) / s.cut;
-  return s;
-}
+typedef VerifySizes Sizes;
 
 // What the drafts of one sequence came to.
 struct Verdict {
@@ -515,7 +494,7 @@ __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyArgs a, Siz
 // What these sizes and all smaller batches and drafts take.  Smaller ones are cut finer: the
 // most pieces of 2048 tokens are those of the last rows, and sequences, below the borders.
 int64_t verify_workspace_bytes(int batch, int n_drafts, bool drafter, int vocab) {
-  const Sizes s = sizes_of(batch, n_drafts, drafter, vocab);
+  const Sizes s = verify_sizes(batch, n_drafts, drafter, vocab);
   const int64_t fine = (vocab + 2047) / 2048;
   const int64_t chunks = std::max((int64_t)s.rows * s.n_chunks,
                                   std::min<int64_t>(s.rows, (kFineLogits - 1) / vocab) * fine);
@@ -526,7 +505,7 @@ int64_t verify_workspace_bytes(int batch, int n_drafts, bool drafter, int vocab)
 
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t stream) {
   static_assert(8 * kThreads >= 8192 / kParts, "one step of the pick covers a part");
-  const Sizes s = sizes_of(a.batch, a.n_drafts, a.drafter != nullptr, a.vocab);
+  const Sizes s = verify_sizes(a.batch, a.n_drafts, a.drafter != nullptr, a.vocab);
   const float c2 = std::min(1.4426950408889634f / a.temperature, 3e38f);
   // Temperatures at which fp32 arguments mean nothing: every test is a close one.
   const double slack = a.temperature < 1e-30f ? INFINITY : 0x1p-13;

@@ -8,6 +8,9 @@ Tolerance of an output element, with A the same mix of |v| in the place of v:
   2^-24 (N + 64) A   sums of N keys in fp32.
 """
 
+import ctypes
+import os
+
 import numpy as np
 import pytest
 import torch
@@ -399,3 +402,66 @@ def test_a_scale_of_zero_reads_as_zeros(n_q, which):
         if which != "k":
             assert np.abs(got[[1, 4]]).max() < 2.0 ** -91
         c.ks, c.vs = scales
+
+
+def _form(c, stride=None):
+    """(row tiles a wave, waves along the rows, a work group a unit) of a case's call."""
+    lib = ctypes.CDLL(os.path.join(os.path.dirname(_P().__file__), "libpdec_host.so"))
+    B, n_q, hq, dh = c.q.shape
+    out = (ctypes.c_int32 * 3)()
+    lib.pp_paged_attn_form(int(c.fp8), B, n_q, hq, c.k.shape[1], dh, stride or c.table.shape[1],
+                           out)
+    return tuple(out)
+
+
+def _widen(c, stride):
+    """A table of more pages than any length reaches, with ids of any kind there."""
+    rng = np.random.default_rng(30)
+    B, have = c.table.shape
+    more = rng.integers(-3, c.P + 3, (B, max(stride - have, 0))).astype(np.int32)
+    c.table = np.ascontiguousarray(np.concatenate([c.table, more], 1))
+
+
+def _take_form(c, tiles, waves):
+    """Widen the table until a work group's share is one that this form serves."""
+    stride = c.table.shape[1]
+    while _form(c, stride)[:2] != (tiles, waves):
+        stride += stride // 4 + 1
+        assert stride < 1 << 20
+    _widen(c, stride)
+    assert _form(c)[:2] == (tiles, waves)
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+@pytest.mark.parametrize("tiles,waves", [(1, 2), (2, 1)])
+@pytest.mark.parametrize("hq,hkv,dh,n_q", [(8, 2, 128, 5), (8, 2, 64, 8), (3, 1, 64, 8),
+                                            (16, 1, 128, 2), (5, 5, 64, 19), (40, 8, 128, 4)])
+def test_both_forms_of_17_to_32_rows(hq, hkv, dh, n_q, tiles, waves, fp8):
+    """Lengths below n_q and around a pair of pages, ids outside the pool, and then keys and
+    values of the last token that hold NaN and infinities."""
+    lens = [0, 1, n_q - 1, n_q, n_q + 1, 31, 32, 33, 63, 64, 65, 97, 300, 1000]
+    c = Case(lens, hq, hkv, dh, n_q=n_q, fp8=fp8, seed=22)
+    _take_form(c, tiles, waves)
+    c.table[6, 1], c.table[10, 0], c.table[12, 7], c.table[13, 60] = -1, c.P, -5, 2 ** 31 - 1
+    c.check()
+    for b, n in enumerate(lens):
+        if n >= n_q and b not in (6, 10):
+            page, slot = c.table[b, (n - 1) // 16], (n - 1) % 16
+            c.k[page, :, slot] = 0x7F if fp8 else np.nan
+            c.v[page, :, :, slot] = 0x7F if fp8 else np.inf
+    rows = [b for b, n in enumerate(lens) if n >= n_q and b not in (6, 10)]
+    got = c.run()
+    assert np.isnan(got[rows, -1]).all()
+    k, v = c.values()
+    ref, size = oo.token_attention(c.q.float().numpy()[:, :-1], k, v, c.table, c.lens - 1)
+    c.q = c.q[:, :-1]
+    assert (np.abs(got[:, :-1] - ref) <= c.bound(ref, size, k))[rows].all()
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+def test_two_row_tiles_a_wave_with_a_work_group_a_unit(fp8):
+    rng = np.random.default_rng(23)
+    c = Case(rng.integers(0, 200, 64), 32, 8, 128, n_q=5, fp8=fp8, seed=23)
+    _widen(c, 132)
+    assert _form(c) == (2, 1, 1)
+    c.check()
