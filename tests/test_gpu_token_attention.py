@@ -465,3 +465,84 @@ def test_two_row_tiles_a_wave_with_a_work_group_a_unit(fp8):
     _widen(c, 132)
     assert _form(c) == (2, 1, 1)
     c.check()
+
+
+def _indicator(c, mod):
+    """q = 0 and V 1 in dim (pair of pages) % mod: every key weighs the same, so an output is
+    the share of a dim's pairs among the keys that a token sees."""
+    c.q = torch.zeros_like(c.q)
+    c.v[:] = 0
+    if c.fp8:
+        c.vs[:] = 1.0
+    for b, n in enumerate(c.lens):
+        for p in range(-(-int(n) // 16)):
+            c.v[c.table[b, p], :, p // 2 % mod] = 0x38 if c.fp8 else 1.0
+
+
+def _shares(lens, n_q, dh, mod):
+    """[B][n_q][dh] of what _indicator's call gives."""
+    out = np.zeros((len(lens), n_q, dh))
+    for b, n in enumerate(lens):
+        for j in range(n_q):
+            m = int(n) - n_q + j + 1
+            if m > 0:
+                out[b, j, :mod] = np.bincount(np.arange(m) // 32 % mod, minlength=mod) / m
+    return out
+
+
+def _check_shares(got, lens, n_q, dh, mod):
+    """Weights are 1, sums of them whole: the inverse, one product and the bf16 rounding."""
+    want = _shares(lens, n_q, dh, mod)[:, :, None]
+    assert (np.abs(got - want) <= (2.0 ** -8 + 2.0 ** -22) * want).all()
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+@pytest.mark.parametrize("n_q,tiles,waves", [(1, 1, 1), (4, 1, 1), (5, 1, 2), (5, 2, 1),
+                                              (13, 0, 0), (26, 2, 4)])
+@pytest.mark.parametrize("lens", [[12000, 3, 0, 900], [20003], "many"])
+def test_every_pair_counts_once_where_stretches_meet(lens, n_q, tiles, waves, fp8):
+    """A pair of pages that two work groups' stretches lose or share moves an output by
+    dh / pairs of it, 5% and more; the tolerance is 2^-8.  Two ways to spread the pairs over
+    the dims, so that a lost pair and a doubled one do not make up for each other in both."""
+    if lens == "many":
+        lens = np.random.default_rng(24).integers(0, 1500, 40)
+        lens[[3, 4, 17]] = 0, 9000, 0
+        if not fp8 and (tiles, waves) == (1, 2):
+            lens = np.minimum(lens, 1600)  # what this form serves of 40 sequences
+    dh, hq, hkv = 128, 8, 2
+    for mod in (dh, dh - 3):
+        c = Case(lens, hq, hkv, dh, n_q=n_q, fp8=fp8, seed=25)
+        if tiles:
+            _take_form(c, tiles, waves)
+        assert not _form(c)[2]
+        _indicator(c, mod)
+        _check_shares(c.run(), c.lens, n_q, dh, mod)
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+@pytest.mark.parametrize("n_q", [1, 5, 13, 26])
+def test_replayed_graph_follows_lengths_that_move_the_stretches(n_q, fp8):
+    """A table of 200 pairs, so equal stretches: units that end, empty ones and one that takes
+    nearly all, with eager calls of the same on other outputs in between."""
+    steps = [[3000, 900, 1, 64], [0, 0, 0, 0], [0, 6400, 0, 31], [6400, 6400, 6400, 6400],
+             [1, 0, 33, 5000], [n_q, n_q - 1, 2 * n_q, 0], [129, 128, 127, 4000]]
+    c = Case([6400] * 4, 8, 2, 128, n_q=n_q, fp8=fp8, seed=26)
+    assert not _form(c)[2]
+    _indicator(c, 125)
+    d = c.device()
+    out, eager = (torch.empty(d["q"].shape, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    ws = torch.empty(_P().paged_token_attention_workspace_bytes(4, n_q, 8, 2, 128,
+                                                                c.table.shape[1]),
+                     dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        _P().paged_token_attention(out=out, workspace=ws, **d)
+    for lens in steps + steps[::-1]:
+        d["lens"].copy_(torch.tensor(lens, dtype=torch.int32))
+        out.fill_(7.0)
+        graph.replay()
+        _P().paged_token_attention(out=eager, workspace=ws, **d)
+        torch.cuda.synchronize()
+        assert torch.equal(out.view(torch.int16), eager.view(torch.int16)), lens
+        _check_shares(out.float().cpu().numpy(), lens, n_q, 128, 125)
