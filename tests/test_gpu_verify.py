@@ -4,6 +4,9 @@ Both sides take masses as whole numbers from one fp64 exponential; two exponenti
 differ in the last place move a mass of 2^40 by one at most, which decides nothing but at
 a distance of 2^-40 from a border."""
 
+import ctypes
+import os
+
 import numpy as np
 import pytest
 import torch
@@ -166,3 +169,29 @@ def test_replayed_graph():
         assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
         dev[3].copy_(torch.rand_like(dev[3]))
         dev[0].mul_(0.9)
+
+
+def _form(B, T, V, drafter):
+    """(tokens of a chunk, of a cut) of a call."""
+    lib = ctypes.CDLL(os.path.join(os.path.dirname(_P().__file__), "libpdec_host.so"))
+    out = (ctypes.c_int32 * 2)()
+    lib.pp_verify_form(B, T, int(drafter), V, out)
+    return tuple(out)
+
+
+@pytest.mark.parametrize("B,T,V,drafter,form", [
+    (98, 1, 32003, False, (2048, 2048)), (99, 1, 32003, False, (2048, 8192)),
+    (99, 1, 32003, True, (8192, 8192)), (13, 3, 151936, False, (2048, 2048)),
+    (14, 3, 151936, False, (8192, 2048)), (9, 3, 151937, True, (8192, 2048)),
+    (25, 2, 128257, False, (8192, 8192)), (20, 1, 163841, True, (8192, 8192))])
+def test_each_way_of_cutting_rows(B, T, V, drafter, form):
+    """Both sides of both borders, vocabularies that end inside a part of a cut, and next
+    tokens from the first part to the last."""
+    assert _form(B, T, V, drafter) == form
+    case = _case(B, T, V, seed=B, drafter=drafter)
+    case[3][:, T] = np.linspace(0.0, 1.0 - 2.0 ** -24, B, dtype=np.float32)
+    case[3][::3, 0] = 0.0  # the first draft is accepted
+    tokens, n = _check(case, 0.9)
+    assert {0, 1} <= set(n)
+    new = tokens[np.arange(B), n]
+    assert new.min() < 512 and new.max() >= V // 2048 * 2048
