@@ -195,3 +195,90 @@ def test_each_way_of_cutting_rows(B, T, V, drafter, form):
     assert {0, 1} <= set(n)
     new = tokens[np.arange(B), n]
     assert new.min() < 512 and new.max() >= V // 2048 * 2048
+
+
+def _sides(case, b, i, temperature, k):
+    """u24 d_x and 2^24 p_x of draft i with u = k / 2^24."""
+    target, d, drafts, _ = case
+    x = drafts[b, i]
+    mass, unit = oo._mass(target[b, i], temperature)
+    right = 2.0 ** 24 * (float(mass[x]) * unit)
+    if d is None:
+        return k * 2.0 ** 50, right
+    mass, unit = oo._mass(d[b, i], temperature)
+    return k * (float(mass[x]) * unit), right
+
+
+def _make_close(case, b, i, temperature, step):
+    """A draft with target mass below the drafter's, and the uniform whose side lies next to
+    the border: step 0 is the last that accepts, 1 the first that refuses."""
+    target, d, drafts, u = case
+    p, unit = oo._mass(target[b, i], temperature)
+    p = p.astype(np.float64) * unit
+    if d is None:
+        x = int(p.argmax())
+        q = 2.0 ** 50
+    else:
+        q, unit = oo._mass(d[b, i], temperature)
+        q = q.astype(np.float64) * unit
+        ratio = p / np.maximum(q, 1.0)
+        x = int(np.where((ratio < 0.99) & (ratio > 2.0 ** -6), q, 0.0).argmax())
+        q = q[x]
+    drafts[b, i] = x
+    k = int(np.ceil(2.0 ** 24 * p[x] / q)) - 1 + step
+    assert 2 ** 16 < k < 2 ** 24
+    u[b, i] = np.float32(k * 2.0 ** -24)
+    left, right = _sides(case, b, i, temperature, k)
+    assert abs(left - right) < 2.0 ** -15 * right and (left < right) == (step <= 0)
+
+
+@pytest.mark.parametrize("drafter", [True, False])
+@pytest.mark.parametrize("B,T,V", [(24, 4, 300), (12, 4, 20000), (99, 1, 32003)])
+def test_uniforms_next_to_the_border(B, T, V, drafter):
+    """Tests that the rows' approximate sums cannot decide: the exact ones of the two rows
+    do.  The first draft, a middle one or the last on either side of its border, and all of
+    a sequence's drafts just accepted."""
+    case = _case(B, T, V, seed=11, std=2.0, drafter=drafter)
+    if not drafter:
+        # A lookup's token has most of the mass, so that its border is a usual one.
+        np.put_along_axis(case[0][:, :T], case[2][..., None].astype(np.int64),
+                          np.log(np.float32(V)) + 2.0, 2)
+    case[3][:, :T] = 0.0  # accepted
+    want = np.full(B, T)
+    for b in range(B):
+        kind, places = b % 4, (0, T // 2, T - 1)
+        for i in places if kind == 3 else places[kind:kind + 1]:
+            step = b // 4 % 2 if kind < 3 else -1
+            _make_close(case, b, i, 0.8, step)
+            if step == 1:
+                want[b] = i
+    _, n = _check(case, 0.8)
+    # every test before the close one, and after it where that accepts, is accepted
+    np.testing.assert_array_equal(n, want)
+
+
+def test_equal_sides_refuse():
+    """p / d is 1/2 exactly (flat over 4 and over 2 tokens): u = 1/2 is the first refused."""
+    t = np.full((3, 2, 1000), -np.inf, np.float32)
+    d = np.full((3, 1, 1000), -np.inf, np.float32)
+    t[:, :, [5, 77, 400, 999]] = 1.25
+    d[:, :, [5, 400]] = -3.0
+    u = np.float32([[0.5 - 2.0 ** -24, 0.3], [0.5, 0.3], [0.5 + 2.0 ** -24, 0.9]])
+    tokens, n = _check([t, d, np.full((3, 1), 400, np.int32), u])
+    assert list(n) == [1, 0, 0] and list(tokens[1:, 0]) == [77, 999]
+
+
+@pytest.mark.parametrize("drafter", [True, False])
+@pytest.mark.parametrize("temperature", [1e-31, 1e-38, 1e-44])
+def test_temperatures_at_which_every_test_is_a_close_one(temperature, drafter):
+    """All mass on a row's maxima: ties share it."""
+    rng = np.random.default_rng(12)
+    case = _case(16, 3, 700, seed=12, drafter=drafter)
+    case[0][:] = rng.integers(0, 3, case[0].shape) * (rng.random(case[0].shape) < 0.05)
+    if drafter:
+        case[1][:] = np.where(rng.random(case[1].shape) < 0.5, case[0][:, :3], 0.0)
+    top = case[0][:, :3].argmax(-1).astype(np.int32)
+    case[2][:] = np.where(rng.random(top.shape) < 0.8, top, case[2])
+    case[3][::2, :3] *= 0.05
+    _, n = _check(case, temperature)
+    assert len(set(n)) > 1
