@@ -282,3 +282,24 @@ def test_temperatures_at_which_every_test_is_a_close_one(temperature, drafter):
     case[3][::2, :3] *= 0.05
     _, n = _check(case, temperature)
     assert len(set(n)) > 1
+
+
+@pytest.mark.parametrize("drafter", [True, False])
+@pytest.mark.parametrize("T", [255, 256, 257, 600, 1024])
+def test_hundreds_of_drafts(T, drafter):
+    """More drafts than a work group has threads; sequences that refuse early, late and never."""
+    case = _case(4, T, 40, seed=13, noise=0.0, drafter=drafter)
+    case[3][:, :T] = 0.0
+    if not drafter:
+        case[2][:] = case[0][:, :T].argmax(-1)
+    for b, i in ((0, 3), (1, T - 1), (2, T // 2 + 100)):
+        case[0][b, i, case[2][b, i]] = -np.inf  # refused
+    _, n = _check(case)
+    assert list(n) == [3, T - 1, T // 2 + 100, T]
+
+
+def test_the_largest_vocabulary():
+    for drafter in (True, False):
+        case = _case(2, 1, 1 << 22, seed=14, drafter=drafter)
+        case[3][:] = [[0.0, 0.7], [0.99, 1.0]]
+        _check(case)
