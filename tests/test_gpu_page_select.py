@@ -117,3 +117,18 @@ def test_replayed_graph_follows_the_lengths():
         torch.cuda.synchronize()
         assert torch.equal(a, b)
         dl += 83
+
+
+@pytest.mark.parametrize("hq,hkv,dh", [(9, 9, 64), (16, 16, 128), (20, 20, 64), (36, 12, 128),
+                                        (160, 10, 64)])
+def test_more_kv_heads_than_a_work_group_takes(hq, hkv, dh):
+    """A page's KV heads by two or three work groups, the last with heads to spare."""
+    _check(*_case([0, 33, 1700, 16 * 70, 16 * 129 + 1], hq, hkv, dh, seed=8), 12)
+
+
+@pytest.mark.parametrize("hq,hkv", [(8, 2), (11, 11)])
+@pytest.mark.parametrize("B", [511, 512, 513, 1100])
+def test_more_sequences_than_a_work_group_has_threads(B, hq, hkv):
+    lens = np.random.default_rng(9).integers(0, 130, B)
+    lens[[0, 5, B - 1]] = 0, 4000, 1500
+    _check(*_case(lens, hq, hkv, 64, seed=9), 5)
