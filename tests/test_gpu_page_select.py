@@ -132,3 +132,39 @@ def test_more_sequences_than_a_work_group_has_threads(B, hq, hkv):
     lens = np.random.default_rng(9).integers(0, 130, B)
     lens[[0, 5, B - 1]] = 0, 4000, 1500
     _check(*_case(lens, hq, hkv, 64, seed=9), 5)
+
+
+@pytest.mark.parametrize("pages", [300, 4000, 9000])
+@pytest.mark.parametrize("spread", ["outlier", "two values", "tiny", "least", "huge"])
+def test_ranges_that_one_histogram_does_not_part(pages, spread):
+    """A score far above the rest, which then share one bin; many equals; scores at the ends
+    of fp32, subnormal ones among them (q of 2^-70 and means of 2^-60 .. 2^-75)."""
+    q, means, table, lens = _case([16 * pages], 4, 2, 64, seed=10)
+    rng = np.random.default_rng(10)
+    if spread == "outlier":
+        means[table[0, pages // 2]] *= 2.0 ** 60
+        means[table[0, pages // 3]] *= -2.0 ** 60
+    elif spread == "two values":
+        means[:] = torch.where(torch.from_numpy(rng.random((len(means), 1, 1)) < 0.3), means[:1],
+                               means[1:2])
+    elif spread in ("tiny", "least"):
+        q *= 2.0 ** -70
+        means *= 2.0 ** (-60 if spread == "tiny" else -75)
+    else:
+        q *= 2.0 ** 60
+        means *= 2.0 ** 62
+    _check(q, means, table, lens, 40)
+    _check(q, means, table, lens, pages - 3)
+
+
+def test_offsets_past_32_bits():
+    """Means at the end of a pool of more than 2^32 bytes."""
+    hkv, dh, P = 8, 128, 2200000
+    q, means, table, lens = _case([700, 1900], 16, hkv, dh, seed=11)
+    big = torch.zeros((P, hkv, dh), dtype=torch.bfloat16, device="cuda")
+    assert big.numel() > 2 ** 31
+    big[P - len(means):] = means.cuda()
+    out = torch.empty((2, hkv, 20), dtype=torch.int32, device="cuda")
+    _P().paged_select(q.cuda(), big, torch.from_numpy(table + np.int32(P - len(means))).cuda(),
+                      torch.from_numpy(lens).cuda(), out)
+    np.testing.assert_array_equal(out.cpu().numpy(), _run(q, means, table, lens, 20))
