@@ -338,3 +338,33 @@ def test_a_sequence_may_end_behind_the_calls_last_row(kind):
     for name in ("kp", "vp", "ks", "vs", "means", "q_out"):
         x, y = getattr(a, name), getattr(b, name)
         assert x is None or torch.equal(x, y), name
+
+
+@pytest.mark.parametrize("kind,src", [("fp8", "bf16"), ("bf16", "f32")])
+def test_many_uneven_sequences(kind, src):
+    """Where a row's sequence lies far from where equal shares would put it."""
+    rng = np.random.default_rng(17)
+    for big in (0, 299):
+        new = rng.integers(0, 4, 300)
+        new[big] = 1500
+        lens = new + rng.integers(0, 40, 300)
+        Case(lens, new, 2, 1, 64, kind, src, seed=17).check()
+
+
+def test_offsets_past_32_bits():
+    """Pages at the end of a pool of more than 2^32 elements."""
+    P, hkv, dh = 270000, 8, 128
+    a, b = (Case([40, 19], [30, 1], 16, hkv, dh, "fp8", "bf16", seed=18) for _ in range(2))
+    a.call()
+    at = P - b.P
+    small = b.kp, b.vp, b.ks, b.vs, b.means
+    big = [torch.zeros((P,) + t.shape[1:], dtype=t.dtype, device="cuda") for t in small]
+    assert big[0].numel() > 2 ** 32
+    for x, y in zip(big, small):
+        x[at:] = y
+    b.kp, b.vp, b.ks, b.vs, b.means = big
+    b.table = b.table + np.int32(at)
+    b.call()
+    for x, y in zip(big, (a.kp, a.vp, a.ks, a.vs, a.means)):
+        assert torch.equal(x[at:], y)
+        assert not x[:at].any()
