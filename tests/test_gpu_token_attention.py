@@ -546,3 +546,49 @@ def test_replayed_graph_follows_lengths_that_move_the_stretches(n_q, fp8):
         torch.cuda.synchronize()
         assert torch.equal(out.view(torch.int16), eager.view(torch.int16)), lens
         _check_shares(out.float().cpu().numpy(), lens, n_q, 128, 125)
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+@pytest.mark.parametrize("hq,hkv,n_q", [(16, 1, 4096), (8, 2, 1030), (3, 1, 2000)])
+def test_thousands_of_tokens(hq, hkv, n_q, fp8):
+    """Prompts: blocks of 128 rows of a KV head, each with its own end of the keys."""
+    c = Case([n_q, n_q + 900, 100, n_q - 1], hq, hkv, 64, n_q=n_q, fp8=fp8, seed=27)
+    for mod in (64, 61):
+        _indicator(c, mod)
+        _check_shares(c.run(), c.lens, n_q, 64, mod)
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+def test_every_listed_page_counts_once(fp8):
+    """Lists of hundreds of pages, in any order, cut into equal stretches."""
+    lens = [9000, 40, 0, 3001]
+    c = Case(lens, 8, 2, 128, fp8=fp8, seed=28)
+    _indicator(c, 128)
+    rng = np.random.default_rng(28)
+    want = np.zeros((4, 1, 2, 128))
+    c.selected = np.full((4, 2, 300), -1, np.int32)
+    for b, n in enumerate(lens):
+        pages = -(-n // 16)
+        for g in range(2):
+            take = rng.permutation(pages)[:300]
+            c.selected[b, g, :len(take)] = take
+            for p in take:
+                want[b, 0, g, p // 2 % 128] += min(16, n - 16 * p)
+    want /= np.maximum(want.sum(-1, keepdims=True), 1)
+    got = c.run()
+    want = want.repeat(4, axis=2)
+    assert (np.abs(got - want) <= (2.0 ** -8 + 2.0 ** -22) * want).all()
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+@pytest.mark.parametrize("n_q", [1, 5, 13, 26])
+def test_a_broken_query_breaks_its_row_alone(n_q, fp8):
+    c = Case([300, 2500], 8, 2, 128, n_q=n_q, fp8=fp8, seed=29)
+    want = c.run()
+    c.q[0, n_q // 2, 3, 5] = float("nan")
+    c.q[1, n_q - 1, 6, 100] = float("inf")
+    got = c.run()
+    bad = np.zeros(got.shape[:3], bool)
+    bad[0, n_q // 2, 3] = bad[1, n_q - 1, 6] = True
+    assert np.isnan(got[bad]).all()
+    np.testing.assert_array_equal(got[~bad], want[~bad])
