@@ -142,7 +142,7 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 def rope_table(max_pos: int, head_dim: int, base: float = 10000.0, device="cuda",
                stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """The (cos, sin) table [max_pos][head_dim / 2][2] that paged_kv_append rotates by."""
-    if max_pos < 1 or head_dim < 2 or head_dim % 2:
+    if not 1 <= max_pos < 1 << 31 or head_dim < 2 or head_dim % 2:
         _refuse("bad rotary table size")
     if torch.device(device).type != "cuda":
         _refuse("the rotary table is made on a GPU")
@@ -280,6 +280,8 @@ def paged_select(q: torch.Tensor, k_means: torch.Tensor, block_table: torch.Tens
     _check(lens, "lens", _I32, (B,), dev)
     n_sel = _dims(selected, "selected", 3)[2]
     _check(selected, "selected", _I32, (B, hkv, n_sel), dev)
+    if not (0 <= keep_first <= n_sel and 1 <= keep_last <= n_sel):
+        _refuse("keep_first >= 0, keep_last >= 1 and their sum at most n_selected")
     handle = _handle(dev, stream)
     ws, at, size = _workspace(workspace, paged_select_workspace_bytes(B, hkv, stride), dev, stream)
     _run(dev, N.load().paged_select, B, hq, hkv, dh, q.data_ptr(), k_means.data_ptr(), n_pages,

@@ -168,3 +168,13 @@ def test_offsets_past_32_bits():
     _P().paged_select(q.cuda(), big, torch.from_numpy(table + np.int32(P - len(means))).cuda(),
                       torch.from_numpy(lens).cuda(), out)
     np.testing.assert_array_equal(out.cpu().numpy(), _run(q, means, table, lens, 20))
+
+
+@pytest.mark.parametrize("kw", [dict(keep_first=1 << 32), dict(keep_last=(1 << 32) + 1),
+                                dict(keep_first=-(1 << 32)), dict(keep_last=1 - (1 << 32))])
+def test_kept_pages_past_the_arguments_type_are_refused(kw):
+    """They would wrap round to numbers that fit."""
+    from paper_2609_36899_amd import PdecError
+    q, means, table, lens = _case([400], 4, 2, 64, seed=12)
+    with pytest.raises(PdecError, match="keep_first"):
+        _run(q, means, table, lens, 5, first=kw.get("keep_first", 1), last=kw.get("keep_last", 1))

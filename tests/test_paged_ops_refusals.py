@@ -198,3 +198,9 @@ def test_more_work_groups_than_a_launch_takes(call):
 def test_rope_table_is_made_on_a_gpu(device):
     with pytest.raises(PdecError, match="GPU"):
         paged.rope_table(8, 64, device=device)
+
+
+@pytest.mark.parametrize("max_pos", [1 << 31, (1 << 32) + 8])
+def test_rope_table_refuses_more_positions_than_its_type_counts(max_pos):
+    with pytest.raises(PdecError, match="table size"):
+        paged.rope_table(max_pos, 2)
