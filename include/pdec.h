@@ -552,8 +552,9 @@ int rope_table(int32_t max_pos, int32_t head_dim, float base, float* table_dev, 
  *   src_dtype PDEC_F32 or PDEC_BF16; kv_dtype PDEC_F32 (from fp32 rows),
  *   PDEC_BF16, or PDEC_FP8_E4M3 with scales: a page's scale for a KV head is
  *   the smallest power of two (2^-100 .. 2^100) that brings its largest
- *   element to 448.  A page that is part full keeps the larger of its scale
- *   and what the new tokens need; where it grows, earlier codes are rounded
+ *   element to 448.  A page that is part full keeps the larger of its scale,
+ *   raised to the next power of two if a caller's is none (and to 2^-100), and
+ *   what the new tokens need; where it grows, earlier codes are rounded
  *   again (value(code) * old / new, to nearest even).  A page written from
  *   slot 0 starts anew.  Larger elements saturate, NaN too.
  *   k_means (nullable; bf16 and E4M3 pages): device bf16 [n_pages]

@@ -203,6 +203,9 @@ int paged_token_attention(int32_t kv_dtype, int32_t batch, int32_t n_q, int32_t 
   a.blocks_per_seq = p.blocks_per_seq;
   a.n_units = (int32_t)p.n_units;
   a.n_groups = p.n_groups;
+  // A pair for each wave.  us at 1, 2, 4, 8: 2 x 2200 tokens of E4M3 pages 14.5, 14.3, 14.4,
+  // 15.8, five tokens over 2 x 2500 15.7, 15.8, 15.6, 16.2; 1 x 2200, and 4 sequences and more,
+  // within the spread of each other.
   a.min_pairs = 4;
   a.unit_groups = p.unit_groups;
   a.scale_log2 = 1.4426950408889634f / std::sqrt((float)head_dim);

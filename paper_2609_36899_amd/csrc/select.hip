@@ -44,9 +44,11 @@ __device__ __forceinline__ double swapped(double v) {
 // side.  They are taken by the waves of one work group, so that a page's means are read as
 // one run, and as many groups as stay resident have equal stretches of tiles, so that the
 // lengths, the queries and the first pages are waited for once.  64 sequences of 8K to 32K,
-// 168 MB: 38 us; with groups of one KV head 41, with groups of 256 pages each 42; the
-// products take 9 of it (17 cycles a tile and dim quad).  The non-temporal hint costs 8%:
-// an instruction takes half of a line, and the other half's finds it gone.
+// 168 MB: 38 us; with groups of one KV head 41, with groups of 256 pages each 42.  The
+// products (9 us, 17 cycles a tile and dim quad) hide behind the loads: 37 without them.  A
+// quarter of the lengths takes 15 us and four times them 144, so 6 us are the beginning and
+// the rest goes at 4.8 to 5.3 TB/s, with one tile of 4 KB in flight a wave.  The non-temporal
+// hint costs 8%: an instruction takes half of a line, and the other half's finds it gone.
 constexpr int kScoreGroups = 512;
 
 template <int DH, int HG>  // HG groups of four query heads; more than one in LDS
@@ -157,8 +159,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) v
 // equal width over the range of the scores leaves a few pages in the bin that holds the
 // last one taken, which a wave ranks; where it leaves more than a wave's lanes (equal
 // scores, an outlier that widens the range), histograms over the scores' bits narrow it
-// down.  A thread holds eight scores meanwhile and reads again what is past them.  Page order comes from ballots and one scan of the
-// waves' counts.  Eight bits at a time from the top of the float, a scan for each step of
+// down.  A thread holds eight scores meanwhile and reads again what is past them.  Page order
+// comes from ballots and one scan of the waves' counts.  Eight bits at a time from the top of the float, a scan for each step of
 // pages, took 57 us for 8188 pages; bits of the range, two or three rounds, 14; this 10.
 template <int T>
 __global__ __launch_bounds__(T) void take_pages_kernel(SelectArgs a) {

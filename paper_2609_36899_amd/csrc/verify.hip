@@ -86,9 +86,10 @@ __device__ __forceinline__ const float* row_ptr(const VerifyArgs& a, int row) {
 // of the 64 fractions in LDS and the series of exp(r) to the fifth power, |r| <= ln 2 / 128
 // (the sixth is below 2^-54).  64 / ln 2 times x has at most 12 bits before the point, so
 // n times the upper part of ln 2 / 64, 40 bits of it, is exact.  One unit in the last place
-// at most, as the library's, in half of its time: the passes over the deciding rows are
-// bound by this arithmetic (64 sequences of 128256 tokens and two rows, judge and rest: 22
-// and 20 us, with the library's and masses as integers 36 and 37).
+// at most, as the library's, in half of its time: of the passes over the deciding rows (64
+// sequences of 128256 tokens and two rows, judge and rest: 21 and 19 us) this arithmetic is 7
+// and 9 (with a comparison in its place 14 and 10, for 66 MB read again and what 1024 work
+// groups do before their first mass); with the library's and masses as integers 36 and 37.
 constexpr double kLn2 = 0.69314718055994530942;
 constexpr double kStepHi = 0x1.62e42fefa0000p-7;  // ln 2 / 64, 40 bits
 constexpr double kStepLo = 0x1.cf79abc9e3b3ap-46;  // and what is left of it
