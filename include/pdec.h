@@ -665,6 +665,140 @@ int verify_drafts(int32_t batch, int32_t n_drafts, int32_t vocab, const float* t
                   int32_t* accepted_dev_out, void* workspace, int64_t workspace_bytes,
                   void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Operators over caller-owned pages of latents (one layer, no engine): for
+ * models that cache one latent vector a token, from which keys and values of
+ * all heads expand, and a rotary key of 64 elements that the heads share.  The
+ * absorbed form multiplies queries by the keys' expansion beforehand and the
+ * result by the values' behind, so that attention reads the latents alone; the
+ * expanded form, for prompts, takes the keys and values themselves.
+ *
+ * Pages hold 16 tokens, a token's row its latent, then its rotary key:
+ * PDEC_BF16 [n_pages][16][latent_dim + 64] bf16, or PDEC_FP8_E4M3 [n_pages][16]
+ * [latent_dim + 128] bytes, the latent as codes and the key in bf16, with
+ * scales device fp32 [n_pages][16], one a token: the latent reads back as
+ * value(code) * scale.  latent_dim 256 or 512.
+ *
+ * As for the operators above, lengths, starts and tables are read on the device
+ * when the call runs and are not trusted, the calls can be captured, are
+ * asynchronous on stream and touch nothing but their arguments; calls that
+ * share a workspace must not overlap.  Pages, q, out, tables of angles, gain
+ * and workspaces are 16-byte aligned; what a call writes overlaps nothing else
+ * that it is given, unless said.
+ * ------------------------------------------------------------------------- */
+
+/* Append the latents and rotary keys of n_rows new tokens of n_seqs sequences.
+ *   Rows, positions and row_start are as paged_kv_append's.  x: rows of
+ *   latent_dim + 64 elements in src_dtype (PDEC_F32 or PDEC_BF16), x_stride
+ *   elements apart: the latent, which becomes
+ *     c = x * (mean(x^2) + eps)^(-1/2) * gain   (gain fp32 [latent_dim];
+ *   null: c = x), and the key, rotated by the table's angle of the position
+ *   (rope_table of 64): pairs (2i, 2i + 1) if interleaved, else (i, i + 32),
+ *   each left in its place.  Arithmetic in fp32, rounded once.  A token's E4M3
+ *   scale is the smallest power of two (2^-100 .. 2^100) that brings the
+ *   largest element of its c to 448; larger elements saturate, NaN too.
+ *   q (nullable): the rotary parts of the queries, heads of 64 elements in
+ *   src_dtype, q_head_stride elements apart in rows q_stride apart, rotated
+ *   likewise into q_out (bf16, strides of its own; it may be q itself, bf16 at
+ *   the same strides).
+ * Left as they were: other slots, and everything of a row that no sequence
+ * holds or whose position is below 0 or at or past max_pos or the table's end.
+ * A row whose page id is not in [0, n_pages) appends nothing; its q is rotated.
+ * No two rows of a call may go to the same slot.
+ * Errors: PDEC_INVALID_ARG, PDEC_UNSUPPORTED, PDEC_HIP_ERROR. */
+int paged_latent_append(int32_t src_dtype, int32_t kv_dtype, int32_t n_rows, int32_t n_seqs,
+                        int32_t n_heads, int32_t latent_dim, const void* x, int64_t x_stride,
+                        const float* gain, float eps, int32_t interleaved, const void* q,
+                        int64_t q_stride, int64_t q_head_stride, const int32_t* lens_dev,
+                        const int32_t* row_start_dev, const int32_t* block_table_dev,
+                        int32_t bt_stride, int64_t n_pages, const float* rope_dev, int32_t max_pos,
+                        void* q_out, int64_t q_out_stride, int64_t q_out_head_stride, void* pages,
+                        float* scales, void* stream);
+
+/* Attention of the last n_q tokens of each sequence over its latents (the
+ * absorbed form):
+ *   out[b][j][h] = softmax(softmax_scale * q[b][j][h] . (c | k)) c over the
+ *   positions 0 .. lens[b] - n_q + j, c their latents and k their rotary keys.
+ *   q: device bf16 [batch][n_q][n_heads][latent_dim + 64]; out: device bf16
+ *   [batch][n_q][n_heads][latent_dim]; lens: device int32 [batch], counting the
+ *   n_q tokens, taken as in [0, bt_stride * 16]; a token that sees no key gets
+ *   zeros.  Tokens whose page id is outside [0, n_pages) are no keys.
+ *   Scores, softmax and sums are fp32; the weights enter the second product
+ *   rounded to bf16, with the token's scale, once more where that is no power of
+ *   two.
+ *   workspace: device, paged_latent_attention_workspace_bytes(...) bytes for the
+ *   same or larger batch, n_q and max_pages (bt_stride); it may be null where
+ *   these are 0 (no table is long).
+ * Errors: PDEC_INVALID_ARG (n_q outside [1, 4096], n_heads outside [1, 1024],
+ * ...), PDEC_UNSUPPORTED, PDEC_HIP_ERROR. */
+int64_t paged_latent_attention_workspace_bytes(int32_t kv_dtype, int32_t batch, int32_t n_q,
+                                               int32_t n_heads, int32_t latent_dim,
+                                               int32_t max_pages);
+int paged_latent_attention(int32_t kv_dtype, int32_t batch, int32_t n_q, int32_t n_heads,
+                           int32_t latent_dim, const void* q, const void* pages,
+                           const float* scales, int64_t n_pages, const int32_t* block_table_dev,
+                           int32_t bt_stride, const int32_t* lens_dev, float softmax_scale,
+                           void* out, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Cached tokens as rows, for the projection that expands their latents: row r is
+ * the token that paged_latent_append would put there (row_start as there: with
+ * counts equal to lens, all tokens of each sequence).  latents: device bf16
+ * [n_rows][latent_dim] (E4M3: value(code) * scale, rounded where the scale is no
+ * power of two); rope_keys: device bf16 [n_rows][64].  A row that no sequence
+ * holds, whose position is below 0 or past the table's end, or whose page id is
+ * not in [0, n_pages), is left as it was.
+ * Errors: PDEC_INVALID_ARG, PDEC_UNSUPPORTED, PDEC_HIP_ERROR. */
+int paged_latent_rows(int32_t kv_dtype, int32_t n_rows, int32_t n_seqs, int32_t latent_dim,
+                      const void* pages, const float* scales, const int32_t* lens_dev,
+                      const int32_t* row_start_dev, const int32_t* block_table_dev,
+                      int32_t bt_stride, int64_t n_pages, void* latents, void* rope_keys,
+                      void* stream);
+
+/* Attention of prompts over expanded keys and values:
+ *   out[i][h] = softmax(softmax_scale * (q[i][h][:head_dim] . k[j][h]
+ *               + q[i][h][head_dim:] . rope_keys[j])) v[j][h]
+ *   over the keys j of row i's sequence up to its own.  Sequence b has the rows
+ *   q_start[b] .. q_start[b + 1] - 1 of q and the keys k_start[b] ..
+ *   k_start[b + 1] - 1 (device int32 [n_seqs + 1], ascending, within n_rows and
+ *   n_keys); its last keys are its rows' own.  A row that sees no key gets
+ *   zeros; rows that no sequence holds are left as they were.
+ *   q: bf16 heads of head_dim + 64 elements (head_dim 64 or 128), k and v of
+ *   head_dim, *_head_stride elements apart in rows *_stride apart (k and v
+ *   side by side for each head, as one projection leaves them, serve as they
+ *   are); rope_keys: bf16 rows of 64, rope_stride apart; strides multiples of 8;
+ *   out: device bf16 [n_rows][n_heads][head_dim].
+ *   Scores, softmax and sums are fp32; the weights enter the second product
+ *   rounded to bf16.
+ *   workspace: device, latent_prompt_attention_workspace_bytes(...) bytes for
+ *   the same n_heads and head_dim and the same or more rows and sequences; it
+ *   may be null where these are 0.
+ * Errors: PDEC_INVALID_ARG, PDEC_UNSUPPORTED, PDEC_HIP_ERROR. */
+int64_t latent_prompt_attention_workspace_bytes(int32_t n_rows, int32_t n_seqs, int32_t n_heads,
+                                                int32_t head_dim);
+int latent_prompt_attention(int32_t n_rows, int32_t n_keys, int32_t n_seqs, int32_t n_heads,
+                            int32_t head_dim, const void* q, int64_t q_stride,
+                            int64_t q_head_stride, const void* k, int64_t k_stride,
+                            int64_t k_head_stride, const void* rope_keys, int64_t rope_stride,
+                            const void* v, int64_t v_stride, int64_t v_head_stride,
+                            const int32_t* q_start_dev, const int32_t* k_start_dev,
+                            float softmax_scale, void* out, void* workspace,
+                            int64_t workspace_bytes, void* stream);
+
+/* Copy pages of a caller's pools to other places in them: for each pair i, page
+ * dst[i] of every pool becomes what page src[i] holds (device int32 [n_pairs]).
+ * Forks of a sequence share its full pages and take a copy of the last,
+ * part-full one each; a fragmented pool's pages move together.  A pool is
+ * anything of n_pages entries of page_bytes[p] bytes: pages, scales, means
+ * (pools and page_bytes are host arrays of n_pools, read before the call
+ * returns).  A page may be the source of many pairs.  What a page holds that is
+ * the destination of two pairs, or of one and the source of another, is not
+ * said; pairs with an id outside [0, n_pages) copy nothing.
+ * Errors: PDEC_INVALID_ARG (n_pools outside [1, 4096], page_bytes outside [1,
+ * 2^27], ...), PDEC_HIP_ERROR. */
+int paged_copy_pages(int32_t n_pools, void* const* pools, const int64_t* page_bytes,
+                     int64_t n_pages, int32_t n_pairs, const int32_t* src_dev,
+                     const int32_t* dst_dev, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -2,7 +2,7 @@
 
 The compiled library (libpdec.so, see include/pdec.h) holds every kernel;
 this package only builds it (``build``) and marshals torch tensors into its
-calls (``engine``, ``paged``).
+calls (``engine``, ``paged``, ``latent``).
 """
 
 from ._native import PAGE_TOKENS, PdecError, BF16, F32, FP8_E4M3  # noqa: F401
@@ -25,6 +25,13 @@ def __getattr__(name):
                 "verify_drafts_workspace_bytes"):
         from . import paged
         globals()[name] = getattr(paged, name)  # found at once from now on
+        return globals()[name]
+    if name in ("paged_latent_append", "paged_latent_attention",
+                "paged_latent_attention_workspace_bytes", "paged_latent_rows",
+                "latent_prompt_attention", "latent_prompt_attention_workspace_bytes",
+                "paged_copy_pages"):
+        from . import latent
+        globals()[name] = getattr(latent, name)  # found at once from now on
         return globals()[name]
     if name in ("PacedRollout", "pacing_plan"):
         from . import driver

@@ -121,6 +121,22 @@ SIGNATURES = {
     "paged_select": (c_int32, [c_int32] * 4 + [c_void_p, c_void_p, c_int64, c_void_p, c_int32,
                                                c_void_p, c_int32, c_int32, c_int32, c_void_p,
                                                c_void_p, c_int64, c_void_p]),
+    "paged_latent_append": (c_int32, [c_int32] * 6 + [c_void_p, c_int64, c_void_p, c_float, c_int32,
+                                                      c_void_p, c_int64, c_int64]
+                            + [c_void_p] * 3 + [c_int32, c_int64, c_void_p, c_int32, c_void_p,
+                                                c_int64, c_int64] + [c_void_p] * 3),
+    "paged_latent_rows": (c_int32, [c_int32] * 4 + [c_void_p] * 5 + [c_int32, c_int64]
+                          + [c_void_p] * 3),
+    "paged_latent_attention_workspace_bytes": (c_int64, [c_int32] * 6),
+    "paged_latent_attention": (c_int32, [c_int32] * 5 + [c_void_p] * 3
+                               + [c_int64, c_void_p, c_int32, c_void_p, c_float, c_void_p, c_void_p,
+                                  c_int64, c_void_p]),
+    "latent_prompt_attention_workspace_bytes": (c_int64, [c_int32] * 4),
+    "latent_prompt_attention": (c_int32, [c_int32] * 5 + [c_void_p, c_int64, c_int64] * 2
+                                + [c_void_p, c_int64, c_void_p, c_int64, c_int64, c_void_p,
+                                   c_void_p, c_float, c_void_p, c_void_p, c_int64, c_void_p]),
+    "paged_copy_pages": (c_int32, [c_int32, POINTER(c_void_p), POINTER(c_int64), c_int64, c_int32,
+                                   c_void_p, c_void_p, c_void_p]),
     "verify_drafts_workspace_bytes": (c_int64, [c_int32] * 4),
     "verify_drafts": (c_int32, [c_int32] * 3 + [c_void_p] * 4 + [c_float] + [c_void_p] * 3
                       + [c_int64, c_void_p]),

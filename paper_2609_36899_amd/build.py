@@ -28,12 +28,15 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 HIP_SOURCES = ["attention.hip", "attention_prefill.hip", "gemm.hip", "pointwise.hip", "kvcopy.hip",
                "sample.hip", "append.hip", "attention_paged.hip", "select.hip", "verify.hip",
-               "engine.cpp", "paged_ops.cpp", "pagepool.cpp", "pacing.cpp"]
+               "latent.hip", "attention_latent.hip", "attention_prompt.hip",
+               "engine.cpp", "paged_ops.cpp", "latent_ops.cpp", "pagepool.cpp", "pacing.cpp"]
 HIP_FLAGS = [
     "-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
     # Packed fp32 VALU ops are kept out of the device code.
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wno-unused-command-line-argument",
+    # The loads into LDS that set m0 by themselves name it as written.
+    "-Wno-inline-asm",
     f"-I{os.path.join(ROOT, 'include')}",
 ]
 

@@ -20,6 +20,7 @@
 // V is taken eight slots of a dim a thread, so that a whole page half is one store.
 #include "hip_common.h"
 #include "kernels.h"
+#include "rows.h"
 #include "wave.h"
 
 #include <algorithm>
@@ -30,17 +31,6 @@ namespace pdec {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-
-typedef uint16_t u16x4_any __attribute__((ext_vector_type(4), aligned(2)));
-
-// Four consecutive elements at element alignment.
-__device__ __forceinline__ f32x4 read4(const float* p) { return *(const f32x4_any*)p; }
-__device__ __forceinline__ f32x4 read4(const uint16_t* p) {
-  const u16x4_any v = *(const u16x4_any*)p;
-  return f32x4{bf16_to_f32(v.x), bf16_to_f32(v.y), bf16_to_f32(v.z), bf16_to_f32(v.w)};
-}
-__device__ __forceinline__ float read1(const float* p) { return *p; }
-__device__ __forceinline__ float read1(const uint16_t* p) { return bf16_to_f32(*p); }
 
 __device__ __forceinline__ float e4m3_to_f32(uint32_t code) {
   return __builtin_amdgcn_cvt_f32_fp8((int)code, 0);
@@ -98,12 +88,6 @@ __device__ __forceinline__ f32x4 back4(const Vec4<T>& v) {
                Elem<T>::back(v.e[3])};
 }
 
-// The smallest power of two s, 2^-100 to 2^100, with amax <= 448 s (448 = 1.75 * 2^8).
-__device__ __forceinline__ float scale_for(float amax) {
-  const uint32_t b = __float_as_uint(amax);
-  const int e = (int)(b >> 23) - 127 - 8 + ((b & 0x7FFFFFu) > 0x600000u);
-  return __uint_as_float((uint32_t)(min(max(amax > 0.f ? e : -100, -100), 100) + 127) << 23);
-}
 // The power of two that a part-full page's scale is kept at: the scale itself where
 // this file made it, the next larger power of two where a caller did.
 __device__ __forceinline__ float kept_scale(float s) {
@@ -111,11 +95,6 @@ __device__ __forceinline__ float kept_scale(float s) {
   const int e = (int)(b >> 23) - 127 + ((b & 0x7FFFFFu) != 0);
   return __uint_as_float((uint32_t)(min(max(s > 0.f ? e : -100, -100), 100) + 127) << 23);
 }
-// One over a power of two of that range.
-__device__ __forceinline__ float inverse_pow2(float s) {
-  return __uint_as_float((254u << 23) - __float_as_uint(s));
-}
-
 // Over the work group; `turn` counts its calls, which take two places in red in turn.
 __device__ __forceinline__ float group_max(float v, float (*red)[kWaves], int turn) {
   float* at = red[turn & 1];
@@ -126,21 +105,6 @@ __device__ __forceinline__ float group_max(float v, float (*red)[kWaves], int tu
 #pragma unroll
   for (int w = 1; w < kWaves; ++w) t = fmaxf(t, at[w]);
   return t;
-}
-
-// The sequence that holds row r, or -1, by every wave for itself: 64 sequences at a time,
-// from where r lies if all have as many rows.
-__device__ __forceinline__ int find_seq(const AppendArgs& a, int r) {
-  const int lane = threadIdx.x & 63, chunks = (a.n_seqs + 63) / 64;
-  int c = (int)((int64_t)r * a.n_seqs / a.n_rows) / 64;
-  for (int i = 0; i < chunks; ++i) {
-    const int b = c * 64 + lane;
-    const bool in = b < a.n_seqs && a.row_start[b] <= r && r < a.row_start[b + 1];
-    const uint64_t hit = __ballot(in);
-    if (hit) return c * 64 + __builtin_ctzll(hit);
-    c = c + 1 < chunks ? c + 1 : 0;
-  }
-  return -1;
 }
 
 __device__ __forceinline__ void rotate4(f32x4& x, f32x4& y, const float2* cs) {
@@ -284,7 +248,7 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs a, int q
   const int limit = (int)min((int64_t)a.max_pos, (int64_t)a.bt_stride * kPage);
   if ((int)blockIdx.x < q_groups) {
     constexpr int H = DH / 2, QR = DH / 8;
-    const int r = blockIdx.x, b = find_seq(a, r);
+    const int r = blockIdx.x, b = find_seq(a.row_start, a.n_seqs, a.n_rows, r);
     if (b < 0) return;
     const int64_t pos = (int64_t)a.lens[b] - ((int64_t)a.row_start[b + 1] - r);
     if (pos < 0 || pos >= limit) return;
@@ -306,7 +270,7 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs a, int q
   int64_t end_pos = 0;  // position behind row seq_end - 1; whatever the lengths hold fits
   while (r < r_end) {
     if (b < 0 || r >= seq_end) {
-      b = find_seq(a, r);
+      b = find_seq(a.row_start, a.n_seqs, a.n_rows, r);
       if (b < 0) {
         ++r;
         continue;

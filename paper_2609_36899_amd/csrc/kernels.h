@@ -207,6 +207,78 @@ struct PagedAttnArgs {  // attention_paged.hip
 hipError_t launch_paged_attention(int kv_fp8, int head_dim, int row_tiles, const PagedAttnArgs& a,
                                   hipStream_t stream);
 
+// ---- operators over latent pages ----------------------------------------------
+constexpr int kLatentRope = 64;
+// Keys that the attention brings into LDS at once, by a key's bytes.
+constexpr int latent_tile(bool fp8, int latent) {
+  return (fp8 ? latent + 2 * kLatentRope : 2 * (latent + kLatentRope)) > 640 ? 32 : 64;
+}
+struct LatentAttnArgs {  // attention_latent.hip
+  const void *q, *pages;
+  const float* scales;  // E4M3 pages
+  const int32_t *block_table, *lens;
+  int32_t bt_stride, max_len, n_q, n_heads;
+  int64_t n_pages;
+  int32_t block_rows, blocks_per_seq, n_units, n_groups, min_tiles, unit_groups;
+  float scale_log2;
+  float *part_ml, *part_acc;  // [n_groups + n_units][16 row_tiles][2 | latent]
+  void* out;
+};
+hipError_t launch_latent_attention(int fp8, int latent, int row_tiles, const LatentAttnArgs& a,
+                                   hipStream_t stream);
+
+struct LatentAppendArgs {  // latent.hip
+  const void *x, *q;  // [n_rows][latent + 64], [n_rows][n_heads][64]; q nullable
+  int64_t x_stride, q_stride, q_head, q_out_stride, q_out_head;
+  int32_t n_rows, n_seqs, n_heads, interleaved;
+  const int32_t *lens, *row_start, *block_table;
+  int32_t bt_stride, max_pos;
+  int64_t n_pages;
+  const float2* rope;
+  const float* gain;  // null: no norm
+  float eps;
+  void *q_out, *pages;
+  float* scales;  // E4M3 pages
+};
+int64_t latent_append_threads(const LatentAppendArgs& a);
+hipError_t launch_latent_append(int src_bf16, int fp8, int latent, const LatentAppendArgs& a,
+                                hipStream_t stream);
+
+struct LatentRowsArgs {  // latent.hip
+  const void* pages;
+  const float* scales;  // E4M3 pages
+  const int32_t *lens, *row_start, *block_table;
+  int32_t bt_stride, n_rows, n_seqs;
+  int64_t n_pages;
+  void *latents, *rope_keys;
+};
+int64_t latent_rows_threads(const LatentRowsArgs& a);
+hipError_t launch_latent_rows(int fp8, int latent, const LatentRowsArgs& a, hipStream_t stream);
+
+struct LatentPromptArgs {  // attention_prompt.hip
+  const uint16_t *q, *k, *rope_keys, *v;
+  int64_t q_stride, q_head, k_stride, k_head, r_stride, v_stride, v_head;
+  const int32_t *q_start, *k_start;
+  int32_t n_rows, n_keys, n_seqs, n_heads;
+  int32_t block_groups, min_tiles;
+  float scale_log2;
+  float *part_ml, *part_acc;  // [n_groups][2][n_heads][32 waves][2 | dim]
+  uint16_t* out;
+};
+hipError_t launch_latent_prompt(int dim, int waves, int n_groups, const LatentPromptArgs& a,
+                                hipStream_t stream);
+
+constexpr int kCopyPools = 16;  // pools of a launch
+struct PageCopyArgs {  // kvcopy.hip
+  void* pool[kCopyPools];
+  int64_t bytes[kCopyPools];  // of a page
+  int32_t n_pools, n_pairs;
+  int64_t n_pages;
+  const int32_t *src, *dst;
+};
+int64_t page_copy_parts(const PageCopyArgs& a);  // work groups a pair
+hipError_t launch_page_copy(const PageCopyArgs& a, hipStream_t stream);
+
 struct SelectArgs {  // select.hip
   const uint16_t *q, *k_means;
   const int32_t *block_table, *lens;

@@ -1,4 +1,5 @@
-// KV snapshot and restore: page gather to, and scatter from, pinned host memory.
+// KV snapshot and restore: page gather to, and scatter from, pinned host memory; and copies of
+// pages within a caller's pools.
 //
 // A trajectory that departs is snapshotted from device memory to host memory
 // over PCIe, freeing its pages while the host copy keeps it available (paper:
@@ -31,7 +32,65 @@ __global__ __launch_bounds__(256) void kv_page_copy_kernel(
   }
 }
 
+// Pages of a caller's pools to other places of the same pools: a work group per pair and part
+// of a page, up to eight loads of a thread in flight.  T is the widest unit that every part of
+// the pool's pages is a whole number of.
+constexpr int kCopyUnits = 8 * 256;  // of a part
+template <typename T>
+__device__ __forceinline__ void copy_part(const char* from, char* to, int64_t n) {
+  T x[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i * 256 + threadIdx.x < n) x[i] = ((const T*)from)[i * 256 + threadIdx.x];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i * 256 + threadIdx.x < n) ((T*)to)[i * 256 + threadIdx.x] = x[i];
+}
+// Pools whose pages are whole 16-byte units are copied by these, others by 4 bytes or by one.
+__host__ __device__ inline int copy_unit(const void* pool, int64_t bytes) {
+  const uint64_t bits = (uint64_t)pool | (uint64_t)bytes;
+  return bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 1;
+}
+__host__ __device__ inline int64_t copy_parts(const void* pool, int64_t bytes) {
+  const int64_t part = (int64_t)copy_unit(pool, bytes) * kCopyUnits;
+  return (bytes + part - 1) / part;
+}
+
+__global__ __launch_bounds__(256) void page_copy_kernel(PageCopyArgs a) {
+  const int64_t src = a.src[blockIdx.x], dst = a.dst[blockIdx.x];
+  if (src < 0 || src >= a.n_pages || dst < 0 || dst >= a.n_pages || src == dst) return;
+  int64_t part = blockIdx.y;
+  int p = 0;
+  for (; p < a.n_pools; ++p) {
+    const int64_t n = copy_parts(a.pool[p], a.bytes[p]);
+    if (part < n) break;
+    part -= n;
+  }
+  if (p == a.n_pools) return;
+  const int64_t bytes = a.bytes[p];
+  const int unit = copy_unit(a.pool[p], bytes);
+  const int64_t at = part * unit * kCopyUnits, n = bytes / unit - part * kCopyUnits;
+  const char* from = (const char*)a.pool[p] + src * bytes + at;
+  char* to = (char*)a.pool[p] + dst * bytes + at;
+  if (unit == 16) copy_part<u32x4>(from, to, n);
+  else if (unit == 4) copy_part<uint32_t>(from, to, n);
+  else copy_part<uint8_t>(from, to, n);
+}
+
 }  // namespace
+
+int64_t page_copy_parts(const PageCopyArgs& a) {
+  int64_t n = 0;
+  for (int p = 0; p < a.n_pools; ++p) n += copy_parts(a.pool[p], a.bytes[p]);
+  return n;
+}
+
+hipError_t launch_page_copy(const PageCopyArgs& a, hipStream_t stream) {
+  if (a.n_pairs == 0 || a.n_pools == 0) return hipSuccess;
+  const dim3 grid(a.n_pairs, (uint32_t)page_copy_parts(a));
+  page_copy_kernel<<<grid, 256, 0, stream>>>(a);
+  return hipGetLastError();
+}
 
 hipError_t launch_kv_page_copy(int n_pages, const int32_t* pages_dev, int n_layers,
                                int64_t n_pool_pages, int64_t block_bytes, void* pool,

@@ -11,17 +11,12 @@
 
 #include "../../include/pdec.h"
 #include "kernels.h"
+#include "paged_checks.h"
 #include "status.h"
 
 using namespace pdec;
 
 namespace {
-
-constexpr int64_t kMaxStride = 1 << 22;  // pages of a table row: 2^26 positions
-constexpr int64_t kMaxBatch = 1 << 20;
-
-int64_t align_up(int64_t v) { return (v + 255) / 256 * 256; }
-bool aligned(const void* p, int bytes) { return (uintptr_t)p % bytes == 0; }
 
 int check_heads(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim) {
   if (n_q_heads < 1 || n_kv_heads < 1 || n_kv_heads > 65535 || n_q_heads % n_kv_heads)
@@ -30,13 +25,6 @@ int check_heads(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim) {
     return fail(PDEC_UNSUPPORTED, "GQA group size must be at most 16");
   if (head_dim != 64 && head_dim != 128)
     return fail(PDEC_UNSUPPORTED, "head_dim must be 64 or 128");
-  return PDEC_OK;
-}
-
-int check_table(int32_t batch, int32_t bt_stride, int64_t n_pages) {
-  if (batch < 1 || batch > kMaxBatch || bt_stride < 1 || bt_stride > kMaxStride || n_pages < 1 ||
-      n_pages > INT32_MAX)
-    return fail(PDEC_INVALID_ARG, "bad batch, bt_stride or n_pages");
   return PDEC_OK;
 }
 

@@ -20,6 +20,8 @@ namespace pdec {
 // slow as 256.
 constexpr int kAttnGroups = 256;
 
+constexpr int64_t kLatentUnits = 512;  // units from which each has a work group of its own
+
 struct PagedAttnPlan {
   int32_t row_tiles, tok_per_block, blocks_per_seq, n_groups;
   int64_t n_units;
@@ -70,6 +72,42 @@ inline PagedAttnForm paged_attention_form(int kv_fp8, int head_dim, int row_tile
   const int64_t group_bytes =
       n_units * max_len * n_kv_heads / kAttnGroups * head_dim * (kv_fp8 ? 2 : 4);
   return group_bytes <= (kv_fp8 ? 1024 : 256) * 1024 ? PagedAttnForm{1, 2} : PagedAttnForm{2, 1};
+}
+
+// ---- attention over latent pages -----------------------------------------------
+struct LatentPlan {
+  int32_t row_tiles, block_rows, blocks_per_seq, n_groups;
+  int64_t n_units;
+  bool unit_groups;  // a work group for each unit and no merge, instead of equal stretches
+};
+// max_len: what no sequence can be longer than; tile: keys of a tile.
+inline LatentPlan plan_latent_attention(int batch, int n_q, int n_heads, int64_t max_len, int tile) {
+  LatentPlan p;
+  // The smallest block that holds a sequence's rows, or blocks of up to 128 of much the same
+  // size, in whole row tiles.
+  const int64_t rows = (int64_t)n_q * n_heads, blocks = (rows + 127) / 128;
+  p.block_rows = (int32_t)((rows + blocks * 16 - 1) / (blocks * 16) * 16);
+  p.row_tiles = p.block_rows <= 16 ? 1 : p.block_rows <= 32 ? 2 : p.block_rows <= 64 ? 4 : 8;
+  p.blocks_per_seq = (int32_t)((rows + p.block_rows - 1) / p.block_rows);
+  p.n_units = (int64_t)batch * p.blocks_per_seq;
+  p.n_groups = kAttnGroups;
+  p.unit_groups = p.n_units >= kLatentUnits || max_len <= 4 * tile;
+  return p;
+}
+
+// ---- attention of prompts -------------------------------------------------------
+struct PromptPlan {
+  int32_t waves, n_groups;  // groups a head
+  bool block_groups;
+};
+inline PromptPlan plan_latent_prompt(int64_t n_rows, int64_t n_seqs, int n_heads) {
+  PromptPlan p;
+  p.waves = 4;
+  const int64_t blocks = n_rows / (32 * p.waves) + n_seqs;  // at most
+  p.block_groups = blocks * n_heads >= 2048 && blocks <= 65535;
+  p.n_groups = p.block_groups ? (int32_t)blocks
+                              : (int32_t)std::max<int64_t>(1, std::min<int64_t>(65535, 512 / n_heads));
+  return p;
 }
 
 // ---- draft verification --------------------------------------------------------
