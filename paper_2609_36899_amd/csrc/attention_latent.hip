@@ -81,16 +81,17 @@ struct Form {
   static constexpr int kTile = latent_tile(FP8, R), kStages = kTile == 32 ? 4 : 3;
   static constexpr int kStage = kTile * kRow;
   static constexpr int kRows = 16 * RT;
-  // Waves along rows and keys in the first product, row and key tiles of 16 for each.
+  // Waves along rows, a tile of 16 each, and along keys in the first product; key tiles of a wave.
   static constexpr int WR = RT;
   static constexpr int WK = kTile / 16 < kWaves / WR ? kTile / 16 : kWaves / WR;
-  static constexpr int RTW = RT / WR, KTW = kTile / 16 / WK;
+  static constexpr int KTW = kTile / 16 / WK;
   // LDS offsets.
   static constexpr int kP = kStages * kStage;             // weights [kRows][kTile] bf16
   static constexpr int kScale = kP + kRows * kTile * 2;   // [kStages][kTile]
   static constexpr int kTop = kScale + (FP8 ? kStages * kTile * 4 : 0);  // [WK][kRows]
   static constexpr int kAlpha = kTop + WK * kRows * 4;    // [kRows]
-  static constexpr int kFlag = kAlpha + kRows * 4;        // [WR], then the bad keys' mask
+  static constexpr int kLim = kAlpha + kRows * 4;         // [kRows]: keys that a row sees
+  static constexpr int kFlag = kLim + kRows * 4;          // [WR], then the bad keys' mask
   static constexpr int kBytes = kFlag + 48;
   static_assert(kBytes <= 160 * 1024 - 64 && kRow % 128 == 0 && kStage % 128 == 0, "LDS layout");
 };
@@ -100,7 +101,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 latent_attn_kernel(LatentAttnArgs a, const int32_t* __restrict__ table) {
   typedef Form<R, RT, FP8> F;
   constexpr int TILE = F::kTile, NST = F::kStages, ROW = F::kRow, WR = F::WR, WK = F::WK;
-  constexpr int RTW = F::RTW, KTW = F::KTW, PPT = TILE / kPage;
+  constexpr int KTW = F::KTW, PPT = TILE / kPage;
   constexpr int KC = (R + kRope) / 32, LC = R / 32;  // k-steps of QK^T; of the latent part
   constexpr int DT = R / 16 / kWaves;                // 16-wide tiles of a wave's part of R
   constexpr int CPR = ROW / 16;                      // chunks of a row
@@ -157,20 +158,14 @@ latent_attn_kernel(LatentAttnArgs a, const int32_t* __restrict__ table) {
       return F::kP + (row >> 1) * 128 + ((((row & 1) << 2) | (c ^ (row >> 1 & 3))) << 4) + (byte & 15);
   };
 
-  // Lane offsets of a wave's loads: eight keys' chunks in LDS order, each from its place in
-  // the page.
-  int voff[NV];
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int n = i * 64 + lane, key = n / CPR, c = n % CPR;
-    voff[i] = key * ROW + ((c ^ key) << 4);
-  }
-  const int key_a = (F::KTW * kw * 16) + key_of(c16);  // this lane's key in the first product
-  const int k_base = key_a * ROW + ((q4 ^ (key_a & 7)) << 4);
-  // In the second one: the lane's key in a block of 32, and its place among the dims.
-  const int v_key = FP8 ? 8 * q4 + (c16 >> 1) : 8 * q4 + 2 * (c16 >> 2);
-  const int v_chunk = FP8 ? wave * DT : wave * DT * 2 + ((c16 & 3) >> 1);
-  const int v_base = v_key * ROW + ((v_chunk ^ (v_key & 7)) << 4) + ((c16 & 1) << 3);
+  // The lane, as a value that the compiler takes for new each time: places worked out from it
+  // and kept over the loop would cost registers that the products need, and loads of spilled
+  // ones would wait for the tiles in flight.
+  auto lane_now = [&] {
+    int l = lane;
+    asm volatile("" : "+v"(l));
+    return l;
+  };
 
   for (; at < end; ++u) {
     const int tiles = unit_tiles<TILE>(a, u);
@@ -214,6 +209,14 @@ latent_attn_kernel(LatentAttnArgs a, const int32_t* __restrict__ table) {
           on ? kPart : 0);
       uint32_t to = lds0 + st * F::kStage + wave * kPart;
       dma_ready(src, to);
+      // Eight keys' chunks in LDS order, each from its place in the page.
+      const int l = lane_now();
+      int voff[NV];
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int n = i * 64 + l, key = n / CPR, c = n % CPR;
+        voff[i] = key * ROW + ((c ^ key) << 4);
+      }
 #pragma unroll
       for (int h = 0; h < KPW / 8; ++h)
 #pragma unroll
@@ -237,35 +240,27 @@ latent_attn_kernel(LatentAttnArgs a, const int32_t* __restrict__ table) {
       next = look(t + 1);
     };
     push(p_begin, 0);
-    bf16x8 qf[RTW][KC];
-    int row_lim[RTW];  // keys that this lane's row sees
-#pragma unroll
-    for (int t = 0; t < RTW; ++t) {
-      // Rows past the block's repeat its last: they are not written.
-      const int row = min((rw * RTW + t) * 16 + c16, rows - 1);
-      row_lim[t] = base_lim + (row0 + row) / a.n_heads;
+    bf16x8 qf[KC];
+    int row_lim;  // keys that this lane's row sees
+    {
+      const int row = min(rw * 16 + c16, rows - 1);  // rows past the block's repeat its last
+      row_lim = base_lim + (row0 + row) / a.n_heads;
+      if (kw == 0 && q4 == 0) *(int*)(lds + F::kLim + (rw * 16 + c16) * 4) = row_lim;
       const uint16_t* src = (const uint16_t*)a.q + (q_row0 + row) * (R + kRope);
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
         const int dim = FP8 && c < LC ? (c >> 1) * 64 + q4 * 16 + (c & 1) * 8 : c * 32 + q4 * 8;
-        qf[t][c] = *(const bf16x8*)(src + dim);
+        qf[c] = *(const bf16x8*)(src + dim);
       }
     }
     // Here the queries are waited for, and the first tile with them; the others' loads follow.
 #pragma unroll
-    for (int t = 0; t < RTW; ++t)
-#pragma unroll
-      for (int c = 0; c < KC; ++c) asm volatile("" : "+v"(qf[t][c]));
+    for (int c = 0; c < KC; ++c) asm volatile("" : "+v"(qf[c]));
 #pragma unroll
     for (int i = 1; i < NST - 1; ++i) push(p_begin + i, i);
 
-    float m[RTW], l[RTW];
+    float m = -INFINITY, l = 0.f;  // a reference for the row's scores; this lane's part of its sum
     f32x4 acc[RT][DT];
-#pragma unroll
-    for (int t = 0; t < RTW; ++t) {
-      m[t] = -INFINITY;
-      l[t] = 0.f;
-    }
 #pragma unroll
     for (int t = 0; t < RT; ++t)
 #pragma unroll
@@ -283,8 +278,8 @@ latent_attn_kernel(LatentAttnArgs a, const int32_t* __restrict__ table) {
       auto there = [&](int key) { return key0 + key < kv_lim && (here >> (key / kPage) & 1); };
       uint64_t bad = 0;  // keys that only some rows see and that are not finite
       if (cut) {
-        uint32_t* mask = (uint32_t*)(lds + F::kFlag + 32);
-        if (threadIdx.x < 2) mask[threadIdx.x] = 0;
+        uint32_t* odd_keys = (uint32_t*)(lds + F::kFlag + 32);
+        if (threadIdx.x < 2) odd_keys[threadIdx.x] = 0;
         __syncthreads();
         // 0 times what a key without data holds may be NaN: it becomes 0.
         constexpr int CL = (FP8 ? R : 2 * R) / 16;  // chunks of a latent
@@ -305,194 +300,231 @@ latent_attn_kernel(LatentAttnArgs a, const int32_t* __restrict__ table) {
                 odd |= (x & 0x7F80) == 0x7F80 || (x >> 16 & 0x7F80) == 0x7F80;
               }
             }
-            if (odd) atomicOr(&mask[key >> 5], 1u << (key & 31));
+            if (odd) atomicOr(&odd_keys[key >> 5], 1u << (key & 31));
           }
         }
         __syncthreads();
-        bad = (uint64_t)mask[1] << 32 | mask[0];
+        bad = (uint64_t)odd_keys[1] << 32 | odd_keys[0];
       }
 
-      f32x4 s[RTW][KTW];
-      f32x4 vs[KTW];
-      if (active) {
-#pragma unroll
-        for (int t = 0; t < RTW; ++t)
-#pragma unroll
-          for (int k = 0; k < KTW; ++k) s[t][k] = f32x4{0.f, 0.f, 0.f, 0.f};
-        const uint8_t* at0 = tile + k_base;
-        const uint8_t* at1 = tile + (k_base ^ 64);
+      const int l1 = lane_now(), row_l = l1 & 15, q_l = l1 >> 4;
+      const int key_a = KTW * kw * 16 + key_of(row_l);  // this lane's key in the first product
+      const int k_base = key_a * ROW + ((q_l ^ (key_a & 7)) << 4);
+      const uint8_t* at0 = tile + k_base;
+      const uint8_t* at1 = tile + (k_base ^ 64);
+      // Scores of key tile k of this wave against its rows: key slot 4 q4 + e of column c16.  Of
+      // E4M3 pages the latent part is scaled, by the tokens' scales vs, before the rotary part.
+      // The reads of a few steps are under way while those before are multiplied, and no more:
+      // they would take the registers that O lies in.
+      auto scores = [&](int k, f32x4 vs) {
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        const uint8_t* k0 = at0 + k * 16 * ROW;
+        const uint8_t* k1 = at1 + k * 16 * ROW;
         if constexpr (FP8) {
+          constexpr int G = 2, N = LC / 2;
+          u32x4 x[2][G];
+          bf16x8 r[2];
+          auto read = [&](int g) {
 #pragma unroll
-          for (int k = 0; k < KTW; ++k) {
+            for (int i = 0; i < G; ++i)
+              x[g & 1][i] = *(const u32x4*)((i & 1 ? k1 : k0) + (g * G + i) / 2 * 128);
+          };
+          read(0);
 #pragma unroll
-            for (int c = 0; c < LC / 2; ++c) {
-              const u32x4 x = *(const u32x4*)((c & 1 ? at1 : at0) + k * 16 * ROW + (c >> 1) * 128);
-              const bf16x8 lo = decode8(u32x2{x.x, x.y}), hi = decode8(u32x2{x.z, x.w});
-#pragma unroll
-              for (int t = 0; t < RTW; ++t) {
-                s[t][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, qf[t][2 * c], s[t][k], 0, 0, 0);
-                s[t][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, qf[t][2 * c + 1], s[t][k], 0, 0, 0);
-              }
+          for (int g = 0; g < N / G; ++g) {
+            if (g + 1 < N / G) {
+              read(g + 1);
+            } else {
+              r[0] = *(const bf16x8*)(k0 + R);
+              r[1] = *(const bf16x8*)(k1 + R);
             }
-            // The tokens' scales, of the latent part alone.
-            vs[k] = *(const f32x4*)(lds + F::kScale + (st * TILE + (kw * KTW + k) * 16 + 4 * q4) * 4);
 #pragma unroll
-            for (int t = 0; t < RTW; ++t) s[t][k] *= vs[k];
-#pragma unroll
-            for (int c = LC; c < KC; ++c) {
-              const bf16x8 x = *(const bf16x8*)((c & 1 ? at1 : at0) + k * 16 * ROW + R);
-#pragma unroll
-              for (int t = 0; t < RTW; ++t)
-                s[t][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, qf[t][c], s[t][k], 0, 0, 0);
+            for (int i = 0; i < G; ++i) {
+              const u32x4 y = x[g & 1][i];
+              o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8(u32x2{y.x, y.y}), qf[2 * (g * G + i)],
+                                                          o, 0, 0, 0);
+              o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8(u32x2{y.z, y.w}),
+                                                          qf[2 * (g * G + i) + 1], o, 0, 0, 0);
             }
+            __builtin_amdgcn_sched_barrier(0);
           }
+          o *= vs;
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+            o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r[c], qf[LC + c], o, 0, 0, 0);
         } else {
+          constexpr int G = KC % 3 == 0 ? 3 : 2;
+          static_assert(KC % G == 0, "whole groups");
+          bf16x8 x[2][G];
+          auto read = [&](int g) {
 #pragma unroll
-          for (int k = 0; k < KTW; ++k)
-#pragma unroll
-            for (int c = 0; c < KC; ++c) {
-              const bf16x8 x = *(const bf16x8*)((c & 1 ? at1 : at0) + k * 16 * ROW + (c >> 1) * 128);
-#pragma unroll
-              for (int t = 0; t < RTW; ++t)
-                s[t][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, qf[t][c], s[t][k], 0, 0, 0);
+            for (int i = 0; i < G; ++i) {
+              const int c = g * G + i;
+              x[g & 1][i] = *(const bf16x8*)((c & 1 ? k1 : k0) + (c >> 1) * 128);
             }
-        }
-      }
-      // Position of the lane's score e of key tile k, within the tile.
-      auto score_key = [&](int k, int e) { return (kw * KTW + k) * 16 + key_of(4 * q4 + e); };
-      auto hidden = [&](int t, int k, int e) {
-        const int key = score_key(k, e);
-        return !there(key) || key0 + key >= row_lim[t];
-      };
-      float top[RTW];
-      if (active) {
+          };
+          read(0);
 #pragma unroll
-        for (int t = 0; t < RTW; ++t) {
-          top[t] = -INFINITY;
+          for (int g = 0; g < KC / G; ++g) {
+            if (g + 1 < KC / G) read(g + 1);
 #pragma unroll
-          for (int k = 0; k < KTW; ++k)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              if (cut && hidden(t, k, e)) s[t][k][e] = -INFINITY;
-              top[t] = fmaxf(top[t], s[t][k][e]);
-            }
-          top[t] = max_over_key_groups(top[t]);
-        }
-      }
-      if constexpr (WK > 1) {  // over the waves that share the rows
-        float* tops = (float*)(lds + F::kTop);
-        if (active && q4 == 0)
-#pragma unroll
-          for (int t = 0; t < RTW; ++t) tops[kw * F::kRows + (rw * RTW + t) * 16 + c16] = top[t];
-        wg_barrier();
-        if (active)
-#pragma unroll
-          for (int t = 0; t < RTW; ++t)
-#pragma unroll
-            for (int k = 0; k < WK; ++k)
-              top[t] = max2(top[t], tops[k * F::kRows + (rw * RTW + t) * 16 + c16]);
-      }
-      if (active) {
-        bool moved = false;
-        float alpha[RTW];
-#pragma unroll
-        for (int t = 0; t < RTW; ++t) {
-          const float now = top[t] * a.scale_log2;
-          const bool need = now > m[t] + kSlack, begun = m[t] > -INFINITY;
-          const float to = need ? now : m[t];
-          alpha[t] = need && begun ? __builtin_amdgcn_exp2f(m[t] - to) : 1.f;
-          l[t] *= alpha[t];
-          m[t] = to;
-          moved |= need && begun;
-        }
-        moved = __any(moved);
-        if (kw == 0) {
-          if (moved && q4 == 0)
-#pragma unroll
-            for (int t = 0; t < RTW; ++t)
-              *(float*)(lds + F::kAlpha + ((rw * RTW + t) * 16 + c16) * 4) = alpha[t];
-          if (lane == 0) *(int*)(lds + F::kFlag + rw * 4) = moved;
-        }
-        // The weights enter the second product in bf16, each off by at most half a step (2^-8);
-        // the normaliser is the fp32 sum of the weights as they were rounded, so that what the
-        // rounding does to a row's large weights cancels.  A token's latent scale goes with its
-        // weight: exact for powers of two, another half step for scales that are none.
-#pragma unroll
-        for (int t = 0; t < RTW; ++t) {
-          const float base = m[t] == -INFINITY ? 0.f : m[t];
-#pragma unroll
-          for (int k = 0; k < KTW; ++k) {
-            u32x2 pw;
-#pragma unroll
-            for (int e = 0; e < 4; e += 2) {
-              f32x2 x = {
-                  __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][k][e], a.scale_log2, -base)),
-                  __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][k][e + 1], a.scale_log2, -base))};
-              uint32_t bits = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
-              x = f32x2{__uint_as_float(bits << 16), __uint_as_float(bits & 0xFFFF0000u)};
-              l[t] += x[0];
-              l[t] += x[1];
-              if constexpr (FP8) {
-                x[0] *= vs[k][e];
-                x[1] *= vs[k][e + 1];
-                if (cut) {  // a scale there may be anything
-                  if (hidden(t, k, e)) x[0] = 0.f;
-                  if (hidden(t, k, e + 1)) x[1] = 0.f;
-                }
-                bits = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
-              }
-              pw[e / 2] = bits;
-            }
-            *(u32x2*)(lds + p_at((rw * RTW + t) * 16 + c16, (kw * KTW + k) * 16 + 4 * q4)) = pw;
+            for (int i = 0; i < G; ++i)
+              o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[g & 1][i], qf[g * G + i], o, 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
           }
         }
+        return o;
+      };
+      auto token_scales = [&](int k) {
+        return FP8 ? *(const f32x4*)(lds + F::kScale + (st * TILE + (kw * KTW + k) * 16 + 4 * q_l) * 4)
+                   : f32x4{1.f, 1.f, 1.f, 1.f};
+      };
+      // Where a row does not see a key the score is -inf, and the scale, which may be anything, 0.
+      auto mask = [&](int k, f32x4& x, f32x4& vs) {
+        if (!cut) return;
+        const int page = kw * KTW + k;
+        int lim = here >> page & 1 ? row_lim - key0 - page * kPage : 0;
+        asm volatile("" : "+v"(lim));  // compared here, not ahead of the branch
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (key_of(4 * q_l + e) >= lim) {
+            x[e] = -INFINITY;
+            vs[e] = 0.f;
+          }
+      };
+      // The weights of key tile k, into LDS; returns their sum.  They enter the second product
+      // in bf16, each off by at most half a step (2^-8); the normaliser is the fp32 sum of the
+      // weights as they were rounded, so that what the rounding does to a row's large weights
+      // cancels.  A token's latent scale goes with its weight: exact for powers of two, another
+      // half step for scales that are none.
+      auto weigh = [&](int k, f32x4 x, f32x4 vs) {
+        const float base = m == -INFINITY ? 0.f : m;
+        u32x2 pw;
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; e += 2) {
+          f32x2 y = {__builtin_amdgcn_exp2f(__builtin_fmaf(x[e], a.scale_log2, -base)),
+                     __builtin_amdgcn_exp2f(__builtin_fmaf(x[e + 1], a.scale_log2, -base))};
+          uint32_t bits = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2));
+          y = f32x2{__uint_as_float(bits << 16), __uint_as_float(bits & 0xFFFF0000u)};
+          sum += y[0] + y[1];
+          if constexpr (FP8) {
+            y[0] *= vs[e];
+            y[1] *= vs[e + 1];
+            bits = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2));
+          }
+          pw[e / 2] = bits;
+        }
+        *(u32x2*)(lds + p_at(rw * 16 + row_l, (kw * KTW + k) * 16 + 4 * q_l)) = pw;
+        return sum;
+      };
+      // The row's reference follows a top that outgrows it; O is rescaled behind the barrier.
+      int moved = 0;
+      auto follow = [&](float top) {
+        const float now = top * a.scale_log2;
+        const bool need = now > m + kSlack, begun = m > -INFINITY;
+        const float alpha = need && begun ? __builtin_amdgcn_exp2f(m - now) : 1.f;
+        if (need) m = now;
+        l *= alpha;
+        moved = __any(need && begun);
+        if (moved && kw == 0 && q_l == 0) *(float*)(lds + F::kAlpha + (rw * 16 + row_l) * 4) = alpha;
+      };
+      if constexpr (WK == 1) {
+        // The weights at the reference as it was; where that was too low (a piece's first tile,
+        // and hardly ever again) all over again.
+        float sum;
+        for (;;) {
+          float top = -INFINITY;
+          sum = 0.f;
+#pragma unroll 1  // unrolled, its places in LDS spill
+          for (int k = 0; k < KTW; ++k) {
+            f32x4 vs = token_scales(k), x = scores(k, vs);
+            mask(k, x, vs);
+            top = fmaxf(fmaxf(fmaxf(top, x[0]), fmaxf(x[1], x[2])), x[3]);
+            sum += weigh(k, x, vs);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          if (!__any(top * a.scale_log2 > m + kSlack)) break;
+          follow(max_over_key_groups(top));
+        }
+        l += sum;
+      } else {
+        f32x4 x[KTW], vs[KTW];
+        float* tops = (float*)(lds + F::kTop);
+        if (active) {
+          float top = -INFINITY;
+#pragma unroll
+          for (int k = 0; k < KTW; ++k) {
+            vs[k] = token_scales(k);
+            x[k] = scores(k, vs[k]);
+            mask(k, x[k], vs[k]);
+            top = fmaxf(fmaxf(fmaxf(top, x[k][0]), fmaxf(x[k][1], x[k][2])), x[k][3]);
+          }
+          top = max_over_key_groups(top);
+          if (q_l == 0) tops[kw * F::kRows + rw * 16 + row_l] = top;
+        }
+        wg_barrier();
+        if (active) {
+          float top = -INFINITY;  // over the waves that share the rows
+#pragma unroll
+          for (int k = 0; k < WK; ++k) top = max2(top, tops[k * F::kRows + rw * 16 + row_l]);
+          follow(top);
+#pragma unroll
+          for (int k = 0; k < KTW; ++k) l += weigh(k, x[k], vs[k]);
+        }
       }
+      if (kw == 0 && l1 == 0) *(int*)(lds + F::kFlag + rw * 4) = moved;
       wg_barrier();
 
-      int moved = 0;
+      int any = 0;
 #pragma unroll
-      for (int i = 0; i < WR; ++i) moved |= *(const int*)(lds + F::kFlag + i * 4);
-      if (__builtin_amdgcn_readfirstlane(moved)) {
+      for (int i = 0; i < WR; ++i) any |= *(const int*)(lds + F::kFlag + i * 4);
+      if (__builtin_amdgcn_readfirstlane(any)) {
+        const int c16 = lane_now() & 15;
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
           // Not written where a wave's own rows did not move.
-          const int mine = *(const int*)(lds + F::kFlag + t / RTW * 4);
+          const int mine = *(const int*)(lds + F::kFlag + t * 4);
           const float f = *(const float*)(lds + F::kAlpha + (t * 16 + c16) * 4);
           const float alpha = mine ? f : 1.f;
 #pragma unroll
           for (int d = 0; d < DT; ++d) acc[t][d] *= alpha;
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
       if (bad) {  // uniform
+        const int l3 = lane_now(), c16 = l3 & 15, q4 = l3 >> 4;
         // Keys that some rows do not see and that are not finite: a weight of 0 would leave
         // NaN of them.  They are added here for the rows that see them, and are 0 behind.
         for (uint64_t rest = bad; rest; rest &= rest - 1) {
-          const int key = __builtin_ctzll(rest);
+          const int key = __builtin_ctzll(rest), slot = slot_of(key);
+          f32x4 v[DT];
 #pragma unroll
           for (int d = 0; d < DT; ++d) {
             const int dim = wave * (R / kWaves) + d * 16 + 4 * q4;
-            f32x4 v;
             if constexpr (FP8) {
               const uint32_t x = *(const uint32_t*)(tile + key * ROW + ((dim >> 4 ^ (key & 7)) << 4) +
                                                     (dim & 15));
               const bf16x8 y = decode8(u32x2{x, 0});
-              v = f32x4{(float)y[0], (float)y[1], (float)y[2], (float)y[3]};
+              v[d] = f32x4{(float)y[0], (float)y[1], (float)y[2], (float)y[3]};
             } else {
               const u32x2 x = *(const u32x2*)(tile + key * ROW + ((dim >> 3 ^ (key & 7)) << 4) +
                                               (dim & 7) * 2);
-              v = f32x4{__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xFFFF0000u),
-                        __uint_as_float(x.y << 16), __uint_as_float(x.y & 0xFFFF0000u)};
+              v[d] = f32x4{__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xFFFF0000u),
+                           __uint_as_float(x.y << 16), __uint_as_float(x.y & 0xFFFF0000u)};
             }
+          }
 #pragma unroll
-            for (int t = 0; t < RT; ++t) {
-              const int row = t * 16 + c16, slot = slot_of(key);
-              const int lim = base_lim + (row0 + row) / a.n_heads;
-              const float p =
-                  bf16_to_f32(*(const uint16_t*)(lds + p_at(row, slot & ~3) + (slot & 3) * 2));
+          for (int t = 0; t < RT; ++t) {
+            const int row = t * 16 + c16;
+            const float w =
+                bf16_to_f32(*(const uint16_t*)(lds + p_at(row, slot & ~3) + (slot & 3) * 2));
+            if (key0 + key < *(const int*)(lds + F::kLim + row * 4))
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-                acc[t][d][e] = key0 + key < lim ? __builtin_fmaf(p, v[e], acc[t][d][e]) : acc[t][d][e];
-            }
+              for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[t][d][e] = __builtin_fmaf(w, v[d][e], acc[t][d][e]);
+            __builtin_amdgcn_sched_barrier(0);
           }
         }
         __syncthreads();
@@ -500,6 +532,11 @@ latent_attn_kernel(LatentAttnArgs a, const int32_t* __restrict__ table) {
           if (bad >> (i / CPR) & 1) *(u32x4*)(lds + st * F::kStage + i * 16) = u32x4{0, 0, 0, 0};
         __syncthreads();
       }
+      // The lane's key in a block of 32 keys, and its place among the wave's dims.
+      const int l2 = lane_now(), row_2 = l2 & 15, q_2 = l2 >> 4;
+      const int v_key = 8 * q_2 + (FP8 ? row_2 >> 1 : 2 * (row_2 >> 2));
+      const int v_chunk = FP8 ? wave * DT : wave * DT * 2 + ((row_2 & 3) >> 1);
+      const int v_base = v_key * ROW + ((v_chunk ^ (v_key & 7)) << 4) + ((row_2 & 1) << 3);
 #pragma unroll
       for (int kb = 0; kb < TILE / 32; ++kb) {
         bf16x8 v[DT];
@@ -520,7 +557,7 @@ latent_attn_kernel(LatentAttnArgs a, const int32_t* __restrict__ table) {
         }
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
-          const bf16x8 pf = *(const bf16x8*)(lds + p_at(t * 16 + c16, kb * 32 + q4 * 8));
+          const bf16x8 pf = *(const bf16x8*)(lds + p_at(t * 16 + row_2, kb * 32 + q_2 * 8));
 #pragma unroll
           for (int d = 0; d < DT; ++d)
             acc[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[d], pf, acc[t][d], 0, 0, 0);
@@ -534,14 +571,11 @@ latent_attn_kernel(LatentAttnArgs a, const int32_t* __restrict__ table) {
     float* sums = (float*)(lds + F::kTop);
     float* tops = (float*)(lds + F::kAlpha);
     if (active) {
-#pragma unroll
-      for (int t = 0; t < RTW; ++t) {
-        const int row = (rw * RTW + t) * 16 + c16;
-        const float sum = sum_over_key_groups(l[t]);
-        if (q4 == 0) {
-          sums[kw * F::kRows + row] = sum;
-          if (kw == 0) tops[row] = m[t];
-        }
+      const int row = rw * 16 + c16;
+      const float sum = sum_over_key_groups(l);
+      if (q4 == 0) {
+        sums[kw * F::kRows + row] = sum;
+        if (kw == 0) tops[row] = m;
       }
     }
     wg_barrier();
