@@ -34,15 +34,16 @@ namespace pdec {
 namespace {
 
 constexpr int kThreads = 512, kWaves = kThreads / 64, kRope = kLatentRope;
-constexpr int kLoaders = 4;  // waves that bring the tiles, one on each SIMD
 // A row's reference maximum moves only where its scores outgrow it by this many powers of
 // two: the weights are then up to 2^16 instead of 1, no less exact, and the accumulators are
 // rescaled a few times a row instead of at most tiles.
 constexpr float kSlack = 16.f;
 
+typedef short s16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef int s32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
 #define PDEC_LDS __attribute__((address_space(3)))
 
 __device__ __forceinline__ int clamp_len(const LatentAttnArgs& a, int b) {
@@ -74,50 +75,72 @@ __device__ __forceinline__ bf16x8 decode8(u32x2 w) {
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
+// a and b as two E4M3 numbers each, times `scale` (a power of two): what is nearest, and what is
+// nearest to the rest.  Into half `which` / 2 of the dwords hi and lo.
+__device__ __forceinline__ void split(float a, float b, float scale, int which, int& hi, int& lo) {
+  s16x2 h = __builtin_bit_cast(s16x2, hi), l = __builtin_bit_cast(s16x2, lo);
+  f32x2 near;
+  if (which) {
+    h = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(h, a, b, scale, true);
+    near = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(__builtin_bit_cast(int, h), scale, true);
+    l = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l, a - near[0], b - near[1], scale, true);
+  } else {
+    h = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(h, a, b, scale, false);
+    near = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(__builtin_bit_cast(int, h), scale, false);
+    l = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l, a - near[0], b - near[1], scale, false);
+  }
+  hi = __builtin_bit_cast(int, h);
+  lo = __builtin_bit_cast(int, l);
+}
+// c + a b over 128 E4M3 codes a row and a column, each lane's part of b times 2^(b_exp - 127).
+__device__ __forceinline__ f32x4 mx_mfma(i32x8 a, i32x8 b, f32x4 c, int b_exp) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, 127, 0, b_exp);
+}
+
 template <int R, int RT, bool FP8>
 struct Form {
   static constexpr int kRow = FP8 ? R + 2 * kRope : (R + kRope) * 2;  // a key's bytes
-  // What LDS holds beside the weights: four stages of 32 wide rows, or three of 64.
-  static constexpr int kTile = latent_tile(FP8, R), kStages = kTile == 32 ? 4 : 3;
+  static constexpr int kTile = latent_tile(FP8, R);
+  // Two tiles are in use, the others on their way.  More stages do not fit beside the weights.
+  static constexpr int kStages = 3;
   static constexpr int kStage = kTile * kRow;
   static constexpr int kRows = 16 * RT;
-  // Waves along rows, a tile of 16 each, and along keys in the first product; key tiles of a wave.
-  static constexpr int WR = RT;
-  static constexpr int WK = kTile / 16 < kWaves / WR ? kTile / 16 : kWaves / WR;
-  static constexpr int KTW = kTile / 16 / WK;
   // LDS offsets.
-  static constexpr int kP = kStages * kStage;             // weights [kRows][kTile] bf16
-  static constexpr int kScale = kP + kRows * kTile * 2;   // [kStages][kTile]
-  static constexpr int kTop = kScale + (FP8 ? kStages * kTile * 4 : 0);  // [WK][kRows]
-  static constexpr int kAlpha = kTop + WK * kRows * 4;    // [kRows]
-  static constexpr int kLim = kAlpha + kRows * 4;         // [kRows]: keys that a row sees
-  static constexpr int kFlag = kLim + kRows * 4;          // [WR], then the bad keys' mask
-  static constexpr int kBytes = kFlag + 48;
+  static constexpr int kWeights = kRows * kTile * 2;          // [kRows][kTile] bf16
+  static constexpr int kP = kStages * kStage;                 // [2]
+  static constexpr int kScale = kP + 2 * kWeights;            // [kStages][kTile]
+  static constexpr int kAlpha = kScale + (FP8 ? kStages * kTile * 4 : 0);  // [2][kRows]
+  static constexpr int kLim = kAlpha + 2 * kRows * 4;         // [kRows]: keys that a row sees
+  static constexpr int kFlag = kLim + kRows * 4;              // [2][8] bytes: rows whose O moves
+  static constexpr int kIds = kFlag + 16;                     // [64]
+  static constexpr int kBytes = kIds + 256;
   static_assert(kBytes <= 160 * 1024 - 64 && kRow % 128 == 0 && kStage % 128 == 0, "LDS layout");
 };
 
 template <int R, int RT, bool FP8>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void
-latent_attn_kernel(LatentAttnArgs a, const int32_t* __restrict__ table) {
+latent_attn_kernel(LatentAttnArgs a) {
   typedef Form<R, RT, FP8> F;
-  constexpr int TILE = F::kTile, NST = F::kStages, ROW = F::kRow, WR = F::WR, WK = F::WK;
-  constexpr int KTW = F::KTW, PPT = TILE / kPage;
-  constexpr int KC = (R + kRope) / 32, LC = R / 32;  // k-steps of QK^T; of the latent part
-  constexpr int DT = R / 16 / kWaves;                // 16-wide tiles of a wave's part of R
-  constexpr int CPR = ROW / 16;                      // chunks of a row
-  constexpr int KPW = TILE / kLoaders;               // keys that a loading wave brings
-  constexpr int NV = 8 * CPR / 64;                   // loads of eight keys
-  constexpr int NL = NV * (KPW / 8) + (FP8 ? 1 : 0);  // a wave's loads of a tile
-  static_assert(8 * CPR % 64 == 0 && KPW % 8 == 0 && (!FP8 || KPW == kPage), "whole loads");
+  constexpr int TILE = F::kTile, NST = F::kStages, ROW = F::kRow, PPT = TILE / kPage;
+  constexpr int NB = TILE / 32;                      // blocks of 32 keys
+  constexpr int DT = R / 16 / kWaves, DW = R / kWaves;  // 16-wide tiles of a wave's part of R
+  constexpr int WIN = ROW / 128, LW = (FP8 ? R : 2 * R) / 128;  // a row's windows; its latent's
+  constexpr int GROUP = 8 * ROW;                     // bytes of eight keys
+  // Loads of a wave: the windows of eight keys, or where a tile is four such groups half of them.
+  constexpr int NW = TILE == 64 ? WIN : (WIN + 1) / 2;
   __shared__ __attribute__((aligned(128))) uint8_t lds[F::kBytes];
   __shared__ int red[kWaves];
   __shared__ int found[2];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int c16 = lane & 15, q4 = lane >> 4;
-  const int rw = wave % WR, kw = wave / WR;
-  const bool active = kw < WK;  // in the first product
-  const int w = blockIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = blockIdx.x;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(PDEC_LDS uint8_t*)lds;
+  // The lane, worked out anew each time: places that follow from it, kept over the loop, would
+  // cost registers that the products need, and loads of spilled ones would wait for the tiles
+  // in flight.
+  auto lane_now = [] {
+    int l;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+    return l;
+  };
 
   int at = 0, end, u = w, first = 0;
   if (a.unit_groups) {
@@ -142,29 +165,21 @@ latent_attn_kernel(LatentAttnArgs a, const int32_t* __restrict__ table) {
     end = __builtin_amdgcn_readfirstlane(end);
   }
 
-  // The order of a tile's keys in the second product.  The transposing read of bf16 gives a
-  // lane four keys, which must differ in their place in the 128 bytes (two chunks of a key
-  // side by side are exchanged by the key's lowest bit): every other key of eight.  So slot
-  // 8 g + i is key 8 g + 2 i for i < 4, 8 g + 2 (i - 4) + 1 behind.  Of E4M3 codes it gives
-  // eight keys, in order.
-  auto key_of = [](int slot) { return FP8 ? slot : (slot & ~7) | ((slot & 3) << 1) | (slot >> 2 & 1); };
-  auto slot_of = [](int key) { return FP8 ? key : (key & ~7) | ((key >> 1) & 3) | ((key & 1) << 2); };
-  // Where row `row`'s weight of slot `slot` lies (a multiple of four): chunks exchanged by the
-  // row, as the keys' are.
-  auto p_at = [](int row, int slot) {
-    const int byte = slot * 2, c = byte >> 4;
-    if constexpr (TILE == 64) return F::kP + row * 128 + ((c ^ (row & 7)) << 4) + (byte & 15);
-    else
-      return F::kP + (row >> 1) * 128 + ((((row & 1) << 2) | (c ^ (row >> 1 & 3))) << 4) + (byte & 15);
+  // Key numbers.  Score e of key tile t (of two) of a block of 32 keys belongs in lane (c, q) to
+  // key_of(q, t, e), and the eight of a lane side by side are what the second product takes:
+  // of bf16 pages t = 0 the four even keys of eight and t = 1 the odd ones, since a transposing
+  // read brings four keys, which must differ in their place by more than one; of E4M3 pages,
+  // where it brings eight, in order.  place(key) is what the chunks of a key's 128 bytes are
+  // exchanged by: eight lanes that read a chunk of eight such keys meet all banks.
+  auto key_of = [](int q, int t, int e) { return FP8 ? 8 * q + 4 * t + e : 8 * q + 2 * e + t; };
+  auto place = [](int key) {
+    return FP8 ? (key & 7) ^ (key >> 1 & 4) : (key & 6) | (key >> 3 & 1);
   };
-
-  // The lane, as a value that the compiler takes for new each time: places worked out from it
-  // and kept over the loop would cost registers that the products need, and loads of spilled
-  // ones would wait for the tiles in flight.
-  auto lane_now = [&] {
-    int l = lane;
-    asm volatile("" : "+v"(l));
-    return l;
+  // The position of a key's weight within its block, and where row `row`'s weights of block
+  // `blk` lie: chunk c of 16 bytes, exchanged by the row.
+  auto p_at = [](int row, int c) {
+    if constexpr (TILE == 64) return row * 128 + ((c ^ (row & 7)) << 4);
+    else return (row >> 1) * 128 + ((((row & 1) << 2) | (c ^ (row >> 1 & 3))) << 4);
   };
 
   for (; at < end; ++u) {
@@ -180,84 +195,111 @@ latent_attn_kernel(LatentAttnArgs a, const int32_t* __restrict__ table) {
     const int n_pages = (kv_lim + kPage - 1) / kPage;
     const int p_begin = at - first, p_end = min(tiles, end - first);
     const int64_t q_row0 = (int64_t)b * a.n_q * a.n_heads + row0;
-    const int32_t* bt = table + (int64_t)b * a.bt_stride;
 
-    // The pages of a tile: the one that this wave brings (-1: none), and which of them there are.
-    struct Spot {
-      int page, ok;
+    // The ids of 64 pages from page0 on, in LDS (each wave puts the same there), and which of
+    // them there are.
+    int page0 = p_begin * PPT;
+    uint64_t there;
+    auto look = [&] {
+      const int l = lane_now(), n = page0 + l;
+      const int id = n < n_pages ? a.block_table[(int64_t)b * a.bt_stride + n] : -1;
+      there = __ballot(id >= 0 && id < a.n_pages);
+      *(int*)(lds + F::kIds + l * 4) = id;
     };
-    auto look = [&](int t) {
-      Spot s = {-1, 0};
-#pragma unroll
-      for (int i = 0; i < PPT; ++i) {
-        const int n = t * PPT + i;
-        int page = t < p_end && n < n_pages ? bt[n] : -1;
-        if (page < 0 || page >= a.n_pages) page = -1;
-        if (page >= 0) s.ok |= 1 << i;
-        if (i == wave * PPT / kLoaders) s.page = page;
+    // Which pages of the tiles in the stages are there, four bits a stage.
+    uint32_t ok = 0;
+    // A wave brings the windows of a group of eight keys, 128 bytes of each key a load: a lane
+    // its chunk.  A page that is not there is a buffer without bytes: its loads bring nothing,
+    // and count.
+    auto push = [&](int t, int st) {
+      int i = t * PPT - page0;
+      if (i >= 64) {
+        page0 += 64;
+        i -= 64;
+        look();
       }
-      return s;
-    };
-    // A page that is not there is a buffer without bytes: its loads bring nothing, and count.
-    auto issue = [&](const Spot& s, int st) {
-      if (wave >= kLoaders) return;
-      const bool on = s.page >= 0;
-      const int64_t page = on ? s.page : 0;
-      constexpr int kPart = KPW * ROW;  // this wave's part of the tile
+      const bool on = t < p_end;
+      ok = (ok & ~(15u << (4 * st))) |
+           (on ? (uint32_t)(there >> i) & ((1 << PPT) - 1) : 0) << (4 * st);
+      const int g = TILE == 64 ? wave : wave >> 1, w0 = TILE == 64 ? 0 : (wave & 1) * NW;
+      const bool on_page = on && there >> (i + (g >> 1)) & 1;
+      const int64_t p =
+          on_page ? __builtin_amdgcn_readfirstlane(*(const int*)(lds + F::kIds + (i + (g >> 1)) * 4)) : 0;
+      const int l = lane_now(), key = (g & 1) * 8 + (l >> 3);
+      const int voff = (l >> 3) * ROW + (((l & 7) ^ place(key)) << 4);
       DmaBuffer src = dma_buffer(
-          (const uint8_t*)a.pages + page * (kPage * ROW) + (KPW < kPage ? (wave & 1) * kPart : 0),
-          on ? kPart : 0);
-      uint32_t to = lds0 + st * F::kStage + wave * kPart;
+          (const uint8_t*)a.pages + p * (kPage * ROW) + (g & 1) * GROUP + w0 * 128,
+          on_page ? GROUP - w0 * 128 : 0);
+      uint32_t to = lds0 + st * F::kStage + g * GROUP + w0 * 1024;
       dma_ready(src, to);
-      // Eight keys' chunks in LDS order, each from its place in the page.
-      const int l = lane_now();
-      int voff[NV];
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int n = i * 64 + l, key = n / CPR, c = n % CPR;
-        voff[i] = key * ROW + ((c ^ key) << 4);
-      }
-#pragma unroll
-      for (int h = 0; h < KPW / 8; ++h)
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-          dma16_unseen(src, voff[i], h * 8 * ROW, to + (h * NV + i) * 1024);
+      for (int i = 0; i < NW; ++i)
+        if (w0 + i < WIN) dma16_unseen(src, voff, i * 128, to + i * 1024);
       if constexpr (FP8) {
-        DmaBuffer sc = dma_buffer(a.scales + page * kPage, on ? kPage * 4 : 0);
-        uint32_t to = lds0 + F::kScale + (st * TILE + wave * kPage) * 4;
-        dma_ready(sc, to);
-        if (lane < kPage) dma4_unseen(sc, lane * 4, to);
+        DmaBuffer sc = dma_buffer(a.scales + p * kPage + (g & 1) * 8, on_page ? 32 : 0);
+        uint32_t at = lds0 + F::kScale + (st * TILE + g * 8) * 4;
+        dma_ready(sc, at);
+        if (l < 8) dma4_unseen(sc, l * 4, at);
       }
     };
 
     wait_vmem<0>();
     __syncthreads();  // the piece before is done with LDS
-    Spot next = look(p_begin);
-    uint32_t ok = 0;  // four bits a stage
-    auto push = [&](int t, int st) {
-      issue(next, st);
-      ok = (ok & ~(15u << (4 * st))) | (uint32_t)next.ok << (4 * st);
-      next = look(t + 1);
-    };
+    look();
     push(p_begin, 0);
-    bf16x8 qf[KC];
+    // This wave's row tile of the first product; a lane's query row c, dims by q.
+    const int rq = wave < RT ? wave : 0;
     int row_lim;  // keys that this lane's row sees
+    bf16x8 qr[2], qf[FP8 ? 1 : 2 * LW];
+    i32x8 qh[FP8 ? LW : 1], ql[FP8 ? LW : 1];
+    int q_exp = 0;
     {
-      const int row = min(rw * 16 + c16, rows - 1);  // rows past the block's repeat its last
+      const int l0 = lane_now(), c16 = l0 & 15, q4 = l0 >> 4;
+      const int row = min(rq * 16 + c16, rows - 1);  // rows past the block's repeat its last
       row_lim = base_lim + (row0 + row) / a.n_heads;
-      if (kw == 0 && q4 == 0) *(int*)(lds + F::kLim + (rw * 16 + c16) * 4) = row_lim;
-      const uint16_t* src = (const uint16_t*)a.q + (q_row0 + row) * (R + kRope);
+      if (wave < RT && q4 == 0) *(int*)(lds + F::kLim + (rq * 16 + c16) * 4) = row_lim;
+      const uint16_t* src = (const uint16_t*)a.q + (q_row0 + row) * (R + kRope) + q4 * 8;
 #pragma unroll
-      for (int c = 0; c < KC; ++c) {
-        const int dim = FP8 && c < LC ? (c >> 1) * 64 + q4 * 16 + (c & 1) * 8 : c * 32 + q4 * 8;
-        qf[c] = *(const bf16x8*)(src + dim);
+      for (int c = 0; c < 2; ++c) qr[c] = *(const bf16x8*)(src + R + c * 32);
+      if constexpr (FP8) {
+        // The query's latent part as the sum of two E4M3 numbers, 2^q_exp times each: four bits
+        // and what they leave of bf16's eight, so exact but below 2^-10 of the row's largest
+        // element, where at most 2^-17 of that is lost.  Two products of twice the rate, and
+        // the codes enter them as they are.  NaN and infinities become NaN.
+        bf16x8 x[4 * LW];
+        float top = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4 * LW; ++i) {
+          x[i] = *(const bf16x8*)(src - q4 * 8 + (i >> 2) * 128 + q4 * 32 + (i & 3) * 8);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)x[i][e]));
+        }
+        top = max_over_key_groups(top);
+        q_exp = min(max((int)(__float_as_uint(top) >> 23), 1), 254) - 127 - 7;
+        const float scale = __uint_as_float((uint32_t)min(max(q_exp + 127, 1), 254) << 23);
+#pragma unroll
+        for (int i = 0; i < 4 * LW; ++i) {
+          int hi[2] = {0, 0}, lo[2] = {0, 0};
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) {
+            const float v0 = (float)x[i][e], v1 = (float)x[i][e + 1];
+            const float s0 = v0 + v0 * 0.f, s1 = v1 + v1 * 0.f;
+            split(s0, s1, scale, e & 2, hi[e >> 2], lo[e >> 2]);
+          }
+          qh[i >> 2][(i & 3) * 2] = hi[0], qh[i >> 2][(i & 3) * 2 + 1] = hi[1];
+          ql[i >> 2][(i & 3) * 2] = lo[0], ql[i >> 2][(i & 3) * 2 + 1] = lo[1];
+        }
+        q_exp = min(max(q_exp + 127, 1), 254);  // as the product takes it
+      } else {
+#pragma unroll
+        for (int c = 0; c < 2 * LW; ++c) qf[c] = *(const bf16x8*)(src + c * 32);
+#pragma unroll
+        for (int c = 0; c < 2 * LW; ++c) asm volatile("" : "+v"(qf[c]));
       }
     }
-    // Here the queries are waited for, and the first tile with them; the others' loads follow.
+    // Here the queries are waited for, and the first tile with them; the next one's loads follow.
 #pragma unroll
-    for (int c = 0; c < KC; ++c) asm volatile("" : "+v"(qf[c]));
-#pragma unroll
-    for (int i = 1; i < NST - 1; ++i) push(p_begin + i, i);
+    for (int c = 0; c < 2; ++c) asm volatile("" : "+v"(qr[c]));
 
     float m = -INFINITY, l = 0.f;  // a reference for the row's scores; this lane's part of its sum
     f32x4 acc[RT][DT];
@@ -266,316 +308,327 @@ latent_attn_kernel(LatentAttnArgs a, const int32_t* __restrict__ table) {
 #pragma unroll
       for (int d = 0; d < DT; ++d) acc[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    int st = 0;
-    for (int p = p_begin; p < p_end; ++p) {
-      wait_vmem<(NST - 2) * NL>();
-      wg_barrier();  // this tile is here, and the one before has been used
-      push(p + NST - 1, st == 0 ? NST - 1 : st - 1);
-      const uint8_t* tile = lds + st * F::kStage;
-      const int key0 = p * TILE, here = ok >> (4 * st) & 15;
-      // Keys that some row does not see, or that are not there.
-      const bool cut = key0 + TILE > min_lim || here != (1 << PPT) - 1;
-      auto there = [&](int key) { return key0 + key < kv_lim && (here >> (key / kPage) & 1); };
-      uint64_t bad = 0;  // keys that only some rows see and that are not finite
-      if (cut) {
-        uint32_t* odd_keys = (uint32_t*)(lds + F::kFlag + 32);
-        if (threadIdx.x < 2) odd_keys[threadIdx.x] = 0;
-        __syncthreads();
-        // 0 times what a key without data holds may be NaN: it becomes 0.
-        constexpr int CL = (FP8 ? R : 2 * R) / 16;  // chunks of a latent
-        for (int i = threadIdx.x; i < TILE * CL; i += kThreads) {
-          const int key = i / CL;
-          u32x4* at = (u32x4*)(lds + st * F::kStage + key * ROW + i % CL * 16);
-          if (!there(key)) {
-            *at = u32x4{0, 0, 0, 0};
-          } else if (key0 + key >= min_lim) {
-            bool odd = false;
+    // Step p: the first product and the weights of tile p, the second product of tile p - 1.
+    // Neither needs the other, so half the waves take one first, half the other, and one
+    // barrier a step serves both.
+    int st = 0, before = NST - 1;  // stages of tiles p and p - 1
+    for (int p = p_begin; p <= p_end; ++p) {
+      wait_vmem<0>();
+      wg_barrier();  // tile p and the weights of p - 1 are here, and tile p - 2 has been used
+      push(p + 1, NST - st - before);
+      const int buf = p & 1;
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half) {
+        if ((half == 0) == (RT < 8 || wave >= kWaves / 2)) {
+          // ---- scores and weights of tile p
+          if (wave >= RT || p == p_end) continue;
+          const int l1 = lane_now(), c16 = l1 & 15, q4 = l1 >> 4;
+          const uint8_t* tile = lds + st * F::kStage;
+          const int key0 = p * TILE;
+          // Keys that some row does not see, or that are not there.
+          const int here = ok >> (4 * st) & 15;
+          const bool cut = key0 + TILE > min_lim || here != (1 << PPT) - 1;
+          uint8_t* p_row = lds + F::kP + buf * F::kWeights;
+          const int row = rq * 16 + c16;
+          int moved = 0;
+          float alpha = 1.f;
+          // The row's reference follows a top that outgrows it by more than the slack.
+          auto follow = [&](float top) {
+            const float now = top * a.scale_log2;
+            const bool need = now > m + kSlack, begun = m > -INFINITY;
+            const float f = need && begun ? __builtin_amdgcn_exp2f(m - now) : 1.f;
+            if (need) m = now;
+            l *= f;
+            alpha *= f;
+            moved |= __any(need && begun);
+          };
+          // Where a row does not see a key its score is -inf, and the token's scale, which may
+          // be anything, 0.
+          auto mask = [&](int blk, int t, f32x4& x, f32x4& vs) {
+            // Of bf16 pages eight keys of one page; of E4M3 pages too (8 q4 ..).
+            int lim = here >> (blk * 2 + (q4 >> 1)) & 1 ? row_lim - key0 - blk * 32 : 0;
+            asm volatile("" : "+v"(lim));  // compared here, not ahead of the branch
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t x = (*at)[e];
-              if constexpr (FP8) {
+            for (int e = 0; e < 4; ++e)
+              if (key_of(q4, t, e) >= lim) {
+                x[e] = -INFINITY;
+                vs[e] = 0.f;
+              }
+          };
+          // Scores of a block, their top, and the tokens' scales.
+          auto scores = [&](int blk, f32x4 (&x)[2], f32x4 (&vs)[2]) {
 #pragma unroll
-                for (int s = 0; s < 32; s += 8) odd |= (x >> s & 0x7F) == 0x7F;
-              } else {
-                odd |= (x & 0x7F80) == 0x7F80 || (x >> 16 & 0x7F80) == 0x7F80;
+            for (int t = 0; t < 2; ++t) x[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            // The lane's key of tile t, as a row of the product: key_of(c16 / 4, t, c16 % 4).
+            const uint8_t* from = tile + (blk * 4 + (c16 >> 2)) * GROUP;
+            if constexpr (FP8) {
+              from += (c16 & 3) * 128;
+              const int sw = place(8 * (c16 >> 2) + (c16 & 3)) << 4;  // of t = 1: place ^ 4
+              i32x8 k[3];
+              auto read = [&](int n) {  // window n / 2 of key tile n % 2
+                const uint8_t* src = from + (n >> 1) * 1024 + (n & 1) * 512;
+                const int at = ((q4 << 5) ^ sw) ^ (n & 1) << 6;
+                const u32x4 y = *(const u32x4*)(src + at), z = *(const u32x4*)(src + (at ^ 16));
+                k[n % 3] = i32x8{(int)y.x, (int)y.y, (int)y.z, (int)y.w,
+                                 (int)z.x, (int)z.y, (int)z.z, (int)z.w};
+              };
+              read(0);
+              read(1);
+              bf16x8 r[2][2];
+#pragma unroll
+              for (int n = 0; n < 2 * LW; ++n) {
+                if (n + 2 < 2 * LW) {
+                  read(n + 2);
+                } else {
+                  const int t = n & 1;
+#pragma unroll
+                  for (int c = 0; c < 2; ++c)
+                    r[t][c] = *(const bf16x8*)(from + LW * 1024 + t * 512 +
+                                               (((q4 << 4) ^ sw ^ t << 6) ^ c << 6));
+                }
+                x[n & 1] = mx_mfma(k[n % 3], qh[n >> 1], x[n & 1], q_exp);
+                x[n & 1] = mx_mfma(k[n % 3], ql[n >> 1], x[n & 1], q_exp);
+                __builtin_amdgcn_sched_barrier(0);
+              }
+#pragma unroll
+              for (int t = 0; t < 2; ++t) {
+                vs[t] = *(const f32x4*)(lds + F::kScale +
+                                             (st * TILE + blk * 32 + 8 * q4 + 4 * t) * 4);
+                x[t] *= vs[t];  // the latent part alone
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                  x[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r[t][c], qr[c], x[t], 0, 0, 0);
+              }
+            } else {
+              constexpr int N = 4 * LW + 4, D = RT == 8 ? 4 : 8;  // reads; of them under way
+              from += (c16 & 3) * 256;
+              const int sw = (q4 ^ place(8 * (c16 >> 2) + 2 * (c16 & 3))) << 4;
+              bf16x8 k[D];
+              auto read = [&](int n) {  // step n / 2 of key tile n % 2
+                const int c = n >> 1;
+                k[n % D] = *(const bf16x8*)(from + (c >> 1) * 1024 + (n & 1) * 128 + (sw ^ (c & 1) << 6));
+              };
+#pragma unroll
+              for (int n = 0; n < D; ++n) read(n);
+#pragma unroll
+              for (int n = 0; n < N; ++n) {
+                const int c = n >> 1;
+                x[n & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                    k[n % D], c < 2 * LW ? qf[c] : qr[c - 2 * LW], x[n & 1], 0, 0, 0);
+                if (n + D < N) read(n + D);
+                if (n & 1) __builtin_amdgcn_sched_barrier(0);
               }
             }
-            if (odd) atomicOr(&odd_keys[key >> 5], 1u << (key & 31));
-          }
-        }
-        __syncthreads();
-        bad = (uint64_t)odd_keys[1] << 32 | odd_keys[0];
-      }
-
-      const int l1 = lane_now(), row_l = l1 & 15, q_l = l1 >> 4;
-      const int key_a = KTW * kw * 16 + key_of(row_l);  // this lane's key in the first product
-      const int k_base = key_a * ROW + ((q_l ^ (key_a & 7)) << 4);
-      const uint8_t* at0 = tile + k_base;
-      const uint8_t* at1 = tile + (k_base ^ 64);
-      // Scores of key tile k of this wave against its rows: key slot 4 q4 + e of column c16.  Of
-      // E4M3 pages the latent part is scaled, by the tokens' scales vs, before the rotary part.
-      // The reads of a few steps are under way while those before are multiplied, and no more:
-      // they would take the registers that O lies in.
-      auto scores = [&](int k, f32x4 vs) {
-        f32x4 o = {0.f, 0.f, 0.f, 0.f};
-        const uint8_t* k0 = at0 + k * 16 * ROW;
-        const uint8_t* k1 = at1 + k * 16 * ROW;
-        if constexpr (FP8) {
-          constexpr int G = 2, N = LC / 2;
-          u32x4 x[2][G];
-          bf16x8 r[2];
-          auto read = [&](int g) {
+            float top = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < G; ++i)
-              x[g & 1][i] = *(const u32x4*)((i & 1 ? k1 : k0) + (g * G + i) / 2 * 128);
+            for (int t = 0; t < 2; ++t) {
+              if (cut) mask(blk, t, x[t], vs[t]);
+              top = max2(max2(top, max2(x[t][0], x[t][1])),
+                         max2(x[t][2], x[t][3]));
+            }
+            return max_over_key_groups(top);
           };
-          read(0);
+          // Their weights, into LDS; returns the lane's part of their sum.  They enter the second
+          // product in bf16, each off by at most half a step (2^-8).  Of bf16 pages the
+          // normaliser sums them as they were rounded, so that what the rounding does to a row's
+          // large weights cancels; E4M3 tokens' scales go with their weights, and the sum is of
+          // the weights before either.
+          auto weigh = [&](int blk, const f32x4 (&x)[2], const f32x4 (&vs)[2]) {
+            const float base = m == -INFINITY ? 0.f : m;
+            uint32_t pw[4];
+            float sum = 0.f;
 #pragma unroll
-          for (int g = 0; g < N / G; ++g) {
-            if (g + 1 < N / G) {
-              read(g + 1);
-            } else {
-              r[0] = *(const bf16x8*)(k0 + R);
-              r[1] = *(const bf16x8*)(k1 + R);
+            for (int e = 0; e < 8; e += 2) {
+              const f32x4 &v = x[e >> 2], &f = vs[e >> 2];
+              f32x2 y = {__builtin_amdgcn_exp2f(__builtin_fmaf(v[e & 3], a.scale_log2, -base)),
+                         __builtin_amdgcn_exp2f(__builtin_fmaf(v[(e & 3) + 1], a.scale_log2, -base))};
+              if constexpr (FP8) {
+                sum += y[0] + y[1];
+                y[0] *= f[e & 3];
+                y[1] *= f[(e & 3) + 1];
+              }
+              pw[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2));
+              if constexpr (!FP8)
+                sum += __uint_as_float(pw[e / 2] << 16) + __uint_as_float(pw[e / 2] & 0xFFFF0000u);
             }
-#pragma unroll
-            for (int i = 0; i < G; ++i) {
-              const u32x4 y = x[g & 1][i];
-              o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8(u32x2{y.x, y.y}), qf[2 * (g * G + i)],
-                                                          o, 0, 0, 0);
-              o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8(u32x2{y.z, y.w}),
-                                                          qf[2 * (g * G + i) + 1], o, 0, 0, 0);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-          }
-          o *= vs;
-#pragma unroll
-          for (int c = 0; c < 2; ++c)
-            o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r[c], qf[LC + c], o, 0, 0, 0);
-        } else {
-          constexpr int G = KC % 3 == 0 ? 3 : 2;
-          static_assert(KC % G == 0, "whole groups");
-          bf16x8 x[2][G];
-          auto read = [&](int g) {
-#pragma unroll
-            for (int i = 0; i < G; ++i) {
-              const int c = g * G + i;
-              x[g & 1][i] = *(const bf16x8*)((c & 1 ? k1 : k0) + (c >> 1) * 128);
-            }
+            *(u32x4*)(p_row + p_at(row, blk * 4 + q4)) = u32x4{pw[0], pw[1], pw[2], pw[3]};
+            return sum;
           };
-          read(0);
-#pragma unroll
-          for (int g = 0; g < KC / G; ++g) {
-            if (g + 1 < KC / G) read(g + 1);
-#pragma unroll
-            for (int i = 0; i < G; ++i)
-              o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[g & 1][i], qf[g * G + i], o, 0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
+          if constexpr (RT < 8 && NB == 2) {
+            f32x4 x[2][2], vs[2][2];
+            const float t0 = scores(0, x[0], vs[0]), t1 = scores(1, x[1], vs[1]);
+            follow(max2(t0, t1));
+            l += weigh(0, x[0], vs[0]);
+            l += weigh(1, x[1], vs[1]);
+          } else {
+            // A block at a time, for its registers; where the second moves the reference, which
+            // is hardly ever, the first again.
+            float sum = 0.f;
+#pragma unroll 1
+            for (int blk = 0; blk < NB; ++blk) {
+              f32x4 x[2], vs[2];
+              const float was = m;
+              follow(scores(blk, x, vs));
+              if (NB > 1 && blk > 0 && __any(m != was)) {
+                sum = 0.f;
+                blk = -1;
+                continue;
+              }
+              sum += weigh(blk, x, vs);
+            }
+            l += sum;
           }
-        }
-        return o;
-      };
-      auto token_scales = [&](int k) {
-        return FP8 ? *(const f32x4*)(lds + F::kScale + (st * TILE + (kw * KTW + k) * 16 + 4 * q_l) * 4)
-                   : f32x4{1.f, 1.f, 1.f, 1.f};
-      };
-      // Where a row does not see a key the score is -inf, and the scale, which may be anything, 0.
-      auto mask = [&](int k, f32x4& x, f32x4& vs) {
-        if (!cut) return;
-        const int page = kw * KTW + k;
-        int lim = here >> page & 1 ? row_lim - key0 - page * kPage : 0;
-        asm volatile("" : "+v"(lim));  // compared here, not ahead of the branch
+          if (moved && q4 == 0) *(float*)(lds + F::kAlpha + (buf * F::kRows + row) * 4) = alpha;
+          if (l1 == 0) lds[F::kFlag + buf * 8 + wave] = (uint8_t)moved;
+        } else if (p > p_begin) {
+          // ---- the second product of tile p - 1
+          uint8_t* tile = lds + before * F::kStage;
+          const uint8_t* p_rows = lds + F::kP + (buf ^ 1) * F::kWeights;
+          const int l2 = lane_now(), c16 = l2 & 15, q4 = l2 >> 4;
+          const int key0 = (p - 1) * TILE, here = ok >> (4 * before) & 15;
+          uint64_t flags = *(const uint64_t*)(lds + F::kFlag + (buf ^ 1) * 8);
+          if constexpr (RT < 8) flags &= (1ull << (8 * RT % 64)) - 1;
+          if (__builtin_amdgcn_readfirstlane((int)(flags | flags >> 32))) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (key_of(4 * q_l + e) >= lim) {
-            x[e] = -INFINITY;
-            vs[e] = 0.f;
-          }
-      };
-      // The weights of key tile k, into LDS; returns their sum.  They enter the second product
-      // in bf16, each off by at most half a step (2^-8); the normaliser is the fp32 sum of the
-      // weights as they were rounded, so that what the rounding does to a row's large weights
-      // cancels.  A token's latent scale goes with its weight: exact for powers of two, another
-      // half step for scales that are none.
-      auto weigh = [&](int k, f32x4 x, f32x4 vs) {
-        const float base = m == -INFINITY ? 0.f : m;
-        u32x2 pw;
-        float sum = 0.f;
+            for (int t = 0; t < RT; ++t) {
+              // Not written where none of the row tile's rows moved.
+              const float f = *(const float*)(lds + F::kAlpha + ((buf ^ 1) * F::kRows + t * 16 + c16) * 4);
+              const float alpha = flags >> (8 * t) & 1 ? f : 1.f;
 #pragma unroll
-        for (int e = 0; e < 4; e += 2) {
-          f32x2 y = {__builtin_amdgcn_exp2f(__builtin_fmaf(x[e], a.scale_log2, -base)),
-                     __builtin_amdgcn_exp2f(__builtin_fmaf(x[e + 1], a.scale_log2, -base))};
-          uint32_t bits = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2));
-          y = f32x2{__uint_as_float(bits << 16), __uint_as_float(bits & 0xFFFF0000u)};
-          sum += y[0] + y[1];
-          if constexpr (FP8) {
-            y[0] *= vs[e];
-            y[1] *= vs[e + 1];
-            bits = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2));
-          }
-          pw[e / 2] = bits;
-        }
-        *(u32x2*)(lds + p_at(rw * 16 + row_l, (kw * KTW + k) * 16 + 4 * q_l)) = pw;
-        return sum;
-      };
-      // The row's reference follows a top that outgrows it; O is rescaled behind the barrier.
-      int moved = 0;
-      auto follow = [&](float top) {
-        const float now = top * a.scale_log2;
-        const bool need = now > m + kSlack, begun = m > -INFINITY;
-        const float alpha = need && begun ? __builtin_amdgcn_exp2f(m - now) : 1.f;
-        if (need) m = now;
-        l *= alpha;
-        moved = __any(need && begun);
-        if (moved && kw == 0 && q_l == 0) *(float*)(lds + F::kAlpha + (rw * 16 + row_l) * 4) = alpha;
-      };
-      if constexpr (WK == 1) {
-        // The weights at the reference as it was; where that was too low (a piece's first tile,
-        // and hardly ever again) all over again.
-        float sum;
-        for (;;) {
-          float top = -INFINITY;
-          sum = 0.f;
-#pragma unroll 1  // unrolled, its places in LDS spill
-          for (int k = 0; k < KTW; ++k) {
-            f32x4 vs = token_scales(k), x = scores(k, vs);
-            mask(k, x, vs);
-            top = fmaxf(fmaxf(fmaxf(top, x[0]), fmaxf(x[1], x[2])), x[3]);
-            sum += weigh(k, x, vs);
-            __builtin_amdgcn_sched_barrier(0);
-          }
-          if (!__any(top * a.scale_log2 > m + kSlack)) break;
-          follow(max_over_key_groups(top));
-        }
-        l += sum;
-      } else {
-        f32x4 x[KTW], vs[KTW];
-        float* tops = (float*)(lds + F::kTop);
-        if (active) {
-          float top = -INFINITY;
-#pragma unroll
-          for (int k = 0; k < KTW; ++k) {
-            vs[k] = token_scales(k);
-            x[k] = scores(k, vs[k]);
-            mask(k, x[k], vs[k]);
-            top = fmaxf(fmaxf(fmaxf(top, x[k][0]), fmaxf(x[k][1], x[k][2])), x[k][3]);
-          }
-          top = max_over_key_groups(top);
-          if (q_l == 0) tops[kw * F::kRows + rw * 16 + row_l] = top;
-        }
-        wg_barrier();
-        if (active) {
-          float top = -INFINITY;  // over the waves that share the rows
-#pragma unroll
-          for (int k = 0; k < WK; ++k) top = max2(top, tops[k * F::kRows + rw * 16 + row_l]);
-          follow(top);
-#pragma unroll
-          for (int k = 0; k < KTW; ++k) l += weigh(k, x[k], vs[k]);
-        }
-      }
-      if (kw == 0 && l1 == 0) *(int*)(lds + F::kFlag + rw * 4) = moved;
-      wg_barrier();
-
-      int any = 0;
-#pragma unroll
-      for (int i = 0; i < WR; ++i) any |= *(const int*)(lds + F::kFlag + i * 4);
-      if (__builtin_amdgcn_readfirstlane(any)) {
-        const int c16 = lane_now() & 15;
-#pragma unroll
-        for (int t = 0; t < RT; ++t) {
-          // Not written where a wave's own rows did not move.
-          const int mine = *(const int*)(lds + F::kFlag + t * 4);
-          const float f = *(const float*)(lds + F::kAlpha + (t * 16 + c16) * 4);
-          const float alpha = mine ? f : 1.f;
-#pragma unroll
-          for (int d = 0; d < DT; ++d) acc[t][d] *= alpha;
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      }
-      if (bad) {  // uniform
-        const int l3 = lane_now(), c16 = l3 & 15, q4 = l3 >> 4;
-        // Keys that some rows do not see and that are not finite: a weight of 0 would leave
-        // NaN of them.  They are added here for the rows that see them, and are 0 behind.
-        for (uint64_t rest = bad; rest; rest &= rest - 1) {
-          const int key = __builtin_ctzll(rest), slot = slot_of(key);
-          f32x4 v[DT];
-#pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            const int dim = wave * (R / kWaves) + d * 16 + 4 * q4;
-            if constexpr (FP8) {
-              const uint32_t x = *(const uint32_t*)(tile + key * ROW + ((dim >> 4 ^ (key & 7)) << 4) +
-                                                    (dim & 15));
-              const bf16x8 y = decode8(u32x2{x, 0});
-              v[d] = f32x4{(float)y[0], (float)y[1], (float)y[2], (float)y[3]};
-            } else {
-              const u32x2 x = *(const u32x2*)(tile + key * ROW + ((dim >> 3 ^ (key & 7)) << 4) +
-                                              (dim & 7) * 2);
-              v[d] = f32x4{__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xFFFF0000u),
-                           __uint_as_float(x.y << 16), __uint_as_float(x.y & 0xFFFF0000u)};
+              for (int d = 0; d < DT; ++d) acc[t][d] *= alpha;
+              __builtin_amdgcn_sched_barrier(0);
             }
           }
+          if (key0 + TILE > min_lim || here != (1 << PPT) - 1) {
+            // 0 times what a key without data holds may be NaN: it becomes 0, each wave's part of
+            // the latent by itself.  So does what only some rows see and is not finite, behind
+            // its own sums for the rows that see it.
+            constexpr int CW = (FP8 ? DW : 2 * DW) / 16;  // chunks of a wave's part of a key
+            auto chunk = [&](int key, int c) {
+              const int byte = wave * (FP8 ? DW : 2 * DW) + c * 16;
+              return tile + (key >> 3) * GROUP + (byte >> 7) * 1024 + (key & 7) * 128 +
+                     (((byte >> 4 & 7) ^ place(key)) << 4);
+            };
+            auto is_there = [&](int key) {
+              return key0 + key < kv_lim && (here >> (key / kPage) & 1);
+            };
+            uint64_t bad = 0;
+#pragma unroll 1
+            for (int i = l2; i < TILE * CW; i += 64) {
+              const int key = i / CW;
+              u32x4* at = (u32x4*)chunk(key, i % CW);
+              bool odd = false;
+              if (!is_there(key)) {
+                *at = u32x4{0, 0, 0, 0};
+              } else if (key0 + key >= min_lim) {
 #pragma unroll
-          for (int t = 0; t < RT; ++t) {
-            const int row = t * 16 + c16;
-            const float w =
-                bf16_to_f32(*(const uint16_t*)(lds + p_at(row, slot & ~3) + (slot & 3) * 2));
-            if (key0 + key < *(const int*)(lds + F::kLim + row * 4))
+                for (int e = 0; e < 4; ++e) {
+                  const uint32_t x = (*at)[e];
+                  if constexpr (FP8) {
+#pragma unroll
+                    for (int s = 0; s < 32; s += 8) odd |= (x >> s & 0x7F) == 0x7F;
+                  } else {
+                    odd |= (x & 0x7F80) == 0x7F80 || (x >> 16 & 0x7F80) == 0x7F80;
+                  }
+                }
+              }
+              // Chunks of 64 / CW keys, in order.
+              const uint64_t hit = __ballot(odd);
+              const int key_first = __builtin_amdgcn_readfirstlane(i) / CW;
+#pragma unroll
+              for (int n = 0; n < 64 / CW; ++n)
+                if (hit >> (n * CW) & ((1ull << CW) - 1)) bad |= 1ull << (key_first + n);
+            }
+#pragma unroll 1
+            for (uint64_t rest = bad; rest; rest &= rest - 1) {
+              const int key = __builtin_ctzll(rest);
+              f32x4 v[DT];
+#pragma unroll
+              for (int d = 0; d < DT; ++d) {
+                const int in = (d * 16 + 4 * q4) * (FP8 ? 1 : 2);
+                const uint8_t* src = chunk(key, in >> 4) + (in & 15);
+                if constexpr (FP8) {
+                  const bf16x8 x = decode8(u32x2{*(const uint32_t*)src, 0});
+                  v[d] = f32x4{(float)x[0], (float)x[1], (float)x[2], (float)x[3]};
+                } else {
+                  const u32x2 x = *(const u32x2*)src;
+                  v[d] = f32x4{__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xFFFF0000u),
+                               __uint_as_float(x.y << 16), __uint_as_float(x.y & 0xFFFF0000u)};
+                }
+              }
+#pragma unroll
+              for (int t = 0; t < RT; ++t) {
+                const int row = t * 16 + c16;
+                const int in = key & 7, pos = FP8 ? key & 31 : (key & 24) + (in >> 1) + (in & 1) * 4;
+                const float wt =
+                    bf16_to_f32(*(const uint16_t*)(p_rows + p_at(row, (key >> 5) * 4 + (pos >> 3)) +
+                                                   (pos & 7) * 2));
+                if (key0 + key < *(const int*)(lds + F::kLim + row * 4))
+#pragma unroll
+                  for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                      acc[t][d][e] = __builtin_fmaf(wt, v[d][e], acc[t][d][e]);
+                __builtin_amdgcn_sched_barrier(0);
+              }
+              if (l2 < CW) *(u32x4*)chunk(key, l2) = u32x4{0, 0, 0, 0};
+            }
+          }
+          // The lane's keys of a block of 32, and its place among the wave's dims.
+          const int byte = wave * DW * (FP8 ? 1 : 2);
+          const int key = FP8 ? c16 >> 1 : 2 * (c16 >> 2);
+          const int ch = (byte >> 4 & 7) + (FP8 ? 0 : (c16 & 3) >> 1);
+          const int v_base = q4 * GROUP + (byte >> 7) * 1024 + key * 128 +
+                             ((ch ^ place(8 * q4 + key)) << 4) + ((c16 & 1) << 3);
+          bf16x8 pf[2];
+          auto weights = [&](int n) {  // of block n / RT, row tile n % RT
+            pf[n & 1] = *(const bf16x8*)(p_rows + p_at(n % RT * 16 + c16, n / RT * 4 + q4));
+          };
+          weights(0);
+#pragma unroll
+          for (int blk = 0; blk < NB; ++blk) {
+            bf16x8 v[DT];
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+              if constexpr (FP8) {
+                const uint8_t* from = tile + ((v_base ^ (d << 4)) + blk * 4 * GROUP);
+                v[d] = decode8(__builtin_bit_cast(
+                    u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((PDEC_LDS s32x2*)from)));
+              } else {
+                const uint8_t* from = tile + ((v_base ^ (d << 5)) + blk * 4 * GROUP);
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((PDEC_LDS s16x4*)from);
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((PDEC_LDS s16x4*)(from + 128));
+                v[d] = __builtin_bit_cast(
+                    bf16x8, s16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+              }
+            }
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+              const int n = blk * RT + t;
+              if (n + 1 < NB * RT) weights(n + 1);
 #pragma unroll
               for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[t][d][e] = __builtin_fmaf(w, v[d][e], acc[t][d][e]);
-            __builtin_amdgcn_sched_barrier(0);
+                acc[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[d], pf[n & 1], acc[t][d], 0, 0, 0);
+              __builtin_amdgcn_sched_barrier(0);
+            }
           }
         }
-        __syncthreads();
-        for (int i = threadIdx.x; i < TILE * CPR; i += kThreads)
-          if (bad >> (i / CPR) & 1) *(u32x4*)(lds + st * F::kStage + i * 16) = u32x4{0, 0, 0, 0};
-        __syncthreads();
       }
-      // The lane's key in a block of 32 keys, and its place among the wave's dims.
-      const int l2 = lane_now(), row_2 = l2 & 15, q_2 = l2 >> 4;
-      const int v_key = 8 * q_2 + (FP8 ? row_2 >> 1 : 2 * (row_2 >> 2));
-      const int v_chunk = FP8 ? wave * DT : wave * DT * 2 + ((row_2 & 3) >> 1);
-      const int v_base = v_key * ROW + ((v_chunk ^ (v_key & 7)) << 4) + ((row_2 & 1) << 3);
-#pragma unroll
-      for (int kb = 0; kb < TILE / 32; ++kb) {
-        bf16x8 v[DT];
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          if constexpr (FP8) {
-            const uint8_t* from = tile + ((v_base ^ (d << 4)) + kb * 32 * ROW);
-            v[d] = decode8(__builtin_bit_cast(
-                u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((PDEC_LDS s32x2*)from)));
-          } else {
-            const uint8_t* from = tile + ((v_base ^ (d << 5)) + kb * 32 * ROW);
-            const uint8_t* odd = tile + ((v_base ^ 16 ^ (d << 5)) + (kb * 32 + 1) * ROW);
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((PDEC_LDS s16x4*)from);
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((PDEC_LDS s16x4*)odd);
-            v[d] = __builtin_bit_cast(
-                bf16x8, s16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
-          }
-        }
-#pragma unroll
-        for (int t = 0; t < RT; ++t) {
-          const bf16x8 pf = *(const bf16x8*)(lds + p_at(t * 16 + row_2, kb * 32 + q_2 * 8));
-#pragma unroll
-          for (int d = 0; d < DT; ++d)
-            acc[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[d], pf, acc[t][d], 0, 0, 0);
-        }
-      }
-      st = st + 1 == NST ? 0 : st + 1;
+      const int free = NST - st - before;
+      before = st;
+      st = free;
     }
 
-    // The rows' sums and maxima meet every wave's part of the output.
+    // The rows' sums and references meet every wave's part of the output.
     wg_barrier();
-    float* sums = (float*)(lds + F::kTop);
-    float* tops = (float*)(lds + F::kAlpha);
-    if (active) {
-      const int row = rw * 16 + c16;
+    const int l4 = lane_now(), c16 = l4 & 15, q4 = l4 >> 4;
+    float* sums = (float*)(lds + F::kAlpha);
+    float* tops = sums + F::kRows;
+    if (wave < RT) {
       const float sum = sum_over_key_groups(l);
       if (q4 == 0) {
-        sums[kw * F::kRows + row] = sum;
-        if (kw == 0) tops[row] = m;
+        sums[rq * 16 + c16] = sum;
+        tops[rq * 16 + c16] = m;
       }
     }
     wg_barrier();
@@ -584,12 +637,10 @@ latent_attn_kernel(LatentAttnArgs a, const int32_t* __restrict__ table) {
     for (int t = 0; t < RT; ++t) {
       const int row = t * 16 + c16;
       if (row >= rows) continue;
-      float sum = 0.f;
-#pragma unroll
-      for (int k = 0; k < WK; ++k) sum += sums[k * F::kRows + row];
+      const float sum = sums[row];
       if (whole) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        uint16_t* o = (uint16_t*)a.out + (q_row0 + row) * R + wave * (R / kWaves) + 4 * q4;
+        uint16_t* o = (uint16_t*)a.out + (q_row0 + row) * R + wave * DW + 4 * q4;
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
           const f32x2 lo = {acc[t][d][0] * inv, acc[t][d][1] * inv};
@@ -601,7 +652,7 @@ latent_attn_kernel(LatentAttnArgs a, const int32_t* __restrict__ table) {
       } else {
         const int64_t pr = ((int64_t)w + u) * F::kRows + row;
         if (wave == 0 && q4 == 0) *(float2*)(a.part_ml + pr * 2) = float2{tops[row], sum};
-        float* o = a.part_acc + pr * R + wave * (R / kWaves) + 4 * q4;
+        float* o = a.part_acc + pr * R + wave * DW + 4 * q4;
 #pragma unroll
         for (int d = 0; d < DT; ++d) *(f32x4*)(o + d * 16) = acc[t][d];
       }
@@ -698,13 +749,13 @@ hipError_t launch_latent_attention(int fp8, int latent, int row_tiles, const Lat
 #define PDEC_LATENT(R_, FP8_)                                                                    \
   do {                                                                                           \
     if (row_tiles == 1)                                                                          \
-      latent_attn_kernel<R_, 1, FP8_><<<grid, kThreads, 0, stream>>>(a, a.block_table);          \
+      latent_attn_kernel<R_, 1, FP8_><<<grid, kThreads, 0, stream>>>(a);          \
     else if (row_tiles == 2)                                                                     \
-      latent_attn_kernel<R_, 2, FP8_><<<grid, kThreads, 0, stream>>>(a, a.block_table);          \
+      latent_attn_kernel<R_, 2, FP8_><<<grid, kThreads, 0, stream>>>(a);          \
     else if (row_tiles == 4)                                                                     \
-      latent_attn_kernel<R_, 4, FP8_><<<grid, kThreads, 0, stream>>>(a, a.block_table);          \
+      latent_attn_kernel<R_, 4, FP8_><<<grid, kThreads, 0, stream>>>(a);          \
     else                                                                                         \
-      latent_attn_kernel<R_, 8, FP8_><<<grid, kThreads, 0, stream>>>(a, a.block_table);          \
+      latent_attn_kernel<R_, 8, FP8_><<<grid, kThreads, 0, stream>>>(a);          \
     hipError_t e = hipGetLastError();                                                            \
     if (e != hipSuccess || a.unit_groups) return e;                                              \
     const dim3 mgrid(a.n_units, std::min(a.block_rows, a.n_q * a.n_heads));                      \
