@@ -43,6 +43,7 @@ typedef short s16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef int s32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 #define PDEC_LDS __attribute__((address_space(3)))
 
@@ -249,15 +250,14 @@ latent_attn_kernel(LatentAttnArgs a) {
     push(p_begin, 0);
     // This wave's row tile of the first product; a lane's query row c, dims by q.
     const int rq = wave < RT ? wave : 0;
-    int row_lim;  // keys that this lane's row sees
     bf16x8 qr[2], qf[FP8 ? 1 : 2 * LW];
     i32x8 qh[FP8 ? LW : 1], ql[FP8 ? LW : 1];
     int q_exp = 0;
     {
       const int l0 = lane_now(), c16 = l0 & 15, q4 = l0 >> 4;
       const int row = min(rq * 16 + c16, rows - 1);  // rows past the block's repeat its last
-      row_lim = base_lim + (row0 + row) / a.n_heads;
-      if (wave < RT && q4 == 0) *(int*)(lds + F::kLim + (rq * 16 + c16) * 4) = row_lim;
+      if (wave < RT && q4 == 0)  // the keys that a row sees
+        *(int*)(lds + F::kLim + (rq * 16 + c16) * 4) = base_lim + (row0 + row) / a.n_heads;
       const uint16_t* src = (const uint16_t*)a.q + (q_row0 + row) * (R + kRope) + q4 * 8;
 #pragma unroll
       for (int c = 0; c < 2; ++c) qr[c] = *(const bf16x8*)(src + R + c * 32);
@@ -269,11 +269,13 @@ latent_attn_kernel(LatentAttnArgs a) {
         bf16x8 x[4 * LW];
         float top = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4 * LW; ++i) {
+        for (int i = 0; i < 4 * LW; ++i)
           x[i] = *(const bf16x8*)(src - q4 * 8 + (i >> 2) * 128 + q4 * 32 + (i & 3) * 8);
+        __builtin_amdgcn_sched_barrier(0);  // all of them under way
+#pragma unroll
+        for (int i = 0; i < 4 * LW; ++i)
 #pragma unroll
           for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)x[i][e]));
-        }
         top = max_over_key_groups(top);
         q_exp = min(max((int)(__float_as_uint(top) >> 23), 1), 254) - 127 - 7;
         const float scale = __uint_as_float((uint32_t)min(max(q_exp + 127, 1), 254) << 23);
@@ -346,7 +348,8 @@ latent_attn_kernel(LatentAttnArgs a) {
           // be anything, 0.
           auto mask = [&](int blk, int t, f32x4& x, f32x4& vs) {
             // Of bf16 pages eight keys of one page; of E4M3 pages too (8 q4 ..).
-            int lim = here >> (blk * 2 + (q4 >> 1)) & 1 ? row_lim - key0 - blk * 32 : 0;
+            int lim = *(const int*)(lds + F::kLim + row * 4) - key0 - blk * 32;
+            if (!(here >> (blk * 2 + (q4 >> 1)) & 1)) lim = 0;
             asm volatile("" : "+v"(lim));  // compared here, not ahead of the branch
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -364,40 +367,35 @@ latent_attn_kernel(LatentAttnArgs a) {
             if constexpr (FP8) {
               from += (c16 & 3) * 128;
               const int sw = place(8 * (c16 >> 2) + (c16 & 3)) << 4;  // of t = 1: place ^ 4
-              i32x8 k[3];
-              auto read = [&](int n) {  // window n / 2 of key tile n % 2
+              constexpr int D = RT == 8 ? 2 : 4;  // reads under way
+              i32x8 k[D];
+              auto read = [&](int n) {  // window n / 2 of key tile n % 2; the rotary part last
                 const uint8_t* src = from + (n >> 1) * 1024 + (n & 1) * 512;
-                const int at = ((q4 << 5) ^ sw) ^ (n & 1) << 6;
-                const u32x4 y = *(const u32x4*)(src + at), z = *(const u32x4*)(src + (at ^ 16));
-                k[n % 3] = i32x8{(int)y.x, (int)y.y, (int)y.z, (int)y.w,
+                const bool rope = n >= 2 * LW;
+                const int at = ((q4 << (rope ? 4 : 5)) ^ sw) ^ (n & 1) << 6;
+                const u32x4 y = *(const u32x4*)(src + at), z = *(const u32x4*)(src + (at ^ (rope ? 64 : 16)));
+                k[n % D] = i32x8{(int)y.x, (int)y.y, (int)y.z, (int)y.w,
                                  (int)z.x, (int)z.y, (int)z.z, (int)z.w};
               };
-              read(0);
-              read(1);
-              bf16x8 r[2][2];
+#pragma unroll
+              for (int n = 0; n < D; ++n) read(n);
 #pragma unroll
               for (int n = 0; n < 2 * LW; ++n) {
-                if (n + 2 < 2 * LW) {
-                  read(n + 2);
-                } else {
-                  const int t = n & 1;
-#pragma unroll
-                  for (int c = 0; c < 2; ++c)
-                    r[t][c] = *(const bf16x8*)(from + LW * 1024 + t * 512 +
-                                               (((q4 << 4) ^ sw ^ t << 6) ^ c << 6));
-                }
-                x[n & 1] = mx_mfma(k[n % 3], qh[n >> 1], x[n & 1], q_exp);
-                x[n & 1] = mx_mfma(k[n % 3], ql[n >> 1], x[n & 1], q_exp);
+                x[n & 1] = mx_mfma(k[n % D], qh[n >> 1], x[n & 1], q_exp);
+                x[n & 1] = mx_mfma(k[n % D], ql[n >> 1], x[n & 1], q_exp);
+                if (n + D < 2 * LW + 2) read(n + D);
                 __builtin_amdgcn_sched_barrier(0);
               }
 #pragma unroll
               for (int t = 0; t < 2; ++t) {
-                vs[t] = *(const f32x4*)(lds + F::kScale +
-                                             (st * TILE + blk * 32 + 8 * q4 + 4 * t) * 4);
+                vs[t] = *(const f32x4*)(lds + F::kScale + (st * TILE + blk * 32 + 8 * q4 + 4 * t) * 4);
                 x[t] *= vs[t];  // the latent part alone
+                const i32x8 r = k[(2 * LW + t) % D];
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
-                  x[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r[t][c], qr[c], x[t], 0, 0, 0);
+                  x[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                      __builtin_bit_cast(bf16x8, i32x4{r[4 * c], r[4 * c + 1], r[4 * c + 2], r[4 * c + 3]}),
+                      qr[c], x[t], 0, 0, 0);
               }
             } else {
               constexpr int N = 4 * LW + 4, D = RT == 8 ? 4 : 8;  // reads; of them under way
@@ -492,7 +490,7 @@ latent_attn_kernel(LatentAttnArgs a) {
 #pragma unroll
             for (int t = 0; t < RT; ++t) {
               // Not written where none of the row tile's rows moved.
-              const float f = *(const float*)(lds + F::kAlpha + ((buf ^ 1) * F::kRows + t * 16 + c16) * 4);
+              const float f = *(const float*)(lds + F::kAlpha + ((buf ^ 1) * F::kRows + c16) * 4 + t * 64);
               const float alpha = flags >> (8 * t) & 1 ? f : 1.f;
 #pragma unroll
               for (int d = 0; d < DT; ++d) acc[t][d] *= alpha;
@@ -541,37 +539,34 @@ latent_attn_kernel(LatentAttnArgs a) {
             }
 #pragma unroll 1
             for (uint64_t rest = bad; rest; rest &= rest - 1) {
-              const int key = __builtin_ctzll(rest);
-              f32x4 v[DT];
+              const int key = __builtin_ctzll(rest), l3 = lane_now(), c16 = l3 & 15, q4 = l3 >> 4;
+              const int in8 = key & 7, pos = FP8 ? key & 31 : (key & 24) + (in8 >> 1) + (in8 & 1) * 4;
 #pragma unroll
               for (int d = 0; d < DT; ++d) {
                 const int in = (d * 16 + 4 * q4) * (FP8 ? 1 : 2);
                 const uint8_t* src = chunk(key, in >> 4) + (in & 15);
+                f32x4 v;
                 if constexpr (FP8) {
                   const bf16x8 x = decode8(u32x2{*(const uint32_t*)src, 0});
-                  v[d] = f32x4{(float)x[0], (float)x[1], (float)x[2], (float)x[3]};
+                  v = f32x4{(float)x[0], (float)x[1], (float)x[2], (float)x[3]};
                 } else {
                   const u32x2 x = *(const u32x2*)src;
-                  v[d] = f32x4{__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xFFFF0000u),
-                               __uint_as_float(x.y << 16), __uint_as_float(x.y & 0xFFFF0000u)};
+                  v = f32x4{__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xFFFF0000u),
+                            __uint_as_float(x.y << 16), __uint_as_float(x.y & 0xFFFF0000u)};
                 }
-              }
 #pragma unroll
-              for (int t = 0; t < RT; ++t) {
-                const int row = t * 16 + c16;
-                const int in = key & 7, pos = FP8 ? key & 31 : (key & 24) + (in >> 1) + (in & 1) * 4;
-                const float wt =
-                    bf16_to_f32(*(const uint16_t*)(p_rows + p_at(row, (key >> 5) * 4 + (pos >> 3)) +
-                                                   (pos & 7) * 2));
-                if (key0 + key < *(const int*)(lds + F::kLim + row * 4))
-#pragma unroll
-                  for (int d = 0; d < DT; ++d)
+                for (int t = 0; t < RT; ++t) {
+                  const float wt = bf16_to_f32(
+                      *(const uint16_t*)(p_rows + p_at(c16, (key >> 5) * 4 + (pos >> 3)) +
+                                         (pos & 7) * 2 + t * (32 * TILE)));
+                  if (key0 + key < *(const int*)(lds + F::kLim + c16 * 4 + t * 64))
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                      acc[t][d][e] = __builtin_fmaf(wt, v[d][e], acc[t][d][e]);
-                __builtin_amdgcn_sched_barrier(0);
+                      acc[t][d][e] = __builtin_fmaf(wt, v[e], acc[t][d][e]);
+                  __builtin_amdgcn_sched_barrier(0);
+                }
               }
-              if (l2 < CW) *(u32x4*)chunk(key, l2) = u32x4{0, 0, 0, 0};
+              if (l3 < CW) *(u32x4*)chunk(key, l3) = u32x4{0, 0, 0, 0};
             }
           }
           // The lane's keys of a block of 32, and its place among the wave's dims.
@@ -582,7 +577,7 @@ latent_attn_kernel(LatentAttnArgs a) {
                              ((ch ^ place(8 * q4 + key)) << 4) + ((c16 & 1) << 3);
           bf16x8 pf[2];
           auto weights = [&](int n) {  // of block n / RT, row tile n % RT
-            pf[n & 1] = *(const bf16x8*)(p_rows + p_at(n % RT * 16 + c16, n / RT * 4 + q4));
+            pf[n & 1] = *(const bf16x8*)(p_rows + p_at(c16, n / RT * 4 + q4) + n % RT * (32 * TILE));
           };
           weights(0);
 #pragma unroll
