@@ -115,7 +115,7 @@ struct Form {
   static constexpr int kFlag = kLim + kRows * 4;              // [2][8] bytes: rows whose O moves
   static constexpr int kIds = kFlag + 16;                     // [64]
   static constexpr int kBytes = kIds + 256;
-  static_assert(kBytes <= 160 * 1024 - 64 && kRow % 128 == 0 && kStage % 128 == 0, "LDS layout");
+  static_assert(kBytes <= 160 * 1024 - 64 && kRow % 128 == 0 && kStage % 256 == 0, "LDS layout");
 };
 
 template <int R, int RT, bool FP8>
@@ -129,7 +129,7 @@ latent_attn_kernel(LatentAttnArgs a) {
   constexpr int GROUP = 8 * ROW;                     // bytes of eight keys
   // Loads of a wave: the windows of eight keys, or where a tile is four such groups half of them.
   constexpr int NW = TILE == 64 ? WIN : (WIN + 1) / 2;
-  __shared__ __attribute__((aligned(128))) uint8_t lds[F::kBytes];
+  __shared__ __attribute__((aligned(256))) uint8_t lds[F::kBytes];
   __shared__ int red[kWaves];
   __shared__ int found[2];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = blockIdx.x;
@@ -170,11 +170,16 @@ latent_attn_kernel(LatentAttnArgs a) {
   // key_of(q, t, e), and the eight of a lane side by side are what the second product takes:
   // of bf16 pages t = 0 the four even keys of eight and t = 1 the odd ones, since a transposing
   // read brings four keys, which must differ in their place by more than one; of E4M3 pages,
-  // where it brings eight, in order.  place(key) is what the chunks of a key's 128 bytes are
-  // exchanged by: eight lanes that read a chunk of eight such keys meet all banks.
+  // where it brings eight, in order.
   auto key_of = [](int q, int t, int e) { return FP8 ? 8 * q + 4 * t + e : 8 * q + 2 * e + t; };
-  auto place = [](int key) {
-    return FP8 ? (key & 7) ^ (key >> 1 & 4) : (key & 6) | (key >> 3 & 1);
+  // Where in a window of eight keys the 16 bytes `c` of key `key` lie.  LDS reads 256 bytes a
+  // cycle if the sixteen lanes that it serves at once, of eight keys and two neighbouring chunks,
+  // differ in their place in 256 bytes: 4.0 cycles a read of a wave so, 8.0 with every second
+  // place unused.
+  auto spot = [](int key, int c) {
+    if constexpr (FP8) return (key & 7) * 128 + ((c ^ (key & 7) ^ (key >> 1 & 4)) << 4);
+    else
+      return (key >> 1 & 3) * 256 + ((((key & 1) << 3 | c) ^ ((key & 6) | (key >> 3 & 1) * 9)) << 4);
   };
   // The position of a key's weight within its block, and where row `row`'s weights of block
   // `blk` lie: chunk c of 16 bytes, exchanged by the row.
@@ -209,38 +214,44 @@ latent_attn_kernel(LatentAttnArgs a) {
     };
     // Which pages of the tiles in the stages are there, four bits a stage.
     uint32_t ok = 0;
-    // A wave brings the windows of a group of eight keys, 128 bytes of each key a load: a lane
-    // its chunk.  A page that is not there is a buffer without bytes: its loads bring nothing,
-    // and count.
+    // A wave brings the windows of a group of eight keys, 128 bytes of each key a load.  A page
+    // that is not there is not brought.
     auto push = [&](int t, int st) {
+      if (t >= p_end) {
+        ok &= ~(15u << (4 * st));
+        return;
+      }
       int i = t * PPT - page0;
       if (i >= 64) {
         page0 += 64;
         i -= 64;
         look();
       }
-      const bool on = t < p_end;
-      ok = (ok & ~(15u << (4 * st))) |
-           (on ? (uint32_t)(there >> i) & ((1 << PPT) - 1) : 0) << (4 * st);
-      const int g = TILE == 64 ? wave : wave >> 1, w0 = TILE == 64 ? 0 : (wave & 1) * NW;
-      const bool on_page = on && there >> (i + (g >> 1)) & 1;
-      const int64_t p =
-          on_page ? __builtin_amdgcn_readfirstlane(*(const int*)(lds + F::kIds + (i + (g >> 1)) * 4)) : 0;
-      const int l = lane_now(), key = (g & 1) * 8 + (l >> 3);
-      const int voff = (l >> 3) * ROW + (((l & 7) ^ place(key)) << 4);
-      DmaBuffer src = dma_buffer(
-          (const uint8_t*)a.pages + p * (kPage * ROW) + (g & 1) * GROUP + w0 * 128,
-          on_page ? GROUP - w0 * 128 : 0);
-      uint32_t to = lds0 + st * F::kStage + g * GROUP + w0 * 1024;
-      dma_ready(src, to);
+      ok = (ok & ~(15u << (4 * st))) | ((uint32_t)(there >> i) & ((1 << PPT) - 1)) << (4 * st);
+      if ((wave < kWaves / 2) != (RT == 8)) return;
+      const int l = lane_now();
 #pragma unroll
-      for (int i = 0; i < NW; ++i)
-        if (w0 + i < WIN) dma16_unseen(src, voff, i * 128, to + i * 1024);
-      if constexpr (FP8) {
-        DmaBuffer sc = dma_buffer(a.scales + p * kPage + (g & 1) * 8, on_page ? 32 : 0);
-        uint32_t at = lds0 + F::kScale + (st * TILE + g * 8) * 4;
-        dma_ready(sc, at);
-        if (l < 8) dma4_unseen(sc, l * 4, at);
+      for (int h = 0; h < TILE / 32; ++h) {
+        const int g = (wave & 3) + h * 4;
+        if (!(there >> (i + (g >> 1)) & 1)) continue;
+        const int64_t p =
+            __builtin_amdgcn_readfirstlane(*(const int*)(lds + F::kIds + (i + (g >> 1)) * 4));
+        const DmaBuffer src = dma_buffer((const uint8_t*)a.pages + p * (kPage * ROW), 2 * GROUP);
+        int voff;  // of what lies in the lane's 16 bytes of a window
+        if constexpr (FP8) {
+          voff = (l >> 3) * ROW + (((l & 7) ^ (l >> 3) ^ ((g & 1) << 2)) << 4);
+        } else {
+          const int hc = (l & 15) ^ ((l >> 4) * 2 | (g & 1) * 9);
+          voff = ((l >> 4) * 2 + (hc >> 3)) * ROW + ((hc & 7) << 4);
+        }
+#pragma unroll
+        for (int n = 0; n < WIN; ++n)
+          dma16_unseen(src, voff, (g & 1) * GROUP + n * 128,
+                       lds0 + st * F::kStage + g * GROUP + n * 1024);
+        if constexpr (FP8) {
+          const DmaBuffer scales = dma_buffer(a.scales + p * kPage + (g & 1) * 8, 32);
+          if (l < 8) dma4_unseen(scales, l * 4, lds0 + F::kScale + (st * TILE + g * 8) * 4);
+        }
       }
     };
 
@@ -270,7 +281,8 @@ latent_attn_kernel(LatentAttnArgs a) {
         float top = 0.f;
 #pragma unroll
         for (int i = 0; i < 4 * LW; ++i)
-          x[i] = *(const bf16x8*)(src - q4 * 8 + (i >> 2) * 128 + q4 * 32 + (i & 3) * 8);
+          x[i] = *(const bf16x8*)(src - q4 * 8 + (i >> 2) * 128 + q4 * 32 +
+                                  (((i & 3) * 8) ^ (q4 & 1) << 4));
         __builtin_amdgcn_sched_barrier(0);  // all of them under way
 #pragma unroll
         for (int i = 0; i < 4 * LW; ++i)
@@ -317,8 +329,8 @@ latent_attn_kernel(LatentAttnArgs a) {
     for (int p = p_begin; p <= p_end; ++p) {
       wait_vmem<0>();
       wg_barrier();  // tile p and the weights of p - 1 are here, and tile p - 2 has been used
-      push(p + 1, NST - st - before);
-      const int buf = p & 1;
+      const int next = NST - st - before, buf = p & 1;
+      push(p + 1, next);
 #pragma unroll 1
       for (int half = 0; half < 2; ++half) {
         if ((half == 0) == (RT < 8 || wave >= kWaves / 2)) {
@@ -365,14 +377,16 @@ latent_attn_kernel(LatentAttnArgs a) {
             // The lane's key of tile t, as a row of the product: key_of(c16 / 4, t, c16 % 4).
             const uint8_t* from = tile + (blk * 4 + (c16 >> 2)) * GROUP;
             if constexpr (FP8) {
-              from += (c16 & 3) * 128;
-              const int sw = place(8 * (c16 >> 2) + (c16 & 3)) << 4;  // of t = 1: place ^ 4
+              from += spot(8 * (c16 >> 2) + (c16 & 3), 0) & ~127;
+              const int sw = spot(8 * (c16 >> 2) + (c16 & 3), 0) & 127;  // of t = 1: ^ 64
               constexpr int D = RT == 8 ? 2 : 4;  // reads under way
               i32x8 k[D];
               auto read = [&](int n) {  // window n / 2 of key tile n % 2; the rotary part last
                 const uint8_t* src = from + (n >> 1) * 1024 + (n & 1) * 512;
                 const bool rope = n >= 2 * LW;
-                const int at = ((q4 << (rope ? 4 : 5)) ^ sw) ^ (n & 1) << 6;
+                // Chunks 2 q4 and 2 q4 + 1, odd q4 the other way round, as the query has them;
+                // of the rotary part q4 and 4 + q4.
+                const int at = ((rope ? q4 << 4 : q4 << 5 | (q4 & 1) << 4) ^ sw) ^ (n & 1) << 6;
                 const u32x4 y = *(const u32x4*)(src + at), z = *(const u32x4*)(src + (at ^ (rope ? 64 : 16)));
                 k[n % D] = i32x8{(int)y.x, (int)y.y, (int)y.z, (int)y.w,
                                  (int)z.x, (int)z.y, (int)z.z, (int)z.w};
@@ -399,12 +413,11 @@ latent_attn_kernel(LatentAttnArgs a) {
               }
             } else {
               constexpr int N = 4 * LW + 4, D = RT == 8 ? 4 : 8;  // reads; of them under way
-              from += (c16 & 3) * 256;
-              const int sw = (q4 ^ place(8 * (c16 >> 2) + 2 * (c16 & 3))) << 4;
+              const int sw = spot(8 * (c16 >> 2) + 2 * (c16 & 3), q4);
               bf16x8 k[D];
               auto read = [&](int n) {  // step n / 2 of key tile n % 2
                 const int c = n >> 1;
-                k[n % D] = *(const bf16x8*)(from + (c >> 1) * 1024 + (n & 1) * 128 + (sw ^ (c & 1) << 6));
+                k[n % D] = *(const bf16x8*)(from + (c >> 1) * 1024 + (sw ^ (c & 1) << 6 ^ (n & 1) << 7));
               };
 #pragma unroll
               for (int n = 0; n < D; ++n) read(n);
@@ -504,12 +517,13 @@ latent_attn_kernel(LatentAttnArgs a) {
             constexpr int CW = (FP8 ? DW : 2 * DW) / 16;  // chunks of a wave's part of a key
             auto chunk = [&](int key, int c) {
               const int byte = wave * (FP8 ? DW : 2 * DW) + c * 16;
-              return tile + (key >> 3) * GROUP + (byte >> 7) * 1024 + (key & 7) * 128 +
-                     (((byte >> 4 & 7) ^ place(key)) << 4);
+              return tile + (key >> 3) * GROUP + (byte >> 7) * 1024 + spot(key, byte >> 4 & 7);
             };
             auto is_there = [&](int key) {
               return key0 + key < kv_lim && (here >> (key / kPage) & 1);
             };
+            uint32_t nil;  // made here: as a constant it is kept in registers over the loop
+            asm volatile("v_mov_b32 %0, 0" : "=v"(nil));
             uint64_t bad = 0;
 #pragma unroll 1
             for (int i = l2; i < TILE * CW; i += 64) {
@@ -517,7 +531,7 @@ latent_attn_kernel(LatentAttnArgs a) {
               u32x4* at = (u32x4*)chunk(key, i % CW);
               bool odd = false;
               if (!is_there(key)) {
-                *at = u32x4{0, 0, 0, 0};
+                *at = u32x4{nil, nil, nil, nil};
               } else if (key0 + key >= min_lim) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -566,15 +580,14 @@ latent_attn_kernel(LatentAttnArgs a) {
                   __builtin_amdgcn_sched_barrier(0);
                 }
               }
-              if (l3 < CW) *(u32x4*)chunk(key, l3) = u32x4{0, 0, 0, 0};
+              if (l3 < CW) *(u32x4*)chunk(key, l3) = u32x4{nil, nil, nil, nil};
             }
           }
           // The lane's keys of a block of 32, and its place among the wave's dims.
           const int byte = wave * DW * (FP8 ? 1 : 2);
           const int key = FP8 ? c16 >> 1 : 2 * (c16 >> 2);
           const int ch = (byte >> 4 & 7) + (FP8 ? 0 : (c16 & 3) >> 1);
-          const int v_base = q4 * GROUP + (byte >> 7) * 1024 + key * 128 +
-                             ((ch ^ place(8 * q4 + key)) << 4) + ((c16 & 1) << 3);
+          const int v_base = q4 * GROUP + (byte >> 7) * 1024 + spot(8 * q4 + key, ch) + ((c16 & 1) << 3);
           bf16x8 pf[2];
           auto weights = [&](int n) {  // of block n / RT, row tile n % RT
             pf[n & 1] = *(const bf16x8*)(p_rows + p_at(c16, n / RT * 4 + q4) + n % RT * (32 * TILE));
@@ -590,9 +603,10 @@ latent_attn_kernel(LatentAttnArgs a) {
                 v[d] = decode8(__builtin_bit_cast(
                     u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((PDEC_LDS s32x2*)from)));
               } else {
-                const uint8_t* from = tile + ((v_base ^ (d << 5)) + blk * 4 * GROUP);
-                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((PDEC_LDS s16x4*)from);
-                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((PDEC_LDS s16x4*)(from + 128));
+                const uint8_t* even = tile + ((v_base ^ (d << 5)) + blk * 4 * GROUP);
+                const uint8_t* odd = tile + ((v_base ^ (d << 5 | 128)) + blk * 4 * GROUP);
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((PDEC_LDS s16x4*)even);
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((PDEC_LDS s16x4*)odd);
                 v[d] = __builtin_bit_cast(
                     bf16x8, s16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
               }
@@ -609,9 +623,8 @@ latent_attn_kernel(LatentAttnArgs a) {
           }
         }
       }
-      const int free = NST - st - before;
       before = st;
-      st = free;
+      st = next;
     }
 
     // The rows' sums and references meet every wave's part of the output.
@@ -659,15 +672,20 @@ latent_attn_kernel(LatentAttnArgs a) {
 }
 
 // Merges the pieces of each unit, and writes zeros for the rows of a unit that sees no key.
-// A work group per row of a unit: R / 4 lanes a piece, the others' pieces side by side, then
-// the results in order.
+// R / 4 lanes hold a row.  A row of up to eight pieces is theirs alone, all its pieces under way
+// at once; of more pieces the S rows' worth of lanes share each row, their results joined in
+// order.  Where there are many rows a work group takes several (rows_per_group), so that what
+// it looks up about the units first is paid once for them.
 template <int R, int TILE>
-__global__ __launch_bounds__(512) void latent_merge_kernel(LatentAttnArgs a, int rows_per_unit) {
-  constexpr int L = R / 4, S = 512 / L;  // lanes of a piece, pieces at once
+__global__ __launch_bounds__(512) void latent_merge_kernel(LatentAttnArgs a, int rows_per_unit,
+                                                           int rows_per_group) {
+  constexpr int L = R / 4, S = 512 / L;  // lanes of a row, rows or pieces at once
   __shared__ int red[2][8];
   __shared__ float sh[S - 1][6][L];
-  const int u = blockIdx.x, row0 = unit_row0(a, u), row = blockIdx.y;
-  if (row >= unit_rows(a, row0)) return;
+  const int u = blockIdx.x, row0 = unit_row0(a, u);
+  const int row_begin = blockIdx.y * rows_per_group;
+  const int row_end = min(row_begin + rows_per_group, unit_rows(a, row0));
+  if (row_begin >= row_end) return;
   int all = 0, before = 0;
   for (int v = threadIdx.x; v < a.n_units; v += 512) {
     const int n = unit_tiles<TILE>(a, v);
@@ -692,8 +710,8 @@ __global__ __launch_bounds__(512) void latent_merge_kernel(LatentAttnArgs a, int
   const int w1 = tiles > 0 ? (first + tiles - 1) / per : w0 - 1;
   if (tiles > 0 && w0 == w1) return;
   const int lane = threadIdx.x % L, part = threadIdx.x / L;
-  float m = -INFINITY, l = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  float m, l;
+  f32x4 o;
   auto join = [&](float mi, float li, f32x4 oi) {
     const float mn = fmaxf(m, mi), mu = mn == -INFINITY ? 0.f : mn;
     const float so = exp2f(m - mu), si = exp2f(mi - mu);
@@ -701,39 +719,60 @@ __global__ __launch_bounds__(512) void latent_merge_kernel(LatentAttnArgs a, int
     o = o * so + oi * si;
     m = mn;
   };
-  for (int w = w0 + part; w <= w1; w += 8 * S) {
-    float2 ml[8];
-    f32x4 x[8];
+  auto join_from = [&](int row, int begin, int step) {
+    m = -INFINITY;
+    l = 0.f;
+    o = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int w = begin; w <= w1; w += 8 * step) {
+      float2 ml[8];
+      f32x4 x[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int64_t pr = ((int64_t)min(w + i * S, w1) + u) * rows_per_unit + row;
-      ml[i] = *(const float2*)(a.part_ml + pr * 2);
-      x[i] = *(const f32x4*)(a.part_acc + pr * R + lane * 4);
+      for (int i = 0; i < 8; ++i)
+        if (w + i * step <= w1) {
+          const int64_t pr = ((int64_t)(w + i * step) + u) * rows_per_unit + row;
+          ml[i] = *(const float2*)(a.part_ml + pr * 2);
+          x[i] = *(const f32x4*)(a.part_acc + pr * R + lane * 4);
+        }
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (w + i * step <= w1) join(ml[i].x, ml[i].y, x[i]);
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (w + i * S <= w1) join(ml[i].x, ml[i].y, x[i]);
+  };
+  auto write = [&](int row) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const f32x2 lo = {o[0] * inv, o[1] * inv}, hi = {o[2] * inv, o[3] * inv};
+    *(u32x2*)((uint16_t*)a.out +
+              ((int64_t)(u / a.blocks_per_seq) * a.n_q * a.n_heads + row0 + row) * R + lane * 4) =
+        u32x2{__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2)),
+              __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2))};
+  };
+  if (w1 - w0 < 8) {
+    for (int row = row_begin + part; row < row_end; row += S) {
+      join_from(row, w0, 1);
+      write(row);
+    }
+    return;
   }
-  if (part > 0) {
-    float(*d)[L] = sh[part - 1];
-    d[0][lane] = m;
-    d[1][lane] = l;
+  for (int row = row_begin; row < row_end; ++row) {
+    join_from(row, w0 + part, S);
+    if (part > 0) {
+      float(*d)[L] = sh[part - 1];
+      d[0][lane] = m;
+      d[1][lane] = l;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) d[2 + e][lane] = o[e];
-  }
-  __syncthreads();
-  if (part > 0) return;
+      for (int e = 0; e < 4; ++e) d[2 + e][lane] = o[e];
+    }
+    __syncthreads();
+    if (part == 0) {
 #pragma unroll
-  for (int i = 0; i < S - 1; ++i) {
-    const float(*d)[L] = sh[i];
-    join(d[0][lane], d[1][lane], f32x4{d[2][lane], d[3][lane], d[4][lane], d[5][lane]});
+      for (int i = 0; i < S - 1; ++i) {
+        const float(*d)[L] = sh[i];
+        join(d[0][lane], d[1][lane], f32x4{d[2][lane], d[3][lane], d[4][lane], d[5][lane]});
+      }
+      write(row);
+    }
+    __syncthreads();
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  const f32x2 lo = {o[0] * inv, o[1] * inv}, hi = {o[2] * inv, o[3] * inv};
-  *(u32x2*)((uint16_t*)a.out +
-            ((int64_t)(u / a.blocks_per_seq) * a.n_q * a.n_heads + row0 + row) * R + lane * 4) =
-      u32x2{__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2)),
-            __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2))};
 }
 
 }  // namespace
@@ -753,8 +792,11 @@ hipError_t launch_latent_attention(int fp8, int latent, int row_tiles, const Lat
       latent_attn_kernel<R_, 8, FP8_><<<grid, kThreads, 0, stream>>>(a);          \
     hipError_t e = hipGetLastError();                                                            \
     if (e != hipSuccess || a.unit_groups) return e;                                              \
-    const dim3 mgrid(a.n_units, std::min(a.block_rows, a.n_q * a.n_heads));                      \
-    latent_merge_kernel<R_, latent_tile(FP8_, R_)><<<mgrid, 512, 0, stream>>>(a, 16 * row_tiles); \
+    const int rows = std::min(a.block_rows, a.n_q * a.n_heads);                                  \
+    const int each = (int64_t)rows * a.n_units >= 4096 ? 8 : 1;                       \
+    const dim3 mgrid(a.n_units, (rows + each - 1) / each);                                       \
+    latent_merge_kernel<R_, latent_tile(FP8_, R_)>                                               \
+        <<<mgrid, 512, 0, stream>>>(a, 16 * row_tiles, each);                                    \
   } while (0)
   if (latent == 512) {
     if (fp8) PDEC_LATENT(512, true);

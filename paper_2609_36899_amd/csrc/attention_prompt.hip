@@ -139,16 +139,13 @@ prompt_attn_kernel(LatentPromptArgs a) {
     auto issue = [&](int t, int st) {
       const int key0 = t * TILE, n = t < p_end ? min(s.nk - key0, TILE) : 0;
       const int64_t k = (int64_t)s.k0 + (n > 0 ? key0 : 0);
-      uint32_t to = lds0 + st * F::kStage;
-      DmaBuffer kb = dma_buffer(a.k + k * a.k_stride + h * a.k_head,
+      const uint32_t to = lds0 + st * F::kStage;
+      const DmaBuffer kb = dma_buffer(a.k + k * a.k_stride + h * a.k_head,
                                 n > 0 ? (n - 1) * k_row + DIM * 2 : 0);
-      DmaBuffer vb = dma_buffer(a.v + k * a.v_stride + h * a.v_head,
+      const DmaBuffer vb = dma_buffer(a.v + k * a.v_stride + h * a.v_head,
                                 n > 0 ? (n - 1) * v_row + DIM * 2 : 0);
-      DmaBuffer rb = dma_buffer(a.rope_keys + k * a.r_stride,
+      const DmaBuffer rb = dma_buffer(a.rope_keys + k * a.r_stride,
                                 n > 0 ? (n - 1) * r_row + kRope * 2 : 0);
-      dma_ready(vb, to);
-      dma_ready(rb, to);
-      dma_ready(kb, to);
 #pragma unroll
       for (int i = 0; i < NK; ++i) dma16_unseen(kb, k_off[i], 0, to + (wave * NK + i) * 1024);
 #pragma unroll
