@@ -51,109 +51,119 @@ __device__ __forceinline__ int block_tiles(const Seq& s, int blk) {
   const int keys = s.nk - s.nq + min((blk + 1) * ROWS, s.nq);
   return max((keys + TILE - 1) / TILE, 1);
 }
+// Tiles of the blocks before blk: of each whole block ROWS / TILE more than of the one before.
+template <int ROWS, int TILE>
+__device__ __forceinline__ int tiles_before(const Seq& s, int blk) {
+  constexpr int K = ROWS / TILE;
+  static_assert(K * TILE == ROWS && (TILE & (TILE - 1)) == 0, "whole tiles a block");
+  const int full = s.nq / ROWS, n = min(blk, full);
+  const int base = (s.nk - s.nq + TILE - 1) & -TILE, first = base / TILE;  // rounded up
+  const int ones = min(max(-first / K, 0), n);  // blocks that no key is seen of
+  const int sum = ones + (n - ones) * first + K * (n * (n + 1) - ones * (ones + 1)) / 2;
+  return blk > full ? sum + block_tiles<ROWS, TILE>(s, full) : sum;
+}
 template <int ROWS, int TILE>
 __device__ __forceinline__ int seq_tiles(const Seq& s) {
-  int n = 0;
-  for (int blk = 0; blk * ROWS < s.nq; ++blk) n += block_tiles<ROWS, TILE>(s, blk);
-  return n;
+  return tiles_before<ROWS, TILE>(s, (s.nq + ROWS - 1) / ROWS);
+}
+// The block that tile `at` of a sequence's lies in.
+template <int ROWS, int TILE>
+__device__ __forceinline__ int block_of(const Seq& s, int at) {
+  int lo = 0, hi = (s.nq + ROWS - 1) / ROWS;  // tiles_before(lo) <= at < tiles_before(hi)
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (tiles_before<ROWS, TILE>(s, mid) <= at) lo = mid;
+    else hi = mid;
+  }
+  return lo;
 }
 
-template <int DIM, int WAVES>
-struct PromptForm {
-  static constexpr int kRows = 32 * WAVES, kTile = WAVES == 8 ? 64 : 32, kStages = 3;
-  static constexpr int kK = kTile * DIM * 2, kR = kTile * kRope * 2;  // bytes of K, and V; of rotary
-  static constexpr int kStage = 2 * kK + kR;
-};
+constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 32 * kWaves, kTile = 32, kStages = 3;
 
-template <int DIM, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2))) void
-prompt_attn_kernel(LatentPromptArgs a) {
-  typedef PromptForm<DIM, WAVES> F;
-  constexpr int TILE = F::kTile, NST = F::kStages, ROWS = F::kRows, THREADS = 64 * WAVES;
-  constexpr int KN = DIM / 32, KC = KN + 2, DT = DIM / 16, KT = TILE / 16;
-  constexpr int NK = F::kK / 1024 / WAVES, NR = F::kR / 1024 / WAVES, NL = 2 * NK + NR;
-  static_assert(NK * 1024 * WAVES == F::kK && NR * 1024 * WAVES == F::kR, "whole loads");
-  __shared__ __attribute__((aligned(128))) uint8_t lds[NST * F::kStage];
-  __shared__ int red[WAVES];
+template <int DIM>
+__global__ __launch_bounds__(kThreads, 2) void prompt_attn_kernel(LatentPromptArgs a) {
+  constexpr int KC = (DIM + kRope) / 32, DT = DIM / 16;  // steps of the first product, tiles of dims
+  // A tile in LDS, by groups of eight keys (a wave brings one): K, rotary, V, each of windows of
+  // 128 bytes of the eight.
+  constexpr int WIN = DIM / 64, GK = WIN * 1024, K = 4 * GK, ROPE = 4 * 1024;
+  constexpr int STAGE = 2 * K + ROPE, NL = 2 * WIN + 1;
+  __shared__ __attribute__((aligned(256))) uint8_t lds[kStages * STAGE];
+  __shared__ __attribute__((aligned(16))) uint8_t weights[kWaves][32 * 64];
+  __shared__ int red[kWaves];
   __shared__ int found[2];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int c16 = lane & 15, q4 = lane >> 4, h = blockIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = blockIdx.x;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(PDEC_LDS uint8_t*)lds;
   // With a group for each block the blocks' order is turned round, so that the long ones begin
   // first.
   const int w = a.block_groups ? gridDim.y - 1 - blockIdx.y : blockIdx.y;
-  const Stretch mine = stretch_of<THREADS>(
+  const Stretch mine = stretch_of<kThreads>(
       a.n_seqs, gridDim.y, a.block_groups ? 1 : a.min_tiles, w, red, found, [&](int b) {
         const Seq s = seq_of(a, b);
-        return a.block_groups ? (s.nq + ROWS - 1) / ROWS : seq_tiles<ROWS, TILE>(s);
+        return a.block_groups ? (s.nq + kRows - 1) / kRows : seq_tiles<kRows, kTile>(s);
       });
   int at = w * mine.per;
   if (at >= mine.total) return;
-  int end = min(at + mine.per, mine.total), first = mine.first, blk = 0;
+  int end = min(at + mine.per, mine.total), first = mine.first;
   int b = min(max(mine.unit, 0), a.n_seqs - 1);  // whatever the starts hold
   Seq s = seq_of(a, b);
+  int blk;
   if (a.block_groups) {
     blk = at - first;
     at = first = 0;
-    end = block_tiles<ROWS, TILE>(s, blk);
+    end = block_tiles<kRows, kTile>(s, blk);
+  } else {
+    blk = block_of<kRows, kTile>(s, at - first);
+    first += tiles_before<kRows, kTile>(s, blk);
   }
 
-  auto f_of = [](int key) { return (key & 6) | (key >> 3 & 1); };  // the key's place in 128 bytes
-  int k_off[NK], v_off[NK], r_off[NR];
+  // The lane's number, made where it is used: what is computed from threadIdx.x ahead of the
+  // loop is kept in registers over it.
+  auto lane_now = [] {
+    int l;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+    return l;
+  };
+  // Where in a window of eight keys the 16 bytes `c` of key `key` lie: the sixteen lanes that an
+  // LDS read serves at once, of eight even (or odd) keys and two neighbouring chunks, differ in
+  // their place in 256 bytes, as do those of a transposing read.
+  auto spot = [](int key, int c) {
+    return (key >> 1 & 3) * 256 + ((((key & 1) << 3 | c) ^ ((key & 6) | (key >> 3 & 1) * 9)) << 4);
+  };
   const int k_row = (int)a.k_stride * 2, v_row = (int)a.v_stride * 2, r_row = (int)a.r_stride * 2;
-#pragma unroll
-  for (int i = 0; i < NK; ++i) {
-    const int n = (wave * NK + i) * 64 + lane, key = n / (DIM / 8), c = n % (DIM / 8) ^ f_of(key);
-    k_off[i] = key * k_row + c * 16;
-    v_off[i] = key * v_row + c * 16;
-  }
-#pragma unroll
-  for (int i = 0; i < NR; ++i) {
-    const int n = (wave * NR + i) * 64 + lane, key = n / 8;
-    r_off[i] = key * r_row + ((n % 8) ^ f_of(key)) * 16;
-  }
-  const int key_a = 8 * (c16 >> 2) + 2 * (c16 & 3);  // this lane's even key of a block of 32
-  const int k_sw = (q4 ^ f_of(key_a)) << 4;
-  const int v_key = 8 * q4 + 2 * (c16 >> 2);
-  const int v_base = v_key * (DIM * 2) + ((((c16 & 3) >> 1) ^ f_of(v_key)) << 4) + ((c16 & 1) << 3);
   const bf16x8 ones = __builtin_bit_cast(
       bf16x8, u16x8{0x3F80, 0x3F80, 0x3F80, 0x3F80, 0x3F80, 0x3F80, 0x3F80, 0x3F80});
 
   for (; at < end; ++blk) {
-    if (blk * ROWS >= s.nq) {
+    if (blk * kRows >= s.nq) {
       if (++b >= a.n_seqs) break;
       s = seq_of(a, b);
       blk = -1;
       continue;
     }
-    const int tiles = block_tiles<ROWS, TILE>(s, blk);
-    if (first + tiles <= at) {
-      first += tiles;
-      continue;
-    }
+    const int tiles = block_tiles<kRows, kTile>(s, blk);
     const int p_begin = max(at - first, 0), p_end = min(tiles, end - first);
     const int base_lim = s.nk - s.nq + 1;  // keys that row 0 of the sequence sees
-    const int row0 = blk * ROWS + wave * 32;
+    const int row0 = blk * kRows + wave * 32;
     const int min_lim = base_lim + row0;   // keys that every row of the wave sees
 
     auto issue = [&](int t, int st) {
-      const int key0 = t * TILE, n = t < p_end ? min(s.nk - key0, TILE) : 0;
+      const int key0 = t * kTile, n = t < p_end ? min(s.nk - key0, kTile) : 0;
       const int64_t k = (int64_t)s.k0 + (n > 0 ? key0 : 0);
-      const uint32_t to = lds0 + st * F::kStage;
       const DmaBuffer kb = dma_buffer(a.k + k * a.k_stride + h * a.k_head,
-                                n > 0 ? (n - 1) * k_row + DIM * 2 : 0);
+                                      n > 0 ? (n - 1) * k_row + DIM * 2 : 0);
       const DmaBuffer vb = dma_buffer(a.v + k * a.v_stride + h * a.v_head,
-                                n > 0 ? (n - 1) * v_row + DIM * 2 : 0);
+                                      n > 0 ? (n - 1) * v_row + DIM * 2 : 0);
       const DmaBuffer rb = dma_buffer(a.rope_keys + k * a.r_stride,
-                                n > 0 ? (n - 1) * r_row + kRope * 2 : 0);
+                                      n > 0 ? (n - 1) * r_row + kRope * 2 : 0);
+      const int l = lane_now(), hc = (l & 15) ^ ((l >> 4) * 2 | (wave & 1) * 9);
+      const int key = wave * 8 + (l >> 4) * 2 + (hc >> 3), in = (hc & 7) << 4;
+      const uint32_t to = lds0 + st * STAGE + wave * GK;
 #pragma unroll
-      for (int i = 0; i < NK; ++i) dma16_unseen(kb, k_off[i], 0, to + (wave * NK + i) * 1024);
+      for (int i = 0; i < WIN; ++i) dma16_unseen(kb, key * k_row + in, i * 128, to + i * 1024);
+      dma16_unseen(rb, key * r_row + in, 0, lds0 + st * STAGE + K + wave * 1024);
 #pragma unroll
-      for (int i = 0; i < NR; ++i)
-        dma16_unseen(rb, r_off[i], 0, to + F::kK + (wave * NR + i) * 1024);
-#pragma unroll
-      for (int i = 0; i < NK; ++i)
-        dma16_unseen(vb, v_off[i], 0, to + F::kK + F::kR + (wave * NK + i) * 1024);
+      for (int i = 0; i < WIN; ++i)
+        dma16_unseen(vb, key * v_row + in, i * 128, to + K + ROPE + i * 1024);
     };
 
     wait_vmem<0>();
@@ -161,20 +171,23 @@ prompt_attn_kernel(LatentPromptArgs a) {
     issue(p_begin, 0);
     bf16x8 qf[2][KC];
     int row_lim[2];
+    {
+      const int l = lane_now(), c16 = l & 15, q4 = l >> 4;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int row = min(row0 + t * 16 + c16, s.nq - 1);  // rows past the last repeat it
-      row_lim[t] = base_lim + row;
-      const uint16_t* src = a.q + ((int64_t)s.q0 + row) * a.q_stride + h * a.q_head;
+      for (int t = 0; t < 2; ++t) {
+        const int row = min(row0 + t * 16 + c16, s.nq - 1);  // rows past the last repeat it
+        row_lim[t] = base_lim + row;
+        const uint16_t* src = a.q + ((int64_t)s.q0 + row) * a.q_stride + h * a.q_head;
 #pragma unroll
-      for (int c = 0; c < KC; ++c) qf[t][c] = *(const bf16x8*)(src + c * 32 + q4 * 8);
+        for (int c = 0; c < KC; ++c) qf[t][c] = *(const bf16x8*)(src + c * 32 + q4 * 8);
+      }
     }
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int c = 0; c < KC; ++c) asm volatile("" : "+v"(qf[t][c]));
 #pragma unroll
-    for (int i = 1; i < NST - 1; ++i) issue(p_begin + i, i);
+    for (int i = 1; i < kStages - 1; ++i) issue(p_begin + i, i);
 
     float m[2] = {-INFINITY, -INFINITY};
     f32x4 acc[2][DT], sum[2];
@@ -186,136 +199,157 @@ prompt_attn_kernel(LatentPromptArgs a) {
     }
 
     int st = 0;
+#pragma unroll 1
     for (int p = p_begin; p < p_end; ++p) {
-      wait_vmem<(NST - 2) * NL>();
+      wait_vmem<(kStages - 2) * NL>();
       wg_barrier();  // this tile is here, and the one before has been used
-      issue(p + NST - 1, st == 0 ? NST - 1 : st - 1);
-      const uint8_t* kt = lds + st * F::kStage;
-      const uint8_t* rt = kt + F::kK;
-      const uint8_t* vt = rt + F::kR;
-      st = st + 1 == NST ? 0 : st + 1;
-      const int key0 = p * TILE;
+      issue(p + kStages - 1, st == 0 ? kStages - 1 : st - 1);
+      const uint8_t* kt = lds + st * STAGE;
+      const uint8_t* vt = kt + K + ROPE;
+      st = st + 1 == kStages ? 0 : st + 1;
+      const int key0 = p * kTile;
       if (key0 >= min_lim + 31 || row0 >= s.nq) continue;  // nothing that a row of the wave sees
-      const bool cut = key0 + TILE > min_lim;
+      const bool cut = key0 + kTile > min_lim;
+      const int l0 = lane_now(), c16 = l0 & 15, q4 = l0 >> 4;
 
-      // Score e of key tile k of this lane belongs to key 32 (k / 2) + 8 q4 + 2 e + k % 2.
-      f32x4 sc[2][KT];
+      // Score e of key tile k of this lane belongs to key 8 q4 + 2 e + k.
+      f32x4 sc[2][2];
 #pragma unroll
-      for (int k = 0; k < KT; ++k) {
-        const int key = (k >> 1) * 32 + key_a + (k & 1);
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int t = 0; t < 2; ++t) sc[t][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < 2; ++k) sc[t][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+      {
+        const int sw = spot(8 * (c16 >> 2) + 2 * (c16 & 3), q4);
+        const uint8_t* from = kt + (c16 >> 2) * GK;
+        const uint8_t* rot = kt + K + (c16 >> 2) * 1024;
+        constexpr int N = 2 * KC, D = 6;  // reads; of them under way
+        bf16x8 x[D];
+        auto read = [&](int n) {  // step n / 2 of key tile n % 2
+          const int c = n >> 1, at = sw ^ (c & 1) << 6 ^ (n & 1) << 7;
+          x[n % D] = *(const bf16x8*)((c < 2 * WIN ? from + (c >> 1) * 1024 : rot) + at);
+        };
 #pragma unroll
-        for (int c = 0; c < KC; ++c) {
-          const uint8_t* row = c < KN ? kt + key * (DIM * 2) + (c >> 1) * 128 : rt + key * (kRope * 2);
-          const bf16x8 x = *(const bf16x8*)(row + (k_sw ^ (c & 1) << 6));
+        for (int n = 0; n < D; ++n) read(n);
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
 #pragma unroll
           for (int t = 0; t < 2; ++t)
-            sc[t][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, qf[t][c], sc[t][k], 0, 0, 0);
+            sc[t][n & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[n % D], qf[t][n >> 1],
+                                                                   sc[t][n & 1], 0, 0, 0);
+          if (n + D < N) read(n + D);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
-      uint32_t pw[2][KT][2];
+      // The values, transposed: even and odd keys of eight, as the weights are.
+      bf16x8 v[DT];
+      {
+        const int ch = (c16 & 3) >> 1;
+        const int base = q4 * GK + spot(8 * q4 + 2 * (c16 >> 2), ch) + ((c16 & 1) << 3);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const uint8_t* even = vt + (d >> 2) * 1024 + (base ^ (d & 3) << 5);
+          const uint8_t* odd = vt + (d >> 2) * 1024 + (base ^ ((d & 3) << 5 | 128));
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((PDEC_LDS s16x4*)even);
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((PDEC_LDS s16x4*)odd);
+          v[d] = __builtin_bit_cast(
+              bf16x8, s16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (cut)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          int lim = row_lim[t] - key0 - 8 * q4;
+          asm volatile("" : "+v"(lim));  // compared here, not ahead of the branch
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (2 * e + k >= lim) sc[t][k][e] = -INFINITY;
+        }
+      float now[2];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        float top = -INFINITY;
+        float top = max2(max2(sc[t][0][0], sc[t][0][1]), max2(sc[t][0][2], sc[t][0][3]));
+        top = max2(top, max2(max2(sc[t][1][0], sc[t][1][1]), max2(sc[t][1][2], sc[t][1][3])));
+        now[t] = max_over_key_groups(top) * a.scale_log2;
+      }
+      if (__any(!(now[0] <= m[0] + kSlack) || !(now[1] <= m[1] + kSlack))) {
 #pragma unroll
-        for (int k = 0; k < KT; ++k)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if (cut && key0 + (k >> 1) * 32 + 8 * q4 + 2 * e + (k & 1) >= row_lim[t])
-              sc[t][k][e] = -INFINITY;
-            top = fmaxf(top, sc[t][k][e]);
-          }
-        const float now = max_over_key_groups(top) * a.scale_log2;
-        const bool need = now > m[t] + kSlack;
-        if (__any(need)) {
-          const float to = need ? now : m[t];
+        for (int t = 0; t < 2; ++t) {
+          const bool need = now[t] > m[t] + kSlack;
+          const float to = need ? now[t] : m[t];
           const float alpha = need ? __builtin_amdgcn_exp2f(m[t] - to) : 1.f;
           m[t] = to;
           sum[t] *= alpha;
 #pragma unroll
           for (int d = 0; d < DT; ++d) acc[t][d] *= alpha;
         }
-        // The weights enter the second product in bf16, each off by at most half a step (2^-8);
-        // the normaliser sums them as they were rounded.
-        const float base = m[t] == -INFINITY ? 0.f : m[t];
-#pragma unroll
-        for (int k = 0; k < KT; ++k)
-#pragma unroll
-          for (int e = 0; e < 4; e += 2) {
-            const f32x2 x = {
-                __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][k][e], a.scale_log2, -base)),
-                __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][k][e + 1], a.scale_log2, -base))};
-            pw[t][k][e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
-          }
       }
+      // The weights enter the second product in bf16, each off by at most half a step (2^-8);
+      // the normaliser sums them as they were rounded.
+      bf16x8 pf[2];
 #pragma unroll
-      for (int kb = 0; kb < TILE / 32; ++kb) {
-        bf16x8 pf[2];
+      for (int t = 0; t < 2; ++t) {
+        const float base = m[t] == -INFINITY ? 0.f : m[t];
+        uint32_t pw[4];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          pf[t] = __builtin_bit_cast(bf16x8, u32x4{pw[t][2 * kb][0], pw[t][2 * kb][1],
-                                                   pw[t][2 * kb + 1][0], pw[t][2 * kb + 1][1]});
-          sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[t], sum[t], 0, 0, 0);
+        for (int e = 0; e < 8; e += 2) {
+          const f32x2 x = {
+              __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][e >> 2][e & 3], a.scale_log2, -base)),
+              __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][e >> 2][(e & 3) + 1], a.scale_log2, -base))};
+          pw[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
         }
-        auto value = [&](int d) {
-          const int at = (v_base ^ ((d & 3) << 5)) + (d >> 2) * 128 + kb * 32 * DIM * 2;
-          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((PDEC_LDS s16x4*)(vt + at));
-          const s16x4 hi =
-              __builtin_amdgcn_ds_read_tr16_b64_v4i16((PDEC_LDS s16x4*)(vt + at + DIM * 2));
-          return __builtin_bit_cast(
-              bf16x8, s16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
-        };
-        // 0 times what a row does not see is 0, unless something there is infinite or NaN:
-        // such blocks of 32 keys are summed key by key, of the rows that see them alone.
-        bool finite = true;
-        if (cut) {
-          f32x4 z = {0.f, 0.f, 0.f, 0.f};
+        pf[t] = __builtin_bit_cast(bf16x8, u32x4{pw[0], pw[1], pw[2], pw[3]});
+        sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[t], sum[t], 0, 0, 0);
+      }
+      // 0 times what a row does not see is 0, unless something there is infinite or NaN:
+      // such tiles are summed key by key, of the rows that see them alone.
+      bool finite = true;
+      if (cut) {
+        f32x4 z = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int d = 0; d < DT; ++d)
-            z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value(d), bf16x8{}, z, 0, 0, 0);
-          finite = !__any(z[0] + z[1] + z[2] + z[3] != 0.f);
-        }
-        if (finite) {
+        for (int d = 0; d < DT; ++d)
+          z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[d], bf16x8{}, z, 0, 0, 0);
+        finite = !__any(z[0] + z[1] + z[2] + z[3] != 0.f);
+      }
+      if (finite) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+            acc[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[d], pf[t], acc[t][d], 0, 0, 0);
+      } else {
+        uint8_t* mine = weights[wave];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          *(bf16x8*)(mine + (t * 16 + c16) * 64 + q4 * 16) = pf[t];
+#pragma unroll 1
+        for (int key = 0; key < kTile; ++key) {
+          const int l1 = lane_now(), c16 = l1 & 15, q4 = l1 >> 4;
+          const uint8_t* from = mine + c16 * 64 + (key >> 3) * 16 + ((key & 1) * 4 + (key >> 1 & 3)) * 2;
+          const float w0 = bf16_to_f32(*(const uint16_t*)from);
+          const float w1 = bf16_to_f32(*(const uint16_t*)(from + 16 * 64));
+          const bool s0 = key0 + key < row_lim[0], s1 = key0 + key < row_lim[1];
 #pragma unroll
           for (int d = 0; d < DT; ++d) {
-            const bf16x8 v = value(d);
+            const u32x2 x = *(const u32x2*)(vt + (key >> 3) * GK + (d >> 2) * 1024 +
+                                            spot(key, (d & 3) * 2 + (q4 >> 1)) + (q4 & 1) * 8);
+            const f32x4 y = {__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xFFFF0000u),
+                             __uint_as_float(x.y << 16), __uint_as_float(x.y & 0xFFFF0000u)};
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
-              acc[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[t], acc[t][d], 0, 0, 0);
-          }
-        } else {
-          for (int g = 0; g < 4; ++g)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const int key = kb * 32 + 8 * g + 2 * (e & 3) + (e >> 2);
-              float pv[2];
-#pragma unroll
-              for (int t = 0; t < 2; ++t) {
-                const uint32_t pair = pw[t][2 * kb + (e >> 2)][(e & 3) / 2];
-                pv[t] = __shfl(__uint_as_float(e & 1 ? pair & 0xFFFF0000u : pair << 16), g * 16 + c16, 64);
-              }
-#pragma unroll
-              for (int d = 0; d < DT; ++d) {
-                const int dim = d * 16 + 4 * q4;
-                const u32x2 x = *(const u32x2*)(vt + key * (DIM * 2) + ((dim >> 3 ^ f_of(key)) << 4) +
-                                                (dim & 7) * 2);
-                const f32x4 v = {__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xFFFF0000u),
-                                 __uint_as_float(x.y << 16), __uint_as_float(x.y & 0xFFFF0000u)};
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                  for (int i = 0; i < 4; ++i)
-                    acc[t][d][i] = key0 + key < row_lim[t]
-                                       ? __builtin_fmaf(pv[t], v[i], acc[t][d][i])
-                                       : acc[t][d][i];
-              }
+            for (int i = 0; i < 4; ++i) {
+              if (s0) acc[0][d][i] = __builtin_fmaf(w0, y[i], acc[0][d][i]);
+              if (s1) acc[1][d][i] = __builtin_fmaf(w1, y[i], acc[1][d][i]);
             }
+            __builtin_amdgcn_sched_barrier(0);
+          }
         }
       }
     }
 
     const bool whole = p_begin == 0 && p_end == tiles;
+    const int l1 = lane_now(), c16 = l1 & 15, q4 = l1 >> 4;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const int row = row0 + t * 16 + c16;
@@ -334,8 +368,8 @@ prompt_attn_kernel(LatentPromptArgs a) {
         }
       } else {
         // The group's first piece, or the one that begins in it and goes on.
-        const int64_t pr = (((int64_t)w * 2 + (first + p_begin != w * mine.per)) * a.n_heads + h) * ROWS +
-                           row - blk * ROWS;
+        const int64_t pr = (((int64_t)w * 2 + (first + p_begin != w * mine.per)) * a.n_heads + h) * kRows +
+                           row - blk * kRows;
         if (q4 == 0) *(float2*)(a.part_ml + pr * 2) = float2{m[t], l};
         float* o = a.part_acc + pr * DIM + 4 * q4;
 #pragma unroll
@@ -351,29 +385,25 @@ prompt_attn_kernel(LatentPromptArgs a) {
 // Merges the block that ends in stretch w and began before it, if there is one: its pieces are
 // the first of w and of the stretches before, and where it began the last.  A group per
 // (stretch, head, 32 rows): DIM / 4 lanes a row.
-template <int DIM, int WAVES>
+template <int DIM>
 __global__ __launch_bounds__(512) void prompt_merge_kernel(LatentPromptArgs a, int n_groups) {
-  constexpr int ROWS = 32 * WAVES, TILE = PromptForm<DIM, WAVES>::kTile;
   constexpr int L = DIM / 4, RB = 512 / L;  // rows at once
   __shared__ int red[8];
   __shared__ int found[2];
   const int w = blockIdx.y, h = blockIdx.x;
   const Stretch mine = stretch_of<512>(a.n_seqs, n_groups, a.min_tiles, w, red, found, [&](int b) {
-    return seq_tiles<ROWS, TILE>(seq_of(a, b));
+    return seq_tiles<kRows, kTile>(seq_of(a, b));
   });
   const int at = w * mine.per;
   if (at >= mine.total) return;
   const int end = min(at + mine.per, mine.total);
   const Seq s = seq_of(a, min(max(mine.unit, 0), a.n_seqs - 1));
-  int blk = 0, first = mine.first, tiles = 0;
-  for (; blk * ROWS < s.nq; ++blk) {
-    tiles = block_tiles<ROWS, TILE>(s, blk);
-    if (first + tiles > at) break;
-    first += tiles;
-  }
-  if (blk * ROWS >= s.nq || first < 0 || first >= at || first + tiles > end) return;
+  const int blk = block_of<kRows, kTile>(s, at - mine.first);
+  const int first = mine.first + tiles_before<kRows, kTile>(s, blk);
+  const int tiles = block_tiles<kRows, kTile>(s, blk);
+  if (blk * kRows >= s.nq || first >= at || first + tiles > end) return;
   const int row = blockIdx.z * RB + threadIdx.x / L, lane = threadIdx.x % L;
-  if (blk * ROWS + row >= s.nq || row >= ROWS) return;
+  if (blk * kRows + row >= s.nq || row >= kRows) return;
   const int w0 = first / mine.per;
   float m = -INFINITY, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -384,7 +414,7 @@ __global__ __launch_bounds__(512) void prompt_merge_kernel(LatentPromptArgs a, i
     for (int i = 0; i < 8; ++i) {
       const int g = min(v + i, w);
       const int64_t pr =
-          (((int64_t)g * 2 + (g == w0 && first != w0 * mine.per)) * a.n_heads + h) * ROWS + row;
+          (((int64_t)g * 2 + (g == w0 && first != w0 * mine.per)) * a.n_heads + h) * kRows + row;
       ml[i] = *(const float2*)(a.part_ml + pr * 2);
       x[i] = *(const f32x4*)(a.part_acc + pr * DIM + lane * 4);
     }
@@ -400,31 +430,26 @@ __global__ __launch_bounds__(512) void prompt_merge_kernel(LatentPromptArgs a, i
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const f32x2 lo = {o[0] * inv, o[1] * inv}, hi = {o[2] * inv, o[3] * inv};
-  *(u32x2*)(a.out + (((int64_t)s.q0 + blk * ROWS + row) * a.n_heads + h) * DIM + lane * 4) =
+  *(u32x2*)(a.out + (((int64_t)s.q0 + blk * kRows + row) * a.n_heads + h) * DIM + lane * 4) =
       u32x2{__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2)),
             __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2))};
 }
 
 }  // namespace
 
-hipError_t launch_latent_prompt(int dim, int waves, int n_groups, const LatentPromptArgs& a,
+hipError_t launch_latent_prompt(int dim, int n_groups, const LatentPromptArgs& a,
                                 hipStream_t stream) {
   const dim3 grid(a.n_heads, n_groups);
-#define PDEC_PROMPT(D_, W_)                                                                   \
-  do {                                                                                        \
-    prompt_attn_kernel<D_, W_><<<grid, 64 * W_, 0, stream>>>(a);                              \
-    hipError_t e = hipGetLastError();                                                         \
-    if (e != hipSuccess || a.block_groups || n_groups == 1) return e;                         \
-    const dim3 mgrid(a.n_heads, n_groups, 32 * W_ * D_ / 4 / 512);                            \
-    prompt_merge_kernel<D_, W_><<<mgrid, 512, 0, stream>>>(a, n_groups);                      \
+#define PDEC_PROMPT(D_)                                                                 \
+  do {                                                                                  \
+    prompt_attn_kernel<D_><<<grid, kThreads, 0, stream>>>(a);                           \
+    hipError_t e = hipGetLastError();                                                   \
+    if (e != hipSuccess || a.block_groups || n_groups == 1) return e;                   \
+    const dim3 mgrid(a.n_heads, n_groups, kRows * D_ / 4 / 512);                        \
+    prompt_merge_kernel<D_><<<mgrid, 512, 0, stream>>>(a, n_groups);                    \
   } while (0)
-  if (dim == 128) {
-    if (waves == 8) PDEC_PROMPT(128, 8);
-    else PDEC_PROMPT(128, 4);
-  } else {
-    if (waves == 8) PDEC_PROMPT(64, 8);
-    else PDEC_PROMPT(64, 4);
-  }
+  if (dim == 128) PDEC_PROMPT(128);
+  else PDEC_PROMPT(64);
 #undef PDEC_PROMPT
   return hipGetLastError();
 }

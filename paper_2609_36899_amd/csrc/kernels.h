@@ -262,10 +262,10 @@ struct LatentPromptArgs {  // attention_prompt.hip
   int32_t n_rows, n_keys, n_seqs, n_heads;
   int32_t block_groups, min_tiles;
   float scale_log2;
-  float *part_ml, *part_acc;  // [n_groups][2][n_heads][32 waves][2 | dim]
+  float *part_ml, *part_acc;  // [n_groups][2][n_heads][128][2 | dim]
   uint16_t* out;
 };
-hipError_t launch_latent_prompt(int dim, int waves, int n_groups, const LatentPromptArgs& a,
+hipError_t launch_latent_prompt(int dim, int n_groups, const LatentPromptArgs& a,
                                 hipStream_t stream);
 
 constexpr int kCopyPools = 16;  // pools of a launch

@@ -57,7 +57,7 @@ Layout layout_of(const LatentPlan& p, int32_t latent) {
 }
 Layout layout_of(const PromptPlan& p, int32_t n_heads, int32_t dim) {
   if (p.block_groups || p.n_groups == 1) return {0, 0};
-  const int64_t rows = (int64_t)p.n_groups * 2 * n_heads * 32 * p.waves;
+  const int64_t rows = (int64_t)p.n_groups * 2 * n_heads * kPromptRows;
   return {align_up(rows * 2 * 4), align_up(rows * dim * 4)};
 }
 
@@ -306,7 +306,7 @@ int latent_prompt_attention(int32_t n_rows, int32_t n_keys, int32_t n_seqs, int3
   a.part_ml = (float*)workspace;
   a.part_acc = (float*)((char*)workspace + l.ml);
   a.out = (uint16_t*)out;
-  HIP_OR_FAIL(launch_latent_prompt(head_dim, p.waves, p.n_groups, a, (hipStream_t)stream));
+  HIP_OR_FAIL(launch_latent_prompt(head_dim, p.n_groups, a, (hipStream_t)stream));
   return PDEC_OK;
 }
 

@@ -96,14 +96,15 @@ inline LatentPlan plan_latent_attention(int batch, int n_q, int n_heads, int64_t
 }
 
 // ---- attention of prompts -------------------------------------------------------
+constexpr int kPromptRows = 128;  // of a block
+
 struct PromptPlan {
-  int32_t waves, n_groups;  // groups a head
+  int32_t n_groups;  // a head
   bool block_groups;
 };
 inline PromptPlan plan_latent_prompt(int64_t n_rows, int64_t n_seqs, int n_heads) {
   PromptPlan p;
-  p.waves = 4;
-  const int64_t blocks = n_rows / (32 * p.waves) + n_seqs;  // at most
+  const int64_t blocks = n_rows / kPromptRows + n_seqs;  // at most
   p.block_groups = blocks * n_heads >= 2048 && blocks <= 65535;
   p.n_groups = p.block_groups ? (int32_t)blocks
                               : (int32_t)std::max<int64_t>(1, std::min<int64_t>(65535, 512 / n_heads));
