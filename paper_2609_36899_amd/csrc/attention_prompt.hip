@@ -303,49 +303,48 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn_kernel(LatentPromptAr
         pf[t] = __builtin_bit_cast(bf16x8, u32x4{pw[0], pw[1], pw[2], pw[3]});
         sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[t], sum[t], 0, 0, 0);
       }
-      // 0 times what a row does not see is 0, unless something there is infinite or NaN:
-      // such tiles are summed key by key, of the rows that see them alone.
-      bool finite = true;
+      // 0 times what a row does not see is 0, unless something there is infinite or NaN: such
+      // tiles are summed key by key, of the rows that see them alone, and their values made 0.
       if (cut) {
         f32x4 z = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int d = 0; d < DT; ++d)
           z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[d], bf16x8{}, z, 0, 0, 0);
-        finite = !__any(z[0] + z[1] + z[2] + z[3] != 0.f);
-      }
-      if (finite) {
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
+        if (__any(z[0] + z[1] + z[2] + z[3] != 0.f)) {
+          uint8_t* mine = weights[wave];
 #pragma unroll
           for (int t = 0; t < 2; ++t)
-            acc[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[d], pf[t], acc[t][d], 0, 0, 0);
-      } else {
-        uint8_t* mine = weights[wave];
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-          *(bf16x8*)(mine + (t * 16 + c16) * 64 + q4 * 16) = pf[t];
+            *(bf16x8*)(mine + (t * 16 + c16) * 64 + q4 * 16) = pf[t];
 #pragma unroll 1
-        for (int key = 0; key < kTile; ++key) {
-          const int l1 = lane_now(), c16 = l1 & 15, q4 = l1 >> 4;
-          const uint8_t* from = mine + c16 * 64 + (key >> 3) * 16 + ((key & 1) * 4 + (key >> 1 & 3)) * 2;
-          const float w0 = bf16_to_f32(*(const uint16_t*)from);
-          const float w1 = bf16_to_f32(*(const uint16_t*)(from + 16 * 64));
-          const bool s0 = key0 + key < row_lim[0], s1 = key0 + key < row_lim[1];
+          for (int key = 0; key < kTile; ++key) {
+            const int l1 = lane_now(), c16 = l1 & 15, q4 = l1 >> 4;
+            const uint8_t* from = mine + c16 * 64 + (key >> 3) * 16 + ((key & 1) * 4 + (key >> 1 & 3)) * 2;
+            const float w0 = bf16_to_f32(*(const uint16_t*)from);
+            const float w1 = bf16_to_f32(*(const uint16_t*)(from + 16 * 64));
+            const bool s0 = key0 + key < row_lim[0], s1 = key0 + key < row_lim[1];
 #pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            const u32x2 x = *(const u32x2*)(vt + (key >> 3) * GK + (d >> 2) * 1024 +
-                                            spot(key, (d & 3) * 2 + (q4 >> 1)) + (q4 & 1) * 8);
-            const f32x4 y = {__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xFFFF0000u),
-                             __uint_as_float(x.y << 16), __uint_as_float(x.y & 0xFFFF0000u)};
+            for (int d = 0; d < DT; ++d) {
+              const u32x2 x = *(const u32x2*)(vt + (key >> 3) * GK + (d >> 2) * 1024 +
+                                              spot(key, (d & 3) * 2 + (q4 >> 1)) + (q4 & 1) * 8);
+              const f32x4 y = {__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xFFFF0000u),
+                               __uint_as_float(x.y << 16), __uint_as_float(x.y & 0xFFFF0000u)};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              if (s0) acc[0][d][i] = __builtin_fmaf(w0, y[i], acc[0][d][i]);
-              if (s1) acc[1][d][i] = __builtin_fmaf(w1, y[i], acc[1][d][i]);
+              for (int i = 0; i < 4; ++i) {
+                if (s0) acc[0][d][i] = __builtin_fmaf(w0, y[i], acc[0][d][i]);
+                if (s1) acc[1][d][i] = __builtin_fmaf(w1, y[i], acc[1][d][i]);
+              }
+              __builtin_amdgcn_sched_barrier(0);
             }
-            __builtin_amdgcn_sched_barrier(0);
           }
+#pragma unroll
+          for (int d = 0; d < DT; ++d) v[d] = bf16x8{};
         }
       }
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          acc[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[d], pf[t], acc[t][d], 0, 0, 0);
     }
 
     const bool whole = p_begin == 0 && p_end == tiles;
@@ -390,7 +389,7 @@ __global__ __launch_bounds__(512) void prompt_merge_kernel(LatentPromptArgs a, i
   constexpr int L = DIM / 4, RB = 512 / L;  // rows at once
   __shared__ int red[8];
   __shared__ int found[2];
-  const int w = blockIdx.y, h = blockIdx.x;
+  const int w = blockIdx.z, h = blockIdx.x;
   const Stretch mine = stretch_of<512>(a.n_seqs, n_groups, a.min_tiles, w, red, found, [&](int b) {
     return seq_tiles<kRows, kTile>(seq_of(a, b));
   });
@@ -402,37 +401,39 @@ __global__ __launch_bounds__(512) void prompt_merge_kernel(LatentPromptArgs a, i
   const int first = mine.first + tiles_before<kRows, kTile>(s, blk);
   const int tiles = block_tiles<kRows, kTile>(s, blk);
   if (blk * kRows >= s.nq || first >= at || first + tiles > end) return;
-  const int row = blockIdx.z * RB + threadIdx.x / L, lane = threadIdx.x % L;
-  if (blk * kRows + row >= s.nq || row >= kRows) return;
-  const int w0 = first / mine.per;
-  float m = -INFINITY, l = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int v = w0; v <= w; v += 8) {
-    float2 ml[8];
-    f32x4 x[8];
+  const int lane = threadIdx.x % L, w0 = first / mine.per;
+  const int row_end = min(kRows, s.nq - blk * kRows);
+  for (int row = blockIdx.y * RB + threadIdx.x / L; row < row_end; row += gridDim.y * RB) {
+    float m = -INFINITY, l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int v = w0; v <= w; v += 8) {
+      float2 ml[8];
+      f32x4 x[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int g = min(v + i, w);
-      const int64_t pr =
-          (((int64_t)g * 2 + (g == w0 && first != w0 * mine.per)) * a.n_heads + h) * kRows + row;
-      ml[i] = *(const float2*)(a.part_ml + pr * 2);
-      x[i] = *(const f32x4*)(a.part_acc + pr * DIM + lane * 4);
-    }
+      for (int i = 0; i < 8; ++i)
+        if (v + i <= w) {
+          const int g = v + i;
+          const int64_t pr =
+              (((int64_t)g * 2 + (g == w0 && first != w0 * mine.per)) * a.n_heads + h) * kRows + row;
+          ml[i] = *(const float2*)(a.part_ml + pr * 2);
+          x[i] = *(const f32x4*)(a.part_acc + pr * DIM + lane * 4);
+        }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (v + i > w) continue;
-      const float mn = fmaxf(m, ml[i].x), mu = mn == -INFINITY ? 0.f : mn;
-      const float so = exp2f(m - mu), si = exp2f(ml[i].x - mu);
-      l = l * so + ml[i].y * si;
-      o = o * so + x[i] * si;
-      m = mn;
+      for (int i = 0; i < 8; ++i) {
+        if (v + i > w) continue;
+        const float mn = fmaxf(m, ml[i].x), mu = mn == -INFINITY ? 0.f : mn;
+        const float so = exp2f(m - mu), si = exp2f(ml[i].x - mu);
+        l = l * so + ml[i].y * si;
+        o = o * so + x[i] * si;
+        m = mn;
+      }
     }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const f32x2 lo = {o[0] * inv, o[1] * inv}, hi = {o[2] * inv, o[3] * inv};
+    *(u32x2*)(a.out + (((int64_t)s.q0 + blk * kRows + row) * a.n_heads + h) * DIM + lane * 4) =
+        u32x2{__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2)),
+              __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2))};
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  const f32x2 lo = {o[0] * inv, o[1] * inv}, hi = {o[2] * inv, o[3] * inv};
-  *(u32x2*)(a.out + (((int64_t)s.q0 + blk * kRows + row) * a.n_heads + h) * DIM + lane * 4) =
-      u32x2{__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2)),
-            __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2))};
 }
 
 }  // namespace
@@ -445,7 +446,7 @@ hipError_t launch_latent_prompt(int dim, int n_groups, const LatentPromptArgs& a
     prompt_attn_kernel<D_><<<grid, kThreads, 0, stream>>>(a);                           \
     hipError_t e = hipGetLastError();                                                   \
     if (e != hipSuccess || a.block_groups || n_groups == 1) return e;                   \
-    const dim3 mgrid(a.n_heads, n_groups, kRows * D_ / 4 / 512);                        \
+    const dim3 mgrid(a.n_heads, 2, n_groups);                                           \
     prompt_merge_kernel<D_><<<mgrid, 512, 0, stream>>>(a, n_groups);                    \
   } while (0)
   if (dim == 128) PDEC_PROMPT(128);
