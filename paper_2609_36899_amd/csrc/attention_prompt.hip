@@ -130,6 +130,20 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn_kernel(LatentPromptAr
     return (key >> 1 & 3) * 256 + ((((key & 1) << 3 | c) ^ ((key & 6) | (key >> 3 & 1) * 9)) << 4);
   };
   const int k_row = (int)a.k_stride * 2, v_row = (int)a.v_stride * 2, r_row = (int)a.r_stride * 2;
+  int k_off, v_off, r_off;  // of what a lane brings of a window: its 16 bytes of eight keys' 128
+  {
+    const int l = lane_now(), hc = (l & 15) ^ ((l >> 4) * 2 | (wave & 1) * 9);
+    const int key = wave * 8 + (l >> 4) * 2 + (hc >> 3), in = (hc & 7) << 4;
+    k_off = key * k_row + in;
+    v_off = key * v_row + in;
+    r_off = key * r_row + in;
+  }
+  const int l0 = lane_now(), c16 = l0 & 15, q4 = l0 >> 4;
+  // Where in a stage the lane reads keys' chunks (key_of even: 8 (c16 / 4) + 2 (c16 % 4); steps
+  // of the first product two to a window, ^ 64) and, transposed, values.
+  const int k_at = (c16 >> 2) * GK + spot(8 * (c16 >> 2) + 2 * (c16 & 3), q4);
+  const int r_at = K + (c16 >> 2) * 1024 + spot(8 * (c16 >> 2) + 2 * (c16 & 3), q4);
+  const int v_at = K + ROPE + q4 * GK + spot(8 * q4 + 2 * (c16 >> 2), (c16 & 3) >> 1) + ((c16 & 1) << 3);
   const bf16x8 ones = __builtin_bit_cast(
       bf16x8, u16x8{0x3F80, 0x3F80, 0x3F80, 0x3F80, 0x3F80, 0x3F80, 0x3F80, 0x3F80});
 
@@ -146,33 +160,45 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn_kernel(LatentPromptAr
     const int row0 = blk * kRows + wave * 32;
     const int min_lim = base_lim + row0;   // keys that every row of the wave sees
 
-    auto issue = [&](int t, int st) {
-      const int key0 = t * kTile, n = t < p_end ? min(s.nk - key0, kTile) : 0;
-      const int64_t k = (int64_t)s.k0 + (n > 0 ? key0 : 0);
-      const DmaBuffer kb = dma_buffer(a.k + k * a.k_stride + h * a.k_head,
-                                      n > 0 ? (n - 1) * k_row + DIM * 2 : 0);
-      const DmaBuffer vb = dma_buffer(a.v + k * a.v_stride + h * a.v_head,
-                                      n > 0 ? (n - 1) * v_row + DIM * 2 : 0);
-      const DmaBuffer rb = dma_buffer(a.rope_keys + k * a.r_stride,
-                                      n > 0 ? (n - 1) * r_row + kRope * 2 : 0);
-      const int l = lane_now(), hc = (l & 15) ^ ((l >> 4) * 2 | (wave & 1) * 9);
-      const int key = wave * 8 + (l >> 4) * 2 + (hc >> 3), in = (hc & 7) << 4;
+    // The tile to be brought next: its place, and the keys from there on.
+    uint64_t k_next, v_next, r_next;
+    int t_next = p_begin, n_next = s.nk - p_begin * kTile;
+    {
+      const int64_t k = (int64_t)s.k0 + p_begin * kTile;
+      k_next = (uint64_t)(a.k + k * a.k_stride + h * a.k_head);
+      v_next = (uint64_t)(a.v + k * a.v_stride + h * a.v_head);
+      r_next = (uint64_t)(a.rope_keys + k * a.r_stride);
+    }
+    auto issue = [&](int st) {  // loads of the tiles behind the piece bring nothing, and count
+      int kn = 31 * k_row + DIM * 2, vn = 31 * v_row + DIM * 2, rn = 31 * r_row + kRope * 2;
+      if (t_next >= p_end || n_next < kTile) {
+        const int n = t_next < p_end ? n_next : 0;
+        kn = n > 0 ? (n - 1) * k_row + DIM * 2 : 0;
+        vn = n > 0 ? (n - 1) * v_row + DIM * 2 : 0;
+        rn = n > 0 ? (n - 1) * r_row + kRope * 2 : 0;
+      }
+      const DmaBuffer kb = dma_buffer((const void*)k_next, kn);
+      const DmaBuffer vb = dma_buffer((const void*)v_next, vn);
+      const DmaBuffer rb = dma_buffer((const void*)r_next, rn);
       const uint32_t to = lds0 + st * STAGE + wave * GK;
 #pragma unroll
-      for (int i = 0; i < WIN; ++i) dma16_unseen(kb, key * k_row + in, i * 128, to + i * 1024);
-      dma16_unseen(rb, key * r_row + in, 0, lds0 + st * STAGE + K + wave * 1024);
+      for (int i = 0; i < WIN; ++i) dma16_unseen(kb, k_off, i * 128, to + i * 1024);
+      dma16_unseen(rb, r_off, 0, lds0 + st * STAGE + K + wave * 1024);
 #pragma unroll
-      for (int i = 0; i < WIN; ++i)
-        dma16_unseen(vb, key * v_row + in, i * 128, to + K + ROPE + i * 1024);
+      for (int i = 0; i < WIN; ++i) dma16_unseen(vb, v_off, i * 128, to + K + ROPE + i * 1024);
+      ++t_next;
+      n_next -= kTile;
+      k_next += (int64_t)kTile * k_row;
+      v_next += (int64_t)kTile * v_row;
+      r_next += (int64_t)kTile * r_row;
     };
 
     wait_vmem<0>();
     __syncthreads();  // the piece before is done with LDS
-    issue(p_begin, 0);
+    issue(0);
     bf16x8 qf[2][KC];
     int row_lim[2];
     {
-      const int l = lane_now(), c16 = l & 15, q4 = l >> 4;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const int row = min(row0 + t * 16 + c16, s.nq - 1);  // rows past the last repeat it
@@ -187,7 +213,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn_kernel(LatentPromptAr
 #pragma unroll
       for (int c = 0; c < KC; ++c) asm volatile("" : "+v"(qf[t][c]));
 #pragma unroll
-    for (int i = 1; i < kStages - 1; ++i) issue(p_begin + i, i);
+    for (int i = 1; i < kStages - 1; ++i) issue(i);
 
     float m[2] = {-INFINITY, -INFINITY};
     f32x4 acc[2][DT], sum[2];
@@ -203,14 +229,13 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn_kernel(LatentPromptAr
     for (int p = p_begin; p < p_end; ++p) {
       wait_vmem<(kStages - 2) * NL>();
       wg_barrier();  // this tile is here, and the one before has been used
-      issue(p + kStages - 1, st == 0 ? kStages - 1 : st - 1);
+      issue(st == 0 ? kStages - 1 : st - 1);
       const uint8_t* kt = lds + st * STAGE;
       const uint8_t* vt = kt + K + ROPE;
       st = st + 1 == kStages ? 0 : st + 1;
       const int key0 = p * kTile;
       if (key0 >= min_lim + 31 || row0 >= s.nq) continue;  // nothing that a row of the wave sees
       const bool cut = key0 + kTile > min_lim;
-      const int l0 = lane_now(), c16 = l0 & 15, q4 = l0 >> 4;
 
       // Score e of key tile k of this lane belongs to key 8 q4 + 2 e + k.
       f32x4 sc[2][2];
@@ -219,14 +244,11 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn_kernel(LatentPromptAr
 #pragma unroll
         for (int k = 0; k < 2; ++k) sc[t][k] = f32x4{0.f, 0.f, 0.f, 0.f};
       {
-        const int sw = spot(8 * (c16 >> 2) + 2 * (c16 & 3), q4);
-        const uint8_t* from = kt + (c16 >> 2) * GK;
-        const uint8_t* rot = kt + K + (c16 >> 2) * 1024;
         constexpr int N = 2 * KC, D = 6;  // reads; of them under way
         bf16x8 x[D];
         auto read = [&](int n) {  // step n / 2 of key tile n % 2
-          const int c = n >> 1, at = sw ^ (c & 1) << 6 ^ (n & 1) << 7;
-          x[n % D] = *(const bf16x8*)((c < 2 * WIN ? from + (c >> 1) * 1024 : rot) + at);
+          const int c = n >> 1, flip = (c & 1) << 6 ^ (n & 1) << 7;
+          x[n % D] = *(const bf16x8*)(kt + (c < 2 * WIN ? (k_at ^ flip) + (c >> 1) * 1024 : r_at ^ flip));
         };
 #pragma unroll
         for (int n = 0; n < D; ++n) read(n);
@@ -243,12 +265,10 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn_kernel(LatentPromptAr
       // The values, transposed: even and odd keys of eight, as the weights are.
       bf16x8 v[DT];
       {
-        const int ch = (c16 & 3) >> 1;
-        const int base = q4 * GK + spot(8 * q4 + 2 * (c16 >> 2), ch) + ((c16 & 1) << 3);
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          const uint8_t* even = vt + (d >> 2) * 1024 + (base ^ (d & 3) << 5);
-          const uint8_t* odd = vt + (d >> 2) * 1024 + (base ^ ((d & 3) << 5 | 128));
+          const uint8_t* even = kt + (d >> 2) * 1024 + (v_at ^ (d & 3) << 5);
+          const uint8_t* odd = kt + (d >> 2) * 1024 + (v_at ^ ((d & 3) << 5 | 128));
           const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((PDEC_LDS s16x4*)even);
           const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((PDEC_LDS s16x4*)odd);
           v[d] = __builtin_bit_cast(
@@ -348,7 +368,6 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn_kernel(LatentPromptAr
     }
 
     const bool whole = p_begin == 0 && p_end == tiles;
-    const int l1 = lane_now(), c16 = l1 & 15, q4 = l1 >> 4;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const int row = row0 + t * 16 + c16;
