@@ -276,7 +276,6 @@ struct PageCopyArgs {  // kvcopy.hip
   int64_t n_pages;
   const int32_t *src, *dst;
 };
-int64_t page_copy_parts(const PageCopyArgs& a);  // work groups a pair
 hipError_t launch_page_copy(const PageCopyArgs& a, hipStream_t stream);
 
 struct SelectArgs {  // select.hip

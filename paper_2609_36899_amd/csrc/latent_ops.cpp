@@ -327,25 +327,13 @@ int paged_copy_pages(int32_t n_pools, void* const* pools, const int64_t* page_by
   for (int i = 0; i < n_pools; ++i) {  // all are looked at before any is written
     if (!pools[i] || page_bytes[i] < 1 || page_bytes[i] > (1 << 27))
       return fail(PDEC_INVALID_ARG, "a pool is null, or its pages not in [1, 2^27] bytes");
-    PageCopyArgs one{};
-    one.n_pools = 1;
-    one.pool[0] = pools[i];
-    one.bytes[0] = page_bytes[i];
-    if (page_copy_parts(one) > 65535)
+    if (page_bytes[i] == 1 << 27 && !aligned(pools[i], 4))  // copied byte by byte
       return fail(PDEC_INVALID_ARG, "pages of unaligned pools too large");
   }
-  // As many pools a launch as fit its arguments and its grid.
-  for (int i = 0; i < n_pools;) {
-    a.n_pools = 0;
-    while (i < n_pools && a.n_pools < kCopyPools) {
+  for (int i = 0; i < n_pools;) {  // as many pools a launch as fit its arguments
+    for (a.n_pools = 0; i < n_pools && a.n_pools < kCopyPools; ++i, ++a.n_pools) {
       a.pool[a.n_pools] = pools[i];
       a.bytes[a.n_pools] = page_bytes[i];
-      ++a.n_pools;
-      if (page_copy_parts(a) > 65535) {
-        --a.n_pools;
-        break;
-      }
-      ++i;
     }
     HIP_OR_FAIL(launch_page_copy(a, (hipStream_t)stream));
   }
