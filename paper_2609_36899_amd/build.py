@@ -28,7 +28,8 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 HIP_SOURCES = ["attention.hip", "attention_prefill.hip", "gemm.hip", "pointwise.hip", "kvcopy.hip",
                "sample.hip", "append.hip", "attention_paged.hip", "select.hip", "verify.hip",
-               "latent.hip", "attention_latent.hip", "attention_prompt.hip",
+               "latent.hip", "attention_latent.hip", "attention_latent_few.hip",
+               "attention_prompt.hip",
                "engine.cpp", "paged_ops.cpp", "latent_ops.cpp", "pagepool.cpp", "pacing.cpp"]
 HIP_FLAGS = [
     "-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",

@@ -22,9 +22,7 @@
 // LDS once in the second product, transposed by the read itself (ds_read_tr).  The tiles come
 // by LDS-DMA into a ring of stages, 16-byte chunk n of a key's row in place n ^ (key & 7) of
 // its 128 bytes, so that eight lanes reading the same chunk of eight keys meet all banks.
-#include "hip_common.h"
-#include "kernels.h"
-#include "stretch.h"
+#include "latent_attn.h"
 
 #include <algorithm>
 #include <type_traits>
@@ -33,70 +31,7 @@ namespace pdec {
 
 namespace {
 
-constexpr int kThreads = 512, kWaves = kThreads / 64, kRope = kLatentRope;
-// A row's reference maximum moves only where its scores outgrow it by this many powers of
-// two: the weights are then up to 2^16 instead of 1, no less exact, and the accumulators are
-// rescaled a few times a row instead of at most tiles.
-constexpr float kSlack = 16.f;
-
-typedef short s16x2 __attribute__((ext_vector_type(2)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
-typedef int s32x2 __attribute__((ext_vector_type(2)));
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-#define PDEC_LDS __attribute__((address_space(3)))
-
-__device__ __forceinline__ int clamp_len(const LatentAttnArgs& a, int b) {
-  return min(max(a.lens[b], 0), a.max_len);
-}
-// Rows of unit u, its first row within the sequence, and the keys that any of them sees.
-__device__ __forceinline__ int unit_row0(const LatentAttnArgs& a, int u) {
-  return u % a.blocks_per_seq * a.block_rows;
-}
-__device__ __forceinline__ int unit_rows(const LatentAttnArgs& a, int row0) {
-  return min(a.block_rows, a.n_q * a.n_heads - row0);
-}
-__device__ __forceinline__ int unit_keys(const LatentAttnArgs& a, int u) {
-  const int row0 = unit_row0(a, u);
-  const int j = (row0 + unit_rows(a, row0) - 1) / a.n_heads;  // its last token
-  return max(clamp_len(a, u / a.blocks_per_seq) - a.n_q + j + 1, 0);
-}
-template <int TILE>
-__device__ __forceinline__ int unit_tiles(const LatentAttnArgs& a, int u) {
-  return (unit_keys(a, u) + TILE - 1) / TILE;
-}
-
-// Eight codes (code i in byte i of the two dwords) to bf16, exactly.
-__device__ __forceinline__ bf16x8 decode8(u32x2 w) {
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.x, 1.f, false);
-  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.x, 1.f, true);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, 1.f, false);
-  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, 1.f, true);
-  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
-
-// a and b as two E4M3 numbers each, times `scale` (a power of two): what is nearest, and what is
-// nearest to the rest.  Into half `which` / 2 of the dwords hi and lo.
-__device__ __forceinline__ void split(float a, float b, float scale, int which, int& hi, int& lo) {
-  s16x2 h = __builtin_bit_cast(s16x2, hi), l = __builtin_bit_cast(s16x2, lo);
-  f32x2 near;
-  if (which) {
-    h = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(h, a, b, scale, true);
-    near = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(__builtin_bit_cast(int, h), scale, true);
-    l = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l, a - near[0], b - near[1], scale, true);
-  } else {
-    h = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(h, a, b, scale, false);
-    near = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(__builtin_bit_cast(int, h), scale, false);
-    l = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l, a - near[0], b - near[1], scale, false);
-  }
-  hi = __builtin_bit_cast(int, h);
-  lo = __builtin_bit_cast(int, l);
-}
-// c + a b over 128 E4M3 codes a row and a column, each lane's part of b times 2^(b_exp - 127).
-__device__ __forceinline__ f32x4 mx_mfma(i32x8 a, i32x8 b, f32x4 c, int b_exp) {
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, 127, 0, b_exp);
-}
+constexpr int kThreads = 512, kWaves = kThreads / 64;
 
 template <int R, int RT, bool FP8>
 struct Form {
@@ -134,15 +69,6 @@ latent_attn_kernel(LatentAttnArgs a) {
   __shared__ int found[2];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = blockIdx.x;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(PDEC_LDS uint8_t*)lds;
-  // The lane, worked out anew each time: places that follow from it, kept over the loop, would
-  // cost registers that the products need, and loads of spilled ones would wait for the tiles
-  // in flight.
-  auto lane_now = [] {
-    int l;
-    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
-    return l;
-  };
-
   int at = 0, end, u = w, first = 0;
   if (a.unit_groups) {
     end = unit_tiles<TILE>(a, u);
@@ -172,15 +98,6 @@ latent_attn_kernel(LatentAttnArgs a) {
   // read brings four keys, which must differ in their place by more than one; of E4M3 pages,
   // where it brings eight, in order.
   auto key_of = [](int q, int t, int e) { return FP8 ? 8 * q + 4 * t + e : 8 * q + 2 * e + t; };
-  // Where in a window of eight keys the 16 bytes `c` of key `key` lie.  LDS reads 256 bytes a
-  // cycle if the sixteen lanes that it serves at once, of eight keys and two neighbouring chunks,
-  // differ in their place in 256 bytes: 4.0 cycles a read of a wave so, 8.0 with every second
-  // place unused.
-  auto spot = [](int key, int c) {
-    if constexpr (FP8) return (key & 7) * 128 + ((c ^ (key & 7) ^ (key >> 1 & 4)) << 4);
-    else
-      return (key >> 1 & 3) * 256 + ((((key & 1) << 3 | c) ^ ((key & 6) | (key >> 3 & 1) * 9)) << 4);
-  };
   // The position of a key's weight within its block, and where row `row`'s weights of block
   // `blk` lie: chunk c of 16 bytes, exchanged by the row.
   auto p_at = [](int row, int c) {
@@ -237,13 +154,7 @@ latent_attn_kernel(LatentAttnArgs a) {
         const int64_t p =
             __builtin_amdgcn_readfirstlane(*(const int*)(lds + F::kIds + (i + (g >> 1)) * 4));
         const DmaBuffer src = dma_buffer((const uint8_t*)a.pages + p * (kPage * ROW), 2 * GROUP);
-        int voff;  // of what lies in the lane's 16 bytes of a window
-        if constexpr (FP8) {
-          voff = (l >> 3) * ROW + (((l & 7) ^ (l >> 3) ^ ((g & 1) << 2)) << 4);
-        } else {
-          const int hc = (l & 15) ^ ((l >> 4) * 2 | (g & 1) * 9);
-          voff = ((l >> 4) * 2 + (hc >> 3)) * ROW + ((hc & 7) << 4);
-        }
+        const int voff = window_offset<FP8, ROW>(l, g);
 #pragma unroll
         for (int n = 0; n < WIN; ++n)
           dma16_unseen(src, voff, (g & 1) * GROUP + n * 128,
@@ -262,7 +173,7 @@ latent_attn_kernel(LatentAttnArgs a) {
     // This wave's row tile of the first product; a lane's query row c, dims by q.
     const int rq = wave < RT ? wave : 0;
     bf16x8 qr[2], qf[FP8 ? 1 : 2 * LW];
-    i32x8 qh[FP8 ? LW : 1], ql[FP8 ? LW : 1];
+    i32x8 qh[LW], ql[LW];  // of E4M3 pages
     int q_exp = 0;
     {
       const int l0 = lane_now(), c16 = l0 & 15, q4 = l0 >> 4;
@@ -273,37 +184,10 @@ latent_attn_kernel(LatentAttnArgs a) {
 #pragma unroll
       for (int c = 0; c < 2; ++c) qr[c] = *(const bf16x8*)(src + R + c * 32);
       if constexpr (FP8) {
-        // The query's latent part as the sum of two E4M3 numbers, 2^q_exp times each: four bits
-        // and what they leave of bf16's eight, so exact but below 2^-10 of the row's largest
-        // element, where at most 2^-17 of that is lost.  Two products of twice the rate, and
-        // the codes enter them as they are.  NaN and infinities become NaN.
         bf16x8 x[4 * LW];
-        float top = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4 * LW; ++i)
-          x[i] = *(const bf16x8*)(src - q4 * 8 + (i >> 2) * 128 + q4 * 32 +
-                                  (((i & 3) * 8) ^ (q4 & 1) << 4));
+        read_query<LW>(src - q4 * 8, q4, x);
         __builtin_amdgcn_sched_barrier(0);  // all of them under way
-#pragma unroll
-        for (int i = 0; i < 4 * LW; ++i)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)x[i][e]));
-        top = max_over_key_groups(top);
-        q_exp = min(max((int)(__float_as_uint(top) >> 23), 1), 254) - 127 - 7;
-        const float scale = __uint_as_float((uint32_t)min(max(q_exp + 127, 1), 254) << 23);
-#pragma unroll
-        for (int i = 0; i < 4 * LW; ++i) {
-          int hi[2] = {0, 0}, lo[2] = {0, 0};
-#pragma unroll
-          for (int e = 0; e < 8; e += 2) {
-            const float v0 = (float)x[i][e], v1 = (float)x[i][e + 1];
-            const float s0 = v0 + v0 * 0.f, s1 = v1 + v1 * 0.f;
-            split(s0, s1, scale, e & 2, hi[e >> 2], lo[e >> 2]);
-          }
-          qh[i >> 2][(i & 3) * 2] = hi[0], qh[i >> 2][(i & 3) * 2 + 1] = hi[1];
-          ql[i >> 2][(i & 3) * 2] = lo[0], ql[i >> 2][(i & 3) * 2 + 1] = lo[1];
-        }
-        q_exp = min(max(q_exp + 127, 1), 254);  // as the product takes it
+        q_exp = split_query<LW>(x, qh, ql);
       } else {
 #pragma unroll
         for (int c = 0; c < 2 * LW; ++c) qf[c] = *(const bf16x8*)(src + c * 32);
@@ -377,8 +261,8 @@ latent_attn_kernel(LatentAttnArgs a) {
             // The lane's key of tile t, as a row of the product: key_of(c16 / 4, t, c16 % 4).
             const uint8_t* from = tile + (blk * 4 + (c16 >> 2)) * GROUP;
             if constexpr (FP8) {
-              from += spot(8 * (c16 >> 2) + (c16 & 3), 0) & ~127;
-              const int sw = spot(8 * (c16 >> 2) + (c16 & 3), 0) & 127;  // of t = 1: ^ 64
+              from += spot<FP8>(8 * (c16 >> 2) + (c16 & 3), 0) & ~127;
+              const int sw = spot<FP8>(8 * (c16 >> 2) + (c16 & 3), 0) & 127;  // of t = 1: ^ 64
               constexpr int D = RT == 8 ? 2 : 4;  // reads under way
               i32x8 k[D];
               auto read = [&](int n) {  // window n / 2 of key tile n % 2; the rotary part last
@@ -413,7 +297,7 @@ latent_attn_kernel(LatentAttnArgs a) {
               }
             } else {
               constexpr int N = 4 * LW + 4, D = RT == 8 ? 4 : 8;  // reads; of them under way
-              const int sw = spot(8 * (c16 >> 2) + 2 * (c16 & 3), q4);
+              const int sw = spot<FP8>(8 * (c16 >> 2) + 2 * (c16 & 3), q4);
               bf16x8 k[D];
               auto read = [&](int n) {  // step n / 2 of key tile n % 2
                 const int c = n >> 1;
@@ -517,7 +401,7 @@ latent_attn_kernel(LatentAttnArgs a) {
             constexpr int CW = (FP8 ? DW : 2 * DW) / 16;  // chunks of a wave's part of a key
             auto chunk = [&](int key, int c) {
               const int byte = wave * (FP8 ? DW : 2 * DW) + c * 16;
-              return tile + (key >> 3) * GROUP + (byte >> 7) * 1024 + spot(key, byte >> 4 & 7);
+              return tile + (key >> 3) * GROUP + (byte >> 7) * 1024 + spot<FP8>(key, byte >> 4 & 7);
             };
             auto is_there = [&](int key) {
               return key0 + key < kv_lim && (here >> (key / kPage) & 1);
@@ -587,7 +471,7 @@ latent_attn_kernel(LatentAttnArgs a) {
           const int byte = wave * DW * (FP8 ? 1 : 2);
           const int key = FP8 ? c16 >> 1 : 2 * (c16 >> 2);
           const int ch = (byte >> 4 & 7) + (FP8 ? 0 : (c16 & 3) >> 1);
-          const int v_base = q4 * GROUP + (byte >> 7) * 1024 + spot(8 * q4 + key, ch) + ((c16 & 1) << 3);
+          const int v_base = q4 * GROUP + (byte >> 7) * 1024 + spot<FP8>(8 * q4 + key, ch) + ((c16 & 1) << 3);
           bf16x8 pf[2];
           auto weights = [&](int n) {  // of block n / RT, row tile n % RT
             pf[n & 1] = *(const bf16x8*)(p_rows + p_at(c16, n / RT * 4 + q4) + n % RT * (32 * TILE));
@@ -779,18 +663,19 @@ __global__ __launch_bounds__(512) void latent_merge_kernel(LatentAttnArgs a, int
 
 hipError_t launch_latent_attention(int fp8, int latent, int row_tiles, const LatentAttnArgs& a,
                                    hipStream_t stream) {
-  const dim3 grid(a.unit_groups ? a.n_units : a.n_groups);
+  const int grid = a.unit_groups ? a.n_units : a.n_groups;
 #define PDEC_LATENT(R_, FP8_)                                                                    \
   do {                                                                                           \
+    hipError_t e = hipSuccess;                                                                   \
     if (row_tiles == 1)                                                                          \
-      latent_attn_kernel<R_, 1, FP8_><<<grid, kThreads, 0, stream>>>(a);          \
+      e = launch_latent_few(FP8_, R_, grid, a, stream);                                          \
     else if (row_tiles == 2)                                                                     \
       latent_attn_kernel<R_, 2, FP8_><<<grid, kThreads, 0, stream>>>(a);          \
     else if (row_tiles == 4)                                                                     \
       latent_attn_kernel<R_, 4, FP8_><<<grid, kThreads, 0, stream>>>(a);          \
     else                                                                                         \
       latent_attn_kernel<R_, 8, FP8_><<<grid, kThreads, 0, stream>>>(a);          \
-    hipError_t e = hipGetLastError();                                                            \
+    if (e == hipSuccess) e = hipGetLastError();                                                  \
     if (e != hipSuccess || a.unit_groups) return e;                                              \
     const int rows = std::min(a.block_rows, a.n_q * a.n_heads);                                  \
     const int each = (int64_t)rows * a.n_units >= 4096 ? 8 : 1;                       \

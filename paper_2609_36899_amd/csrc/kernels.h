@@ -224,6 +224,9 @@ struct LatentAttnArgs {  // attention_latent.hip
   float *part_ml, *part_acc;  // [n_groups + n_units][16 row_tiles][2 | latent]
   void* out;
 };
+// Units of at most sixteen rows (attention_latent_few.hip); a group per stretch or unit.
+hipError_t launch_latent_few(int fp8, int latent, int grid, const LatentAttnArgs& a,
+                             hipStream_t stream);
 hipError_t launch_latent_attention(int fp8, int latent, int row_tiles, const LatentAttnArgs& a,
                                    hipStream_t stream);
 

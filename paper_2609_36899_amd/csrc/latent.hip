@@ -12,8 +12,8 @@
 //
 // Gather.  Bound by memory (a row's 1152 or 644 bytes read, 1152 written), and for few rows by the
 // chain of looks from a row to its page, which the lanes go at once, one a row.  A wave takes four
-// rows, all their loads in flight; 27 000 E4M3 rows of 512 in 18.2 us (2.7 TB/s; the copies
-// are still in the caches), by two rows a wave 18.9, by eight, whose registers halve the waves, 33.7.
+// rows, all their loads in flight; 54 000 E4M3 rows of 512 in 18.2 us (5.3 TB/s, some of it
+// from the caches), by two rows a wave 18.9, by eight, whose registers leave few waves, 33.7.
 #include "hip_common.h"
 #include "kernels.h"
 #include "rows.h"
