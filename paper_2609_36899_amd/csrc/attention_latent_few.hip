@@ -2,47 +2,58 @@
 // small models): attention_latent.hip's formula, units and split of the work.
 //
 // Bound by HBM: a key's 2 (2 R + 64) operations a row are a few cycles of the matrix units beside
-// its R + 132 (E4M3) or 2 R + 128 bytes.  What such a call needs is bytes on their way at all
-// times, so each of a group's four waves goes over pages of its own (every fourth of the piece)
-// with a ring of its own in LDS, and none waits for another until the end of the piece, where
-// their sums are joined through LDS.  A page's sixteen keys are one tile of the first product,
-// S^T = K Q^T, and a lane's four weights are the operand P of the second, O^T = C^T P^T, over
-// sixteen keys as they are; O takes R / 4 registers of the 512 that a wave alone on its unit has.
+// its R + 132 (E4M3) or 2 R + 128 bytes.  Such a call needs bytes on their way at all times, and
+// the chain from a page to its part of the output, which one wave takes thousands of cycles for,
+// off their path.  So a group's waves go in pairs, each over every n-th page of the piece with a
+// ring of four pages in LDS: one wave brings the pages and multiplies S^T = K Q^T, its other half
+// takes the weights through LDS a step later and multiplies O^T = C^T P^T.  A page's sixteen keys
+// are one tile of the first product, and a lane's four weights are the operand P of the second,
+// over sixteen keys, as they are.  At the end of a piece the pairs' sums are joined through LDS.
 #include "latent_attn.h"
 
 namespace pdec {
 
 namespace {
 
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
-
 template <int R, bool FP8>
 struct FewForm {
   static constexpr int kRow = FP8 ? R + 2 * kRope : (R + kRope) * 2;  // a key's bytes
-  static constexpr int kTile = kPage * kRow;
-  // As many pages of a wave as fit: 2 of bf16 latents of 512, else 3 or 4.
-  static constexpr int kStages = kTile * 4 * kWaves <= 144 * 1024 ? 4 : kTile * 3 * kWaves <= 144 * 1024 ? 3 : 2;
-  static constexpr int kRing = kStages * kTile * kWaves, kJoin = kWaves * 16 * R * 4;
-  static constexpr int kScale = kRing > kJoin ? kRing : kJoin;  // [kWaves][kStages][16]
-  static constexpr int kSums = kScale + (FP8 ? kWaves * kStages * kPage * 4 : 0);  // [kWaves][2][16]
-  static constexpr int kBytes = kSums + kWaves * 2 * 16 * 4;
+  static constexpr int kTile = kPage * kRow, kStages = 4;
+  // As many pairs as four pages each fit for: 2 with bf16 latents of 512, else 3 or 4.
+  static constexpr int kPairs =
+      16 * kTile <= 144 * 1024 ? 4 : 12 * kTile <= 144 * 1024 ? 3 : 2;
+  static constexpr int kThreads = 128 * kPairs;
+  static constexpr int kRing = kStages * kTile * kPairs, kJoin = kPairs * 16 * R * 4;
+  // LDS offsets.
+  static constexpr int kScale = kRing > kJoin ? kRing : kJoin;  // [kPairs][kStages][16]
+  static constexpr int kP = kScale + (FP8 ? kPairs * kStages * kPage * 4 : 0);  // [kPairs][2][64] x 8
+  static constexpr int kAlpha = kP + kPairs * 2 * 512;          // [kPairs][2][16]
+  static constexpr int kSums = kAlpha + kPairs * 2 * 64;        // [kPairs][2][16]
+  static constexpr int kFlag = kSums + kPairs * 2 * 64;         // [kPairs][2]: page there, rows moved
+  static constexpr int kBytes = kFlag + kPairs * 2 * 4;
   static_assert(kBytes <= 160 * 1024 - 64 && kTile % 256 == 0, "LDS layout");
 };
 
 template <int R, bool FP8, int UNIT_TILE>
-__global__ __launch_bounds__(2 * kThreads) __attribute__((amdgpu_waves_per_eu(2))) void
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void
 latent_few_kernel(LatentAttnArgs a) {
   typedef FewForm<R, FP8> F;
-  constexpr int ROW = F::kRow, NST = F::kStages, WIN = ROW / 128, LW = (FP8 ? R : 2 * R) / 128;
+  constexpr int ROW = F::kRow, NST = F::kStages, PAIRS = F::kPairs, THREADS = F::kThreads;
+  constexpr int WIN = ROW / 128, LW = (FP8 ? R : 2 * R) / 128;
   constexpr int GROUP = 8 * ROW, DT = R / 16, PPT = UNIT_TILE / kPage;
   constexpr int NL = 2 * WIN + (FP8 ? 1 : 0);  // loads of a page
   __shared__ __attribute__((aligned(256))) uint8_t lds[F::kBytes];
-  __shared__ int red[kWaves];
+  __shared__ int red[THREADS / 64];
   __shared__ int found[2];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = blockIdx.x;
-  const uint32_t ring = (uint32_t)(uintptr_t)(PDEC_LDS uint8_t*)lds + wave * NST * F::kTile;
-  const uint32_t scales_at =
-      (uint32_t)(uintptr_t)(PDEC_LDS uint8_t*)lds + F::kScale + wave * NST * kPage * 4;
+  const bool first_half = wave < PAIRS;  // the half of a pair that takes the first product
+  const int pair = first_half ? wave : wave - PAIRS;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(PDEC_LDS uint8_t*)lds;
+  const uint32_t ring = lds0 + pair * NST * F::kTile;
+  float* scales = (float*)(lds + F::kScale) + pair * NST * kPage;
+  uint8_t* p_at = lds + F::kP + pair * 2 * 512;
+  float* alphas = (float*)(lds + F::kAlpha) + pair * 2 * 16;
+  int* flags = (int*)(lds + F::kFlag) + pair * 2;
 
   int at = 0, end, u = w, first = 0;
   if (a.unit_groups) {
@@ -51,12 +62,12 @@ latent_few_kernel(LatentAttnArgs a) {
       const int row0 = unit_row0(a, u), rows = unit_rows(a, row0);
       uint16_t* o = (uint16_t*)a.out +
                     ((int64_t)(u / a.blocks_per_seq) * a.n_q * a.n_heads + row0) * R;
-      for (int i = threadIdx.x; i < rows * (R / 8); i += kThreads)
+      for (int i = threadIdx.x; i < rows * (R / 8); i += THREADS)
         *(u32x4*)(o + i * 8) = u32x4{0, 0, 0, 0};
       return;
     }
   } else {
-    const Stretch mine = stretch_of<kThreads>(a.n_units, a.n_groups, a.min_tiles, w, red, found,
+    const Stretch mine = stretch_of<THREADS>(a.n_units, a.n_groups, a.min_tiles, w, red, found,
                                               [&](int v) { return unit_tiles<UNIT_TILE>(a, v); });
     at = w * mine.per;
     if (at >= mine.total) return;
@@ -72,6 +83,24 @@ latent_few_kernel(LatentAttnArgs a) {
   // in their place by more than one; of E4M3 pages, where it brings eight, they go in order.
   auto key_of = [](int q, int e) { return FP8 ? 4 * q + e : 2 * e + (q & 1) + 8 * (q >> 1); };
 
+  // A row's reference and sum over all pairs, and what this pair's part of the output is times.
+  struct Join {
+    float top, sum, own;
+  };
+  auto join_of = [&](int row) {
+    const float* sums = (const float*)(lds + F::kSums) + row;  // references, then sums
+    Join o = {-INFINITY, 0.f, 0.f};
+#pragma unroll
+    for (int v = 0; v < PAIRS; ++v) o.top = fmaxf(o.top, sums[v * 32]);
+#pragma unroll
+    for (int v = 0; v < PAIRS; ++v) {
+      const float m = sums[v * 32], f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - o.top);
+      o.sum = __builtin_fmaf(sums[v * 32 + 16], f, o.sum);
+      if (v == pair) o.own = f;
+    }
+    return o;
+  };
+
   for (; at < end; ++u) {
     const int tiles = unit_tiles<UNIT_TILE>(a, u);
     if (first + tiles <= at) {  // empty unit
@@ -85,315 +114,327 @@ latent_few_kernel(LatentAttnArgs a) {
     const int n_pages = (kv_lim + kPage - 1) / kPage;
     const int p_begin = at - first, p_end = min(tiles, end - first);
     const int64_t q_row0 = (int64_t)b * a.n_q * a.n_heads + row0;
-    // The wave's pages: g_begin, g_begin + kWaves ...
-    const int g_begin = p_begin * PPT + wave, g_end = min(p_end * PPT, n_pages);
-    const int mine = g_begin < g_end ? (g_end - g_begin + kWaves - 1) / kWaves : 0;
+    // The pair's pages: g_begin, g_begin + PAIRS ...; a step takes one of each pair's.
+    const int g_begin = p_begin * PPT + pair, g_end = min(p_end * PPT, n_pages);
+    const int steps = max(g_end - p_begin * PPT + PAIRS - 1, 0) / PAIRS;
+    const bool whole = p_begin == 0 && p_end == tiles;
     __syncthreads();  // the piece before is done with LDS
 
-    bf16x8 qr[2], x[(FP8 ? 4 : 2) * LW];
-    int row_lim;
-    {
-      const int l0 = lane_now(), c16 = l0 & 15, q4 = l0 >> 4;
-      const int row = min(c16, rows - 1);  // rows past the unit's repeat its last
-      row_lim = base_lim + (row0 + row) / a.n_heads;
-      const uint16_t* src = (const uint16_t*)a.q + (q_row0 + row) * (R + kRope);
+    if (first_half) {
+      bf16x8 qr[2], x[(FP8 ? 4 : 2) * LW];
+      int row_lim;
+      {
+        const int l0 = lane_now(), c16 = l0 & 15, q4 = l0 >> 4;
+        const int row = min(c16, rows - 1);  // rows past the unit's repeat its last
+        row_lim = base_lim + (row0 + row) / a.n_heads;
+        const uint16_t* src = (const uint16_t*)a.q + (q_row0 + row) * (R + kRope);
 #pragma unroll
-      for (int c = 0; c < 2; ++c) qr[c] = *(const bf16x8*)(src + R + c * 32 + q4 * 8);
-      if constexpr (FP8) read_query<LW>(src, q4, x);
-      else
+        for (int c = 0; c < 2; ++c) qr[c] = *(const bf16x8*)(src + R + c * 32 + q4 * 8);
+        if constexpr (FP8) read_query<LW>(src, q4, x);
+        else
 #pragma unroll
-        for (int c = 0; c < 2 * LW; ++c) x[c] = *(const bf16x8*)(src + c * 32 + q4 * 8);
-    }
-    // Ids of 64 of the wave's pages, one a lane.
-    int ids = -1;
-    auto look = [&](int i0) {
-      const int n = g_begin + (i0 + lane_now()) * kWaves;
-      ids = n < g_end ? a.block_table[(int64_t)b * a.bt_stride + n] : -1;
-      if (ids >= a.n_pages) ids = -1;
-    };
-    look(0);
-    // Here the queries are waited for: their loads would wait for the pages' if later.
-#pragma unroll
-    for (int c = 0; c < 2; ++c) asm volatile("" : "+v"(qr[c]));
-#pragma unroll
-    for (int c = 0; c < (FP8 ? 4 : 2) * LW; ++c) asm volatile("" : "+v"(x[c]));
-    asm volatile("" : "+v"(ids));
-
-    // Loads of the wave's page i into stage st; one that is not there, or behind the last, is a
-    // buffer without bytes: zeros come, and count.  Returns whether it is there.
-    auto issue = [&](int i, int st) {
-      if ((i & 63) == 0 && i > 0) look(i);
-      const int id = __builtin_amdgcn_readlane(ids, i & 63);
-      const int64_t p = max(id, 0);
-      const DmaBuffer from =
-          dma_buffer((const uint8_t*)a.pages + p * F::kTile, id >= 0 ? F::kTile : 0);
-      const int l = lane_now();
-#pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        const int voff = window_offset<FP8, ROW>(l, g);
-#pragma unroll
-        for (int n = 0; n < WIN; ++n)
-          dma16_unseen(from, voff, g * GROUP + n * 128, ring + st * F::kTile + g * GROUP + n * 1024);
+          for (int c = 0; c < 2 * LW; ++c) x[c] = *(const bf16x8*)(src + c * 32 + q4 * 8);
       }
-      if constexpr (FP8) {
-        const DmaBuffer scales = dma_buffer(a.scales + p * kPage, id >= 0 ? kPage * 4 : 0);
-        if (l < kPage) dma4_unseen(scales, l * 4, scales_at + st * kPage * 4);
-      }
-      return id >= 0;
-    };
-    uint32_t ok = 0;  // which stages' pages are there
+      // Ids of 64 of the pair's pages, one a lane.
+      int ids = -1;
+      auto look = [&](int i0) {
+        const int n = g_begin + (i0 + lane_now()) * PAIRS;
+        ids = n < g_end ? a.block_table[(int64_t)b * a.bt_stride + n] : -1;
+        if (ids >= a.n_pages) ids = -1;
+      };
+      look(0);
+      // Here the queries are waited for: their loads would wait for the pages' if later.
 #pragma unroll
-    for (int i = 0; i < NST; ++i) ok |= (uint32_t)issue(i, i) << i;
-
-    i32x8 qh[LW], ql[LW];  // of E4M3 pages
-    int q_exp = 0;
-    if constexpr (FP8) q_exp = split_query<LW>(x, qh, ql);
-
-    float m = -INFINITY, l = 0.f;  // a reference for the row's scores; this lane's part of its sum
-    f32x4 acc[DT];
+      for (int c = 0; c < 2; ++c) asm volatile("" : "+v"(qr[c]));
 #pragma unroll
-    for (int d = 0; d < DT; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int c = 0; c < (FP8 ? 4 : 2) * LW; ++c) asm volatile("" : "+v"(x[c]));
+      asm volatile("" : "+v"(ids));
 
-    int st = 0;
-#pragma unroll 1
-    for (int i = 0; i < mine; ++i) {
-      wait_vmem<(NST - 1) * NL>();
-      if (ok >> st & 1) {
-        uint8_t* tile = lds + (wave * NST + st) * F::kTile;
-        const int key0 = (g_begin + i * kWaves) * kPage;
-        const bool cut = key0 + kPage > min_lim;
-        const int l1 = lane_now(), c16 = l1 & 15, q4 = l1 >> 4;
-        // Where the lane reads keys' chunks.
-        const int k_key = key_of(c16 >> 2, c16 & 3);
-        const int k_at = (k_key >> 3) * GROUP +
-                         (FP8 ? spot<FP8>(k_key, 0) & ~127 : spot<FP8>(k_key, q4));
-        const int k_sw = spot<FP8>(k_key, 0) & 127;  // of E4M3 pages
-        f32x4 s = {0.f, 0.f, 0.f, 0.f}, vs = {1.f, 1.f, 1.f, 1.f};
+      // Loads of the pair's page i into stage st; one that is not there, or behind the last, is a
+      // buffer without bytes: zeros come, and count.  Returns whether it is there.
+      auto issue = [&](int i, int st) {
+        if ((i & 63) == 0 && i > 0) look(i);
+        const int id = __builtin_amdgcn_readlane(ids, i & 63);
+        const int64_t p = max(id, 0);
+        const DmaBuffer from =
+            dma_buffer((const uint8_t*)a.pages + p * F::kTile, id >= 0 ? F::kTile : 0);
+        const int l = lane_now();
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const int voff = window_offset<FP8, ROW>(l, g);
+#pragma unroll
+          for (int n = 0; n < WIN; ++n)
+            dma16_unseen(from, voff, g * GROUP + n * 128, ring + st * F::kTile + g * GROUP + n * 1024);
+        }
         if constexpr (FP8) {
-          f32x4 s2 = {0.f, 0.f, 0.f, 0.f};
-          auto read = [&](int at, int flip) {  // chunks 2 q4 and 2 q4 + 1, exchanged for odd q4
-            const u32x4 y = *(const u32x4*)(tile + at), z = *(const u32x4*)(tile + (at ^ flip));
-            return i32x8{(int)y.x, (int)y.y, (int)y.z, (int)y.w,
-                         (int)z.x, (int)z.y, (int)z.z, (int)z.w};
-          };
-          i32x8 k[2];  // one under way
-          auto latent = [&](int n) { return read(k_at + n * 1024 + ((q4 << 5 | (q4 & 1) << 4) ^ k_sw), 16); };
-          auto rope = [&] { return read(k_at + LW * 1024 + (q4 << 4 ^ k_sw), 64); };
-          k[0] = latent(0);
-#pragma unroll
-          for (int n = 0; n < LW; ++n) {
-            k[(n + 1) & 1] = n + 1 < LW ? latent(n + 1) : rope();
-            s = mx_mfma(k[n & 1], qh[n], s, q_exp);
-            s2 = mx_mfma(k[n & 1], ql[n], s2, q_exp);
-            __builtin_amdgcn_sched_barrier(0);
-          }
-          vs = *(const f32x4*)(lds + F::kScale + ((wave * NST + st) * kPage + 4 * q4) * 4);
-          s = (s + s2) * vs;  // the latent part alone
-          const i32x8 r = k[LW & 1];
-#pragma unroll
-          for (int c = 0; c < 2; ++c)
-            s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                __builtin_bit_cast(bf16x8, i32x4{r[4 * c], r[4 * c + 1], r[4 * c + 2], r[4 * c + 3]}),
-                qr[c], s, 0, 0, 0);
-        } else {
-          constexpr int N = 2 * LW + 2, D = 4;  // reads; of them under way
-          bf16x8 k[D];
-          auto read = [&](int c) {
-            k[c % D] = *(const bf16x8*)(tile + (k_at ^ (c & 1) << 6) + (c >> 1) * 1024);
-          };
-#pragma unroll
-          for (int c = 0; c < D; ++c) read(c);
-#pragma unroll
-          for (int c = 0; c < N; ++c) {
-            s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[c % D], c < 2 * LW ? x[c] : qr[c - 2 * LW],
-                                                        s, 0, 0, 0);
-            if (c + D < N) read(c + D);
-            __builtin_amdgcn_sched_barrier(0);
-          }
+          const DmaBuffer f = dma_buffer(a.scales + p * kPage, id >= 0 ? kPage * 4 : 0);
+          if (l < kPage) dma4_unseen(f, l * 4, lds0 + F::kScale + (pair * NST + st) * kPage * 4);
         }
-        // Where a row does not see a key its score is -inf, and the token's scale, which may be
-        // anything, 0.
-        if (cut) {
-          int lim = row_lim - key0;
-          asm volatile("" : "+v"(lim));
+        return id >= 0;
+      };
+      uint32_t ok = (uint32_t)issue(0, 0);  // which stages' pages are there
+      ok |= (uint32_t)issue(1, 1) << 1;
+
+      i32x8 qh[LW], ql[LW];  // of E4M3 pages
+      int q_exp = 0;
+      if constexpr (FP8) q_exp = split_query<LW>(x, qh, ql);
+
+      float m = -INFINITY, l = 0.f;  // a reference for the row's scores; this lane's part of its sum
+#pragma unroll 1
+      for (int j = 0; j <= steps; ++j) {
+        wg_barrier();  // the second half is done with page j - 2, and the weights of page j - 1 are there
+        if (j == steps) break;
+        const int st = j & (NST - 1), ahead = (j + 2) & (NST - 1);
+        ok = (ok & ~(1u << ahead)) | (uint32_t)issue(j + 2, ahead) << ahead;
+        wait_vmem<2 * NL>();
+        int flag = ok >> st & 1;
+        if (flag) {
+          const uint8_t* tile = lds + (pair * NST + st) * F::kTile;
+          const int key0 = (g_begin + j * PAIRS) * kPage;
+          const bool cut = key0 + kPage > min_lim;
+          const int l1 = lane_now(), c16 = l1 & 15, q4 = l1 >> 4;
+          // Where the lane reads keys' chunks.
+          const int k_key = key_of(c16 >> 2, c16 & 3);
+          const int k_at = (k_key >> 3) * GROUP +
+                           (FP8 ? spot<FP8>(k_key, 0) & ~127 : spot<FP8>(k_key, q4));
+          const int k_sw = spot<FP8>(k_key, 0) & 127;  // of E4M3 pages
+          f32x4 s = {0.f, 0.f, 0.f, 0.f}, vs = {1.f, 1.f, 1.f, 1.f};
+          if constexpr (FP8) {
+            f32x4 s2 = {0.f, 0.f, 0.f, 0.f};
+            auto read = [&](int at, int flip) {  // chunks 2 q4 and 2 q4 + 1, exchanged for odd q4
+              const u32x4 y = *(const u32x4*)(tile + at), z = *(const u32x4*)(tile + (at ^ flip));
+              return i32x8{(int)y.x, (int)y.y, (int)y.z, (int)y.w,
+                           (int)z.x, (int)z.y, (int)z.z, (int)z.w};
+            };
+            i32x8 k[2];  // one under way
+            auto latent = [&](int n) { return read(k_at + n * 1024 + ((q4 << 5 | (q4 & 1) << 4) ^ k_sw), 16); };
+            auto rope = [&] { return read(k_at + LW * 1024 + (q4 << 4 ^ k_sw), 64); };
+            k[0] = latent(0);
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (key_of(q4, e) >= lim) {
-              s[e] = -INFINITY;
-              vs[e] = 0.f;
+            for (int n = 0; n < LW; ++n) {
+              k[(n + 1) & 1] = n + 1 < LW ? latent(n + 1) : rope();
+              s = mx_mfma(k[n & 1], qh[n], s, q_exp);
+              s2 = mx_mfma(k[n & 1], ql[n], s2, q_exp);
+              __builtin_amdgcn_sched_barrier(0);
             }
+            vs = *(const f32x4*)(scales + st * kPage + 4 * q4);
+            s = (s + s2) * vs;  // the latent part alone
+            const i32x8 r = k[LW & 1];
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+              s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                  __builtin_bit_cast(bf16x8, i32x4{r[4 * c], r[4 * c + 1], r[4 * c + 2], r[4 * c + 3]}),
+                  qr[c], s, 0, 0, 0);
+          } else {
+            constexpr int N = 2 * LW + 2, D = 4;  // reads; of them under way
+            bf16x8 k[D];
+            auto read = [&](int c) {
+              k[c % D] = *(const bf16x8*)(tile + (k_at ^ (c & 1) << 6) + (c >> 1) * 1024);
+            };
+#pragma unroll
+            for (int c = 0; c < D; ++c) read(c);
+#pragma unroll
+            for (int c = 0; c < N; ++c) {
+              s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[c % D], c < 2 * LW ? x[c] : qr[c - 2 * LW],
+                                                          s, 0, 0, 0);
+              if (c + D < N) read(c + D);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+          }
+          // Where a row does not see a key its score is -inf, and the token's scale, which may be
+          // anything, 0.
+          if (cut) {
+            int lim = row_lim - key0;
+            asm volatile("" : "+v"(lim));
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (key_of(q4, e) >= lim) {
+                s[e] = -INFINITY;
+                vs[e] = 0.f;
+              }
+          }
+          const float now =
+              max_over_key_groups(max2(max2(s[0], s[1]), max2(s[2], s[3]))) * a.scale_log2;
+          if (__any(!(now <= m + kSlack))) {
+            const bool need = now > m + kSlack;
+            const float f = need ? __builtin_amdgcn_exp2f(m - now) : 1.f;
+            if (need) m = now;
+            l *= f;
+            if (q4 == 0) alphas[(j & 1) * 16 + c16] = f;
+            flag = 3;
+          }
+          // The weights enter the second product in bf16, each off by at most half a step (2^-8).
+          // Of bf16 pages the normaliser sums them as they were rounded; E4M3 tokens' scales go
+          // with their weights, and the sum is of the weights before either.
+          const float base = m == -INFINITY ? 0.f : m;
+          uint32_t pw[2];
+#pragma unroll
+          for (int e = 0; e < 4; e += 2) {
+            f32x2 y = {__builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.scale_log2, -base)),
+                       __builtin_amdgcn_exp2f(__builtin_fmaf(s[e + 1], a.scale_log2, -base))};
+            if constexpr (FP8) {
+              l += y[0] + y[1];
+              y[0] *= vs[e];
+              y[1] *= vs[e + 1];
+            }
+            pw[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2));
+            if constexpr (!FP8)
+              l += __uint_as_float(pw[e / 2] << 16) + __uint_as_float(pw[e / 2] & 0xFFFF0000u);
+          }
+          *(u32x2*)(p_at + (j & 1) * 512 + l1 * 8) = u32x2{pw[0], pw[1]};
         }
-        const float now =
-            max_over_key_groups(max2(max2(s[0], s[1]), max2(s[2], s[3]))) * a.scale_log2;
-        if (__any(!(now <= m + kSlack))) {
-          const bool need = now > m + kSlack;
-          const float f = need ? __builtin_amdgcn_exp2f(m - now) : 1.f;
-          if (need) m = now;
-          l *= f;
+        if (lane_now() == 0) flags[j & 1] = flag;
+      }
+      // The rows' references and sums.
+      const int l0 = lane_now();
+      const float sum = sum_over_key_groups(l);
+      float* sums = (float*)(lds + F::kSums) + pair * 32;
+      if (l0 < 16) {
+        sums[l0] = m;
+        sums[16 + l0] = sum;
+      }
+      wait_vmem<0>();
+      wg_barrier();  // every ring has been read
+    } else {
+      f32x4 acc[DT];
+#pragma unroll
+      for (int d = 0; d < DT; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+      for (int j = 0; j <= steps; ++j) {
+        wg_barrier();
+        if (j == 0) continue;
+        const int i = j - 1, st = i & (NST - 1);
+        const int flag = __builtin_amdgcn_readfirstlane(flags[i & 1]);
+        if (flag == 0) continue;
+        uint8_t* tile = lds + (pair * NST + st) * F::kTile;
+        const uint8_t* weights = p_at + (i & 1) * 512;
+        const int key0 = (g_begin + i * PAIRS) * kPage;
+        if (flag & 2) {
+          const float f = alphas[(i & 1) * 16 + (lane_now() & 15)];
 #pragma unroll
           for (int d = 0; d < DT; ++d) {
             acc[d] *= f;
             __builtin_amdgcn_sched_barrier(0);
           }
         }
-        // The weights enter the second product in bf16, each off by at most half a step (2^-8).
-        // Of bf16 pages the normaliser sums them as they were rounded; E4M3 tokens' scales go
-        // with their weights, and the sum is of the weights before either.
-        const float base = m == -INFINITY ? 0.f : m;
-        uint32_t pw[2];
-#pragma unroll
-        for (int e = 0; e < 4; e += 2) {
-          f32x2 y = {__builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.scale_log2, -base)),
-                     __builtin_amdgcn_exp2f(__builtin_fmaf(s[e + 1], a.scale_log2, -base))};
-          if constexpr (FP8) {
-            l += y[0] + y[1];
-            y[0] *= vs[e];
-            y[1] *= vs[e + 1];
-          }
-          pw[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2));
-          if constexpr (!FP8)
-            l += __uint_as_float(pw[e / 2] << 16) + __uint_as_float(pw[e / 2] & 0xFFFF0000u);
-        }
-        const s16x4 pf = __builtin_bit_cast(s16x4, u32x2{pw[0], pw[1]});
-        if (cut) {
-          // 0 times what a key without data holds may be NaN: it becomes 0.  So does what only
-          // some rows see and is not finite, behind its own sums for the rows that see it.
-          constexpr int CW = (FP8 ? R : 2 * R) / 16;  // chunks of a key's latent
-          auto chunk = [&](int key, int c) {
-            return (u32x4*)(tile + (key >> 3) * GROUP + (c >> 3) * 1024 + spot<FP8>(key, c & 7));
-          };
-          uint32_t nil, bad = 0;  // made here: as a constant it is kept in registers over the loop
-          asm volatile("v_mov_b32 %0, 0" : "=v"(nil));
+        if (key0 + kPage > min_lim) {
+            // 0 times what a key without data holds may be NaN: it becomes 0.  So does what only
+            // some rows see and is not finite, behind its own sums for the rows that see it.
+            constexpr int CW = (FP8 ? R : 2 * R) / 16;  // chunks of a key's latent
+            auto chunk = [&](int key, int c) {
+              return (u32x4*)(tile + (key >> 3) * GROUP + (c >> 3) * 1024 + spot<FP8>(key, c & 7));
+            };
+            uint32_t nil, bad = 0;  // made here: as a constant it is kept in registers over the loop
+            asm volatile("v_mov_b32 %0, 0" : "=v"(nil));
 #pragma unroll 1
-          for (int n = lane_now(); n < kPage * CW; n += 64) {
-            const int key = n / CW;
-            u32x4* to = chunk(key, n % CW);
-            bool odd = false;
-            if (key0 + key >= kv_lim) {
-              *to = u32x4{nil, nil, nil, nil};
-            } else if (key0 + key >= min_lim) {
+            for (int n = lane_now(); n < kPage * CW; n += 64) {
+              const int key = n / CW;
+              u32x4* to = chunk(key, n % CW);
+              bool odd = false;
+              if (key0 + key >= kv_lim) {
+                *to = u32x4{nil, nil, nil, nil};
+              } else if (key0 + key >= min_lim) {
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const uint32_t y = (*to)[e];
-                if constexpr (FP8) {
+                for (int e = 0; e < 4; ++e) {
+                  const uint32_t y = (*to)[e];
+                  if constexpr (FP8) {
 #pragma unroll
-                  for (int h = 0; h < 32; h += 8) odd |= (y >> h & 0x7F) == 0x7F;
-                } else {
-                  odd |= (y & 0x7F80) == 0x7F80 || (y >> 16 & 0x7F80) == 0x7F80;
+                    for (int h = 0; h < 32; h += 8) odd |= (y >> h & 0x7F) == 0x7F;
+                  } else {
+                    odd |= (y & 0x7F80) == 0x7F80 || (y >> 16 & 0x7F80) == 0x7F80;
+                  }
                 }
               }
-            }
-            const uint64_t hit = __ballot(odd);
-            const int key_first = __builtin_amdgcn_readfirstlane(n) / CW;
+              const uint64_t hit = __ballot(odd);
+              const int key_first = __builtin_amdgcn_readfirstlane(n) / CW;
 #pragma unroll
-            for (int k = 0; k < (CW < 64 ? 64 / CW : 1); ++k)
-              if (CW < 64 ? hit >> (k * CW % 64) & ((1ull << CW % 64) - 1) : hit)
-                bad |= 1u << (key_first + k);
-          }
+              for (int k = 0; k < (CW < 64 ? 64 / CW : 1); ++k)
+                if (CW < 64 ? hit >> (k * CW % 64) & ((1ull << CW % 64) - 1) : hit)
+                  bad |= 1u << (key_first + k);
+            }
 #pragma unroll 1
-          for (uint32_t rest = bad; rest; rest &= rest - 1) {
-            const int key = __builtin_ctz(rest);
-            // The group of lanes that has the key's weights, and which of theirs it is.
-            const int l1 = lane_now(), c16 = l1 & 15, q4 = l1 >> 4;
-            const int q = FP8 ? key >> 2 : (key >> 3) * 2 + (key & 1);
-            const int e = FP8 ? key & 3 : key >> 1 & 3;
-            const uint32_t pair = e & 2 ? pw[1] : pw[0];
-            const float wt =
-                __shfl(__uint_as_float(e & 1 ? pair & 0xFFFF0000u : pair << 16), q * 16 + c16, 64);
-            const bool seen = key0 + key < row_lim;
+            for (uint32_t rest = bad; rest; rest &= rest - 1) {
+              const int key = __builtin_ctz(rest);
+              // The group of lanes that had the key's weights, and which of theirs it is.
+              const int l1 = lane_now(), c16 = l1 & 15, q4 = l1 >> 4;
+              const int q = FP8 ? key >> 2 : (key >> 3) * 2 + (key & 1);
+              const int e = FP8 ? key & 3 : key >> 1 & 3;
+              const float wt = bf16_to_f32(*(const uint16_t*)(weights + (q * 16 + c16) * 8 + e * 2));
+              const bool seen = key0 + key < base_lim + (row0 + min(c16, rows - 1)) / a.n_heads;
 #pragma unroll
-            for (int d = 0; d < DT; ++d) {
-              const int in = (d * 16 + 4 * q4) * (FP8 ? 1 : 2);
-              const uint8_t* from = (const uint8_t*)chunk(key, in >> 4) + (in & 15);
-              f32x4 v;
-              if constexpr (FP8) {
-                const bf16x8 y = decode8(u32x2{*(const uint32_t*)from, 0});
-                v = f32x4{(float)y[0], (float)y[1], (float)y[2], (float)y[3]};
-              } else {
-                const u32x2 y = *(const u32x2*)from;
-                v = f32x4{__uint_as_float(y.x << 16), __uint_as_float(y.x & 0xFFFF0000u),
-                          __uint_as_float(y.y << 16), __uint_as_float(y.y & 0xFFFF0000u)};
+              for (int d = 0; d < DT; ++d) {
+                const int in = (d * 16 + 4 * q4) * (FP8 ? 1 : 2);
+                const uint8_t* from = (const uint8_t*)chunk(key, in >> 4) + (in & 15);
+                f32x4 v;
+                if constexpr (FP8) {
+                  const bf16x8 y = decode8(u32x2{*(const uint32_t*)from, 0});
+                  v = f32x4{(float)y[0], (float)y[1], (float)y[2], (float)y[3]};
+                } else {
+                  const u32x2 y = *(const u32x2*)from;
+                  v = f32x4{__uint_as_float(y.x << 16), __uint_as_float(y.x & 0xFFFF0000u),
+                            __uint_as_float(y.y << 16), __uint_as_float(y.y & 0xFFFF0000u)};
+                }
+                if (seen)
+#pragma unroll
+                  for (int h = 0; h < 4; ++h) acc[d][h] = __builtin_fmaf(wt, v[h], acc[d][h]);
+                __builtin_amdgcn_sched_barrier(0);
               }
-              if (seen)
-#pragma unroll
-                for (int h = 0; h < 4; ++h) acc[d][h] = __builtin_fmaf(wt, v[h], acc[d][h]);
-              __builtin_amdgcn_sched_barrier(0);
+              if (l1 < CW) *chunk(key, l1) = u32x4{nil, nil, nil, nil};
             }
-            if (l1 < CW) *chunk(key, l1) = u32x4{nil, nil, nil, nil};
           }
-        }
-        // Values, transposed.  Of E4M3 pages eight keys of a dim; the lane's four are the first or
-        // the last of them.
-        const int l3 = lane_now(), v_c = l3 & 15, v_q = l3 >> 4;
-        const int v_key = FP8 ? 8 * (v_q >> 1) + (v_c >> 1) : key_of(v_q, v_c >> 2);
-        const int v_at = (v_q >> 1) * GROUP + spot<FP8>(v_key, FP8 ? 0 : (v_c & 3) >> 1) + ((v_c & 1) << 3);
-        constexpr int D = 8;  // reads under way
-        u32x2 v[D];
-        auto read = [&](int d) {
-          if constexpr (FP8)
-            v[d % D] = __builtin_bit_cast(
-                u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                           (PDEC_LDS s32x2*)(tile + (d >> 3) * 1024 + (v_at ^ (d & 7) << 4))));
-          else
-            v[d % D] = __builtin_bit_cast(
-                u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                           (PDEC_LDS s16x4*)(tile + (d >> 2) * 1024 + (v_at ^ (d & 3) << 5))));
-        };
+          const s16x4 pf = *(const s16x4*)(weights + lane_now() * 8);
+          // Values, transposed.  Of E4M3 pages eight keys of a dim; the lane's four are the first or
+          // the last of them.
+          const int l3 = lane_now(), v_c = l3 & 15, v_q = l3 >> 4;
+          const int v_key = FP8 ? 8 * (v_q >> 1) + (v_c >> 1) : key_of(v_q, v_c >> 2);
+          const int v_at = (v_q >> 1) * GROUP + spot<FP8>(v_key, FP8 ? 0 : (v_c & 3) >> 1) + ((v_c & 1) << 3);
+          constexpr int D = 8;  // reads under way
+          u32x2 v[D];
+          auto read = [&](int d) {
+            if constexpr (FP8)
+              v[d % D] = __builtin_bit_cast(
+                  u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                             (PDEC_LDS s32x2*)(tile + (d >> 3) * 1024 + (v_at ^ (d & 7) << 4))));
+            else
+              v[d % D] = __builtin_bit_cast(
+                  u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                             (PDEC_LDS s16x4*)(tile + (d >> 2) * 1024 + (v_at ^ (d & 3) << 5))));
+          };
 #pragma unroll
-        for (int d = 0; d < D; ++d) read(d);
+          for (int d = 0; d < D; ++d) read(d);
 #pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          u32x2 y = v[d % D];
-          if constexpr (FP8) {
-            const uint32_t codes = v_q & 1 ? y.y : y.x;
-            y.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.f, false));
-            y.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.f, true));
+          for (int d = 0; d < DT; ++d) {
+            u32x2 y = v[d % D];
+            if constexpr (FP8) {
+              const uint32_t codes = v_q & 1 ? y.y : y.x;
+              y.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.f, false));
+              y.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.f, true));
+            }
+            acc[d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, y), pf, acc[d], 0, 0, 0);
+            if (d + D < DT) read(d + D);
+            __builtin_amdgcn_sched_barrier(0);
           }
-          acc[d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, y), pf, acc[d], 0, 0, 0);
-          if (d + D < DT) read(d + D);
-          __builtin_amdgcn_sched_barrier(0);
-        }
       }
-      wait_lds();  // the stage has been read
-      ok = (ok & ~(1u << st)) | (uint32_t)issue(i + NST, st) << st;
-      st = st + 1 == NST ? 0 : st + 1;
+      wg_barrier();
+      const int l0 = lane_now();
+      const float f = join_of(l0 & 15).own;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) ((f32x4*)lds)[(pair * DT + d) * 64 + l0] = acc[d] * f;
     }
 
-    // The waves' sums meet: each wave joins all four's part of a quarter of the latent, in order.
-    wait_vmem<0>();
+    // The pairs' sums meet, in order; the waves share the latent's tiles.
+    wg_barrier();
     const int l2 = lane_now(), c16 = l2 & 15, q4 = l2 >> 4;
-    float* sums = (float*)(lds + F::kSums);
-    const float sum = sum_over_key_groups(l);
-    if (q4 == 0) {
-      sums[wave * 32 + c16] = m;
-      sums[wave * 32 + 16 + c16] = sum;
-    }
-    __syncthreads();  // and every ring has been read
-    float top = -INFINITY, total = 0.f, mine_f = 0.f;
-#pragma unroll
-    for (int v = 0; v < kWaves; ++v) top = fmaxf(top, sums[v * 32 + c16]);
-#pragma unroll
-    for (int v = 0; v < kWaves; ++v) {
-      const float mv = sums[v * 32 + c16];
-      const float f = mv == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mv - top);
-      total = __builtin_fmaf(sums[v * 32 + 16 + c16], f, total);
-      if (v == wave) mine_f = f;
-    }
-    f32x4* join = (f32x4*)lds;  // [kWaves][DT][64]
-#pragma unroll
-    for (int d = 0; d < DT; ++d) join[(wave * DT + d) * 64 + l2] = acc[d] * mine_f;
-    __syncthreads();
-    const bool whole = p_begin == 0 && p_end == tiles;
-    const float inv = total == 0.f ? 0.f : 1.f / total;
+    const Join all = join_of(c16);
+    const float inv = all.sum == 0.f ? 0.f : 1.f / all.sum;
+    const f32x4* join = (const f32x4*)lds;  // [PAIRS][DT][64]
     const int64_t pr = ((int64_t)w + u) * 16 + c16;
     if (c16 < rows) {
-      if (!whole && wave == 0 && q4 == 0) *(float2*)(a.part_ml + pr * 2) = float2{top, total};
-#pragma unroll
-      for (int j = 0; j < DT / kWaves; ++j) {
-        const int d = wave * (DT / kWaves) + j;
+      if (!whole && wave == 0 && q4 == 0) *(float2*)(a.part_ml + pr * 2) = float2{all.top, all.sum};
+      for (int d = wave; d < DT; d += 2 * PAIRS) {
         f32x4 o = join[d * 64 + l2];
 #pragma unroll
-        for (int v = 1; v < kWaves; ++v) o += join[(v * DT + d) * 64 + l2];
+        for (int v = 1; v < PAIRS; ++v) o += join[(v * DT + d) * 64 + l2];
         if (whole) {
           const f32x2 lo = {o[0] * inv, o[1] * inv}, hi = {o[2] * inv, o[3] * inv};
           *(u32x2*)((uint16_t*)a.out + (q_row0 + c16) * R + d * 16 + 4 * q4) =
@@ -414,7 +455,8 @@ latent_few_kernel(LatentAttnArgs a) {
 hipError_t launch_latent_few(int fp8, int latent, int grid, const LatentAttnArgs& a,
                              hipStream_t stream) {
 #define PDEC_FEW(R_, FP8_) \
-  latent_few_kernel<R_, FP8_, latent_tile(FP8_, R_)><<<grid, kThreads, 0, stream>>>(a)
+  latent_few_kernel<R_, FP8_, latent_tile(FP8_, R_)>            \
+      <<<grid, FewForm<R_, FP8_>::kThreads, 0, stream>>>(a)
   if (latent == 512) {
     if (fp8) PDEC_FEW(512, true);
     else PDEC_FEW(512, false);
