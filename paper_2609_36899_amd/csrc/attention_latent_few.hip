@@ -19,17 +19,16 @@ template <int R, bool FP8>
 struct FewForm {
   static constexpr int kRow = FP8 ? R + 2 * kRope : (R + kRope) * 2;  // a key's bytes
   static constexpr int kTile = kPage * kRow, kStages = 4;
-  // As many pairs as four pages each fit for: 2 with bf16 latents of 512, else 3 or 4.
-  static constexpr int kPairs =
-      16 * kTile <= 144 * 1024 ? 4 : 12 * kTile <= 144 * 1024 ? 3 : 2;
-  static constexpr int kThreads = 128 * kPairs;
+  // Pairs of waves, by what four pages each leave room for: 2 with bf16 latents of 512, else 3.
+  static constexpr int kPairs = 12 * kTile <= 144 * 1024 ? 3 : 2;
+  static constexpr int kThreads = 128 * kPairs + 128;
   static constexpr int kRing = kStages * kTile * kPairs, kJoin = kPairs * 16 * R * 4;
   // LDS offsets.
   static constexpr int kScale = kRing > kJoin ? kRing : kJoin;  // [kPairs][kStages][16]
   static constexpr int kP = kScale + (FP8 ? kPairs * kStages * kPage * 4 : 0);  // [kPairs][2][64] x 8
   static constexpr int kAlpha = kP + kPairs * 2 * 512;          // [kPairs][2][16]
   static constexpr int kSums = kAlpha + kPairs * 2 * 64;        // [kPairs][2][16]
-  static constexpr int kFlag = kSums + kPairs * 2 * 64;         // [kPairs][2]: page there, rows moved
+  static constexpr int kFlag = kSums + kPairs * 2 * 64;         // [kPairs][2]: references that moved
   static constexpr int kBytes = kFlag + kPairs * 2 * 4;
   static_assert(kBytes <= 160 * 1024 - 64 && kTile % 256 == 0, "LDS layout");
 };
@@ -41,15 +40,14 @@ latent_few_kernel(LatentAttnArgs a) {
   constexpr int ROW = F::kRow, NST = F::kStages, PAIRS = F::kPairs, THREADS = F::kThreads;
   constexpr int WIN = ROW / 128, LW = (FP8 ? R : 2 * R) / 128;
   constexpr int GROUP = 8 * ROW, DT = R / 16, PPT = UNIT_TILE / kPage;
-  constexpr int NL = 2 * WIN + (FP8 ? 1 : 0);  // loads of a page
+  constexpr int NL = WIN + (FP8 ? 1 : 0);  // loads of half a page
   __shared__ __attribute__((aligned(256))) uint8_t lds[F::kBytes];
   __shared__ int red[THREADS / 64];
   __shared__ int found[2];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = blockIdx.x;
   const bool first_half = wave < PAIRS;  // the half of a pair that takes the first product
-  const int pair = first_half ? wave : wave - PAIRS;
+  const int pair = first_half ? wave : wave - PAIRS;  // the last two waves, of none, load
   const uint32_t lds0 = (uint32_t)(uintptr_t)(PDEC_LDS uint8_t*)lds;
-  const uint32_t ring = lds0 + pair * NST * F::kTile;
   float* scales = (float*)(lds + F::kScale) + pair * NST * kPage;
   uint8_t* p_at = lds + F::kP + pair * 2 * 512;
   float* alphas = (float*)(lds + F::kAlpha) + pair * 2 * 16;
@@ -121,6 +119,21 @@ latent_few_kernel(LatentAttnArgs a) {
     __syncthreads();  // the piece before is done with LDS
 
     if (first_half) {
+      // Ids of 64 of the pair's pages, one a lane.
+      int ids;
+      auto look = [&](int i0) {
+        const int n = g_begin + (i0 + lane_now()) * PAIRS;
+        ids = n < g_end ? a.block_table[(int64_t)b * a.bt_stride + n] : -1;
+        if (ids >= a.n_pages) ids = -1;
+      };
+      look(0);
+      uint32_t ok = 0;  // which stages' pages are there
+      auto note = [&](int i) {  // page i, and returns its id or -1
+        if ((i & 63) == 0 && i > 0) look(i);
+        const int id = __builtin_amdgcn_readlane(ids, i & 63);
+        ok = (ok & ~(1u << (i & (NST - 1)))) | (uint32_t)(id >= 0) << (i & (NST - 1));
+        return id;
+      };
       bf16x8 qr[2], x[(FP8 ? 4 : 2) * LW];
       int row_lim;
       {
@@ -135,60 +148,23 @@ latent_few_kernel(LatentAttnArgs a) {
 #pragma unroll
           for (int c = 0; c < 2 * LW; ++c) x[c] = *(const bf16x8*)(src + c * 32 + q4 * 8);
       }
-      // Ids of 64 of the pair's pages, one a lane.
-      int ids = -1;
-      auto look = [&](int i0) {
-        const int n = g_begin + (i0 + lane_now()) * PAIRS;
-        ids = n < g_end ? a.block_table[(int64_t)b * a.bt_stride + n] : -1;
-        if (ids >= a.n_pages) ids = -1;
-      };
-      look(0);
-      // Here the queries are waited for: their loads would wait for the pages' if later.
-#pragma unroll
-      for (int c = 0; c < 2; ++c) asm volatile("" : "+v"(qr[c]));
-#pragma unroll
-      for (int c = 0; c < (FP8 ? 4 : 2) * LW; ++c) asm volatile("" : "+v"(x[c]));
-      asm volatile("" : "+v"(ids));
-
-      // Loads of the pair's page i into stage st; one that is not there, or behind the last, is a
-      // buffer without bytes: zeros come, and count.  Returns whether it is there.
-      auto issue = [&](int i, int st) {
-        if ((i & 63) == 0 && i > 0) look(i);
-        const int id = __builtin_amdgcn_readlane(ids, i & 63);
-        const int64_t p = max(id, 0);
-        const DmaBuffer from =
-            dma_buffer((const uint8_t*)a.pages + p * F::kTile, id >= 0 ? F::kTile : 0);
-        const int l = lane_now();
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          const int voff = window_offset<FP8, ROW>(l, g);
-#pragma unroll
-          for (int n = 0; n < WIN; ++n)
-            dma16_unseen(from, voff, g * GROUP + n * 128, ring + st * F::kTile + g * GROUP + n * 1024);
-        }
-        if constexpr (FP8) {
-          const DmaBuffer f = dma_buffer(a.scales + p * kPage, id >= 0 ? kPage * 4 : 0);
-          if (l < kPage) dma4_unseen(f, l * 4, lds0 + F::kScale + (pair * NST + st) * kPage * 4);
-        }
-        return id >= 0;
-      };
-      uint32_t ok = (uint32_t)issue(0, 0);  // which stages' pages are there
-      ok |= (uint32_t)issue(1, 1) << 1;
-
       i32x8 qh[LW], ql[LW];  // of E4M3 pages
       int q_exp = 0;
       if constexpr (FP8) q_exp = split_query<LW>(x, qh, ql);
 
+      note(0);
+      note(1);
       float m = -INFINITY, l = 0.f;  // a reference for the row's scores; this lane's part of its sum
 #pragma unroll 1
       for (int j = 0; j <= steps; ++j) {
-        wg_barrier();  // the second half is done with page j - 2, and the weights of page j - 1 are there
+        wg_barrier();  // page j and the weights of page j - 1 are here, and page j - 2 has been used
         if (j == steps) break;
-        const int st = j & (NST - 1), ahead = (j + 2) & (NST - 1);
-        ok = (ok & ~(1u << ahead)) | (uint32_t)issue(j + 2, ahead) << ahead;
-        wait_vmem<2 * NL>();
-        int flag = ok >> st & 1;
-        if (flag) {
+        const int st = j & (NST - 1);
+        const int here = ok >> st & 1;
+        int moved = 0;
+        u32x2 weights = {0, 0};
+        note(j + 2);
+        if (here) {
           const uint8_t* tile = lds + (pair * NST + st) * F::kTile;
           const int key0 = (g_begin + j * PAIRS) * kPage;
           const bool cut = key0 + kPage > min_lim;
@@ -206,27 +182,27 @@ latent_few_kernel(LatentAttnArgs a) {
               return i32x8{(int)y.x, (int)y.y, (int)y.z, (int)y.w,
                            (int)z.x, (int)z.y, (int)z.z, (int)z.w};
             };
-            i32x8 k[2];  // one under way
-            auto latent = [&](int n) { return read(k_at + n * 1024 + ((q4 << 5 | (q4 & 1) << 4) ^ k_sw), 16); };
-            auto rope = [&] { return read(k_at + LW * 1024 + (q4 << 4 ^ k_sw), 64); };
-            k[0] = latent(0);
+            i32x8 k[LW + 1];
+#pragma unroll
+            for (int n = 0; n < LW; ++n)
+              k[n] = read(k_at + n * 1024 + ((q4 << 5 | (q4 & 1) << 4) ^ k_sw), 16);
+            k[LW] = read(k_at + LW * 1024 + (q4 << 4 ^ k_sw), 64);
+            __builtin_amdgcn_sched_barrier(0);  // all of them under way
 #pragma unroll
             for (int n = 0; n < LW; ++n) {
-              k[(n + 1) & 1] = n + 1 < LW ? latent(n + 1) : rope();
-              s = mx_mfma(k[n & 1], qh[n], s, q_exp);
-              s2 = mx_mfma(k[n & 1], ql[n], s2, q_exp);
-              __builtin_amdgcn_sched_barrier(0);
+              s = mx_mfma(k[n], qh[n], s, q_exp);
+              s2 = mx_mfma(k[n], ql[n], s2, q_exp);
             }
             vs = *(const f32x4*)(scales + st * kPage + 4 * q4);
             s = (s + s2) * vs;  // the latent part alone
-            const i32x8 r = k[LW & 1];
+            const i32x8 r = k[LW];
 #pragma unroll
             for (int c = 0; c < 2; ++c)
               s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
                   __builtin_bit_cast(bf16x8, i32x4{r[4 * c], r[4 * c + 1], r[4 * c + 2], r[4 * c + 3]}),
                   qr[c], s, 0, 0, 0);
           } else {
-            constexpr int N = 2 * LW + 2, D = 4;  // reads; of them under way
+            constexpr int N = 2 * LW + 2, D = 10;  // reads; of them under way
             bf16x8 k[D];
             auto read = [&](int c) {
               k[c % D] = *(const bf16x8*)(tile + (k_at ^ (c & 1) << 6) + (c >> 1) * 1024);
@@ -261,7 +237,7 @@ latent_few_kernel(LatentAttnArgs a) {
             if (need) m = now;
             l *= f;
             if (q4 == 0) alphas[(j & 1) * 16 + c16] = f;
-            flag = 3;
+            moved = 1;
           }
           // The weights enter the second product in bf16, each off by at most half a step (2^-8).
           // Of bf16 pages the normaliser sums them as they were rounded; E4M3 tokens' scales go
@@ -281,9 +257,11 @@ latent_few_kernel(LatentAttnArgs a) {
             if constexpr (!FP8)
               l += __uint_as_float(pw[e / 2] << 16) + __uint_as_float(pw[e / 2] & 0xFFFF0000u);
           }
-          *(u32x2*)(p_at + (j & 1) * 512 + l1 * 8) = u32x2{pw[0], pw[1]};
+          weights = u32x2{pw[0], pw[1]};
         }
-        if (lane_now() == 0) flags[j & 1] = flag;
+        const int l2 = lane_now();
+        *(u32x2*)(p_at + (j & 1) * 512 + l2 * 8) = weights;
+        if (l2 == 0) flags[j & 1] = moved;
       }
       // The rows' references and sums.
       const int l0 = lane_now();
@@ -293,23 +271,65 @@ latent_few_kernel(LatentAttnArgs a) {
         sums[l0] = m;
         sums[16 + l0] = sum;
       }
+      wg_barrier();  // every ring has been read, and no load is in flight
+    } else if (wave >= 2 * PAIRS) {
+      // A loader, of half of every page's keys.  Ids of 256 of the piece's pages, four a lane:
+      // looking for more waits for the pages in flight.
+      const int g = wave - 2 * PAIRS, lane = lane_now(), offset = window_offset<FP8, ROW>(lane, g);
+      int ids[4];
+      // Every pair's page j into its ring.  A page that is not there, or behind the last, is a
+      // buffer without bytes: zeros come, and count.
+      auto load = [&](int j) {
+#pragma unroll
+        for (int k = 0; k < PAIRS; ++k) {
+          const int i = j * PAIRS + k, st = j & (NST - 1);
+          if ((i & 255) == 0)
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+              const int n = p_begin * PPT + i + h * 64 + lane;
+              ids[h] = n < g_end ? a.block_table[(int64_t)b * a.bt_stride + n] : -1;
+              if (ids[h] >= a.n_pages) ids[h] = -1;
+            }
+          const int which = i >> 6 & 3, at = i & 63;
+          const int id = __builtin_amdgcn_readlane(
+              which == 0 ? ids[0] : which == 1 ? ids[1] : which == 2 ? ids[2] : ids[3], at);
+          const int64_t p = max(id, 0);
+          const DmaBuffer from =
+              dma_buffer((const uint8_t*)a.pages + p * F::kTile, id >= 0 ? F::kTile : 0);
+          const uint32_t to = lds0 + (k * NST + st) * F::kTile + g * GROUP;
+#pragma unroll
+          for (int n = 0; n < WIN; ++n) dma16_unseen(from, offset, g * GROUP + n * 128, to + n * 1024);
+          if constexpr (FP8) {
+            const DmaBuffer f = dma_buffer(a.scales + p * kPage + g * 8, id >= 0 ? 32 : 0);
+            if (lane < 8)
+              dma4_unseen(f, lane * 4, lds0 + F::kScale + ((k * NST + st) * kPage + g * 8) * 4);
+          }
+        }
+      };
+      load(0);
+      load(1);
+#pragma unroll 1
+      for (int j = 0; j <= steps; ++j) {
+        wait_vmem<PAIRS * NL>();  // the pages j are here
+        wg_barrier();
+        if (j < steps) load(j + 2);
+      }
       wait_vmem<0>();
-      wg_barrier();  // every ring has been read
+      wg_barrier();
     } else {
       f32x4 acc[DT];
 #pragma unroll
       for (int d = 0; d < DT; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+      wg_barrier();
 #pragma unroll 1
-      for (int j = 0; j <= steps; ++j) {
+      for (int j = 1; j <= steps; ++j) {  // page i; one that is not there is zeros, and so are its weights
         wg_barrier();
-        if (j == 0) continue;
         const int i = j - 1, st = i & (NST - 1);
-        const int flag = __builtin_amdgcn_readfirstlane(flags[i & 1]);
-        if (flag == 0) continue;
+        const int moved = __builtin_amdgcn_readfirstlane(flags[i & 1]);
         uint8_t* tile = lds + (pair * NST + st) * F::kTile;
         const uint8_t* weights = p_at + (i & 1) * 512;
         const int key0 = (g_begin + i * PAIRS) * kPage;
-        if (flag & 2) {
+        if (moved) {
           const float f = alphas[(i & 1) * 16 + (lane_now() & 15)];
 #pragma unroll
           for (int d = 0; d < DT; ++d) {
@@ -403,19 +423,29 @@ latent_few_kernel(LatentAttnArgs a) {
 #pragma unroll
           for (int d = 0; d < D; ++d) read(d);
 #pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            u32x2 y = v[d % D];
-            if constexpr (FP8) {
-              const uint32_t codes = v_q & 1 ? y.y : y.x;
-              y.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.f, false));
-              y.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.f, true));
+          for (int d0 = 0; d0 < DT; d0 += 4) {
+            u32x2 y[4];
+#pragma unroll
+            for (int h = 0; h < 4; ++h) y[h] = v[(d0 + h) % D];
+            if constexpr (FP8)
+#pragma unroll
+              for (int h = 0; h < 4; ++h) {
+                const uint32_t codes = v_q & 1 ? y[h].y : y[h].x;
+                y[h].x = __builtin_bit_cast(
+                    uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.f, false));
+                y[h].y = __builtin_bit_cast(
+                    uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.f, true));
+              }
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+              acc[d0 + h] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
+                  __builtin_bit_cast(s16x4, y[h]), pf, acc[d0 + h], 0, 0, 0);
+              if (d0 + h + D < DT) read(d0 + h + D);
             }
-            acc[d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, y), pf, acc[d], 0, 0, 0);
-            if (d + D < DT) read(d + D);
             __builtin_amdgcn_sched_barrier(0);
           }
       }
-      wg_barrier();
+      wg_barrier();  // every ring has been read, and no load is in flight
       const int l0 = lane_now();
       const float f = join_of(l0 & 15).own;
 #pragma unroll
@@ -431,7 +461,7 @@ latent_few_kernel(LatentAttnArgs a) {
     const int64_t pr = ((int64_t)w + u) * 16 + c16;
     if (c16 < rows) {
       if (!whole && wave == 0 && q4 == 0) *(float2*)(a.part_ml + pr * 2) = float2{all.top, all.sum};
-      for (int d = wave; d < DT; d += 2 * PAIRS) {
+      for (int d = wave; d < DT; d += THREADS / 64) {
         f32x4 o = join[d * 64 + l2];
 #pragma unroll
         for (int v = 1; v < PAIRS; ++v) o += join[(v * DT + d) * 64 + l2];
