@@ -82,7 +82,7 @@ latent_attn_kernel(LatentAttnArgs a) {
     }
   } else {
     const Stretch mine = stretch_of<kThreads>(a.n_units, a.n_groups, a.min_tiles, w, red, found,
-                                              [&](int v) { return unit_tiles<TILE>(a, v); });
+                                              [&](int v) { return unit_size<TILE>(a, v); });
     at = w * mine.per;
     if (at >= mine.total) return;
     end = min(at + mine.per, mine.total);
@@ -106,17 +106,17 @@ latent_attn_kernel(LatentAttnArgs a) {
   };
 
   for (; at < end; ++u) {
-    const int tiles = unit_tiles<TILE>(a, u);
-    if (first + tiles <= at) {  // empty unit
-      first += tiles;
-      continue;
-    }
+    const int tiles = unit_tiles<TILE>(a, u), size = unit_size<TILE>(a, u);
+    const int body = first + size - tiles;  // where its tiles begin
+    first += size;
+    const int p_begin = max(at - body, 0), p_end = min(tiles, end - body);
+    at = min(max(first, at), end);
+    if (p_end <= p_begin) continue;  // an empty unit, or no tile of it
     const int b = u / a.blocks_per_seq, row0 = unit_row0(a, u), rows = unit_rows(a, row0);
     const int base_lim = clamp_len(a, b) - a.n_q + 1;  // keys that token 0 sees
     const int kv_lim = max(base_lim + (row0 + rows - 1) / a.n_heads, 0);
     const int min_lim = max(base_lim + row0 / a.n_heads, 0);  // keys that every row sees
     const int n_pages = (kv_lim + kPage - 1) / kPage;
-    const int p_begin = at - first, p_end = min(tiles, end - first);
     const int64_t q_row0 = (int64_t)b * a.n_q * a.n_heads + row0;
 
     // The ids of 64 pages from page0 on, in LDS (each wave puts the same there), and which of
@@ -549,8 +549,6 @@ latent_attn_kernel(LatentAttnArgs a) {
         for (int d = 0; d < DT; ++d) *(f32x4*)(o + d * 16) = acc[t][d];
       }
     }
-    at = first + p_end;
-    first += tiles;
   }
   wait_vmem<0>();  // no LDS write may still be in flight when the group ends
 }
@@ -572,7 +570,7 @@ __global__ __launch_bounds__(512) void latent_merge_kernel(LatentAttnArgs a, int
   if (row_begin >= row_end) return;
   int all = 0, before = 0;
   for (int v = threadIdx.x; v < a.n_units; v += 512) {
-    const int n = unit_tiles<TILE>(a, v);
+    const int n = unit_size<TILE>(a, v);
     all += n;
     before += v < u ? n : 0;
   }
@@ -590,8 +588,8 @@ __global__ __launch_bounds__(512) void latent_merge_kernel(LatentAttnArgs a, int
     first += red[1][i];
   }
   const int per = max((total + a.n_groups - 1) / a.n_groups, a.min_tiles);
-  const int tiles = unit_tiles<TILE>(a, u), w0 = first / per;
-  const int w1 = tiles > 0 ? (first + tiles - 1) / per : w0 - 1;
+  const int tiles = unit_tiles<TILE>(a, u), body = first + unit_head<TILE>(a), w0 = body / per;
+  const int w1 = tiles > 0 ? (body + tiles - 1) / per : w0 - 1;
   if (tiles > 0 && w0 == w1) return;
   const int lane = threadIdx.x % L, part = threadIdx.x / L;
   float m, l;

@@ -66,7 +66,7 @@ latent_few_kernel(LatentAttnArgs a) {
     }
   } else {
     const Stretch mine = stretch_of<THREADS>(a.n_units, a.n_groups, a.min_tiles, w, red, found,
-                                              [&](int v) { return unit_tiles<UNIT_TILE>(a, v); });
+                                              [&](int v) { return unit_size<UNIT_TILE>(a, v); });
     at = w * mine.per;
     if (at >= mine.total) return;
     end = min(at + mine.per, mine.total);
@@ -100,17 +100,17 @@ latent_few_kernel(LatentAttnArgs a) {
   };
 
   for (; at < end; ++u) {
-    const int tiles = unit_tiles<UNIT_TILE>(a, u);
-    if (first + tiles <= at) {  // empty unit
-      first += tiles;
-      continue;
-    }
+    const int tiles = unit_tiles<UNIT_TILE>(a, u), size = unit_size<UNIT_TILE>(a, u);
+    const int body = first + size - tiles;  // where its tiles begin
+    first += size;
+    const int p_begin = max(at - body, 0), p_end = min(tiles, end - body);
+    at = min(max(first, at), end);
+    if (p_end <= p_begin) continue;  // an empty unit, or no tile of it
     const int b = u / a.blocks_per_seq, row0 = unit_row0(a, u), rows = unit_rows(a, row0);
     const int base_lim = clamp_len(a, b) - a.n_q + 1;  // keys that token 0 sees
     const int kv_lim = max(base_lim + (row0 + rows - 1) / a.n_heads, 0);
     const int min_lim = max(base_lim + row0 / a.n_heads, 0);  // keys that every row sees
     const int n_pages = (kv_lim + kPage - 1) / kPage;
-    const int p_begin = at - first, p_end = min(tiles, end - first);
     const int64_t q_row0 = (int64_t)b * a.n_q * a.n_heads + row0;
     // The pair's pages: g_begin, g_begin + PAIRS ...; a step takes one of each pair's.
     const int g_begin = p_begin * PPT + pair, g_end = min(p_end * PPT, n_pages);
@@ -475,8 +475,6 @@ latent_few_kernel(LatentAttnArgs a) {
         }
       }
     }
-    at = first + p_end;
-    first += tiles;
   }
 }
 

@@ -42,6 +42,21 @@ __device__ __forceinline__ int unit_tiles(const LatentAttnArgs& a, int u) {
   return (unit_keys(a, u) + TILE - 1) / TILE;
 }
 
+// A piece of a unit costs as much as some 256 keys before its first tile and after its last (its
+// queries, its first pages' way, its output): the units are laid end to end with so much ahead of
+// each, so that a group with two pieces has less of them.  us without / with: 128 heads over 64 x
+// 1K to 8K bf16 CC_A, 32 heads x 4 tokens over 8 x 64K to 128K E4M3 CC_B, 16 heads over 64 x 1K to
+// 8K E4M3 CC_C.
+template <int TILE>
+__device__ __forceinline__ int unit_head(const LatentAttnArgs& a) {
+  return a.unit_groups ? 0 : 256 / TILE;
+}
+template <int TILE>
+__device__ __forceinline__ int unit_size(const LatentAttnArgs& a, int u) {
+  const int n = unit_tiles<TILE>(a, u);
+  return n > 0 ? n + unit_head<TILE>(a) : 0;
+}
+
 // Eight codes (code i in byte i of the two dwords) to bf16, exactly.
 __device__ __forceinline__ bf16x8 decode8(u32x2 w) {
   const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.x, 1.f, false);
