@@ -51,28 +51,32 @@ __device__ __forceinline__ int block_tiles(const Seq& s, int blk) {
   const int keys = s.nk - s.nq + min((blk + 1) * ROWS, s.nq);
   return max((keys + TILE - 1) / TILE, 1);
 }
-// Tiles of the blocks before blk: of each whole block ROWS / TILE more than of the one before.
+// The same and what a piece of a block costs beside its tiles (its queries, the first tiles' way,
+// its output), in tiles, which the split counts ahead of each block's.  us at 0 / 4 / 12: 20 heads
+// over 4096 150 / 144 / 146, 32 heads over five turns 186 / 189 / 191.
+constexpr int kHead = 4;
+// That of the blocks before blk: of each whole block ROWS / TILE more than of the one before.
 template <int ROWS, int TILE>
-__device__ __forceinline__ int tiles_before(const Seq& s, int blk) {
+__device__ __forceinline__ int size_before(const Seq& s, int blk) {
   constexpr int K = ROWS / TILE;
   static_assert(K * TILE == ROWS && (TILE & (TILE - 1)) == 0, "whole tiles a block");
   const int full = s.nq / ROWS, n = min(blk, full);
   const int base = (s.nk - s.nq + TILE - 1) & -TILE, first = base / TILE;  // rounded up
   const int ones = min(max(-first / K, 0), n);  // blocks that no key is seen of
-  const int sum = ones + (n - ones) * first + K * (n * (n + 1) - ones * (ones + 1)) / 2;
+  const int sum = kHead * blk + ones + (n - ones) * first + K * (n * (n + 1) - ones * (ones + 1)) / 2;
   return blk > full ? sum + block_tiles<ROWS, TILE>(s, full) : sum;
 }
 template <int ROWS, int TILE>
-__device__ __forceinline__ int seq_tiles(const Seq& s) {
-  return tiles_before<ROWS, TILE>(s, (s.nq + ROWS - 1) / ROWS);
+__device__ __forceinline__ int seq_size(const Seq& s) {
+  return size_before<ROWS, TILE>(s, (s.nq + ROWS - 1) / ROWS);
 }
 // The block that tile `at` of a sequence's lies in.
 template <int ROWS, int TILE>
 __device__ __forceinline__ int block_of(const Seq& s, int at) {
-  int lo = 0, hi = (s.nq + ROWS - 1) / ROWS;  // tiles_before(lo) <= at < tiles_before(hi)
+  int lo = 0, hi = (s.nq + ROWS - 1) / ROWS;  // size_before(lo) <= at < size_before(hi)
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (tiles_before<ROWS, TILE>(s, mid) <= at) lo = mid;
+    if (size_before<ROWS, TILE>(s, mid) <= at) lo = mid;
     else hi = mid;
   }
   return lo;
@@ -99,7 +103,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn_kernel(LatentPromptAr
   const Stretch mine = stretch_of<kThreads>(
       a.n_seqs, gridDim.y, a.block_groups ? 1 : a.min_tiles, w, red, found, [&](int b) {
         const Seq s = seq_of(a, b);
-        return a.block_groups ? (s.nq + kRows - 1) / kRows : seq_tiles<kRows, kTile>(s);
+        return a.block_groups ? (s.nq + kRows - 1) / kRows : seq_size<kRows, kTile>(s);
       });
   int at = w * mine.per;
   if (at >= mine.total) return;
@@ -113,7 +117,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn_kernel(LatentPromptAr
     end = block_tiles<kRows, kTile>(s, blk);
   } else {
     blk = block_of<kRows, kTile>(s, at - first);
-    first += tiles_before<kRows, kTile>(s, blk);
+    first += size_before<kRows, kTile>(s, blk);
   }
 
   // The lane's number, made where it is used: what is computed from threadIdx.x ahead of the
@@ -155,7 +159,11 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn_kernel(LatentPromptAr
       continue;
     }
     const int tiles = block_tiles<kRows, kTile>(s, blk);
-    const int p_begin = max(at - first, 0), p_end = min(tiles, end - first);
+    const int body = first + (a.block_groups ? 0 : kHead);  // where its tiles begin
+    first = body + tiles;
+    const int p_begin = max(at - body, 0), p_end = min(tiles, end - body);
+    at = min(first, end);
+    if (p_end <= p_begin) continue;  // no tile of it
     const int base_lim = s.nk - s.nq + 1;  // keys that row 0 of the sequence sees
     const int row0 = blk * kRows + wave * 32;
     const int min_lim = base_lim + row0;   // keys that every row of the wave sees
@@ -386,7 +394,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn_kernel(LatentPromptAr
         }
       } else {
         // The group's first piece, or the one that begins in it and goes on.
-        const int64_t pr = (((int64_t)w * 2 + (first + p_begin != w * mine.per)) * a.n_heads + h) * kRows +
+        const int64_t pr = (((int64_t)w * 2 + (body + p_begin != w * mine.per)) * a.n_heads + h) * kRows +
                            row - blk * kRows;
         if (q4 == 0) *(float2*)(a.part_ml + pr * 2) = float2{m[t], l};
         float* o = a.part_acc + pr * DIM + 4 * q4;
@@ -394,8 +402,6 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn_kernel(LatentPromptAr
         for (int d = 0; d < DT; ++d) *(f32x4*)(o + d * 16) = acc[t][d];
       }
     }
-    at = first + p_end;
-    first += tiles;
   }
   wait_vmem<0>();  // no LDS write may still be in flight when the group ends
 }
@@ -410,17 +416,17 @@ __global__ __launch_bounds__(512) void prompt_merge_kernel(LatentPromptArgs a, i
   __shared__ int found[2];
   const int w = blockIdx.z, h = blockIdx.x;
   const Stretch mine = stretch_of<512>(a.n_seqs, n_groups, a.min_tiles, w, red, found, [&](int b) {
-    return seq_tiles<kRows, kTile>(seq_of(a, b));
+    return seq_size<kRows, kTile>(seq_of(a, b));
   });
   const int at = w * mine.per;
   if (at >= mine.total) return;
   const int end = min(at + mine.per, mine.total);
   const Seq s = seq_of(a, min(max(mine.unit, 0), a.n_seqs - 1));
   const int blk = block_of<kRows, kTile>(s, at - mine.first);
-  const int first = mine.first + tiles_before<kRows, kTile>(s, blk);
+  const int body = mine.first + size_before<kRows, kTile>(s, blk) + kHead;
   const int tiles = block_tiles<kRows, kTile>(s, blk);
-  if (blk * kRows >= s.nq || first >= at || first + tiles > end) return;
-  const int lane = threadIdx.x % L, w0 = first / mine.per;
+  if (blk * kRows >= s.nq || body >= at || body + tiles > end) return;
+  const int lane = threadIdx.x % L, w0 = body / mine.per;
   const int row_end = min(kRows, s.nq - blk * kRows);
   for (int row = blockIdx.y * RB + threadIdx.x / L; row < row_end; row += gridDim.y * RB) {
     float m = -INFINITY, l = 0.f;
@@ -433,7 +439,7 @@ __global__ __launch_bounds__(512) void prompt_merge_kernel(LatentPromptArgs a, i
         if (v + i <= w) {
           const int g = v + i;
           const int64_t pr =
-              (((int64_t)g * 2 + (g == w0 && first != w0 * mine.per)) * a.n_heads + h) * kRows + row;
+              (((int64_t)g * 2 + (g == w0 && body != w0 * mine.per)) * a.n_heads + h) * kRows + row;
           ml[i] = *(const float2*)(a.part_ml + pr * 2);
           x[i] = *(const f32x4*)(a.part_acc + pr * DIM + lane * 4);
         }

@@ -42,14 +42,14 @@ __device__ __forceinline__ int unit_tiles(const LatentAttnArgs& a, int u) {
   return (unit_keys(a, u) + TILE - 1) / TILE;
 }
 
-// A piece of a unit costs as much as some 256 keys before its first tile and after its last (its
-// queries, its first pages' way, its output): the units are laid end to end with so much ahead of
+// A piece of a unit costs as much as some tiles before its first one and after its last (its
+// queries, its first pages' way, its output): the units are laid end to end with so many ahead of
 // each, so that a group with two pieces has less of them.  us without / with: 128 heads over 64 x
-// 1K to 8K bf16 CC_A, 32 heads x 4 tokens over 8 x 64K to 128K E4M3 CC_B, 16 heads over 64 x 1K to
-// 8K E4M3 CC_C.
+// 1K to 8K bf16 154 / 131, 32 heads x 4 tokens over 8 x 64K to 128K E4M3 230 / 214, 16 heads over
+// 64 x 1K to 8K E4M3 54 / 50; with half as many 135, 224 and 53.
 template <int TILE>
 __device__ __forceinline__ int unit_head(const LatentAttnArgs& a) {
-  return a.unit_groups ? 0 : 256 / TILE;
+  return a.unit_groups ? 0 : TILE == 64 ? 6 : 8;
 }
 template <int TILE>
 __device__ __forceinline__ int unit_size(const LatentAttnArgs& a, int u) {
