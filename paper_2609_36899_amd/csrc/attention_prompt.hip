@@ -59,11 +59,14 @@ constexpr int kHead = 4;
 template <int ROWS, int TILE>
 __device__ __forceinline__ int size_before(const Seq& s, int blk) {
   constexpr int K = ROWS / TILE;
-  static_assert(K * TILE == ROWS && (TILE & (TILE - 1)) == 0, "whole tiles a block");
+  static_assert(K * TILE == ROWS && K % 2 == 0 && (TILE & (TILE - 1)) == 0, "whole tiles a block");
   const int full = s.nq / ROWS, n = min(blk, full);
   const int base = (s.nk - s.nq + TILE - 1) & -TILE, first = base / TILE;  // rounded up
   const int ones = min(max(-first / K, 0), n);  // blocks that no key is seen of
-  const int sum = kHead * blk + ones + (n - ones) * first + K * (n * (n + 1) - ones * (ones + 1)) / 2;
+  // Modulo 2^32, where terms of a sequence with more rows than keys may be large.
+  const uint32_t live = n - ones;
+  const int sum = (int)(kHead * (uint32_t)blk + ones + live * (uint32_t)first +
+                        K / 2 * live * (uint32_t)(n + ones + 1));
   return blk > full ? sum + block_tiles<ROWS, TILE>(s, full) : sum;
 }
 template <int ROWS, int TILE>

@@ -177,13 +177,18 @@ int64_t paged_latent_attention_workspace_bytes(int32_t kv_dtype, int32_t batch, 
   if (rc != PDEC_OK) return rc;
   if (max_pages < 1 || max_pages > kMaxStride) return fail(PDEC_INVALID_ARG, "bad max_pages");
   // Fewer sequences, tokens or pages of the same take blocks of as many row tiles or fewer, and
-  // as many units or fewer, but have partials where these units may be too many to have any.
+  // as many units or fewer, but have partials where these units may be too many to have any:
+  // those of blocks of one row tile, a sequence each, up to more units than others.
   const int64_t max_len = (int64_t)max_pages * PDEC_PAGE_TOKENS;
   const LatentPlan p = plan_latent_attention(
       batch, n_q, n_heads, max_len, latent_tile(kv_dtype == PDEC_FP8_E4M3, latent_dim));
-  if (p.unit_groups && p.n_units < kLatentUnits) return 0;  // no table is long
-  const Layout l = layout_of(std::min(p.n_units, kLatentUnits - 1), p, latent_dim);
-  return l.ml + l.acc;
+  if (p.unit_groups && p.n_units < latent_units(p.row_tiles)) return 0;  // no table is long
+  LatentPlan few = p;
+  few.row_tiles = 1;
+  const Layout l =
+      layout_of(std::min(p.n_units, latent_units(p.row_tiles) - 1), p, latent_dim);
+  const Layout f = layout_of(std::min<int64_t>(batch, latent_units(1) - 1), few, latent_dim);
+  return std::max(l.ml + l.acc, f.ml + f.acc);
 }
 
 int paged_latent_attention(int32_t kv_dtype, int32_t batch, int32_t n_q, int32_t n_heads,
@@ -238,9 +243,8 @@ int64_t latent_prompt_attention_workspace_bytes(int32_t n_rows, int32_t n_seqs, 
                                                 int32_t head_dim) {
   const int rc = check_prompt(n_rows, n_seqs, n_heads, head_dim);
   if (rc != PDEC_OK) return rc;
-  PromptPlan p = plan_latent_prompt(n_rows, n_seqs, n_heads);
-  if (p.block_groups) p = plan_latent_prompt(0, 1, n_heads);  // what fewer rows would take
-  const Layout l = layout_of(p, n_heads, head_dim);
+  // Whatever n_keys is, and what fewer rows would take.
+  const Layout l = layout_of(plan_latent_prompt(0, 0, 1, n_heads), n_heads, head_dim);
   return l.ml + l.acc;
 }
 
@@ -273,9 +277,9 @@ int latent_prompt_attention(int32_t n_rows, int32_t n_keys, int32_t n_seqs, int3
     return fail(PDEC_INVALID_ARG, "rows, heads, out and workspace must be 16-byte aligned");
   if (k_stride > kMaxRowStride || v_stride > kMaxRowStride || rope_stride > kMaxRowStride)
     return fail(PDEC_INVALID_ARG, "rows further than 2^24 elements apart");
-  const PromptPlan p = plan_latent_prompt(n_rows, n_seqs, n_heads);
-  // A block and a tile are at least 128 rows and 32 keys.
-  if (((int64_t)n_rows / 128 + n_seqs) * ((int64_t)n_keys / 32 + 2) > INT32_MAX ||
+  const PromptPlan p = plan_latent_prompt(n_rows, n_keys, n_seqs, n_heads);
+  // Blocks are of 128 rows, tiles of 32 keys, and four count for what a block costs beside.
+  if (((int64_t)n_rows / 128 + n_seqs) * ((int64_t)n_keys / 32 + 6) > INT32_MAX ||
       (int64_t)p.n_groups * n_heads * 512 > kMaxLaunch)
     return fail(PDEC_INVALID_ARG, "too many rows and keys for one call");
   const Layout l = layout_of(p, n_heads, head_dim);

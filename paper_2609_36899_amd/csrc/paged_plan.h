@@ -20,7 +20,6 @@ namespace pdec {
 // slow as 256.
 constexpr int kAttnGroups = 256;
 
-constexpr int64_t kLatentUnits = 512;  // units from which each has a work group of its own
 
 struct PagedAttnPlan {
   int32_t row_tiles, tok_per_block, blocks_per_seq, n_groups;
@@ -80,6 +79,11 @@ struct LatentPlan {
   int64_t n_units;
   bool unit_groups;  // a work group for each unit and no merge, instead of equal stretches
 };
+// Units from which each has a work group of its own.  us in equal stretches / in groups of their
+// own: 16 heads, E4M3, 128 x 0.5K to 4K 51 / 90, 512 of them 138 / 164, 1024 x 0.2K to 2K 163 /
+// 175, 1024 x 16 to 256 61 / 61; 128 heads, bf16, 256 x 0.5K to 4K 200 / 251, 512 x 0.2K to 2K 231
+// / 228.  Beyond, the partials of equal stretches only take more room.
+inline int64_t latent_units(int row_tiles) { return row_tiles == 1 ? 2048 : 512; }
 // max_len: what no sequence can be longer than; tile: keys of a tile.
 inline LatentPlan plan_latent_attention(int batch, int n_q, int n_heads, int64_t max_len, int tile) {
   LatentPlan p;
@@ -91,7 +95,7 @@ inline LatentPlan plan_latent_attention(int batch, int n_q, int n_heads, int64_t
   p.blocks_per_seq = (int32_t)((rows + p.block_rows - 1) / p.block_rows);
   p.n_units = (int64_t)batch * p.blocks_per_seq;
   p.n_groups = kAttnGroups;
-  p.unit_groups = p.n_units >= kLatentUnits || max_len <= 4 * tile;
+  p.unit_groups = p.n_units >= latent_units(p.row_tiles) || max_len <= 4 * tile;
   return p;
 }
 
@@ -102,10 +106,15 @@ struct PromptPlan {
   int32_t n_groups;  // a head
   bool block_groups;
 };
-inline PromptPlan plan_latent_prompt(int64_t n_rows, int64_t n_seqs, int n_heads) {
+// A group for each block, where there are enough of them: prompts' blocks differ in length, and
+// the long ones begin first; behind long contexts they are alike, and the last ones leave units
+// idle.  us in equal stretches / in groups of their own, blocks of all heads: 4096 tokens x 16
+// heads 131 / 139 (512), x 32 heads 224 / 204 (1024), x 64 heads 402 / 363 (2048); 8192 x 32 735 /
+// 641 (2048); 8 x 256 behind 2000 each, 128 heads 474 / 413 (2048 and more).
+inline PromptPlan plan_latent_prompt(int64_t n_rows, int64_t n_keys, int64_t n_seqs, int n_heads) {
   PromptPlan p;
   const int64_t blocks = n_rows / kPromptRows + n_seqs;  // at most
-  p.block_groups = blocks * n_heads >= 2048 && blocks <= 65535;
+  p.block_groups = blocks * n_heads >= (n_keys <= 2 * n_rows ? 1024 : 2048) && blocks <= 65535;
   p.n_groups = p.block_groups ? (int32_t)blocks
                               : (int32_t)std::max<int64_t>(1, std::min<int64_t>(65535, 512 / n_heads));
   return p;
