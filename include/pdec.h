@@ -723,9 +723,11 @@ int paged_latent_append(int32_t src_dtype, int32_t kv_dtype, int32_t n_rows, int
  *   [batch][n_q][n_heads][latent_dim]; lens: device int32 [batch], counting the
  *   n_q tokens, taken as in [0, bt_stride * 16]; a token that sees no key gets
  *   zeros.  Tokens whose page id is outside [0, n_pages) are no keys.
- *   Scores, softmax and sums are fp32; the weights enter the second product
- *   rounded to bf16, with the token's scale, once more where that is no power of
- *   two.
+ *   Scores, softmax and sums are fp32; the weights, times the token's scale,
+ *   enter the second product rounded to bf16.  Of E4M3 pages the latent part of
+ *   a query is taken as the sum of two E4M3 numbers with a power of two for the
+ *   row: exact but for elements below 2^-10 of the row's largest, which lose at
+ *   most 2^-17 of it, and an infinite element makes its row's scores NaN.
  *   workspace: device, paged_latent_attention_workspace_bytes(...) bytes for the
  *   same or larger batch, n_q and max_pages (bt_stride); it may be null where
  *   these are 0 (no table is long).

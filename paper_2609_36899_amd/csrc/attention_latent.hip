@@ -8,7 +8,7 @@
 // blocks of up to 128, a unit each; a tile of 32 or 64 keys comes into LDS once for the block.
 // Per key 2 (2 R + 64) operations a row stand against (R + 64) 2 bytes (bf16), R + 132 (E4M3):
 // at R = 512 HBM bounds blocks of up to some 64 rows (E4M3) or 115 (bf16), the matrix units
-// more.
+// more.  Units of at most 16 rows are attention_latent_few.hip's.
 //
 // Work split.  The units' tiles laid end to end are cut into n_groups equal stretches, one for
 // each work group, found from the lengths on the device (stretch.h).  The piece of unit u in
@@ -16,12 +16,19 @@
 // unit that one group covers whole is written out at once, and where there are many units, or
 // none can be long, each has a group of its own.
 //
-// One tile.  S^T = K Q^T with the waves along rows and keys, then the weights P go through LDS
-// and every wave multiplies all of the block's P by its eighth of the latent's width: O^T =
-// C^T P^T.  So O takes 16 registers a row tile instead of 128, and each latent is read from
-// LDS once in the second product, transposed by the read itself (ds_read_tr).  The tiles come
-// by LDS-DMA into a ring of stages, 16-byte chunk n of a key's row in place n ^ (key & 7) of
-// its 128 bytes, so that eight lanes reading the same chunk of eight keys meet all banks.
+// One step.  S^T = K Q^T of tile p, a wave a row tile, whose weights P go through LDS; beside
+// it the second product of tile p - 1, by every wave for its eighth of the latent's width: O^T =
+// C^T P^T.  So O takes 16 registers a row tile instead of 128, and each latent is read from LDS
+// once in the second product, transposed by the read itself (ds_read_tr).  Neither product of a
+// step needs the other's: half the waves take one first, half the other, and one barrier a step
+// serves both.  E4M3 codes enter the first product as they are, against queries split in two;
+// the second takes them decoded to bf16.
+//
+// The tiles come by LDS-DMA into a ring of three stages, by the four waves that wait at the
+// barrier otherwise (all eight: 189 against 182 us).  Nothing is spilled in the loop: a reload
+// would wait, as loads return in order, for the tile on its way (128 heads 584 us with spills,
+// 192 without).  128 heads over 64 x 1K to 8K bf16 131 us (0.66 PFLOP/s; steps 111, the pieces'
+// beginnings and ends, the merge 20), 32 heads x 4 tokens over 8 x 64K to 128K E4M3 218 (0.93).
 #include "latent_attn.h"
 
 #include <algorithm>

@@ -8,7 +8,9 @@
 // Append.  c = x * rsqrt(mean(x^2) + eps) * gain over the row's first R elements, rounded once,
 // to the page's type; the last 64 are rotated at the token's position, as are 64 elements of
 // each query head.  A wave takes a row's latent and key, or eight query heads of a row; each
-// finds its sequence, page and slot by itself.
+// finds its sequence, page and slot by itself.  Bound by memory: 4096 rows from fp32, with 32
+// heads' queries, 65 MB in 14 us (4.6 TB/s); 64 rows 4.5 us, the chain of looks from a row to
+// its page.
 //
 // Gather.  Bound by memory (a row's 1152 or 644 bytes read, 1152 written), and for few rows by the
 // chain of looks from a row to its page, which the lanes go at once, one a row.  A wave takes four
