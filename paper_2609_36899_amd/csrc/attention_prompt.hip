@@ -24,6 +24,7 @@
 // one's weights in each wave, heads gathered by die, the loads one by one between the products.
 #include "hip_common.h"
 #include "kernels.h"
+#include "lds_dma.h"
 #include "stretch.h"
 
 #include <algorithm>

@@ -60,33 +60,6 @@ __device__ __forceinline__ void dma16_buf(Buffer src, int voff, int soff, void* 
                                            voff, soff, 0, STREAM ? 2 : 0);
 }
 
-// The same for rings whose stage is chosen at run time: of the builtins' loads the compiler
-// takes every LDS read to want the bytes, and waits for all of them.  These it does not see:
-// callers wait with wait_vmem, for loads that may be in flight at the end of the kernel too.
-// They write no register.  A vector instruction that wrote one of the scalar operands has to
-// be five wait states behind, which the compiler does not see to either.
-struct DmaBuffer {
-  u32x4 words;
-};
-__device__ __forceinline__ DmaBuffer dma_buffer(const void* base, uint32_t bytes) {
-  const uint64_t b = (uint64_t)base;
-  return {u32x4{(uint32_t)b, (uint32_t)(b >> 32) & 0xFFFFu, bytes, 0x00020000u}};
-}
-__device__ __forceinline__ void dma16_unseen(const DmaBuffer& src, int voff, int soff,
-                                             uint32_t lds) {
-  asm volatile(
-      "s_mov_b32 m0, %3\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(voff),
-      "s"(src.words), "s"(soff), "s"(lds)
-      : "memory", "m0");
-}
-// Four bytes per active lane, lane i's at lds + 4 i.
-__device__ __forceinline__ void dma4_unseen(const DmaBuffer& src, int voff, uint32_t lds) {
-  asm volatile(
-      "s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(voff),
-      "s"(src.words), "s"(lds)
-      : "memory", "m0");
-}
-
 // Wait until at most N vector-memory operations of this wave are outstanding
 // (loads retire in issue order), leaving the other counters alone.
 template <int N>

@@ -4,6 +4,7 @@
 
 #include "hip_common.h"
 #include "kernels.h"
+#include "lds_dma.h"
 #include "stretch.h"
 
 namespace pdec {
