@@ -4,17 +4,17 @@
 // Bound by HBM: a key's 2 (2 R + 64) operations a row are a few cycles of the matrix units beside
 // its R + 132 (E4M3) or 2 R + 128 bytes.  Such a call needs bytes on their way at all times, and
 // the chain from a page to its part of the output, which one wave takes thousands of cycles for,
-// off their path.  So a group's waves go in pairs, each over every n-th page of the piece with a
-// ring of four pages in LDS: one half multiplies S^T = K Q^T, the other takes the weights through
-// LDS a step later and multiplies O^T = C^T P^T.  Two waves more do nothing but bring the pages:
-// a load holds its wave for 60 cycles, which the others' products cannot spare.  A page's sixteen
-// keys are one tile of the first product, and a lane's four weights are the operand P of the
-// second, over sixteen keys, as they are.  At the end of a piece the pairs' sums are joined
-// through LDS.
+// off their path.  So a group's waves go in teams, each over every n-th page of the piece with a
+// ring of four pages in LDS: one wave multiplies S^T = K Q^T, two take the weights through LDS a
+// step later and multiply O^T = C^T P^T, each half of the latent.  Two waves more do nothing but
+// bring the pages: a load holds its wave for 60 cycles and more.  A page's sixteen keys are one
+// tile of the first product, and a lane's four weights are the operand P of the second, over
+// sixteen keys, as they are.  At the end of a piece the teams' sums are joined through LDS.
 //
-// 16 heads over 64 x 1K to 8K E4M3 43 us and the merge's 7 (205 MB: 4.1 TB/s), four short
-// sequences of R = 256 8.3 us.  By the form for more rows 61 us, by waves that do all of a page by
-// themselves 51, with the loads among the first half's products 49.
+// 16 heads over 64 x 1K to 8K E4M3 43 us and the merge's 7 (205 MB): a step of three pages takes
+// 2450 cycles, 6.7 TB/s over all units, and the pieces' beginnings and ends 13 us.  Four short
+// sequences of R = 256 7.5 to 8.6 us.  By the form for more rows 61 us, by waves that do all of a
+// page by themselves 51, with the loads among the first product's 49.
 #include "latent_attn.h"
 
 namespace pdec {
@@ -25,39 +25,41 @@ template <int R, bool FP8>
 struct FewForm {
   static constexpr int kRow = FP8 ? R + 2 * kRope : (R + kRope) * 2;  // a key's bytes
   static constexpr int kTile = kPage * kRow, kStages = 4;
-  // Pairs of waves, by what four pages each leave room for: 2 with bf16 latents of 512, else 3.
-  static constexpr int kPairs = 12 * kTile <= 144 * 1024 ? 3 : 2;
-  static constexpr int kThreads = 128 * kPairs + 128;
-  static constexpr int kRing = kStages * kTile * kPairs, kJoin = kPairs * 16 * R * 4;
+  // Teams of three waves, by what four pages each leave room for: 2 with bf16 latents of 512,
+  // else 3.
+  static constexpr int kTeams = 12 * kTile <= 144 * 1024 ? 3 : 2;
+  static constexpr int kThreads = 192 * kTeams + 128;
+  static constexpr int kRing = kStages * kTile * kTeams, kJoin = kTeams * 16 * R * 4;
   // LDS offsets.
-  static constexpr int kScale = kRing > kJoin ? kRing : kJoin;  // [kPairs][kStages][16]
-  static constexpr int kP = kScale + (FP8 ? kPairs * kStages * kPage * 4 : 0);  // [kPairs][2][64] x 8
-  static constexpr int kAlpha = kP + kPairs * 2 * 512;          // [kPairs][2][16]
-  static constexpr int kSums = kAlpha + kPairs * 2 * 64;        // [kPairs][2][16]
-  static constexpr int kFlag = kSums + kPairs * 2 * 64;         // [kPairs][2]: references that moved
-  static constexpr int kBytes = kFlag + kPairs * 2 * 4;
+  static constexpr int kScale = kRing > kJoin ? kRing : kJoin;  // [kTeams][kStages][16]
+  static constexpr int kP = kScale + (FP8 ? kTeams * kStages * kPage * 4 : 0);  // [kTeams][2][64] x 8
+  static constexpr int kAlpha = kP + kTeams * 2 * 512;          // [kTeams][2][16]
+  static constexpr int kSums = kAlpha + kTeams * 2 * 64;        // [kTeams][2][16]
+  static constexpr int kFlag = kSums + kTeams * 2 * 64;         // [kTeams][2]: references that moved
+  static constexpr int kBytes = kFlag + kTeams * 2 * 4;
   static_assert(kBytes <= 160 * 1024 - 64 && kTile % 256 == 0, "LDS layout");
 };
 
 template <int R, bool FP8, int UNIT_TILE>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void
-latent_few_kernel(LatentAttnArgs a) {
+__global__ __launch_bounds__((FewForm<R, FP8>::kThreads)) void latent_few_kernel(LatentAttnArgs a) {
   typedef FewForm<R, FP8> F;
-  constexpr int ROW = F::kRow, NST = F::kStages, PAIRS = F::kPairs, THREADS = F::kThreads;
+  constexpr int ROW = F::kRow, NST = F::kStages, TEAMS = F::kTeams, THREADS = F::kThreads;
   constexpr int WIN = ROW / 128, LW = (FP8 ? R : 2 * R) / 128;
-  constexpr int GROUP = 8 * ROW, DT = R / 16, PPT = UNIT_TILE / kPage;
+  constexpr int GROUP = 8 * ROW, DT = R / 16, DH = DT / 2, PPT = UNIT_TILE / kPage;
   constexpr int NL = WIN + (FP8 ? 1 : 0);  // loads of half a page
   __shared__ __attribute__((aligned(256))) uint8_t lds[F::kBytes];
   __shared__ int red[THREADS / 64];
   __shared__ int found[2];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = blockIdx.x;
-  const bool first_half = wave < PAIRS;  // the half of a pair that takes the first product
-  const int pair = first_half ? wave : wave - PAIRS;  // the last two waves, of none, load
+  // A team's waves: one takes the first product, two the second, each half of the latent.  The
+  // last two waves of the group, of no team, load.
+  const bool scorer = wave < TEAMS, loader = wave >= 3 * TEAMS;
+  const int team = scorer ? wave : (wave - TEAMS) >> 1, half = (wave - TEAMS) & 1;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(PDEC_LDS uint8_t*)lds;
-  float* scales = (float*)(lds + F::kScale) + pair * NST * kPage;
-  uint8_t* p_at = lds + F::kP + pair * 2 * 512;
-  float* alphas = (float*)(lds + F::kAlpha) + pair * 2 * 16;
-  int* flags = (int*)(lds + F::kFlag) + pair * 2;
+  float* scales = (float*)(lds + F::kScale) + team * NST * kPage;
+  uint8_t* p_at = lds + F::kP + team * 2 * 512;
+  float* alphas = (float*)(lds + F::kAlpha) + team * 2 * 16;
+  int* flags = (int*)(lds + F::kFlag) + team * 2;
 
   int at = 0, end, u = w, first = 0;
   if (a.unit_groups) {
@@ -87,7 +89,7 @@ latent_few_kernel(LatentAttnArgs a) {
   // in their place by more than one; of E4M3 pages, where it brings eight, they go in order.
   auto key_of = [](int q, int e) { return FP8 ? 4 * q + e : 2 * e + (q & 1) + 8 * (q >> 1); };
 
-  // A row's reference and sum over all pairs, and what this pair's part of the output is times.
+  // A row's reference and sum over all teams, and what this team's part of the output is times.
   struct Join {
     float top, sum, own;
   };
@@ -95,12 +97,12 @@ latent_few_kernel(LatentAttnArgs a) {
     const float* sums = (const float*)(lds + F::kSums) + row;  // references, then sums
     Join o = {-INFINITY, 0.f, 0.f};
 #pragma unroll
-    for (int v = 0; v < PAIRS; ++v) o.top = fmaxf(o.top, sums[v * 32]);
+    for (int v = 0; v < TEAMS; ++v) o.top = fmaxf(o.top, sums[v * 32]);
 #pragma unroll
-    for (int v = 0; v < PAIRS; ++v) {
+    for (int v = 0; v < TEAMS; ++v) {
       const float m = sums[v * 32], f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - o.top);
       o.sum = __builtin_fmaf(sums[v * 32 + 16], f, o.sum);
-      if (v == pair) o.own = f;
+      if (v == team) o.own = f;
     }
     return o;
   };
@@ -118,17 +120,17 @@ latent_few_kernel(LatentAttnArgs a) {
     const int min_lim = max(base_lim + row0 / a.n_heads, 0);  // keys that every row sees
     const int n_pages = (kv_lim + kPage - 1) / kPage;
     const int64_t q_row0 = (int64_t)b * a.n_q * a.n_heads + row0;
-    // The pair's pages: g_begin, g_begin + PAIRS ...; a step takes one of each pair's.
-    const int g_begin = p_begin * PPT + pair, g_end = min(p_end * PPT, n_pages);
-    const int steps = max(g_end - p_begin * PPT + PAIRS - 1, 0) / PAIRS;
+    // The team's pages: g_begin, g_begin + TEAMS ...; a step takes one of each team's.
+    const int g_begin = p_begin * PPT + team, g_end = min(p_end * PPT, n_pages);
+    const int steps = max(g_end - p_begin * PPT + TEAMS - 1, 0) / TEAMS;
     const bool whole = p_begin == 0 && p_end == tiles;
     __syncthreads();  // the piece before is done with LDS
 
-    if (first_half) {
-      // Ids of 64 of the pair's pages, one a lane.
+    if (scorer) {
+      // Ids of 64 of the team's pages, one a lane.
       int ids;
       auto look = [&](int i0) {
-        const int n = g_begin + (i0 + lane_now()) * PAIRS;
+        const int n = g_begin + (i0 + lane_now()) * TEAMS;
         ids = n < g_end ? a.block_table[(int64_t)b * a.bt_stride + n] : -1;
         if (ids >= a.n_pages) ids = -1;
       };
@@ -171,8 +173,8 @@ latent_few_kernel(LatentAttnArgs a) {
         u32x2 weights = {0, 0};
         note(j + 2);
         if (here) {
-          const uint8_t* tile = lds + (pair * NST + st) * F::kTile;
-          const int key0 = (g_begin + j * PAIRS) * kPage;
+          const uint8_t* tile = lds + (team * NST + st) * F::kTile;
+          const int key0 = (g_begin + j * TEAMS) * kPage;
           const bool cut = key0 + kPage > min_lim;
           const int l1 = lane_now(), c16 = l1 & 15, q4 = l1 >> 4;
           // Where the lane reads keys' chunks.
@@ -272,23 +274,23 @@ latent_few_kernel(LatentAttnArgs a) {
       // The rows' references and sums.
       const int l0 = lane_now();
       const float sum = sum_over_key_groups(l);
-      float* sums = (float*)(lds + F::kSums) + pair * 32;
+      float* sums = (float*)(lds + F::kSums) + team * 32;
       if (l0 < 16) {
         sums[l0] = m;
         sums[16 + l0] = sum;
       }
       wg_barrier();  // every ring has been read, and no load is in flight
-    } else if (wave >= 2 * PAIRS) {
+    } else if (loader) {
       // A loader, of half of every page's keys.  Ids of 256 of the piece's pages, four a lane:
       // looking for more waits for the pages in flight.
-      const int g = wave - 2 * PAIRS, lane = lane_now(), offset = window_offset<FP8, ROW>(lane, g);
+      const int g = wave - 3 * TEAMS, lane = lane_now(), offset = window_offset<FP8, ROW>(lane, g);
       int ids[4];
-      // Every pair's page j into its ring.  A page that is not there, or behind the last, is a
+      // Every team's page j into its ring.  A page that is not there, or behind the last, is a
       // buffer without bytes: zeros come, and count.
       auto load = [&](int j) {
 #pragma unroll
-        for (int k = 0; k < PAIRS; ++k) {
-          const int i = j * PAIRS + k, st = j & (NST - 1);
+        for (int k = 0; k < TEAMS; ++k) {
+          const int i = j * TEAMS + k, st = j & (NST - 1);
           if ((i & 255) == 0)
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
@@ -316,161 +318,160 @@ latent_few_kernel(LatentAttnArgs a) {
       load(1);
 #pragma unroll 1
       for (int j = 0; j <= steps; ++j) {
-        wait_vmem<PAIRS * NL>();  // the pages j are here
+        wait_vmem<TEAMS * NL>();  // the pages j are here
         wg_barrier();
         if (j < steps) load(j + 2);
       }
       wait_vmem<0>();
       wg_barrier();
     } else {
-      f32x4 acc[DT];
+      f32x4 acc[DH];
 #pragma unroll
-      for (int d = 0; d < DT; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int d = 0; d < DH; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
       wg_barrier();
 #pragma unroll 1
       for (int j = 1; j <= steps; ++j) {  // page i; one that is not there is zeros, and so are its weights
         wg_barrier();
         const int i = j - 1, st = i & (NST - 1);
         const int moved = __builtin_amdgcn_readfirstlane(flags[i & 1]);
-        uint8_t* tile = lds + (pair * NST + st) * F::kTile;
+        uint8_t* tile = lds + (team * NST + st) * F::kTile + half * (LW * 512);  // its windows
         const uint8_t* weights = p_at + (i & 1) * 512;
-        const int key0 = (g_begin + i * PAIRS) * kPage;
+        const int key0 = (g_begin + i * TEAMS) * kPage;
         if (moved) {
           const float f = alphas[(i & 1) * 16 + (lane_now() & 15)];
 #pragma unroll
-          for (int d = 0; d < DT; ++d) {
+          for (int d = 0; d < DH; ++d) {
             acc[d] *= f;
             __builtin_amdgcn_sched_barrier(0);
           }
         }
         if (key0 + kPage > min_lim) {
-            // 0 times what a key without data holds may be NaN: it becomes 0.  So does what only
-            // some rows see and is not finite, behind its own sums for the rows that see it.
-            constexpr int CW = (FP8 ? R : 2 * R) / 16;  // chunks of a key's latent
-            auto chunk = [&](int key, int c) {
-              return (u32x4*)(tile + (key >> 3) * GROUP + (c >> 3) * 1024 + spot<FP8>(key, c & 7));
-            };
-            uint32_t nil, bad = 0;  // made here: as a constant it is kept in registers over the loop
-            asm volatile("v_mov_b32 %0, 0" : "=v"(nil));
-#pragma unroll 1
-            for (int n = lane_now(); n < kPage * CW; n += 64) {
-              const int key = n / CW;
-              u32x4* to = chunk(key, n % CW);
-              bool odd = false;
-              if (key0 + key >= kv_lim) {
-                *to = u32x4{nil, nil, nil, nil};
-              } else if (key0 + key >= min_lim) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const uint32_t y = (*to)[e];
-                  if constexpr (FP8) {
-#pragma unroll
-                    for (int h = 0; h < 32; h += 8) odd |= (y >> h & 0x7F) == 0x7F;
-                  } else {
-                    odd |= (y & 0x7F80) == 0x7F80 || (y >> 16 & 0x7F80) == 0x7F80;
-                  }
-                }
-              }
-              const uint64_t hit = __ballot(odd);
-              const int key_first = __builtin_amdgcn_readfirstlane(n) / CW;
-#pragma unroll
-              for (int k = 0; k < (CW < 64 ? 64 / CW : 1); ++k)
-                if (CW < 64 ? hit >> (k * CW % 64) & ((1ull << CW % 64) - 1) : hit)
-                  bad |= 1u << (key_first + k);
-            }
-#pragma unroll 1
-            for (uint32_t rest = bad; rest; rest &= rest - 1) {
-              const int key = __builtin_ctz(rest);
-              // The group of lanes that had the key's weights, and which of theirs it is.
-              const int l1 = lane_now(), c16 = l1 & 15, q4 = l1 >> 4;
-              const int q = FP8 ? key >> 2 : (key >> 3) * 2 + (key & 1);
-              const int e = FP8 ? key & 3 : key >> 1 & 3;
-              const float wt = bf16_to_f32(*(const uint16_t*)(weights + (q * 16 + c16) * 8 + e * 2));
-              const bool seen = key0 + key < base_lim + (row0 + min(c16, rows - 1)) / a.n_heads;
-#pragma unroll
-              for (int d = 0; d < DT; ++d) {
-                const int in = (d * 16 + 4 * q4) * (FP8 ? 1 : 2);
-                const uint8_t* from = (const uint8_t*)chunk(key, in >> 4) + (in & 15);
-                f32x4 v;
-                if constexpr (FP8) {
-                  const bf16x8 y = decode8(u32x2{*(const uint32_t*)from, 0});
-                  v = f32x4{(float)y[0], (float)y[1], (float)y[2], (float)y[3]};
-                } else {
-                  const u32x2 y = *(const u32x2*)from;
-                  v = f32x4{__uint_as_float(y.x << 16), __uint_as_float(y.x & 0xFFFF0000u),
-                            __uint_as_float(y.y << 16), __uint_as_float(y.y & 0xFFFF0000u)};
-                }
-                if (seen)
-#pragma unroll
-                  for (int h = 0; h < 4; ++h) acc[d][h] = __builtin_fmaf(wt, v[h], acc[d][h]);
-                __builtin_amdgcn_sched_barrier(0);
-              }
-              if (l1 < CW) *chunk(key, l1) = u32x4{nil, nil, nil, nil};
-            }
-          }
-          const s16x4 pf = *(const s16x4*)(weights + lane_now() * 8);
-          // Values, transposed.  Of E4M3 pages eight keys of a dim; the lane's four are the first or
-          // the last of them.
-          const int l3 = lane_now(), v_c = l3 & 15, v_q = l3 >> 4;
-          const int v_key = FP8 ? 8 * (v_q >> 1) + (v_c >> 1) : key_of(v_q, v_c >> 2);
-          const int v_at = (v_q >> 1) * GROUP + spot<FP8>(v_key, FP8 ? 0 : (v_c & 3) >> 1) + ((v_c & 1) << 3);
-          constexpr int D = 8;  // reads under way
-          u32x2 v[D];
-          auto read = [&](int d) {
-            if constexpr (FP8)
-              v[d % D] = __builtin_bit_cast(
-                  u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                             (PDEC_LDS s32x2*)(tile + (d >> 3) * 1024 + (v_at ^ (d & 7) << 4))));
-            else
-              v[d % D] = __builtin_bit_cast(
-                  u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                             (PDEC_LDS s16x4*)(tile + (d >> 2) * 1024 + (v_at ^ (d & 3) << 5))));
+          // 0 times what a key without data holds may be NaN: it becomes 0.  So does what only
+          // some rows see and is not finite, behind its own sums for the rows that see it.
+          constexpr int CW = (FP8 ? R : 2 * R) / 32;  // chunks of half a key's latent
+          auto chunk = [&](int key, int c) {
+            return (u32x4*)(tile + (key >> 3) * GROUP + (c >> 3) * 1024 + spot<FP8>(key, c & 7));
           };
+          uint32_t nil, bad = 0;  // made here: as a constant it is kept in registers over the loop
+          asm volatile("v_mov_b32 %0, 0" : "=v"(nil));
+#pragma unroll 1
+          for (int n = lane_now(); n < kPage * CW; n += 64) {
+            const int key = n / CW;
+            u32x4* to = chunk(key, n % CW);
+            bool odd = false;
+            if (key0 + key >= kv_lim) {
+              *to = u32x4{nil, nil, nil, nil};
+            } else if (key0 + key >= min_lim) {
 #pragma unroll
-          for (int d = 0; d < D; ++d) read(d);
+              for (int e = 0; e < 4; ++e) {
+                const uint32_t y = (*to)[e];
+                if constexpr (FP8) {
 #pragma unroll
-          for (int d0 = 0; d0 < DT; d0 += 4) {
-            u32x2 y[4];
-#pragma unroll
-            for (int h = 0; h < 4; ++h) y[h] = v[(d0 + h) % D];
-            if constexpr (FP8)
-#pragma unroll
-              for (int h = 0; h < 4; ++h) {
-                const uint32_t codes = v_q & 1 ? y[h].y : y[h].x;
-                y[h].x = __builtin_bit_cast(
-                    uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.f, false));
-                y[h].y = __builtin_bit_cast(
-                    uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.f, true));
+                  for (int h = 0; h < 32; h += 8) odd |= (y >> h & 0x7F) == 0x7F;
+                } else {
+                  odd |= (y & 0x7F80) == 0x7F80 || (y >> 16 & 0x7F80) == 0x7F80;
+                }
               }
+            }
+            const uint64_t hit = __ballot(odd);
+            const int key_first = __builtin_amdgcn_readfirstlane(n) / CW;
+#pragma unroll
+            for (int k = 0; k < 64 / CW; ++k)
+              if (hit >> (k * CW) & ((1ull << CW) - 1)) bad |= 1u << (key_first + k);
+          }
+#pragma unroll 1
+          for (uint32_t rest = bad; rest; rest &= rest - 1) {
+            const int key = __builtin_ctz(rest);
+            // The group of lanes that had the key's weights, and which of theirs it is.
+            const int l1 = lane_now(), c16 = l1 & 15, q4 = l1 >> 4;
+            const int q = FP8 ? key >> 2 : (key >> 3) * 2 + (key & 1);
+            const int e = FP8 ? key & 3 : key >> 1 & 3;
+            const float wt = bf16_to_f32(*(const uint16_t*)(weights + (q * 16 + c16) * 8 + e * 2));
+            const bool seen = key0 + key < base_lim + (row0 + min(c16, rows - 1)) / a.n_heads;
+#pragma unroll
+            for (int d = 0; d < DH; ++d) {
+              const int in = (d * 16 + 4 * q4) * (FP8 ? 1 : 2);
+              const uint8_t* from = (const uint8_t*)chunk(key, in >> 4) + (in & 15);
+              f32x4 v;
+              if constexpr (FP8) {
+                const bf16x8 y = decode8(u32x2{*(const uint32_t*)from, 0});
+                v = f32x4{(float)y[0], (float)y[1], (float)y[2], (float)y[3]};
+              } else {
+                const u32x2 y = *(const u32x2*)from;
+                v = f32x4{__uint_as_float(y.x << 16), __uint_as_float(y.x & 0xFFFF0000u),
+                          __uint_as_float(y.y << 16), __uint_as_float(y.y & 0xFFFF0000u)};
+              }
+              if (seen)
+#pragma unroll
+                for (int h = 0; h < 4; ++h) acc[d][h] = __builtin_fmaf(wt, v[h], acc[d][h]);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+            if (l1 < CW) *chunk(key, l1) = u32x4{nil, nil, nil, nil};
+          }
+        }
+        const s16x4 pf = *(const s16x4*)(weights + lane_now() * 8);
+        // Values, transposed.  Of E4M3 pages eight keys of a dim; the lane's four are the first or
+        // the last of them.
+        const int l3 = lane_now(), v_c = l3 & 15, v_q = l3 >> 4;
+        const int v_key = FP8 ? 8 * (v_q >> 1) + (v_c >> 1) : key_of(v_q, v_c >> 2);
+        const int v_at = (v_q >> 1) * GROUP + spot<FP8>(v_key, FP8 ? 0 : (v_c & 3) >> 1) + ((v_c & 1) << 3);
+        constexpr int D = 8;  // reads under way
+        u32x2 v[D];
+        auto read = [&](int d) {
+          if constexpr (FP8)
+            v[d % D] = __builtin_bit_cast(
+                u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                           (PDEC_LDS s32x2*)(tile + (d >> 3) * 1024 + (v_at ^ (d & 7) << 4))));
+          else
+            v[d % D] = __builtin_bit_cast(
+                u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                           (PDEC_LDS s16x4*)(tile + (d >> 2) * 1024 + (v_at ^ (d & 3) << 5))));
+        };
+#pragma unroll
+        for (int d = 0; d < D; ++d) read(d);
+#pragma unroll
+        for (int d0 = 0; d0 < DH; d0 += 4) {
+          u32x2 y[4];
+#pragma unroll
+          for (int h = 0; h < 4; ++h) y[h] = v[(d0 + h) % D];
+          if constexpr (FP8)
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
-              acc[d0 + h] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
-                  __builtin_bit_cast(s16x4, y[h]), pf, acc[d0 + h], 0, 0, 0);
-              if (d0 + h + D < DT) read(d0 + h + D);
+              const uint32_t codes = v_q & 1 ? y[h].y : y[h].x;
+              y[h].x = __builtin_bit_cast(
+                  uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.f, false));
+              y[h].y = __builtin_bit_cast(
+                  uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.f, true));
             }
-            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int h = 0; h < 4; ++h) {
+            acc[d0 + h] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
+                __builtin_bit_cast(s16x4, y[h]), pf, acc[d0 + h], 0, 0, 0);
+            if (d0 + h + D < DH) read(d0 + h + D);
           }
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
       wg_barrier();  // every ring has been read, and no load is in flight
       const int l0 = lane_now();
       const float f = join_of(l0 & 15).own;
 #pragma unroll
-      for (int d = 0; d < DT; ++d) ((f32x4*)lds)[(pair * DT + d) * 64 + l0] = acc[d] * f;
+      for (int d = 0; d < DH; ++d) ((f32x4*)lds)[(team * DT + half * DH + d) * 64 + l0] = acc[d] * f;
     }
 
-    // The pairs' sums meet, in order; the waves share the latent's tiles.
+    // The teams' sums meet, in order; the waves share the latent's tiles.
     wg_barrier();
     const int l2 = lane_now(), c16 = l2 & 15, q4 = l2 >> 4;
     const Join all = join_of(c16);
     const float inv = all.sum == 0.f ? 0.f : 1.f / all.sum;
-    const f32x4* join = (const f32x4*)lds;  // [PAIRS][DT][64]
+    const f32x4* join = (const f32x4*)lds;  // [TEAMS][DT][64]
     const int64_t pr = ((int64_t)w + u) * 16 + c16;
     if (c16 < rows) {
       if (!whole && wave == 0 && q4 == 0) *(float2*)(a.part_ml + pr * 2) = float2{all.top, all.sum};
       for (int d = wave; d < DT; d += THREADS / 64) {
         f32x4 o = join[d * 64 + l2];
 #pragma unroll
-        for (int v = 1; v < PAIRS; ++v) o += join[(v * DT + d) * 64 + l2];
+        for (int v = 1; v < TEAMS; ++v) o += join[(v * DT + d) * 64 + l2];
         if (whole) {
           const f32x2 lo = {o[0] * inv, o[1] * inv}, hi = {o[2] * inv, o[3] * inv};
           *(u32x2*)((uint16_t*)a.out + (q_row0 + c16) * R + d * 16 + 4 * q4) =
