@@ -162,10 +162,10 @@ latent_attn_kernel(LatentAttnArgs a) {
             __builtin_amdgcn_readfirstlane(*(const int*)(lds + F::kIds + (i + (g >> 1)) * 4));
         const DmaBuffer src = dma_buffer((const uint8_t*)a.pages + p * (kPage * ROW), 2 * GROUP);
         const int voff = window_offset<FP8, ROW>(l, g);
-#pragma unroll
-        for (int n = 0; n < WIN; ++n)
-          dma16_unseen(src, voff, (g & 1) * GROUP + n * 128,
-                       lds0 + st * F::kStage + g * GROUP + n * 1024);
+        each<WIN>([&](auto n) {
+          dma16_unseen<n * 128, n * 1024>(src, voff, (g & 1) * GROUP,
+                                          lds0 + st * F::kStage + g * GROUP);
+        });
         if constexpr (FP8) {
           const DmaBuffer scales = dma_buffer(a.scales + p * kPage + (g & 1) * 8, 32);
           if (l < 8) dma4_unseen(scales, l * 4, lds0 + F::kScale + (st * TILE + g * 8) * 4);

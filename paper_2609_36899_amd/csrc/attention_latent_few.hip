@@ -305,8 +305,9 @@ __global__ __launch_bounds__((FewForm<R, FP8>::kThreads)) void latent_few_kernel
           const DmaBuffer from =
               dma_buffer((const uint8_t*)a.pages + p * F::kTile, id >= 0 ? F::kTile : 0);
           const uint32_t to = lds0 + (k * NST + st) * F::kTile + g * GROUP;
-#pragma unroll
-          for (int n = 0; n < WIN; ++n) dma16_unseen(from, offset, g * GROUP + n * 128, to + n * 1024);
+          each<WIN>([&](auto n) {
+            dma16_unseen<n * 128, n * 1024>(from, offset, g * GROUP, to);
+          });
           if constexpr (FP8) {
             const DmaBuffer f = dma_buffer(a.scales + p * kPage + g * 8, id >= 0 ? 32 : 0);
             if (lane < 8)

@@ -199,11 +199,9 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn_kernel(LatentPromptAr
       const DmaBuffer vb = dma_buffer((const void*)v_next, vn);
       const DmaBuffer rb = dma_buffer((const void*)r_next, rn);
       const uint32_t to = lds0 + st * STAGE + wave * GK;
-#pragma unroll
-      for (int i = 0; i < WIN; ++i) dma16_unseen(kb, k_off, i * 128, to + i * 1024);
-      dma16_unseen(rb, r_off, 0, lds0 + st * STAGE + K + wave * 1024);
-#pragma unroll
-      for (int i = 0; i < WIN; ++i) dma16_unseen(vb, v_off, i * 128, to + K + ROPE + i * 1024);
+      each<WIN>([&](auto i) { dma16_unseen<i * 128, i * 1024>(kb, k_off, 0, to); });
+      dma16_unseen<0, K>(rb, r_off, 0, lds0 + st * STAGE + wave * 1024);
+      each<WIN>([&](auto i) { dma16_unseen<i * 128, K + ROPE + i * 1024>(vb, v_off, 0, to); });
       ++t_next;
       n_next -= kTile;
       k_next += (int64_t)kTile * k_row;
