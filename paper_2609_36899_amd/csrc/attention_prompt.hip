@@ -18,9 +18,9 @@
 // its block began before, and its last, where it goes on behind, leave partials; the merge pass
 // joins each block that was cut.  Where there are enough blocks each has a group of its own.
 //
-// 20 heads over 4096 tokens, D = 128: 141 us (0.75 PFLOP/s), of which the merge 15; each head
-// more costs 5 us (1.07 PFLOP/s, where a large matrix product reaches 1.33), the beginnings,
-// partials and merge some 50.  Tried without gain: the next tile's first product beside this
+// 20 heads over 4096 tokens, D = 128: 132 us (0.81 PFLOP/s) by a group a block, 141 by equal
+// stretches, of which the merge 15; there each head more costs 5 us (1.07 PFLOP/s, where a large
+// matrix product reaches 1.33), the beginnings, partials and merge some 50.  Tried without gain: the next tile's first product beside this
 // one's weights in each wave, heads gathered by die, the loads one by one between the products.
 #include "hip_common.h"
 #include "kernels.h"
@@ -59,7 +59,7 @@ __device__ __forceinline__ int block_tiles(const Seq& s, int blk) {
   return max((keys + TILE - 1) / TILE, 1);
 }
 // The same and what a piece of a block costs beside its tiles (its queries, the first tiles' way,
-// its output), in tiles, which the split counts ahead of each block's.  us at 0 / 4 / 12: 20 heads
+// its output), in tiles, which equal stretches count ahead of each block's.  us at 0 / 4 / 12: 20 heads
 // over 4096 150 / 144 / 146, 32 heads over five turns 186 / 189 / 191.
 constexpr int kHead = 4;
 // That of the blocks before blk: of each whole block ROWS / TILE more than of the one before.

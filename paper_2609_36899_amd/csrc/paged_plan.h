@@ -106,15 +106,17 @@ struct PromptPlan {
   int32_t n_groups;  // a head
   bool block_groups;
 };
-// A group for each block, where there are enough of them: prompts' blocks differ in length, and
-// the long ones begin first; behind long contexts they are alike, and the last ones leave units
-// idle.  us in equal stretches / in groups of their own, blocks of all heads: 4096 tokens x 16
-// heads 131 / 139 (512), x 32 heads 224 / 204 (1024), x 64 heads 402 / 363 (2048); 8192 x 32 735 /
-// 641 (2048); 8 x 256 behind 2000 each, 128 heads 474 / 413 (2048 and more).
+// A group for each block, where there are enough of them, more than the 512 groups at work at
+// once: prompts' blocks differ in length, and the long ones begin first; behind long contexts they
+// are alike, and the last ones leave units idle.  us in equal stretches / in groups of their own,
+// blocks of all heads: 2048 tokens x 16 heads 56 / 66 (272), 4096 x 16 131 / 139 (528), x 20 141 /
+// 133 (660), x 24 185 / 154 (792), x 32 224 / 204 (1056), x 64 402 / 363 (2112), 8192 x 32 735 /
+// 641 (2080); behind contexts, five of 100 to 700 behind 1000 to 6000, 32 heads, 192 / 241 (some
+// 700), 8 x 256 behind 2000, 128 heads, 474 / 413 (over 2048).
 inline PromptPlan plan_latent_prompt(int64_t n_rows, int64_t n_keys, int64_t n_seqs, int n_heads) {
   PromptPlan p;
   const int64_t blocks = n_rows / kPromptRows + n_seqs;  // at most
-  p.block_groups = blocks * n_heads >= (n_keys <= 2 * n_rows ? 1024 : 2048) && blocks <= 65535;
+  p.block_groups = blocks * n_heads >= (n_keys <= 2 * n_rows ? 600 : 2048) && blocks <= 65535;
   p.n_groups = p.block_groups ? (int32_t)blocks
                               : (int32_t)std::max<int64_t>(1, std::min<int64_t>(65535, 512 / n_heads));
   return p;
