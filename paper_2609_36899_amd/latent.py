@@ -246,18 +246,21 @@ def paged_copy_pages(pools: Union[torch.Tensor, Sequence[torch.Tensor]], src: to
     _check(dst, "dst", _I32, (n,), dev)
     if not pools:
         _refuse("no pools")
-    count = len(pools)
-    places, sizes, n_pages = (ctypes.c_void_p * count)(), (ctypes.c_int64 * count)(), None
-    for i, t in enumerate(pools):
+    places, sizes, n_pages = [], [], None
+    for t in pools:
         if not isinstance(t, torch.Tensor) or t.dim() < 1 or t.get_device() != dev \
                 or not t.is_contiguous():
             _refuse("pools must be contiguous tensors on the pairs' GPU")
+        here, size = len(t), t.nbytes
         if n_pages is None:
-            n_pages = t.shape[0]
-        if t.shape[0] != n_pages or t.numel() == 0:
+            n_pages = here
+        if here != n_pages or size == 0:
             _refuse("pools must have the same number of pages, and pages with something in them")
-        places[i] = t.data_ptr()
-        sizes[i] = t.numel() // n_pages * t.element_size()
+        places.append(t.data_ptr())
+        sizes.append(size // n_pages)
+    count = len(places)
+    places = (ctypes.c_void_p * count)(*places)
+    sizes = (ctypes.c_int64 * count)(*sizes)
     handle = _handle(dev, stream)
     if n == 0:
         return
