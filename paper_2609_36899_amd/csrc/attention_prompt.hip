@@ -20,8 +20,9 @@
 //
 // 20 heads over 4096 tokens, D = 128: 132 us (0.81 PFLOP/s) by a group a block, 141 by equal
 // stretches, of which the merge 15; there each head more costs 5 us (1.07 PFLOP/s, where a large
-// matrix product reaches 1.33), the beginnings, partials and merge some 50.  Tried without gain: the next tile's first product beside this
-// one's weights in each wave, heads gathered by die, the loads one by one between the products.
+// matrix product reaches 1.33), the beginnings, partials and merge some 50.  Tried without gain:
+// the next tile's first product beside this one's weights in each wave, heads gathered by die,
+// the loads one by one between the products.
 #include "hip_common.h"
 #include "kernels.h"
 #include "lds_dma.h"
