@@ -9,7 +9,8 @@
 // step later and multiply O^T = C^T P^T, each half of the latent.  Two waves more do nothing but
 // bring the pages: a load holds its wave for 60 cycles and more.  A page's sixteen keys are one
 // tile of the first product, and a lane's four weights are the operand P of the second, over
-// sixteen keys, as they are.  At the end of a piece the teams' sums are joined through LDS.
+// sixteen keys, as they are.  At the end of a piece the teams' sums are joined through LDS.  A
+// unit reads its pages once, so they do not stay in the caches (pages from HBM: 55 us, then 50).
 //
 // 16 heads over 64 x 1K to 8K E4M3 43 us and the merge's 7 (205 MB): a step of three pages takes
 // 2450 cycles, 6.7 TB/s over all units, and the pieces' beginnings and ends 13 us.  Four short
@@ -306,7 +307,7 @@ __global__ __launch_bounds__((FewForm<R, FP8>::kThreads)) void latent_few_kernel
               dma_buffer((const uint8_t*)a.pages + p * F::kTile, id >= 0 ? F::kTile : 0);
           const uint32_t to = lds0 + (k * NST + st) * F::kTile + g * GROUP;
           each<WIN>([&](auto n) {
-            dma16_unseen<n * 128, n * 1024>(from, offset, g * GROUP, to);
+            dma16_unseen<n * 128, n * 1024, true>(from, offset, g * GROUP, to);
           });
           if constexpr (FP8) {
             const DmaBuffer f = dma_buffer(a.scales + p * kPage + g * 8, id >= 0 ? 32 : 0);

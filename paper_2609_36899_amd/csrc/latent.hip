@@ -14,8 +14,9 @@
 //
 // Gather.  Bound by memory (a row's 1152 or 644 bytes read, 1152 written), and for few rows by the
 // chain of looks from a row to its page, which the lanes go at once, one a row.  A wave takes four
-// rows, all their loads in flight; 54 000 E4M3 rows of 512 in 18.2 us (5.3 TB/s, some of it
-// from the caches), by two rows a wave 18.9, by eight, whose registers leave few waves, 33.7.
+// rows, all their loads in flight; 54 000 E4M3 rows of 512 in 20.7 us (4.7 TB/s), by cached stores
+// 27.5; with these by two rows a wave 29.3, by one 35.0, by six, whose registers leave few waves,
+// 35.3.
 #include "hip_common.h"
 #include "kernels.h"
 #include "rows.h"
@@ -161,7 +162,8 @@ __global__ __launch_bounds__(kThreads) void latent_append_kernel(LatentAppendArg
   }
 }
 
-template <bool FP8, int R>
+// PAST: latents are written past the caches.
+template <bool FP8, int R, bool PAST>
 __global__ __launch_bounds__(kThreads) void latent_rows_kernel(LatentRowsArgs a) {
   constexpr int kRowBytes = FP8 ? R + 2 * kRope : 2 * (R + kRope);
   constexpr int CL = R / 8;  // lanes of a latent, eight elements each; eight more of the key
@@ -225,7 +227,11 @@ __global__ __launch_bounds__(kThreads) void latent_rows_kernel(LatentRowsArgs a)
       }
       x[i] = o;
     }
-    if (lane < CL) *(u32x4*)((uint16_t*)a.latents + (r0 + i) * R + lane * 8) = x[i];
+    u32x4* to = (u32x4*)((uint16_t*)a.latents + (r0 + i) * R + lane * 8);
+    if (lane < CL) {
+      if constexpr (PAST) __builtin_nontemporal_store(x[i], to);
+      else *to = x[i];
+    }
     if (lane < 8) *(u32x4*)((uint16_t*)a.rope_keys + (r0 + i) * kRope + lane * 8) = k[i];
   }
 }
@@ -267,13 +273,21 @@ hipError_t launch_latent_append(int src_bf16, int fp8, int latent, const LatentA
 hipError_t launch_latent_rows(int fp8, int latent, const LatentRowsArgs& a, hipStream_t stream) {
   if (a.n_rows == 0) return hipSuccess;
   const dim3 grid((uint32_t)rows_groups(a)), block(kThreads);
+  // What the L2 caches (32 MB in all) would not hold for who reads it next goes past them.
+  const bool past = (int64_t)a.n_rows * latent * 2 > 32 << 20;
+#define PDEC_ROWS(FP8_, R_)                                                     \
+  do {                                                                          \
+    if (past) latent_rows_kernel<FP8_, R_, true><<<grid, block, 0, stream>>>(a); \
+    else latent_rows_kernel<FP8_, R_, false><<<grid, block, 0, stream>>>(a);    \
+  } while (0)
   if (latent == 512) {
-    if (fp8) latent_rows_kernel<true, 512><<<grid, block, 0, stream>>>(a);
-    else latent_rows_kernel<false, 512><<<grid, block, 0, stream>>>(a);
+    if (fp8) PDEC_ROWS(true, 512);
+    else PDEC_ROWS(false, 512);
   } else {
-    if (fp8) latent_rows_kernel<true, 256><<<grid, block, 0, stream>>>(a);
-    else latent_rows_kernel<false, 256><<<grid, block, 0, stream>>>(a);
+    if (fp8) PDEC_ROWS(true, 256);
+    else PDEC_ROWS(false, 256);
   }
+#undef PDEC_ROWS
   return hipGetLastError();
 }
 

@@ -20,12 +20,18 @@ __device__ __forceinline__ DmaBuffer dma_buffer(const void* base, uint32_t bytes
   return {u32x4{(uint32_t)b, (uint32_t)(b >> 32) & 0xFFFFu, bytes, 0x00020000u}};
 }
 // Sixteen bytes a lane, from voff + soff + FROM, lane i's to lds + TO + 16 i.  (The instruction's
-// own offset counts for both places.)
-template <int FROM, int TO>
+// own offset counts for both places.)  ONCE: for bytes that no one else reads soon.
+template <int FROM, int TO, bool ONCE = false>
 __device__ __forceinline__ void dma16_unseen(const DmaBuffer& src, int voff, int soff,
                                              uint32_t lds) {
   static_assert(FROM >= 0 && FROM < 4096, "the instruction's offset");
-  asm volatile(
+  if constexpr (ONCE)
+    asm volatile(
+        "s_add_u32 m0, %3, %4\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, %2 offen offset:%5 nt lds" ::
+            "v"(voff),
+        "s"(src.words), "s"(soff), "s"(lds), "n"(TO - FROM), "n"(FROM)
+        : "memory", "m0", "scc");
+  else asm volatile(
       "s_add_u32 m0, %3, %4\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, %2 offen offset:%5 lds" ::"v"(
           voff),
       "s"(src.words), "s"(soff), "s"(lds), "n"(TO - FROM), "n"(FROM)
