@@ -14,9 +14,9 @@
 //
 // Gather.  Bound by memory (a row's 1152 or 644 bytes read, 1152 written), and for few rows by the
 // chain of looks from a row to its page, which the lanes go at once, one a row.  A wave takes four
-// rows, all their loads in flight; 54 000 E4M3 rows of 512 in 20.7 us (4.7 TB/s), by cached stores
-// 27.5; with these by two rows a wave 29.3, by one 35.0, by six, whose registers leave few waves,
-// 35.3.
+// rows, all their loads in flight; 54 000 E4M3 rows of 512 in 17.3 us (5.6 TB/s), 27.5 by stores
+// that the caches keep; with these two rows a wave 29.3, one 35.0, six, whose registers leave few
+// waves, 35.3.
 #include "hip_common.h"
 #include "kernels.h"
 #include "rows.h"
@@ -162,7 +162,7 @@ __global__ __launch_bounds__(kThreads) void latent_append_kernel(LatentAppendArg
   }
 }
 
-// PAST: latents are written past the caches.
+// PAST: rows are written past the caches.
 template <bool FP8, int R, bool PAST>
 __global__ __launch_bounds__(kThreads) void latent_rows_kernel(LatentRowsArgs a) {
   constexpr int kRowBytes = FP8 ? R + 2 * kRope : 2 * (R + kRope);
@@ -228,11 +228,14 @@ __global__ __launch_bounds__(kThreads) void latent_rows_kernel(LatentRowsArgs a)
       x[i] = o;
     }
     u32x4* to = (u32x4*)((uint16_t*)a.latents + (r0 + i) * R + lane * 8);
-    if (lane < CL) {
-      if constexpr (PAST) __builtin_nontemporal_store(x[i], to);
-      else *to = x[i];
+    u32x4* key_to = (u32x4*)((uint16_t*)a.rope_keys + (r0 + i) * kRope + lane * 8);
+    if constexpr (PAST) {
+      if (lane < CL) __builtin_nontemporal_store(x[i], to);
+      if (lane < 8) __builtin_nontemporal_store(k[i], key_to);
+    } else {
+      if (lane < CL) *to = x[i];
+      if (lane < 8) *key_to = k[i];
     }
-    if (lane < 8) *(u32x4*)((uint16_t*)a.rope_keys + (r0 + i) * kRope + lane * 8) = k[i];
   }
 }
 
@@ -274,7 +277,7 @@ hipError_t launch_latent_rows(int fp8, int latent, const LatentRowsArgs& a, hipS
   if (a.n_rows == 0) return hipSuccess;
   const dim3 grid((uint32_t)rows_groups(a)), block(kThreads);
   // What the L2 caches (32 MB in all) would not hold for who reads it next goes past them.
-  const bool past = (int64_t)a.n_rows * latent * 2 > 32 << 20;
+  const bool past = (int64_t)a.n_rows * (latent + kRope) * 2 > 32 << 20;
 #define PDEC_ROWS(FP8_, R_)                                                     \
   do {                                                                          \
     if (past) latent_rows_kernel<FP8_, R_, true><<<grid, block, 0, stream>>>(a); \
