@@ -27,8 +27,10 @@
 // The tiles come by LDS-DMA into a ring of three stages, by the four waves that wait at the
 // barrier otherwise (all eight: 189 against 182 us).  Nothing is spilled in the loop: a reload
 // would wait, as loads return in order, for the tile on its way (128 heads 584 us with spills,
-// 192 without).  128 heads over 64 x 1K to 8K bf16 131 us (0.66 PFLOP/s; steps 111, the pieces'
-// beginnings and ends, the merge 20), 32 heads x 4 tokens over 8 x 64K to 128K E4M3 218 (0.93).
+// 192 without).  128 heads over 64 x 1K to 8K bf16 124 us (0.71 PFLOP/s; of it the pieces'
+// beginnings and ends 18 and the merge 20), 32 heads x 4 tokens over 8 x 64K to 128K E4M3 220
+// (0.97).  Tried without gain: loads one by one between the products (142), weights read two or
+// three tiles ahead, a higher priority for either half of the waves.
 #include "latent_attn.h"
 
 #include <algorithm>

@@ -12,7 +12,7 @@
 // sixteen keys, as they are.  At the end of a piece the teams' sums are joined through LDS.  A
 // unit reads its pages once, so they do not stay in the caches (pages from HBM: 55 us, then 50).
 //
-// 16 heads over 64 x 1K to 8K E4M3 43 us and the merge's 7 (205 MB): a step of three pages takes
+// 16 heads over 64 x 1K to 8K E4M3 43 us and the merge's 6 (205 MB): a step of three pages takes
 // 2450 cycles, 6.7 TB/s over all units, and the pieces' beginnings and ends 13 us.  Four short
 // sequences of R = 256 7.5 to 8.6 us.  By the form for more rows 61 us, by waves that do all of a
 // page by themselves 51, with the loads among the first product's 49.

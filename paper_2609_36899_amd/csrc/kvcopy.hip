@@ -37,9 +37,9 @@ __global__ __launch_bounds__(256) void kv_page_copy_kernel(
 // Pages of a caller's pools to other places of the same pools: a work group per pair and part
 // of a page, two units a thread: bound by memory, and many short groups keep more of it under way
 // than few long ones.  What is written is not read again here, and passes by the caches.  8190
-// pages of 18 KB: 8 units a thread 158 us, 4 49, 2 50, 1 56; written past the caches 2 units 41
-// and 1 41, 7.4 TB/s read and written.  T is the widest unit that every part of the pool's pages
-// is a whole number of.
+// pages of 18 KB over and over: 8 units a thread 158 us, 4 49, 2 50, 1 56, written past the caches
+// 2 units 41 and 1 41; others each time, from HBM: 67, 4.5 TB/s read and written (a large copy
+// 4.9).  T is the widest unit that every part of the pool's pages is a whole number of.
 constexpr int kCopyEach = 2, kCopyUnits = kCopyEach * 256;  // of a thread, of a part
 template <typename T>
 __device__ __forceinline__ void copy_part(const char* from, char* to, int64_t n) {
