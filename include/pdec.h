@@ -763,7 +763,8 @@ int paged_latent_rows(int32_t kv_dtype, int32_t n_rows, int32_t n_seqs, int32_t 
  *   q_start[b] .. q_start[b + 1] - 1 of q and the keys k_start[b] ..
  *   k_start[b + 1] - 1 (device int32 [n_seqs + 1], ascending, within n_rows and
  *   n_keys); its last keys are its rows' own.  A row that sees no key gets
- *   zeros; rows that no sequence holds are left as they were.
+ *   zeros; rows that no sequence holds are left as they were, and all rows where
+ *   q_start descends anywhere.
  *   q: bf16 heads of head_dim + 64 elements (head_dim 64 or 128), k and v of
  *   head_dim, *_head_stride elements apart in rows *_stride apart (k and v
  *   side by side for each head, as one projection leaves them, serve as they

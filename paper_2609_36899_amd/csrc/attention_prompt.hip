@@ -41,7 +41,9 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 #define PDEC_LDS __attribute__((address_space(3)))
 
-// A sequence's rows and keys; starts are not trusted.
+// A sequence's rows and keys; starts are not trusted.  Where the rows' descend anywhere the call
+// does nothing: sequences that share rows may be of more tiles in all than 32 bits count, and then
+// no place among them means anything.
 struct Seq {
   int q0, nq, k0, nk;
 };
@@ -111,15 +113,18 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn_kernel(LatentPromptAr
   // With a group for each block the blocks' order is turned round, so that the long ones begin
   // first.
   const int w = a.block_groups ? gridDim.y - 1 - blockIdx.y : blockIdx.y;
+  bool descends = false;
   const Stretch mine = stretch_of<kThreads>(
       a.n_seqs, gridDim.y, a.block_groups ? 1 : a.min_tiles, w, red, found, [&](int b) {
+        descends |= a.q_start[b] > a.q_start[b + 1];
         const Seq s = seq_of(a, b);
         return a.block_groups ? (s.nq + kRows - 1) / kRows : seq_size<kRows, kTile>(s);
       });
+  if (__syncthreads_or(descends)) return;
   int at = w * mine.per;
   if (at >= mine.total) return;
   int end = min(at + mine.per, mine.total), first = mine.first;
-  int b = min(max(mine.unit, 0), a.n_seqs - 1);  // whatever the starts hold
+  int b = mine.unit;
   Seq s = seq_of(a, b);
   int blk;
   if (a.block_groups) {
@@ -424,13 +429,16 @@ __global__ __launch_bounds__(512) void prompt_merge_kernel(LatentPromptArgs a, i
   __shared__ int red[8];
   __shared__ int found[2];
   const int w = blockIdx.z, h = blockIdx.x;
+  bool descends = false;
   const Stretch mine = stretch_of<512>(a.n_seqs, n_groups, a.min_tiles, w, red, found, [&](int b) {
+    descends |= a.q_start[b] > a.q_start[b + 1];
     return seq_size<kRows, kTile>(seq_of(a, b));
   });
+  if (__syncthreads_or(descends)) return;
   const int at = w * mine.per;
   if (at >= mine.total) return;
   const int end = min(at + mine.per, mine.total);
-  const Seq s = seq_of(a, min(max(mine.unit, 0), a.n_seqs - 1));
+  const Seq s = seq_of(a, mine.unit);
   const int blk = block_of<kRows, kTile>(s, at - mine.first);
   const int body = mine.first + size_before<kRows, kTile>(s, blk) + kHead;
   const int tiles = block_tiles<kRows, kTile>(s, blk);
