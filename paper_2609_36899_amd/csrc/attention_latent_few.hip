@@ -284,10 +284,12 @@ __global__ __launch_bounds__((FewForm<R, FP8>::kThreads)) void latent_few_kernel
     } else if (loader) {
       // A loader, of half of every page's keys.  Ids of 256 of the piece's pages, four a lane:
       // looking for more waits for the pages in flight.
-      const int g = wave - 3 * TEAMS, lane = lane_now(), offset = window_offset<FP8, ROW>(lane, g);
+      const int g = wave - 3 * TEAMS, lane = lane_now();
+      const int offset = window_offset<FP8, ROW>(lane, g) + g * GROUP;
       int ids[4];
       // Every team's page j into its ring.  A page that is not there, or behind the last, is a
-      // buffer without bytes: zeros come, and count.
+      // buffer without bytes: zeros come, and count.  All of the place is in the lane's offset,
+      // the one that is certain to be held against the buffer's size.
       auto load = [&](int j) {
 #pragma unroll
         for (int k = 0; k < TEAMS; ++k) {
@@ -307,7 +309,7 @@ __global__ __launch_bounds__((FewForm<R, FP8>::kThreads)) void latent_few_kernel
               dma_buffer((const uint8_t*)a.pages + p * F::kTile, id >= 0 ? F::kTile : 0);
           const uint32_t to = lds0 + (k * NST + st) * F::kTile + g * GROUP;
           each<WIN>([&](auto n) {
-            dma16_unseen<n * 128, n * 1024, true>(from, offset, g * GROUP, to);
+            dma16_unseen<n * 128, n * 1024, true>(from, offset, 0, to);
           });
           if constexpr (FP8) {
             const DmaBuffer f = dma_buffer(a.scales + p * kPage + g * 8, id >= 0 ? 32 : 0);
