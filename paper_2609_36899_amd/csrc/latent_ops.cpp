@@ -177,17 +177,17 @@ int64_t paged_latent_attention_workspace_bytes(int32_t kv_dtype, int32_t batch, 
   if (rc != PDEC_OK) return rc;
   if (max_pages < 1 || max_pages > kMaxStride) return fail(PDEC_INVALID_ARG, "bad max_pages");
   // Fewer sequences, tokens or pages of the same take blocks of as many row tiles or fewer, and
-  // as many units or fewer, but have partials where these units may be too many to have any:
-  // those of blocks of one row tile, a sequence each, up to more units than others.
+  // as many units or fewer, but have partials where these units may be too many to have any: as
+  // many as just have, of this call's blocks, and of blocks of one row tile, a sequence each.
   const int64_t max_len = (int64_t)max_pages * PDEC_PAGE_TOKENS;
   const LatentPlan p = plan_latent_attention(
       batch, n_q, n_heads, max_len, latent_tile(kv_dtype == PDEC_FP8_E4M3, latent_dim));
-  if (p.unit_groups && p.n_units < latent_units(p.row_tiles)) return 0;  // no table is long
+  const int64_t most = latent_units(p.row_tiles, max_len), most_few = latent_units(1, max_len);
+  if (p.unit_groups && p.n_units < most) return 0;  // no table is long
   LatentPlan few = p;
   few.row_tiles = 1;
-  const Layout l =
-      layout_of(std::min(p.n_units, latent_units(p.row_tiles) - 1), p, latent_dim);
-  const Layout f = layout_of(std::min<int64_t>(batch, latent_units(1) - 1), few, latent_dim);
+  const Layout l = layout_of(std::min(p.n_units, most - 1), p, latent_dim);
+  const Layout f = layout_of(std::min<int64_t>(batch, most_few - 1), few, latent_dim);
   return std::max(l.ml + l.acc, f.ml + f.acc);
 }
 

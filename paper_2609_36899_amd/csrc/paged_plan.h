@@ -79,11 +79,23 @@ struct LatentPlan {
   int64_t n_units;
   bool unit_groups;  // a work group for each unit and no merge, instead of equal stretches
 };
-// Units from which each has a work group of its own.  us in equal stretches / in groups of their
-// own: 16 heads, E4M3, 128 x 0.5K to 4K 51 / 90, 512 of them 138 / 164, 1024 x 0.2K to 2K 163 /
-// 175, 1024 x 16 to 256 61 / 61; 128 heads, bf16, 256 x 0.5K to 4K 200 / 251, 512 x 0.2K to 2K 231
-// / 228.  Beyond, the partials of equal stretches only take more room.
-inline int64_t latent_units(int row_tiles) { return row_tiles == 1 ? 2048 : 512; }
+// Units from which each has a work group of its own: where no sequence can be long, as the call
+// waits for the longest one, which one group reads alone; and however long, where the merge's look
+// at all units for each costs more than equal stretches give.  us in equal stretches / in groups of
+// their own, lengths up to the table's even / one in 97 as long as the table, others 64:
+//   32 heads, E4M3, 512 units, tables of 512 tokens 78 / 65 and 52 / 44, of 1024 98 / 99 and 55 /
+//     60, of 2048 138 / 161 and 56 / 91; 1024 units, of 1024 167 / 172 and 85 / 97;
+//   128 heads, bf16, 512 units, of 512 133 / 99 and 96 / 73, of 1024 183 / 161 and 99 / 101, of
+//     2048 253 / 272 and 99 / 156; 2048 units, of 1024 625 / 520 and 360 / 262;
+//   16 heads, E4M3, 128 x 0.5K to 4K 51 / 90, 1024 x 16 to 256 61 / 61, 1024 x 0.2K to 2K 163 /
+//     175; 2048 units, of 1024 213 / 206 and 123 / 125, of 2048 330 / 347 and 123 / 142.
+// One sequence of 128K among 512 of 0.2K to 2K, 32 heads, E4M3: 179 / 4104; 128 heads, bf16, 361 /
+// 7179.  Under a wide table that holds short sequences alone the stretches lose: 512 units of 16 to
+// 256 tokens 68 / 48 and 115 / 70; 4096 422 / 338 and 877 / 485 (0.2K to 2K 929 / 950 and 1970 /
+// 1746), 8192 of 32 heads 991 / 660.
+inline int64_t latent_units(int row_tiles, int64_t max_len) {
+  return max_len > 1024 ? 4096 : row_tiles == 1 ? 2048 : 512;
+}
 // max_len: what no sequence can be longer than; tile: keys of a tile.
 inline LatentPlan plan_latent_attention(int batch, int n_q, int n_heads, int64_t max_len, int tile) {
   LatentPlan p;
@@ -95,7 +107,7 @@ inline LatentPlan plan_latent_attention(int batch, int n_q, int n_heads, int64_t
   p.blocks_per_seq = (int32_t)((rows + p.block_rows - 1) / p.block_rows);
   p.n_units = (int64_t)batch * p.blocks_per_seq;
   p.n_groups = kAttnGroups;
-  p.unit_groups = p.n_units >= latent_units(p.row_tiles) || max_len <= 4 * tile;
+  p.unit_groups = p.n_units >= latent_units(p.row_tiles, max_len) || max_len <= 4 * tile;
   return p;
 }
 
