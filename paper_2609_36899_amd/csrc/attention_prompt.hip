@@ -110,8 +110,8 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn_kernel(LatentPromptAr
   __shared__ int found[2];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = blockIdx.x;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(PDEC_LDS uint8_t*)lds;
-  // With a group for each block the blocks' order is turned round, so that the long ones begin
-  // first.
+  // With a group for each block the blocks' order is turned round, so that the long ones of a
+  // prompt begin first (and of several prompts the last one's).
   const int w = a.block_groups ? gridDim.y - 1 - blockIdx.y : blockIdx.y;
   bool descends = false;
   const Stretch mine = stretch_of<kThreads>(

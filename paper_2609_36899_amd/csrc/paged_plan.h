@@ -119,16 +119,28 @@ struct PromptPlan {
   bool block_groups;
 };
 // A group for each block, where there are enough of them, more than the 512 groups at work at
-// once: prompts' blocks differ in length, and the long ones begin first; behind long contexts they
-// are alike, and the last ones leave units idle.  us in equal stretches / in groups of their own,
-// blocks of all heads: 2048 tokens x 16 heads 56 / 66 (272), 4096 x 16 131 / 139 (528), x 20 141 /
-// 133 (660), x 24 185 / 154 (792), x 32 224 / 204 (1056), x 64 402 / 363 (2112), 8192 x 32 735 /
-// 641 (2080); behind contexts, five of 100 to 700 behind 1000 to 6000, 32 heads, 192 / 241 (some
-// 700), 8 x 256 behind 2000, 128 heads, 474 / 413 (over 2048).
+// once: prompts' blocks differ in length, and the long ones of one prompt begin first; behind long
+// contexts they are alike, and the last ones leave units idle.  us in equal stretches / in groups of
+// their own, blocks of all heads: 2048 tokens x 16 heads 56 / 66 (272), 4096 x 16 131 / 139 (528), x
+// 20 151 / 139 (660), x 32 203 / 186 (1056), x 64 402 / 363 (2112), 8192 x 32 735 / 641 (2080);
+// ragged prompts, 20 heads, 3000 ahead of ten of 100 93 / 97, behind them 96 / 92 (840), five of 800
+// 58 / 49 (720), 32 heads 137 / 118, 133 / 112 and 83 / 67; behind contexts, five of 100 to 700
+// behind 1000 to 6000, 32 heads, 192 / 241 (some 700), eight of 256 behind 2000, 128 heads, 487 /
+// 430 (3072), behind 500 to 4000 548 / 463, five of 800 behind 600, 32 heads, 136 / 115 (1152).
+// But all contexts may be of one sequence, whose block one group then reads alone: 20 heads, 100 of
+// 64, one of them behind 6000, 67 / 175; 16 heads, 400 of 64, one behind 25000, 171 / 690; 128
+// heads, 16 of 32, one behind 64K, 765 / 1655.  So together they may be no more than four times an
+// even share of the least that the tiles can be: the contexts' and those of prompts as long as one
+// another, n_rows / n_seqs.  (Where that refuses what is alike: 32 heads, 60 of 32 behind 1000, 217
+// / 201.)
 inline PromptPlan plan_latent_prompt(int64_t n_rows, int64_t n_keys, int64_t n_seqs, int n_heads) {
   PromptPlan p;
   const int64_t blocks = n_rows / kPromptRows + n_seqs;  // at most
-  p.block_groups = blocks * n_heads >= (n_keys <= 2 * n_rows ? 600 : 2048) && blocks <= 65535;
+  const double behind = std::max<int64_t>(n_keys - n_rows, 0);
+  const double least = n_heads * (behind + (double)n_rows * n_rows / (2.0 * kPromptRows * n_seqs));
+  const bool even = n_seqs == 1 || behind <= 4 * least / 512;  // in keys a block
+  p.block_groups =
+      even && blocks * n_heads >= (n_keys <= 2 * n_rows ? 600 : 2048) && blocks <= 65535;
   p.n_groups = p.block_groups ? (int32_t)blocks
                               : (int32_t)std::max<int64_t>(1, std::min<int64_t>(65535, 512 / n_heads));
   return p;

@@ -30,3 +30,11 @@ def test_a_workspace_for_the_widest_serves_narrower_and_fewer():
         lens[3] = top
         case = Case(lens, 20, n_q, 256, False, seed=batch)
         case.check(case.run(workspace=ws))
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("heads,rows,keys", [
+    (20, [64] * 40, [64] * 39 + [2564]), (20, [64] * 40, [2564] + [64] * 39),
+    (8, [3] * 100, [3] * 50 + [4003] + [3] * 49), (130, [32] * 17, [40] * 16 + [3000])])
+def test_one_long_context_among_fresh_prompts(heads, rows, keys, dim):
+    Prompt(rows, keys, heads, dim, seed=heads).check()

@@ -4,7 +4,7 @@ workspaces tell: partials are what such a split leaves.  No launch is made."""
 import pytest
 
 from paper_2609_36899_amd import _native as N
-from test_latent_refusals import _attn, _ws
+from test_latent_refusals import _attn, _prompt, _ws
 
 
 @pytest.mark.parametrize("kv", [N.BF16, N.FP8_E4M3])
@@ -19,3 +19,13 @@ def test_many_sequences_of_wide_tables_are_split(kv, heads, batch):
         assert b"workspace too small" in N.load().last_error()
         rows = 16 if heads == 16 else heads  # of a unit, in whole row tiles
         assert _ws(kv, batch, 1, heads, 512, pages) >= (256 + batch) * rows * (512 + 2) * 4
+
+
+@pytest.mark.parametrize("heads,seqs,rows,keys", [(20, 100, 6400, 12400), (16, 400, 25600, 50600),
+                                                  (64, 60, 1920, 61920), (32, 5, 2000, 20000 + 2000),
+                                                  (64, 33, 1000, 100000)])
+def test_contexts_that_one_prompt_may_have_alone_are_split(heads, seqs, rows, keys):
+    wide = dict(qs=heads * 192, ks=heads * 256, vs=heads * 256)
+    assert _prompt(rows=rows, keys=keys, seqs=seqs, heads=heads, **wide, ws=None,
+                   ws_bytes=0) == N.INVALID_ARG
+    assert b"workspace too small" in N.load().last_error()
