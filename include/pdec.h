@@ -797,7 +797,7 @@ int latent_prompt_attention(int32_t n_rows, int32_t n_keys, int32_t n_seqs, int3
  * the destination of two pairs, or of one and the source of another, is not
  * said; pairs with an id outside [0, n_pages) copy nothing.
  * Errors: PDEC_INVALID_ARG (n_pools outside [1, 4096], page_bytes outside [1,
- * 2^27], ...), PDEC_HIP_ERROR. */
+ * 2^27], 2^27 itself of a pool that is not 4-byte aligned, ...), PDEC_HIP_ERROR. */
 int paged_copy_pages(int32_t n_pools, void* const* pools, const int64_t* page_bytes,
                      int64_t n_pages, int32_t n_pairs, const int32_t* src_dev,
                      const int32_t* dst_dev, void* stream);
