@@ -14,9 +14,11 @@
 //
 // Gather.  Bound by memory (a row's 1152 or 644 bytes read, 1152 written), and for few rows by the
 // chain of looks from a row to its page, which the lanes go at once, one a row.  A wave takes four
-// rows, all their loads in flight; 54 000 E4M3 rows of 512 in 24.3 us (4.0 TB/s), which the caches
-// keep for who reads them next, 90 000 in 26.8 past them (6.0 TB/s); two rows a wave 29.3 us, one
-// 35.0, six, whose registers leave few waves, 35.3.
+// rows, all their loads in flight; 54 000 E4M3 rows of 512 in 24 us (4.0 TB/s); two rows a wave
+// 29.3, one 35.0, six, whose registers leave few waves, 35.3.  Stores past the caches make the call
+// shorter (17 us), but the projection that reads the rows next longer by more: both together, to
+// 1280 / 2560 / 5120 / 8192 columns, take +25 / +3 / -1 / +2 us, of 30 000 rows +12 / +11 / +56 /
+// +7, of 100 000 +9 / 0 / 0 / 0.
 #include "hip_common.h"
 #include "kernels.h"
 #include "rows.h"
@@ -162,8 +164,7 @@ __global__ __launch_bounds__(kThreads) void latent_append_kernel(LatentAppendArg
   }
 }
 
-// PAST: rows are written past the caches.
-template <bool FP8, int R, bool PAST>
+template <bool FP8, int R>
 __global__ __launch_bounds__(kThreads) void latent_rows_kernel(LatentRowsArgs a) {
   constexpr int kRowBytes = FP8 ? R + 2 * kRope : 2 * (R + kRope);
   constexpr int CL = R / 8;  // lanes of a latent, eight elements each; eight more of the key
@@ -229,13 +230,8 @@ __global__ __launch_bounds__(kThreads) void latent_rows_kernel(LatentRowsArgs a)
     }
     u32x4* to = (u32x4*)((uint16_t*)a.latents + (r0 + i) * R + lane * 8);
     u32x4* key_to = (u32x4*)((uint16_t*)a.rope_keys + (r0 + i) * kRope + lane * 8);
-    if constexpr (PAST) {
-      if (lane < CL) __builtin_nontemporal_store(x[i], to);
-      if (lane < 8) __builtin_nontemporal_store(k[i], key_to);
-    } else {
-      if (lane < CL) *to = x[i];
-      if (lane < 8) *key_to = k[i];
-    }
+    if (lane < CL) *to = x[i];
+    if (lane < 8) *key_to = k[i];
   }
 }
 
@@ -276,18 +272,7 @@ hipError_t launch_latent_append(int src_bf16, int fp8, int latent, const LatentA
 hipError_t launch_latent_rows(int fp8, int latent, const LatentRowsArgs& a, hipStream_t stream) {
   if (a.n_rows == 0) return hipSuccess;
   const dim3 grid((uint32_t)rows_groups(a)), block(kThreads);
-  // Past the caches go more rows than they keep for the projection that reads them next, the
-  // memory-side one (256 MB) with what it writes beside.  us of rows of 512 and a projection to
-  // 2560 / 5120 / 8192 columns, with the hint - without, E4M3 pages: 30000 rows +8 / +54 / -2,
-  // 44000 +14 / 0 / -4, 52000 +8 / -2 / -6, 60000 +10 / +6 / -1, 70000 -3 / -7 / -3, 100000 -2 / +1
-  // / -3; bf16: 30000 +6 / +50 / -2, 60000 +10 / +4 / -3, 70000 -6 / -8 / -6, 100000 +1 / -3 / -5.
-  // The rows alone gain from 40000 on: 54000 24.3 to 16.9 us.
-  const bool past = (int64_t)a.n_rows * (latent + kRope) * 2 > 72 << 20;
-#define PDEC_ROWS(FP8_, R_)                                                     \
-  do {                                                                          \
-    if (past) latent_rows_kernel<FP8_, R_, true><<<grid, block, 0, stream>>>(a); \
-    else latent_rows_kernel<FP8_, R_, false><<<grid, block, 0, stream>>>(a);    \
-  } while (0)
+#define PDEC_ROWS(FP8_, R_) latent_rows_kernel<FP8_, R_><<<grid, block, 0, stream>>>(a)
   if (latent == 512) {
     if (fp8) PDEC_ROWS(true, 512);
     else PDEC_ROWS(false, 512);
