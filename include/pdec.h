@@ -587,8 +587,8 @@ int paged_kv_append(int32_t src_dtype, int32_t kv_dtype, int32_t n_rows, int32_t
  *   [n_selected], logical page indices, distinct; the first min(n_selected,
  *   ceil(lens[b] / 16)) of them are read, and the softmax runs over the
  *   positions below lens[b] in those pages alone.
- *   Scores, softmax and sums are fp32; the weights enter the second product
- *   rounded to bf16.
+ *   Scores, softmax and sums are fp32 (values as the latents above); the weights
+ *   enter the second product rounded to bf16.
  *   workspace: device, paged_token_attention_workspace_bytes(...) bytes for
  *   the same or larger batch, n_q and max_pages; max_pages is bt_stride, or the
  *   smaller of it and n_selected with a selection.  It may be null where these
@@ -723,8 +723,9 @@ int paged_latent_append(int32_t src_dtype, int32_t kv_dtype, int32_t n_rows, int
  *   [batch][n_q][n_heads][latent_dim]; lens: device int32 [batch], counting the
  *   n_q tokens, taken as in [0, bt_stride * 16]; a token that sees no key gets
  *   zeros.  Tokens whose page id is outside [0, n_pages) are no keys.
- *   Scores, softmax and sums are fp32; the weights, times the token's scale,
- *   enter the second product rounded to bf16.  Of E4M3 pages the latent part of
+ *   Scores, softmax and sums are fp32, the weights up to 2^16 before they are
+ *   normalised: sums of n keys overflow where latents exceed 2^112 / n.  The
+ *   weights, times the token's scale, enter the second product rounded to bf16.  Of E4M3 pages the latent part of
  *   a query is taken as the sum of two E4M3 numbers with a power of two for the
  *   row: exact but for elements below 2^-10 of the row's largest, which lose at
  *   most 2^-17 of it, and an infinite element makes its row's scores NaN.
@@ -770,8 +771,8 @@ int paged_latent_rows(int32_t kv_dtype, int32_t n_rows, int32_t n_seqs, int32_t 
  *   side by side for each head, as one projection leaves them, serve as they
  *   are); rope_keys: bf16 rows of 64, rope_stride apart; strides multiples of 8;
  *   out: device bf16 [n_rows][n_heads][head_dim].
- *   Scores, softmax and sums are fp32; the weights enter the second product
- *   rounded to bf16.
+ *   Scores, softmax and sums are fp32 (values as the latents above); the weights
+ *   enter the second product rounded to bf16.
  *   workspace: device, latent_prompt_attention_workspace_bytes(...) bytes for
  *   the same n_heads and head_dim and the same or more rows and sequences; it
  *   may be null where these are 0.

@@ -10,7 +10,11 @@
 // bring the pages: a load holds its wave for 60 cycles and more.  A page's sixteen keys are one
 // tile of the first product, and a lane's four weights are the operand P of the second, over
 // sixteen keys, as they are.  At the end of a piece the teams' sums are joined through LDS.  A
-// unit reads its pages once, so they do not stay in the caches (pages from HBM: 55 us, then 50).
+// unit reads its pages once, so they do not stay in the caches.  us so / kept there, 16 heads: 64
+// sequences of 4K that share nothing 45 / 51 (E4M3) and 61 / 70 (bf16); eight forks each of eight
+// prompts, of 4K shared and 50 to 400 tokens of their own 45 / 42 and 49 / 35, of 2K shared and 0.5K
+// to 4K 46 / 44 and 62 / 58, of 0.5K and 0.5K to 4K 40 / 37 and 44 / 46, of 1K and 1K to 8K 55 / 57
+// and 75 / 76.  Which pages are shared only the tables on the device say.
 //
 // 16 heads over 64 x 1K to 8K E4M3 43 us and the merge's 6 (205 MB): a step of three pages takes
 // 2450 cycles, 6.7 TB/s over all units, and the pieces' beginnings and ends 13 us.  Four short

@@ -35,7 +35,7 @@ namespace pdec {
 namespace {
 
 constexpr int kRope = kLatentRope;
-constexpr float kSlack = 16.f;  // powers of two that scores may outgrow a row's reference by
+constexpr float kSlack = 16.f;  // as of the attention over latents
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
@@ -62,8 +62,10 @@ __device__ __forceinline__ int block_tiles(const Seq& s, int blk) {
   return max((keys + TILE - 1) / TILE, 1);
 }
 // The same and what a piece of a block costs beside its tiles (its queries, the first tiles' way,
-// its output), in tiles, which equal stretches count ahead of each block's.  us at 0 / 4 / 12: 20 heads
-// over 4096 150 / 144 / 146, 32 heads over five turns 186 / 189 / 191.
+// its output), in tiles, which equal stretches count ahead of each block's.  us at 0 / 2 / 4 / 12: 16
+// heads over 4096 120 / 117 / 113 / 119, over 2048 53.5 / 52.8 / 50.7 / 51.2, four over 8192 115 / 113 /
+// 111 / 112, 20 heads, 200 behind 20K, 102 / 101 / 100 / 99, 32 heads over five turns of 100 to 700
+// 253 / 248 / 249 / 252.
 constexpr int kHead = 4;
 // That of the blocks before blk: of each whole block ROWS / TILE more than of the one before.
 template <int ROWS, int TILE>

@@ -12,7 +12,8 @@ namespace pdec {
 constexpr int kRope = kLatentRope;
 // A row's reference maximum moves only where its scores outgrow it by this many powers of
 // two: the weights are then up to 2^16 instead of 1, no less exact, and the accumulators are
-// rescaled a few times a row instead of at most tiles.
+// rescaled a few times a row instead of at most tiles.  The sums of n keys overflow where values
+// exceed 2^112 / n.
 constexpr float kSlack = 16.f;
 
 typedef short s16x2 __attribute__((ext_vector_type(2)));
