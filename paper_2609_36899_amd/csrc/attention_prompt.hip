@@ -55,6 +55,18 @@ __device__ __forceinline__ Seq seq_of(const LatentPromptArgs& a, int b) {
   s.nk = min(max(a.k_start[b + 1], s.k0), a.n_keys) - s.k0;
   return s;
 }
+// Whether they descend: each wave notes it of the sequences that stretch_of shows it, in a place of
+// its own, whose barriers pass it on to descends().
+__device__ __forceinline__ void note_descent(const LatentPromptArgs& a, int b, int* down) {
+  if (a.q_start[b] > a.q_start[b + 1]) down[threadIdx.x >> 6] = 1;
+}
+template <int T>
+__device__ __forceinline__ bool descends(const int* down) {
+  int any = 0;
+#pragma unroll
+  for (int w = 0; w < T / 64; ++w) any |= down[w];
+  return any;
+}
 // Tiles of block blk: those of the keys that its last row sees, at least one.
 template <int ROWS, int TILE>
 __device__ __forceinline__ int block_tiles(const Seq& s, int blk) {
@@ -115,14 +127,15 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn_kernel(LatentPromptAr
   // With a group for each block the blocks' order is turned round, so that the long ones of a
   // prompt begin first (and of several prompts the last one's).
   const int w = a.block_groups ? gridDim.y - 1 - blockIdx.y : blockIdx.y;
-  bool descends = false;
+  __shared__ int down[kWaves];
+  if ((threadIdx.x & 63) == 0) down[wave] = 0;
   const Stretch mine = stretch_of<kThreads>(
       a.n_seqs, gridDim.y, a.block_groups ? 1 : a.min_tiles, w, red, found, [&](int b) {
-        descends |= a.q_start[b] > a.q_start[b + 1];
+        note_descent(a, b, down);
         const Seq s = seq_of(a, b);
         return a.block_groups ? (s.nq + kRows - 1) / kRows : seq_size<kRows, kTile>(s);
       });
-  if (__syncthreads_or(descends)) return;
+  if (descends<kThreads>(down)) return;
   int at = w * mine.per;
   if (at >= mine.total) return;
   int end = min(at + mine.per, mine.total), first = mine.first;
@@ -431,12 +444,13 @@ __global__ __launch_bounds__(512) void prompt_merge_kernel(LatentPromptArgs a, i
   __shared__ int red[8];
   __shared__ int found[2];
   const int w = blockIdx.z, h = blockIdx.x;
-  bool descends = false;
+  __shared__ int down[8];
+  if ((threadIdx.x & 63) == 0) down[threadIdx.x >> 6] = 0;
   const Stretch mine = stretch_of<512>(a.n_seqs, n_groups, a.min_tiles, w, red, found, [&](int b) {
-    descends |= a.q_start[b] > a.q_start[b + 1];
+    note_descent(a, b, down);
     return seq_size<kRows, kTile>(seq_of(a, b));
   });
-  if (__syncthreads_or(descends)) return;
+  if (descends<512>(down)) return;
   const int at = w * mine.per;
   if (at >= mine.total) return;
   const int end = min(at + mine.per, mine.total);

@@ -128,11 +128,11 @@ struct PromptPlan {
 // behind 1000 to 6000, 32 heads, 192 / 241 (some 700), eight of 256 behind 2000, 128 heads, 487 /
 // 430 (3072), behind 500 to 4000 548 / 463, five of 800 behind 600, 32 heads, 136 / 115 (1152).
 // But all contexts may be of one sequence, whose block one group then reads alone: 20 heads, 100 of
-// 64, one of them behind 6000, 67 / 175; 16 heads, 400 of 64, one behind 25000, 171 / 690; 128
-// heads, 16 of 32, one behind 64K, 765 / 1655.  So together they may be no more than four times an
-// even share of the least that the tiles can be: the contexts' and those of prompts as long as one
-// another, n_rows / n_seqs.  (Where that refuses what is alike: 32 heads, 60 of 32 behind 1000, 217
-// / 201.)
+// 64, one of them behind 6000, 67 / 175; 16 heads, 400 of 64, one behind 25000, 171 / 690.  So
+// together they may be no more than four times an even share of the least that the tiles can be:
+// the contexts' and those of prompts as long as one another, n_rows / n_seqs.  (What that lets be:
+// 128 heads, 16 of 32, one behind 64K, 765 / 1655.  What it refuses although alike: 32 heads, 60 of
+// 32 behind 1000, 217 / 201.)
 inline PromptPlan plan_latent_prompt(int64_t n_rows, int64_t n_keys, int64_t n_seqs, int n_heads) {
   PromptPlan p;
   const int64_t blocks = n_rows / kPromptRows + n_seqs;  // at most
