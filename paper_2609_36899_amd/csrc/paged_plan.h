@@ -126,7 +126,7 @@ struct PromptPlan {
 // ragged prompts, 20 heads, 3000 ahead of ten of 100 93 / 97, behind them 96 / 92 (840), five of 800
 // 58 / 49 (720), 32 heads 137 / 118, 133 / 112 and 83 / 67; behind contexts, five of 100 to 700
 // behind 1000 to 6000, 32 heads, 192 / 241 (some 700), eight of 256 behind 2000, 128 heads, 487 /
-// 430 (3072), behind 500 to 4000 548 / 463, five of 800 behind 600, 32 heads, 136 / 115 (1152).
+// 430 (over 2048), behind 500 to 4000 548 / 463, five of 800 behind 600, 32 heads, 136 / 115 (1152).
 // But all contexts may be of one sequence, whose block one group then reads alone: 20 heads, 100 of
 // 64, one of them behind 6000, 67 / 175; 16 heads, 400 of 64, one behind 25000, 171 / 690.  So
 // together they may be no more than four times an even share of the least that the tiles can be:
